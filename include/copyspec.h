@@ -446,6 +446,114 @@ cs_status cs_lm_head(cs_ctx* ctx, const void* X, int rows, int32_t* ids, float* 
 cs_status cs_lm_head_static(const void* X, const void* W, int rows, int vocab, int d_model,
                             int32_t* ids, void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators around a paged KV cache, for servers that keep many sequences of unknown length (the paper keeps one
+ * contiguous cache per sequence; a block of rows is verified against pages as against that, Sec. 3.2, App. B.2).
+ *
+ * A cache is two pools of pages, K and V, of one layer: page `p`, KV head `h`, slot `s` begins at element
+ * p * page_stride + h * head_stride + s * slot_stride of either pool, head_dim elements of `dtype` in a row.  Position
+ * j of sequence b lies in page page_table[b][j / page_size], slot j % page_size.  Any order of the strides (heads
+ * outside or inside a page's slots); pools 16-byte aligned, strides multiples of 8 elements.
+ *
+ * Blocks: sequence b's block is len[b] >= 0 rows, rows start[b] .. start[b] + len[b] - 1 of the tensors of rows; row r
+ * of it sits at absolute position kv_len[b] + r, as in cs_verify_step, so kv_len[b] counts the positions before the
+ * block.  Rows of no block are not written.  Nothing advances kv_len: rows that are rejected later are
+ * dropped by not counting them.  Page-table entries behind the last position in use may be anything.
+ *
+ * Types: CS_BF16 and CS_F16 caches; everything is computed in 32 bits and rounded (to nearest even) once, when it is
+ * stored.  Softmax weights enter their product with V in 16 bits (two terms of them in the kernel for few rows). */
+typedef enum { CS_BF16 = 0, CS_F16 = 1, CS_F32 = 2 } cs_dtype;
+
+typedef struct cs_paged_cache cs_paged_cache; /* opaque; host memory owned by the library */
+
+typedef struct {
+  void *k, *v;                                    /* pools of pages                                         */
+  int64_t page_stride, head_stride, slot_stride;  /* elements, the same in both                             */
+  int32_t n_pages, page_size;                     /* page_size a power of two from 16 on                    */
+  int32_t n_kv_heads, head_dim;                   /* head_dim 32, 64 or 128                                 */
+  int32_t dtype;                                  /* CS_BF16 or CS_F16                                      */
+} cs_paged_config;
+
+typedef struct {
+  const int32_t *start, *len, *kv_len;  /* [n_seqs] each                                                    */
+  const int32_t* page_table;            /* [n_seqs][table_width]                                            */
+  int32_t n_seqs, table_width;
+  int32_t rows;                         /* rows the tensors of rows have                                    */
+} cs_blocks;
+
+/* Heads of rows that are normed and rotated: n_heads x head_dim elements of x per row go to y.  Strides in elements,
+ * multiples of 16 bytes, bases 16-byte aligned; y may be x.  gain [head_dim] in y's type, NULL = no norm. */
+typedef struct {
+  const void* x;
+  int64_t row_stride, head_stride;
+  void* y;
+  int64_t y_row_stride, y_head_stride;
+  const void* gain;
+  int32_t n_heads;
+} cs_heads;
+
+/* Which keys row r of a block attends to, position p = kv_len + r: [max(0, p + 1 - window), hi), window 0 = no limit on
+ * the left, and hi = p + 1 (CS_MASK_CAUSAL), kv_len (CS_MASK_PREFIX: what was cached before the block) or
+ * kv_len + len (CS_MASK_FULL: the block's rows see one another). */
+typedef enum { CS_MASK_CAUSAL = 0, CS_MASK_PREFIX = 1, CS_MASK_FULL = 2 } cs_mask;
+
+/* Rotation factors: table [n_positions][rot_dim] fp32, row p holding cos(p * theta^(-2i / rot_dim)), i < rot_dim / 2, then
+ * the sines; worked out in 64 bits.  Callers with other frequencies write their own.  rot_dim even.  Async.
+ * Errors: CS_ERR_ARG, CS_ERR_CUDA. */
+cs_status cs_rope_table(float* table, int n_positions, int rot_dim, float theta, void* stream);
+
+/* Norms of queries and keys for each head and their rotation, one pass and one launch: for every row and head
+ *   u = x * rsqrt(mean(x^2) + eps) * gain   (u = x without a gain),
+ *   y[i] = u[i] cos_i - u[i + h] sin_i,  y[i + h] = u[i + h] cos_i + u[i] sin_i,  i < h = rot_dim / 2,
+ * y = u from rot_dim on, with the table's row pos[row].  q or k may be NULL or have no heads.  head_dim 32, 64 or 128;
+ * rot_dim a multiple of 16, at most head_dim, 0 = no rotation (rope and pos may be NULL).  Types: y in x's type, or x in CS_F32 and y in
+ * 16 bits.  Where a position lies outside the table, the row's rotated elements come out as NaN.  Needs no context.  Async.
+ * Errors: CS_ERR_ARG (NULL, sizes, alignment), CS_ERR_SHAPE, CS_ERR_CUDA. */
+cs_status cs_qk_norm_rope(const cs_heads* q, const cs_heads* k, int rows, int head_dim, cs_dtype in, cs_dtype out,
+                          const int32_t* pos, const float* rope, int n_positions, int rot_dim, float eps, void* stream);
+
+/* Bytes of device workspace cs_paged_create needs (0 on a bad configuration).  Host-only arithmetic; needs no GPU. */
+size_t cs_paged_workspace_bytes(const cs_paged_config* cfg);
+
+/* Describes a cache to the calls below.  `cfg` is a host struct (copied); `workspace` is a 256-byte aligned device buffer
+ * of at least cs_paged_workspace_bytes(cfg) bytes; both pools and the workspace must outlive the handle.  Clears the
+ * workspace's counters and status on `stream` (async).  Work of one handle must stay on one stream at a time; handles of
+ * several layers whose work is on one stream may share a workspace, and then share what cs_paged_status says.  Errors: CS_ERR_ARG, CS_ERR_SHAPE, CS_ERR_CAPACITY, CS_ERR_CUDA;
+ * the text is cs_paged_last_error(NULL). */
+cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void* workspace, size_t workspace_bytes,
+                          void* stream);
+void cs_paged_destroy(cs_paged_cache* cache);
+const char* cs_paged_last_error(const cs_paged_cache* cache);
+
+/* Waits for `stream`, then returns and clears what the device found wrong: CS_ERR_CAPACITY (a block that does not fit its
+ * row of the page table, or positions behind the rotation table), CS_ERR_ARG (a negative length, rows outside the tensors,
+ * a page that does not exist among those a block needs), CS_ERR_TIMEOUT.  Sequences that fail a check of lengths are left out: none of
+ * their rows is written.  Where single pages do not exist, appended rows that belong there are dropped and
+ * attention takes their keys and values for zeros. */
+cs_status cs_paged_status(cs_paged_cache* cache, void* stream);
+
+/* Appends the blocks' keys and values to their sequences' pages: position kv_len[b] + r gets k's row (normed with its
+ * gain, rotated for that position, as above) and v's row, rounded to the cache's type.  With `q` the block's queries are
+ * normed and rotated in the same launch, into q->y in the cache's type.  k->y, v->y and v->gain are not used.  `in` is the
+ * type of q, k and v: the cache's, or CS_F32.  Blocks must not share positions of one sequence's page.  Async.
+ * Errors: CS_ERR_ARG, CS_ERR_SHAPE, CS_ERR_CUDA. */
+cs_status cs_paged_append(cs_paged_cache* cache, const cs_blocks* blocks, const cs_heads* k, const cs_heads* v,
+                          const cs_heads* q, cs_dtype in, const float* rope, int n_positions, int rot_dim, float eps,
+                          void* stream);
+
+/* Attention of the blocks' rows over the pages, the block's own among them once they are appended:
+ *   out[row][h] = softmax_j(scale * q[row][h] . K_j) V_j,  lse[row][h] = log sum_j exp(scale * q[row][h] . K_j)
+ * over the keys the mask leaves, query head h with KV head h / (n_heads / n_kv_heads).  Blocks of any height, one token
+ * or a prompt's chunk, side by side.  q and out [rows][n_heads][head_dim] in the cache's type, q by strides (elements,
+ * multiples of 8; base 16-byte aligned), out contiguous and 16-byte aligned; lse fp32 [rows][n_heads] or NULL.  A row that no key is left for, or whose
+ * scores are all -inf, gets zeros and lse -inf.  Keys and values outside the range that a row of its block attends to are
+ * never looked at, whatever they hold; non-finite values at positions that a row does not attend to do not reach it.
+ * n_heads a multiple of n_kv_heads, at most 128 per KV head.  scale > 0; window >= 0.  Async.
+ * Results are reproducible from run to run.  Errors: CS_ERR_ARG, CS_ERR_SHAPE, CS_ERR_CUDA. */
+cs_status cs_paged_attention(cs_paged_cache* cache, const cs_blocks* blocks, const void* q, int64_t q_row_stride,
+                             int64_t q_head_stride, int n_heads, cs_mask mask, int window, float scale, void* out,
+                             float* lse, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -19,7 +19,9 @@ CS_ERR_ARG, CS_ERR_SHAPE, CS_ERR_CAPACITY, CS_ERR_CUDA, CS_ERR_TIMEOUT, CS_ERR_U
 CS_ERR_LIMIT = -7
 LATEST, FIRST = 0, 1
 STAMP_FAMILIES = ("gemm", "attention", "lm_head", "merge", "other")
+MASK_CAUSAL, MASK_PREFIX, MASK_FULL = 0, 1, 2
 TAU_HIST = 65
+_DTYPE = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 _STATUS = {0: "CS_OK", -1: "CS_ERR_ARG", -2: "CS_ERR_SHAPE", -3: "CS_ERR_CAPACITY", -4: "CS_ERR_CUDA",
            -5: "CS_ERR_TIMEOUT", -6: "CS_ERR_UNSUPPORTED", -7: "CS_ERR_LIMIT"}
@@ -51,13 +53,30 @@ class CsStats(C.Structure):
                 "emitted": self.emitted, "no_match": self.no_match, "tau_hist": list(self.tau_hist)}
 
 
+class CsPagedConfig(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p)] + [(n, C.c_int64) for n in ("page_stride", "head_stride", "slot_stride")] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")]
+
+
+class CsBlocks(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("start", "len", "kv_len", "page_table")] + \
+               [(n, C.c_int32) for n in ("n_seqs", "table_width", "rows")]
+
+
+class CsHeads(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("y", C.c_void_p),
+                ("y_row_stride", C.c_int64), ("y_head_stride", C.c_int64), ("gain", C.c_void_p), ("n_heads", C.c_int32)]
+
+
 WORKSPACE_GUARD, GUARD_BYTE = 4096, 0xA5   # guard bands around a Context's workspace
 EXPORTS = ("cs_workspace_bytes", "cs_create", "cs_destroy", "cs_last_error", "cs_sync_status",
            "cs_find_match", "cs_verify_step", "cs_kv_truncate", "cs_decode_loop", "cs_decode_loop_drafted", "cs_step_host",
            "cs_prefill", "cs_linear", "cs_step_host_reset", "cs_debug_drop_tile", "cs_debug_drop_chain_tile", "cs_debug_leave_shares",
            "cs_loop_begin", "cs_loop_steps", "cs_loop_poll", "cs_loop_end", "cs_loop_last_step", "cs_set_stamps", "cs_stamp_layout", "cs_set_match_index",
            "cs_loop_launches_per_step", "cs_lm_head", "cs_lm_head_static", "cs_gram_index_bytes",
-           "cs_gram_index_reset", "cs_gram_index_update", "cs_find_match_indexed", "cs_gram_index_status")
+           "cs_gram_index_reset", "cs_gram_index_update", "cs_find_match_indexed", "cs_gram_index_status",
+           "cs_rope_table", "cs_qk_norm_rope", "cs_paged_workspace_bytes", "cs_paged_create", "cs_paged_destroy", "cs_paged_last_error",
+           "cs_paged_status", "cs_paged_append", "cs_paged_attention")
 
 _lib = None
 _search = None      # cs_find_match in native code, for plain arguments
@@ -145,6 +164,25 @@ def load(build_if_missing: bool = True) -> C.CDLL:
     lib.cs_gram_index_status.argtypes = [vp, i, i, vp]
     lib.cs_linear.restype = i
     lib.cs_linear.argtypes = [vp, vp, vp, i, i, i, vp, vp]
+    heads, blocks, f, ll = C.POINTER(CsHeads), C.POINTER(CsBlocks), C.c_float, C.c_int64
+    lib.cs_rope_table.restype = i
+    lib.cs_rope_table.argtypes = [vp, i, i, f, vp]
+    lib.cs_qk_norm_rope.restype = i
+    lib.cs_qk_norm_rope.argtypes = [heads, heads, i, i, i, i, ip, vp, i, i, f, vp]
+    lib.cs_paged_workspace_bytes.restype = C.c_size_t
+    lib.cs_paged_workspace_bytes.argtypes = [C.POINTER(CsPagedConfig)]
+    lib.cs_paged_create.restype = i
+    lib.cs_paged_create.argtypes = [C.POINTER(C.c_void_p), C.POINTER(CsPagedConfig), vp, C.c_size_t, vp]
+    lib.cs_paged_destroy.restype = None
+    lib.cs_paged_destroy.argtypes = [vp]
+    lib.cs_paged_last_error.restype = C.c_char_p
+    lib.cs_paged_last_error.argtypes = [vp]
+    lib.cs_paged_status.restype = i
+    lib.cs_paged_status.argtypes = [vp, vp]
+    lib.cs_paged_append.restype = i
+    lib.cs_paged_append.argtypes = [vp, blocks, heads, heads, heads, i, vp, i, i, f, vp]
+    lib.cs_paged_attention.restype = i
+    lib.cs_paged_attention.argtypes = [vp, blocks, vp, ll, ll, i, i, i, f, vp, vp, vp]
     _search = _native_search()
     _lib = lib
     return lib
@@ -535,3 +573,172 @@ class Context:
         rc = self.lib.cs_linear(self.handle, _ptr(X), _ptr(W), rows, N, K, _ptr(Y), _stream())
         self._check(rc, "cs_linear")
         return Y
+
+
+# ------------------------------------------------------------------ operators around a paged KV cache
+def cs_rope_table(n_positions, rot_dim, theta=10000.0, device="cuda"):
+    """Rotation factors fp32 [n_positions][rot_dim] (cosines, then sines) for the calls below, worked out in 64 bits."""
+    table = torch.empty(n_positions, rot_dim, dtype=torch.float32, device=device)
+    with torch.cuda.device(table.device):
+        rc = load().cs_rope_table(table.data_ptr(), n_positions, rot_dim, theta, _stream())
+    if rc != CS_OK:
+        raise CsError(rc, "cs_rope_table")
+    return table
+
+
+def _rows(t, name):
+    """(data pointer, row stride, head stride) of a [rows][heads][head_dim] CUDA tensor whose heads are contiguous."""
+    if not t.is_cuda or t.dim() != 3 or t.dtype not in _DTYPE or (t.shape[2] > 1 and t.stride(2) != 1):
+        raise ValueError(f"{name} must be a CUDA tensor [rows][heads][head_dim] of bf16, fp16 or fp32 with contiguous heads")
+    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else 0), (t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def _heads(x, y, gain, dtype, name):
+    h = CsHeads()
+    if x is None:
+        return h
+    h.x, h.row_stride, h.head_stride = _rows(x, name)
+    h.n_heads = x.shape[1]
+    if y is not None:
+        if y.shape != x.shape or y.dtype != dtype or y.device != x.device:
+            raise ValueError(f"{name}'s output must have its shape, its device and type {dtype}")
+        h.y, h.y_row_stride, h.y_head_stride = _rows(y, f"{name}'s output")
+    if gain is not None:
+        if not gain.is_cuda or not gain.is_contiguous() or gain.dtype != dtype or gain.shape != (x.shape[2],):
+            raise ValueError(f"{name}'s gain must be a contiguous CUDA tensor [head_dim] of type {dtype}")
+        h.gain = gain.data_ptr()
+    return h
+
+
+def _table(rope, name="rope"):
+    """(pointer, positions, rotated elements of a head)"""
+    if rope is None:
+        return None, 0, 0
+    if not rope.is_cuda or not rope.is_contiguous() or rope.dtype is not torch.float32 or rope.dim() != 2:
+        raise ValueError(f"{name} must be a contiguous fp32 CUDA tensor [positions][rotated elements]")
+    return rope.data_ptr(), rope.shape[0], rope.shape[1]
+
+
+def cs_qk_norm_rope(q, k, pos, rope, q_gain=None, k_gain=None, eps=1e-5, dtype=None, out=None):
+    """RMS norms of queries q [rows][H][D] and keys k [rows][Hkv][D] for each head (where there is a gain [D]) and their
+    rotation by the rows `pos` [rows] of the table `rope` (cs_rope_table; None = no rotation), in one launch.  Either of q and k may be None.
+    Returns (q, k) in `dtype` (default: the inputs' type; 16-bit types from fp32 inputs); `out` may supply those tensors, the inputs
+    themselves among them."""
+    some = q if q is not None else k
+    if some is None or (q is not None and k is not None and (q.dtype != k.dtype or q.shape[0] != k.shape[0] or q.shape[2:] != k.shape[2:])):
+        raise ValueError("q and k must have the same rows, head size and type")
+    dtype = dtype or some.dtype
+    if dtype not in _DTYPE or some.dtype not in _DTYPE:
+        raise ValueError("bf16, fp16 and fp32 are known")
+    if rope is not None and (pos is None or pos.shape != some.shape[:1]):
+        raise ValueError("pos must have one position per row")
+    if out is None:
+        out = tuple(None if x is None else torch.empty(x.shape, dtype=dtype, device=x.device) for x in (q, k))
+    hq, hk = _heads(q, out[0], q_gain, dtype, "q"), _heads(k, out[1], k_gain, dtype, "k")
+    table, n, rot = _table(rope)
+    rc = load().cs_qk_norm_rope(hq, hk, some.shape[0], some.shape[2], _DTYPE[some.dtype], _DTYPE[dtype], _i32(pos, "pos"), table, n, rot, eps, _stream())
+    if rc != CS_OK:
+        raise CsError(rc, "cs_qk_norm_rope")
+    return out
+
+
+class PagedCache:
+    """One layer's paged KV cache: k_pages and v_pages are the caller's pools [n_pages][Hkv][page_size][D] (bf16 or fp16; any
+    order of the strides, the same in both, heads contiguous), kept alive here.  Owns the workspace and the handle; caches of several layers whose work is on one stream
+    may share a workspace (`workspace`: another PagedCache).
+
+    Blocks of rows are given by three int32 CUDA tensors [B]: sequence b's block is the rows block_start[b] .. block_start[b] +
+    block_len[b] - 1 of the tensors of rows and begins at position kv_len[b]; page_table [B][pages] int32 says where
+    positions are kept."""
+
+    def __init__(self, k_pages, v_pages, workspace=None):
+        if not k_pages.is_cuda or k_pages.dim() != 4 or k_pages.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("k_pages must be a CUDA tensor [n_pages][heads][page_size][head_dim] of bf16 or fp16")
+        if v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype or v_pages.device != k_pages.device or v_pages.stride() != k_pages.stride():
+            raise ValueError("v_pages must have k_pages' shape, strides, type and device")
+        if k_pages.stride(3) != 1:
+            raise ValueError("heads must be contiguous")
+        self.lib = load()
+        self.k_pages, self.v_pages = k_pages, v_pages
+        self.dtype = k_pages.dtype
+        n, h, s, d = k_pages.shape
+        st = k_pages.stride()
+        self.c_cfg = CsPagedConfig(k_pages.data_ptr(), v_pages.data_ptr(), st[0], st[1], st[2], n, s, h, d, _DTYPE[self.dtype])
+        with torch.cuda.device(k_pages.device):
+            if workspace is None:
+                nbytes = self.lib.cs_paged_workspace_bytes(C.byref(self.c_cfg))
+                self.workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=k_pages.device)
+            else:
+                self.workspace = workspace.workspace
+                if self.workspace.device != k_pages.device:
+                    raise ValueError("the workspace is another device's")
+            self.handle = C.c_void_p()
+            rc = self.lib.cs_paged_create(C.byref(self.handle), C.byref(self.c_cfg), self.workspace.data_ptr(), self.workspace.numel(), _stream())
+        if rc != CS_OK:
+            msg = self.lib.cs_paged_last_error(None)
+            raise CsError(rc, "cs_paged_create", msg.decode() if msg else "")
+
+    def close(self):
+        if getattr(self, "handle", None):
+            self.lib.cs_paged_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, rc, where):
+        if rc != CS_OK:
+            msg = self.lib.cs_paged_last_error(self.handle)
+            raise CsError(rc, where, msg.decode() if msg else "")
+
+    def _blocks(self, start, length, kv_len, table, rows):
+        B = start.shape[0]
+        if length.shape != (B,) or kv_len.shape != (B,) or start.dim() != 1 or table.dim() != 2 or table.shape[0] != B:
+            raise ValueError("block_start, block_len and kv_len must be [B], page_table [B][pages]")
+        return CsBlocks(_i32(start, "block_start"), _i32(length, "block_len"), _i32(kv_len, "kv_len"), _i32(table, "page_table"), B, table.shape[1], rows)
+
+    def cs_paged_append(self, k, v, block_start, block_len, kv_len, page_table, rope=None, k_gain=None, q=None, q_gain=None, eps=1e-5, q_out=None):
+        """Appends the blocks' keys (normed where there is a gain, rotated) and values [rows][Hkv][D] to their pages; with `q`
+        [rows][H][D] norms and rotates the block's queries in the same launch and returns them in the cache's type."""
+        d = self.k_pages.shape[3]
+        if k.dtype != v.dtype or k.shape != v.shape or k.dim() != 3 or k.shape[2] != d or (q is not None and (q.dtype != k.dtype or q.shape[0] != k.shape[0] or q.shape[2] != d)):
+            raise ValueError("q, k and v must have the same rows and type and the cache's head size")
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=self.dtype, device=q.device)
+        hk, hv, hq = _heads(k, None, k_gain, self.dtype, "k"), _heads(v, None, None, self.dtype, "v"), _heads(q, q_out, q_gain, self.dtype, "q")
+        blocks = self._blocks(block_start, block_len, kv_len, page_table, k.shape[0])
+        table, n, rot = _table(rope)
+        self._check(self.lib.cs_paged_append(self.handle, blocks, hk, hv, hq, _DTYPE[k.dtype], table, n, rot, eps, _stream()), "cs_paged_append")
+        return q_out
+
+    def cs_paged_attention(self, q, block_start, block_len, kv_len, page_table, mask=MASK_CAUSAL, window=0, scale=None, out=None, with_lse=False, lse=None):
+        """Attention of the blocks' rows q [rows][H][D] over their sequences' pages.  `mask`: MASK_CAUSAL (the cached keys and the block's up to the row's own),
+        MASK_PREFIX (the cached keys) or MASK_FULL (the cached keys and the whole block); `window` > 0: only the last so many positions up to
+        the row's own; `scale`: 1 / sqrt(D) by default.  Returns out [rows][H][D], with `with_lse` (or an `lse` tensor) also log sum exp [rows][H] fp32.
+        Rows of no block are left as they were."""
+        if q.dtype != self.dtype:
+            raise ValueError(f"q must be {self.dtype}, the cache's type")
+        ptr, row, head = _rows(q, "q")
+        T, H, D = q.shape
+        if D != self.k_pages.shape[3]:
+            raise ValueError("q must have the cache's head size")
+        if out is None:
+            out = torch.empty(T, H, D, dtype=q.dtype, device=q.device)
+        elif out.shape != q.shape or out.dtype != q.dtype or not out.is_cuda or not out.is_contiguous():
+            raise ValueError("out must be contiguous, of q's shape and type")
+        if lse is None and with_lse:
+            lse = torch.empty(T, H, dtype=torch.float32, device=q.device)
+        elif lse is not None and (lse.shape != (T, H) or lse.dtype is not torch.float32 or not lse.is_cuda or not lse.is_contiguous()):
+            raise ValueError("lse must be a contiguous fp32 CUDA tensor [rows][heads]")
+        blocks = self._blocks(block_start, block_len, kv_len, page_table, T)
+        rc = self.lib.cs_paged_attention(self.handle, blocks, ptr, row, head, H, mask, window, D ** -0.5 if scale is None else scale, out.data_ptr(),
+                                         None if lse is None else lse.data_ptr(), _stream())
+        self._check(rc, "cs_paged_attention")
+        return out if lse is None else (out, lse)
+
+    def cs_paged_status(self):
+        """Waits for the stream; what the device found wrong since the last call (CS_OK: nothing)."""
+        return self.lib.cs_paged_status(self.handle, _stream())

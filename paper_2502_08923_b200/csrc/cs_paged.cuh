@@ -1,0 +1,256 @@
+// Shared by the operators around the paged KV cache: the handle, what kernels get of a cache and its blocks, and how the
+// attention kernels deal their work out.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "cs_common.cuh"
+
+static constexpr int kPagedMaxCtas = 160;      // CTAs of an attention launch at most
+static constexpr int kPagedMaxRows = 256;      // query rows (rows x heads of a group) of one work item at most
+static constexpr int kPagedTile = 128;         // keys of a tile, the unit work is dealt out in
+static constexpr int kPagedMaxSeqs = 1024;     // sequences of one attention launch; more are further launches
+
+struct PagedView {
+  char *k, *v;
+  long long page_stride, head_stride, slot_stride;   // elements
+  int n_pages, page_size, page_shift, n_kv_heads;
+};
+
+struct BlocksView {
+  const int *start, *len, *kv_len, *table;
+  int n_seqs, table_width, rows;
+};
+
+struct cs_paged_cache {
+  cs_paged_config cfg;
+  PagedView view;
+  CUtensorMap tmK, tmV;        // [page][head][slot][dim], boxes of 64 dims x up to 128 slots (head sizes 64 and 128)
+  int* status;                 // device status word
+  int* counters;               // pieces of an item that are done, by the CTA that holds its first tile; 0 between launches
+  float* parts;                // un-normalised pieces [kPagedMaxCtas][2][kPagedMaxRows][head_dim]
+  float* parts_ml;             // their (reference point, sum) [kPagedMaxCtas][2][kPagedMaxRows][2]
+  int num_sms;
+  unsigned attr_set;           // shared-memory opt-ins made, a bit per kernel instance
+  unsigned long long wait_limit_ns;
+  char err[256];
+};
+
+// what an attention launch is about
+struct PagedAttnArgs {
+  PagedView kv;
+  BlocksView blk;
+  const char* q;
+  long long q_row, q_head;     // strides, elements
+  char* out;
+  float* lse;
+  int n_heads, group;          // query heads, and per KV head
+  int mask, window;
+  float scale_log2e, scale;
+  int item_rows;               // query rows (row of the block x head of the group) per work item
+  float *parts, *parts_ml;
+  int *counters, *status;
+  unsigned long long wait_ns;
+};
+
+cs_status cs_launch_paged_few(cs_paged_cache* c, const PagedAttnArgs& a, cudaStream_t st);
+
+#ifdef __CUDACC__
+namespace {
+
+// One sequence's block as the device finds it.  `keys` is where the highest key any row attends to ends.
+struct PagedBlock {
+  int start, len, kv;
+};
+
+// false: the sequence is left out (the flag says why); len 0 is in order
+__device__ __forceinline__ bool paged_block(const BlocksView& s, int page_size, int b, bool own_rows, PagedBlock& o, int* status) {
+  o.start = __ldcg(s.start + b);
+  o.len = __ldcg(s.len + b);
+  o.kv = __ldcg(s.kv_len + b);
+  int flag = 0;
+  if (o.len < 0 || o.kv < 0 || (o.len > 0 && (o.start < 0 || (long long)o.start + o.len > s.rows))) flag = CS_DEV_BADARG;
+  else {
+    const long long keys = (long long)o.kv + (own_rows ? o.len : 0), room = (long long)s.table_width * page_size;
+    if (o.len > 0 && (keys > room || (long long)o.kv + o.len > 0x7fffff00ll)) flag = CS_DEV_CAPACITY;
+  }
+  if (flag != 0) {
+    atomicOr(status, flag);
+    o.len = 0;
+  }
+  return flag == 0;
+}
+
+// Keys [lo, hi) that rows r0 .. r1 of a block attend to between them.
+__device__ __forceinline__ void paged_range(int mask, int window, int len, int kv, int r0, int r1, int& lo, int& hi) {
+  hi = mask == CS_MASK_CAUSAL ? kv + r1 + 1 : mask == CS_MASK_PREFIX ? kv : kv + len;
+  lo = window > 0 ? max(0, kv + r0 + 1 - window) : 0;
+}
+
+// Work is dealt out in key tiles.  An item is one (sequence, KV head, group of item_rows query rows); its tiles are the
+// kPagedTile-aligned ones its rows attend to, one at least (a row without keys is written too).  Items in the order
+// (sequence, head, row group) make one line of tiles, of which every CTA takes an equal run: CTA i of n the tiles
+// [total * i / n, total * (i + 1) / n).  So no CTA waits for another, none has more than one tile more than the
+// others whatever the lengths are, and at most two items of a CTA are shared with others.
+__device__ __forceinline__ int paged_item_tiles(const PagedAttnArgs& a, int len, int kv, int rg) {
+  const int G = a.group, r0 = (int)((long long)rg * a.item_rows / G);
+  const int r1 = (int)min((long long)len - 1, (((long long)rg + 1) * a.item_rows - 1) / G);
+  int lo, hi;
+  paged_range(a.mask, a.window, len, kv, r0, r1, lo, hi);
+  return hi > lo ? (hi + kPagedTile - 1) / kPagedTile - lo / kPagedTile : 1;
+}
+__device__ __forceinline__ int paged_row_groups(const PagedAttnArgs& a, int len) {
+  return (int)(((long long)len * a.group + a.item_rows - 1) / a.item_rows);
+}
+
+// a block's items of one KV head, by a whole warp: their tiles together
+__device__ __forceinline__ long long paged_block_tiles(const PagedAttnArgs& a, int len, int kv, int lane) {
+  const int n = paged_row_groups(a, len);
+  long long sum = 0;
+  for (int g = lane; g < n; g += 32) sum += paged_item_tiles(a, len, kv, g);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  return sum;
+}
+
+struct PagedPlan {                              // in shared memory
+  long long before[kPagedMaxSeqs + 1];          // tiles of the sequences before this one
+  int start[kPagedMaxSeqs], len[kPagedMaxSeqs], kv[kPagedMaxSeqs];
+  long long warp_sum[32];
+  int tall[kPagedMaxSeqs], n_tall;              // sequences whose row groups a warp adds up
+};
+
+// By all threads of a CTA of at least 128 (a multiple of 32).  Ends with a barrier.
+__device__ __forceinline__ void paged_plan(const PagedAttnArgs& a, PagedPlan& p) {
+  const int tid = threadIdx.x, nt = blockDim.x, warp = tid >> 5, lane = tid & 31, B = a.blk.n_seqs;
+  if (tid == 0) p.n_tall = 0;
+  __syncthreads();
+  for (int b = tid; b < B; b += nt) {
+    PagedBlock k;
+    paged_block(a.blk, a.kv.page_size, b, a.mask != CS_MASK_PREFIX, k, a.status);
+    p.start[b] = k.start; p.len[b] = k.len; p.kv[b] = k.kv;
+    const int n = paged_row_groups(a, k.len);
+    long long t = 0;
+    if (n <= 4) {
+      for (int g = 0; g < n; ++g) t += paged_item_tiles(a, k.len, k.kv, g);
+    } else {
+      p.tall[atomicAdd(&p.n_tall, 1)] = b;
+    }
+    p.before[b + 1] = t * a.kv.n_kv_heads;
+  }
+  __syncthreads();
+  for (int i = warp; i < p.n_tall; i += nt >> 5) {
+    const int b = p.tall[i];
+    const long long t = paged_block_tiles(a, p.len[b], p.kv[b], lane);
+    if (lane == 0) p.before[b + 1] = t * a.kv.n_kv_heads;
+  }
+  if (tid == 0) p.before[0] = 0;
+  __syncthreads();
+  // running sums, in the same order whoever takes part: a thread's run, the warp's, the CTA's
+  const int per = (B + nt - 1) / nt, first = tid * per, last = min(B, first + per);
+  long long run = 0;
+  for (int b = first; b < last; ++b) run += p.before[b + 1];
+  long long inc = run;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long v = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += v;
+  }
+  if (lane == 31) p.warp_sum[warp] = inc;
+  __syncthreads();
+  long long at = inc - run;
+  for (int w = 0; w < warp; ++w) at += p.warp_sum[w];
+  for (int b = first; b < last; ++b) {
+    at += p.before[b + 1];
+    p.before[b + 1] = at;
+  }
+  __syncthreads();
+}
+
+// A CTA's share of one item.
+struct PagedPiece {
+  int start, len, kv;          // the block
+  int seq, head, rg;
+  int lo, hi;                  // keys the item's rows attend to between them
+  int tile0, n_tiles;          // first tile (absolute: key / kPagedTile) and how many are this CTA's
+  int item_tiles;
+  long long item_at;           // where the item's tiles begin in the line
+  bool whole;
+};
+
+// Piece that begins at tile `at` of the line, by a whole warp (all lanes get it); `end`: where the CTA's run ends.
+__device__ __forceinline__ PagedPiece paged_piece(const PagedAttnArgs& a, const PagedPlan& p, long long at, long long end, int lane) {
+  PagedPiece o;
+  int b = 0;
+  for (int step = 512; step > 0; step >>= 1)
+    if (b + step <= a.blk.n_seqs - 1 && p.before[b + step] <= at) b += step;
+  o.seq = b; o.start = p.start[b]; o.len = p.len[b]; o.kv = p.kv[b];
+  const long long all = p.before[b + 1] - p.before[b], per_head = all / a.kv.n_kv_heads;
+  long long rest = at - p.before[b];
+  o.head = (int)(rest / per_head);
+  rest -= o.head * per_head;
+  // row group: 32 at a time
+  const int n = paged_row_groups(a, o.len);
+  int g0 = 0, tiles = 0;
+  for (;; g0 += 32) {
+    const int t = g0 + lane < n ? paged_item_tiles(a, o.len, o.kv, g0 + lane) : 0;
+    int inc = t;
+#pragma unroll
+    for (int s = 1; s < 32; s <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, inc, s);
+      if (lane >= s) inc += v;
+    }
+    const unsigned ends_behind = __ballot_sync(0xffffffffu, (long long)inc > rest);
+    if (ends_behind != 0 || g0 + 32 >= n) {
+      const int l = ends_behind != 0 ? __ffs(ends_behind) - 1 : 0;
+      tiles = __shfl_sync(0xffffffffu, t, l);
+      rest -= __shfl_sync(0xffffffffu, inc, l) - tiles;
+      g0 += l;
+      break;
+    }
+    rest -= __shfl_sync(0xffffffffu, inc, 31);
+  }
+  o.rg = g0;
+  const int G = a.group, r0 = (int)((long long)g0 * a.item_rows / G);
+  const int r1 = (int)min((long long)o.len - 1, (((long long)g0 + 1) * a.item_rows - 1) / G);
+  paged_range(a.mask, a.window, o.len, o.kv, r0, r1, o.lo, o.hi);
+  o.item_tiles = tiles;
+  o.item_at = at - rest;
+  o.tile0 = (o.hi > o.lo ? o.lo / kPagedTile : 0) + (int)rest;
+  o.n_tiles = (int)min((long long)tiles - rest, end - at);
+  o.whole = o.n_tiles == tiles;
+  return o;
+}
+// the CTA (of n) whose run holds tile x of a line of `total`
+__device__ __forceinline__ int paged_owner(long long x, long long total, int n) { return (int)(((x + 1) * n - 1) / total); }
+
+// 2^x, hardware approximation (relative error about 2^-22; -inf gives 0)
+__device__ __forceinline__ float paged_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float paged_lg2(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+template <typename T> struct PagedType;
+template <> struct PagedType<__nv_bfloat16> {
+  static __device__ __forceinline__ uint32_t pack(float x, float y) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+};
+template <> struct PagedType<__half> {
+  static __device__ __forceinline__ uint32_t pack(float x, float y) {
+    const __half2 h = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+  }
+  static __device__ __forceinline__ float2 unpack(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+};
+
+}  // namespace
+#endif
