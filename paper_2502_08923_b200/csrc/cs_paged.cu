@@ -12,7 +12,7 @@
 
 namespace {
 
-constexpr int kThreads = 256, kUnroll = 4;
+constexpr int kWarps = 8, kThreads = kWarps * 32;
 
 // what k_heads does with a row
 struct HeadsArgs {
@@ -20,7 +20,8 @@ struct HeadsArgs {
   char *yq, *yk;                     // destinations of rows (yk: unless they go to pages)
   long long q_row, q_head, k_row, k_head, v_row, v_head, yq_row, yq_head, yk_row, yk_head;   // elements
   const char *q_gain, *k_gain;
-  int n_q, n_k, n_v;
+  int n_q, n_k, n_v, n_rows;
+  int warps_per_row;                 // 1, 2, 4 or 8
   const int* pos;                    // positions of rows, unless blocks give them
   const float* rope;
   int n_positions, rot_dim;
@@ -30,6 +31,25 @@ struct HeadsArgs {
   int* status;
 };
 
+// two fp32 values in one 64-bit register and the packed fp32 arithmetic of this architecture
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2(f32x2 r, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(r)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
 template <typename T> __device__ __forceinline__ void load8(const char* p, uint32_t (&w)[sizeof(T) == 4 ? 8 : 4]) {
   const uint4 a = __ldcg(reinterpret_cast<const uint4*>(p));
   w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
@@ -38,19 +58,21 @@ template <typename T> __device__ __forceinline__ void load8(const char* p, uint3
     w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
   }
 }
-template <typename T, int N> __device__ __forceinline__ void widen(const uint32_t (&w)[N], float (&f)[8]) {
-  if constexpr (N == 8) {
+template <typename T, int N> __device__ __forceinline__ void widen(const uint32_t (&w)[N], f32x2 (&f)[4]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(w[i]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (N == 8) {
+      f[i] = pack2(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+    } else {
       const float2 x = PagedType<T>::unpack(w[i]);
-      f[2 * i] = x.x; f[2 * i + 1] = x.y;
+      f[i] = pack2(x.x, x.y);
     }
   }
 }
-template <typename T> __device__ __forceinline__ void store8(char* p, const float (&f)[8]) {
+template <typename T> __device__ __forceinline__ void store8(char* p, const f32x2 (&v)[4]) {
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) unpack2(v[i], f[2 * i], f[2 * i + 1]);
   if constexpr (sizeof(T) == 4) {
     reinterpret_cast<float4*>(p)[0] = make_float4(f[0], f[1], f[2], f[3]);
     reinterpret_cast<float4*>(p)[1] = make_float4(f[4], f[5], f[6], f[7]);
@@ -58,149 +80,198 @@ template <typename T> __device__ __forceinline__ void store8(char* p, const floa
     *reinterpret_cast<uint4*>(p) = make_uint4(PagedType<T>::pack(f[0], f[1]), PagedType<T>::pack(f[2], f[3]), PagedType<T>::pack(f[4], f[5]), PagedType<T>::pack(f[6], f[7]));
   }
 }
-// eight gains; without any, ones
+__device__ __forceinline__ float nan_f() { return __int_as_float(0x7fc00000); }
+// eight gains
 template <typename T> __device__ __forceinline__ void gain8(const char* g, int chunk, float (&f)[8]) {
-  if (g == nullptr) {
+  uint32_t w[sizeof(T) == 4 ? 8 : 4];
+  const uint4* p = reinterpret_cast<const uint4*>(g + chunk * 8 * (int)sizeof(T));
+  const uint4 x = p[0];
+  w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+  if constexpr (sizeof(T) == 4) {
+    const uint4 y = p[1];
+    w[4] = y.x; w[5] = y.y; w[6] = y.z; w[7] = y.w;
+  }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = 1.f;
-  } else {
-    uint32_t w[sizeof(T) == 4 ? 8 : 4];
-    load8<T>(g + (long long)chunk * 8 * sizeof(T), w);
-    widen<T>(w, f);
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      f[2 * i] = __uint_as_float(w[2 * i]); f[2 * i + 1] = __uint_as_float(w[2 * i + 1]);
+    } else {
+      const float2 y = PagedType<T>::unpack(w[i]);
+      f[2 * i] = y.x; f[2 * i + 1] = y.y;
+    }
   }
 }
 
 template <typename S, typename D, int DH, bool kPaged>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 2)
 k_heads(HeadsArgs a) {
   CS_PDL_PROLOGUE();
-  constexpr int kLanes = DH / 8, kGroups = kThreads / kLanes, kW = sizeof(S) == 4 ? 8 : 4;
-  __shared__ int s_seq;
-  const int tid = threadIdx.x, grp = tid / kLanes, c = tid % kLanes;
-  const long long row = blockIdx.x;
-  const int n_heads = a.n_q + a.n_k + a.n_v;
+  constexpr int kLanes = DH / 16, kPer = 32 / kLanes, kW = sizeof(S) == 4 ? 8 : 4;    // lanes of a head, heads of a unit, words of a chunk
+  constexpr int kFlight = sizeof(S) == 4 ? 2 : 3;
+  __shared__ int s_seq[kWarps], s_pos[kWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = lane % kLanes, sub = lane / kLanes;
+  const long long row0 = (long long)blockIdx.x * (kWarps / a.warps_per_row), row = row0 + warp / a.warps_per_row;
+  // a row's units: up to kPer neighbouring heads, of queries, then keys, then values
+  const int uq = (a.n_q + kPer - 1) / kPer, uk = uq + (a.n_k + kPer - 1) / kPer, units = row < a.n_rows ? uk + (a.n_v + kPer - 1) / kPer : 0;
+  const int step = a.warps_per_row, u0 = warp % step;
+  // this lane's chunks: partners of the rotation, or two neighbours behind what is rotated
+  const int half = a.rot_dim >> 4;
+  const bool rotated = pair < half;
+  const int c0 = rotated ? pair : 2 * pair, c1 = rotated ? pair + half : c0 + 1;
 
-  uint32_t w[kUnroll][kW];
-  auto source = [&](int h) -> const char* {
-    if (h < a.n_q) return a.q + (row * a.q_row + h * a.q_head) * (long long)sizeof(S) + c * 8 * sizeof(S);
-    h -= a.n_q;
-    if (h < a.n_k) return a.k + (row * a.k_row + h * a.k_head) * (long long)sizeof(S) + c * 8 * sizeof(S);
-    h -= a.n_k;
-    return a.v + (row * a.v_row + h * a.v_head) * (long long)sizeof(S) + c * 8 * sizeof(S);
-  };
-  auto load = [&](int h0) {
-#pragma unroll
-    for (int i = 0; i < kUnroll; ++i) {
-      const int h = h0 + i * kGroups;
-      if (h < n_heads) load8<S>(source(h), w[i]);
+  // Fetching runs kFlight units ahead of the rest.
+  uint32_t w[kFlight][2][kW];
+  int fu = u0, f_end = 0, f_h = 0, f_n = 0;      // next unit, where its kind's units end, this lane's head of it, the kind's heads
+  const char* f_p = nullptr;
+  long long f_step = 0;
+  auto fetch = [&](uint32_t (&d)[2][kW]) {
+    if (fu >= f_end && fu < units) {             // (the same in the whole warp)
+      const int kind = fu < uq ? 0 : fu < uk ? 1 : 2;
+      const long long rs = kind == 0 ? a.q_row : kind == 1 ? a.k_row : a.v_row, hs = kind == 0 ? a.q_head : kind == 1 ? a.k_head : a.v_head;
+      f_h = (fu - (kind == 0 ? 0 : kind == 1 ? uq : uk)) * kPer + sub;
+      f_n = kind == 0 ? a.n_q : kind == 1 ? a.n_k : a.n_v;
+      f_end = kind == 0 ? uq : kind == 1 ? uk : units;
+      f_p = (kind == 0 ? a.q : kind == 1 ? a.k : a.v) + (row * rs + f_h * hs + c0 * 8) * (long long)sizeof(S);
+      f_step = step * kPer * hs * (long long)sizeof(S);
     }
+    if (fu < units && f_h < f_n) {
+      load8<S>(f_p, d[0]);
+      load8<S>(f_p + (c1 - c0) * 8 * (int)sizeof(S), d[1]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kW; ++j) d[0][j] = d[1][j] = 0u;
+    }
+    fu += step; f_h += step * kPer; f_p += f_step;
   };
-  load(grp);                                     // (whose row it is takes two loads in a row: these are under way meanwhile)
+#pragma unroll
+  for (int i = 0; i < kFlight; ++i) fetch(w[i]);   // (whose row it is, and where it goes, takes three loads in a row: these are under way meanwhile)
 
-  int pos;
-  long long at = 0;                              // element of the pools where slot (page, head 0) of this row begins
+  int pos = 0;
+  long long at = 0;                              // element of the pools where this row's slot of head 0 begins
   bool stored = true;
   if constexpr (kPaged) {
-    // the block this row belongs to
-    if (tid == 0) s_seq = -1;
+    // the blocks these rows belong to
+    if (threadIdx.x < kWarps) s_seq[threadIdx.x] = -1;
     __syncthreads();
-    for (int b = tid; b < a.blk.n_seqs; b += kThreads) {
-      const int start = __ldcg(a.blk.start + b), len = __ldcg(a.blk.len + b);
-      if (row >= start && row - start < len) s_seq = b;
-    }
-    if (row == 0)                                // one CTA reports blocks that are left out
-      for (int b = tid; b < a.blk.n_seqs; b += kThreads) {
-        PagedBlock k;
-        paged_block(a.blk, a.kv.page_size, b, true, k, a.status);
+    const int n_here = kWarps / a.warps_per_row;
+    for (int b = threadIdx.x; b < a.blk.n_seqs; b += kThreads) {
+      const int start = __ldcg(a.blk.start + b), len = __ldcg(a.blk.len + b), kv = __ldcg(a.blk.kv_len + b);
+      const int flag = paged_block_flag(a.blk, a.kv.page_size, true, start, len, kv);
+      if (flag != 0) {
+        if (blockIdx.x == 0) atomicOr(a.status, flag);
+      } else {
+        for (int i = 0; i < n_here; ++i)
+          if (row0 + i >= start && row0 + i - start < len) { s_seq[i] = b; s_pos[i] = kv + (int)(row0 + i - start); }
       }
-    __syncthreads();
-    const int b = s_seq;
-    if (b < 0) return;
-    PagedBlock k;
-    if (!paged_block(a.blk, a.kv.page_size, b, true, k, a.status)) return;
-    pos = k.kv + (int)(row - k.start);
-    const int page = __ldcg(a.blk.table + (long long)b * a.blk.table_width + (pos >> a.kv.page_shift));
-    if ((unsigned)page >= (unsigned)a.kv.n_pages) {
-      stored = false;
-      if (tid == 0) atomicOr(a.status, CS_DEV_BADARG);
-    } else {
-      at = page * a.kv.page_stride + (long long)(pos & (a.kv.page_size - 1)) * a.kv.slot_stride;
     }
+    __syncthreads();
+    const int b = s_seq[warp / a.warps_per_row];
+    if (b < 0 || row >= a.n_rows) return;
+    pos = s_pos[warp / a.warps_per_row];
     if (a.rot_dim > 0 && pos >= a.n_positions) {
-      if (tid == 0) atomicOr(a.status, CS_DEV_CAPACITY);
+      if (lane == 0) atomicOr(a.status, CS_DEV_CAPACITY);
       return;
     }
+    const int page = __ldcg(a.blk.table + (long long)b * a.blk.table_width + (pos >> a.kv.page_shift));
+    stored = (unsigned)page < (unsigned)a.kv.n_pages;
+    if (stored) at = page * a.kv.page_stride + (long long)(pos & (a.kv.page_size - 1)) * a.kv.slot_stride;
+    else if (lane == 0) atomicOr(a.status, CS_DEV_BADARG);
   } else {
-    pos = a.rot_dim > 0 ? __ldcg(a.pos + row) : 0;
+    if (row >= a.n_rows) return;
+    if (a.rot_dim > 0) pos = __ldcg(a.pos + row);
   }
 
-  // rotation factors of this lane's elements; its partner's lane; what a chunk that is not rotated has: y = r x gain
-  const int half = a.rot_dim >> 4;               // chunks of h elements
-  const int pc = c < half ? c + half : c < 2 * half ? c - half : c;
-  float cs[8], sn[8];
-  if (pc == c) {
+  // y0 = r (x0 C0 - x1 S1), y1 = r (x1 C1 + x0 S0), C = gain cos, S = gain sin: worked out once for the queries and once for the keys.  (Table
+  // and gains are read through L1: all warps of a row want the same.)
+  f32x2 C0[4], C1[4], S0[4], S1[4];
+  int end = 0, h = 0, n = 0;
+  bool norm = false, plain = false;              // (values are neither normed nor rotated)
+  char* dst = nullptr;
+  long long dst_step = 0;
+  for (int ub = u0; ub < units; ub += kFlight * step) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) { cs[i] = 1.f; sn[i] = 0.f; }
-  } else if ((unsigned)pos >= (unsigned)a.n_positions) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) cs[i] = sn[i] = __int_as_float(0x7fc00000);
-  } else {
-    const float* r = a.rope + (long long)pos * a.rot_dim + (c < half ? c : c - half) * 8;
-    const float sign = c < half ? -1.f : 1.f;
-#pragma unroll
-    for (int i = 0; i < 8; i += 4) {
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(r + i)), y = __ldcg(reinterpret_cast<const float4*>(r + 8 * half + i));
-      cs[i] = x.x; cs[i + 1] = x.y; cs[i + 2] = x.z; cs[i + 3] = x.w;
-      sn[i] = sign * y.x; sn[i + 1] = sign * y.y; sn[i + 2] = sign * y.z; sn[i + 3] = sign * y.w;
-    }
-  }
-  const int lane = tid & 31, partner = (lane & ~(kLanes - 1)) | pc;
-
-  for (int h0 = grp; h0 - grp < n_heads; h0 += kUnroll * kGroups) {
-    if (h0 != grp) load(h0);
-#pragma unroll
-    for (int i = 0; i < kUnroll; ++i) {
-      if (h0 - grp + i * kGroups >= n_heads) break;          // (the same in the whole CTA)
-      const int h = h0 + i * kGroups;
-      const bool is_v = h >= a.n_q + a.n_k, is_q = h < a.n_q, live = h < n_heads;
-      float x[8], y[8], p[8];
-      uint32_t pw[kW];
-#pragma unroll
-      for (int j = 0; j < kW; ++j) {
-        if (!live) w[i][j] = 0u;
-        pw[j] = __shfl_sync(0xffffffffu, w[i][j], partner);
-      }
-      widen<S>(w[i], x);
-      widen<S>(pw, p);
-      const char* gain = is_v ? nullptr : is_q ? a.q_gain : a.k_gain;
-      float sq = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sq = fmaf(x[j], x[j], sq);
-#pragma unroll
-      for (int o = 1; o < kLanes; o <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-      if (!live) continue;
-      if (is_v) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = x[j];
-      } else {
-        const float r = gain != nullptr ? 1.f / sqrtf(sq * (1.f / DH) + a.eps) : 1.f;
-        float g[8], gp[8];
-        gain8<D>(gain, c, g);
-        gain8<D>(gain, pc, gp);
-        // (a chunk that is not rotated takes no part of its "partner", or infinities would make NaN of it)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = pc == c ? x[j] * r * g[j] : fmaf(x[j] * r * g[j], cs[j], p[j] * r * gp[j] * sn[j]);
-      }
-      if (is_q) {
-        store8<D>(a.yq + (row * a.yq_row + h * a.yq_head + c * 8) * (long long)sizeof(D), y);
-      } else if constexpr (kPaged) {
-        if (stored) {
-          const long long e = at + (long long)(is_v ? h - a.n_q - a.n_k : h - a.n_q) * a.kv.head_stride + c * 8;
-          store8<D>((is_v ? a.kv.v : a.kv.k) + e * (long long)sizeof(D), y);
+    for (int i = 0; i < kFlight; ++i) {
+      const int u = ub + i * step;
+      if (u >= units) break;                     // (the same in the whole warp)
+      if (u >= end) {
+        const int kind = u < uq ? 0 : u < uk ? 1 : 2;
+        h = (u - (kind == 0 ? 0 : kind == 1 ? uq : uk)) * kPer + sub;
+        n = kind == 0 ? a.n_q : kind == 1 ? a.n_k : a.n_v;
+        end = kind == 0 ? uq : kind == 1 ? uk : units;
+        plain = kind == 2;
+        if (kind == 0) {
+          dst = a.yq + (row * a.yq_row + h * a.yq_head + c0 * 8) * (long long)sizeof(D);
+          dst_step = step * kPer * a.yq_head * (long long)sizeof(D);
+        } else if constexpr (kPaged) {
+          dst = (kind == 1 ? a.kv.k : a.kv.v) + (at + h * a.kv.head_stride + c0 * 8) * (long long)sizeof(D);
+          dst_step = step * kPer * a.kv.head_stride * (long long)sizeof(D);
+          if (!stored) n = 0;
+        } else {
+          dst = a.yk + (row * a.yk_row + h * a.yk_head + c0 * 8) * (long long)sizeof(D);
+          dst_step = step * kPer * a.yk_head * (long long)sizeof(D);
         }
-      } else {
-        store8<D>(a.yk + (row * a.yk_row + (h - a.n_q) * a.yk_head + c * 8) * (long long)sizeof(D), y);
+        const char* gain = kind == 0 ? a.q_gain : kind == 1 ? a.k_gain : nullptr;
+        norm = gain != nullptr;
+        if (!plain) {
+          float g0[8], g1[8];
+          if (norm) {
+            gain8<D>(gain, c0, g0);
+            gain8<D>(gain, c1, g1);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g0[j] = g1[j] = 1.f;
+          }
+          const float4* r = reinterpret_cast<const float4*>(a.rope + (long long)pos * a.rot_dim + c0 * 8);
+          const bool in_table = (unsigned)pos < (unsigned)a.n_positions;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const float4 one = make_float4(1.f, 1.f, 1.f, 1.f), none = make_float4(nan_f(), nan_f(), nan_f(), nan_f());
+            const float4 x = !rotated ? one : in_table ? r[j] : none, y = !rotated ? one : in_table ? r[2 * half + j] : none;
+            C0[2 * j] = pack2(g0[4 * j] * x.x, g0[4 * j + 1] * x.y); C0[2 * j + 1] = pack2(g0[4 * j + 2] * x.z, g0[4 * j + 3] * x.w);
+            C1[2 * j] = pack2(g1[4 * j] * x.x, g1[4 * j + 1] * x.y); C1[2 * j + 1] = pack2(g1[4 * j + 2] * x.z, g1[4 * j + 3] * x.w);
+            S0[2 * j] = pack2(g0[4 * j] * y.x, g0[4 * j + 1] * y.y); S0[2 * j + 1] = pack2(g0[4 * j + 2] * y.z, g0[4 * j + 3] * y.w);
+            S1[2 * j] = pack2(-g1[4 * j] * y.x, -g1[4 * j + 1] * y.y); S1[2 * j + 1] = pack2(-g1[4 * j + 2] * y.z, -g1[4 * j + 3] * y.w);
+          }
+        }
       }
+      f32x2 x0[4], x1[4];
+      widen<S>(w[i][0], x0);
+      widen<S>(w[i][1], x1);
+      fetch(w[i]);
+      if (!plain) {
+        if (norm) {
+          f32x2 s2 = mul2(x0[0], x0[0]);
+#pragma unroll
+          for (int j = 1; j < 4; ++j) s2 = fma2(x0[j], x0[j], s2);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s2 = fma2(x1[j], x1[j], s2);
+          float lo, hi;
+          unpack2(s2, lo, hi);
+          float sq = lo + hi;
+#pragma unroll
+          for (int o = 1; o < kLanes; o <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+          const float r = rsqrtf(sq * (1.f / DH) + a.eps);
+          const f32x2 r2 = pack2(r, r);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) { x0[j] = mul2(x0[j], r2); x1[j] = mul2(x1[j], r2); }
+        }
+        if (rotated) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f32x2 y0 = fma2(x0[j], C0[j], mul2(x1[j], S1[j]));
+            x1[j] = fma2(x1[j], C1[j], mul2(x0[j], S0[j]));
+            x0[j] = y0;
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) { x0[j] = mul2(x0[j], C0[j]); x1[j] = mul2(x1[j], C1[j]); }
+        }
+      }
+      if (h < n) {
+        store8<D>(dst, x0);
+        store8<D>(dst + (c1 - c0) * 8 * (int)sizeof(D), x1);
+      }
+      h += step * kPer; dst += dst_step;
     }
   }
 }
@@ -223,11 +294,16 @@ k_rope_table(float* table, int n_positions, int rot_dim, double log_theta) {
 thread_local char t_paged_err[256] = "";
 
 template <typename S, typename D, bool kPaged>
-cudaError_t launch_heads(const HeadsArgs& a, int rows, int head_dim, cudaStream_t st) {
+cudaError_t launch_heads(HeadsArgs a, int rows, int head_dim, cudaStream_t st) {
+  const int per = 512 / head_dim, units = cs_ceil_div(a.n_q, per) + cs_ceil_div(a.n_k, per) + cs_ceil_div(a.n_v, per);
+  a.n_rows = rows;
+  a.warps_per_row = 8;
+  while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)rows * a.warps_per_row > 2 * 148 * 32)) a.warps_per_row /= 2;
+  const dim3 grid((unsigned)(((long long)rows * a.warps_per_row + kWarps - 1) / kWarps));
   switch (head_dim) {
-    case 32: return cs_launch_pdl(k_heads<S, D, 32, kPaged>, dim3(rows), dim3(kThreads), 0, st, a);
-    case 64: return cs_launch_pdl(k_heads<S, D, 64, kPaged>, dim3(rows), dim3(kThreads), 0, st, a);
-    default: return cs_launch_pdl(k_heads<S, D, 128, kPaged>, dim3(rows), dim3(kThreads), 0, st, a);
+    case 32: return cs_launch_pdl(k_heads<S, D, 32, kPaged>, grid, dim3(kThreads), 0, st, a);
+    case 64: return cs_launch_pdl(k_heads<S, D, 64, kPaged>, grid, dim3(kThreads), 0, st, a);
+    default: return cs_launch_pdl(k_heads<S, D, 128, kPaged>, grid, dim3(kThreads), 0, st, a);
   }
 }
 

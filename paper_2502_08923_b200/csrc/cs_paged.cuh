@@ -58,27 +58,11 @@ cs_status cs_launch_paged_few(cs_paged_cache* c, const PagedAttnArgs& a, cudaStr
 #ifdef __CUDACC__
 namespace {
 
-// One sequence's block as the device finds it.  `keys` is where the highest key any row attends to ends.
-struct PagedBlock {
-  int start, len, kv;
-};
-
-// false: the sequence is left out (the flag says why); len 0 is in order
-__device__ __forceinline__ bool paged_block(const BlocksView& s, int page_size, int b, bool own_rows, PagedBlock& o, int* status) {
-  o.start = __ldcg(s.start + b);
-  o.len = __ldcg(s.len + b);
-  o.kv = __ldcg(s.kv_len + b);
-  int flag = 0;
-  if (o.len < 0 || o.kv < 0 || (o.len > 0 && (o.start < 0 || (long long)o.start + o.len > s.rows))) flag = CS_DEV_BADARG;
-  else {
-    const long long keys = (long long)o.kv + (own_rows ? o.len : 0), room = (long long)s.table_width * page_size;
-    if (o.len > 0 && (keys > room || (long long)o.kv + o.len > 0x7fffff00ll)) flag = CS_DEV_CAPACITY;
-  }
-  if (flag != 0) {
-    atomicOr(status, flag);
-    o.len = 0;
-  }
-  return flag == 0;
+// What is wrong with a sequence's block (0: nothing).  `own_rows`: its own rows need room in the pages.
+__device__ __forceinline__ int paged_block_flag(const BlocksView& s, int page_size, bool own_rows, int start, int len, int kv) {
+  if (len < 0 || kv < 0 || (len > 0 && (start < 0 || (long long)start + len > s.rows))) return CS_DEV_BADARG;
+  const long long keys = (long long)kv + (own_rows ? len : 0), room = (long long)s.table_width * page_size;
+  return len > 0 && (keys > room || (long long)kv + len > 0x7fffff00ll) ? CS_DEV_CAPACITY : 0;
 }
 
 // Keys [lo, hi) that rows r0 .. r1 of a block attend to between them.
@@ -126,13 +110,18 @@ __device__ __forceinline__ void paged_plan(const PagedAttnArgs& a, PagedPlan& p)
   if (tid == 0) p.n_tall = 0;
   __syncthreads();
   for (int b = tid; b < B; b += nt) {
-    PagedBlock k;
-    paged_block(a.blk, a.kv.page_size, b, a.mask != CS_MASK_PREFIX, k, a.status);
-    p.start[b] = k.start; p.len[b] = k.len; p.kv[b] = k.kv;
-    const int n = paged_row_groups(a, k.len);
+    const int start = __ldcg(a.blk.start + b), kv = __ldcg(a.blk.kv_len + b);
+    int len = __ldcg(a.blk.len + b);
+    const int flag = paged_block_flag(a.blk, a.kv.page_size, a.mask != CS_MASK_PREFIX, start, len, kv);
+    if (flag != 0) {                            // (left out)
+      if (blockIdx.x == 0) atomicOr(a.status, flag);
+      len = 0;
+    }
+    p.start[b] = start; p.len[b] = len; p.kv[b] = kv;
+    const int n = paged_row_groups(a, len);
     long long t = 0;
     if (n <= 4) {
-      for (int g = 0; g < n; ++g) t += paged_item_tiles(a, k.len, k.kv, g);
+      for (int g = 0; g < n; ++g) t += paged_item_tiles(a, len, kv, g);
     } else {
       p.tall[atomicAdd(&p.n_tall, 1)] = b;
     }
