@@ -15,7 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libcopyspec.so")
 HEADER = os.path.join(ROOT, "include", "copyspec.h")
 NATIVE_SOURCE = os.path.join(CSRC, "cs_python.cpp")
-SOURCES = ["cs_match.cu", "cs_index.cu", "cs_gemm.cu", "cs_gemm_pair.cu", "cs_chain.cu", "cs_small.cu", "cs_layers.cu", "cs_attn.cu", "cs_attn_tc.cu", "cs_attn_tcw.cu", "cs_api.cu", "cs_drafted.cu", "cs_paged.cu", "cs_paged_attn.cu"]
+SOURCES = ["cs_match.cu", "cs_index.cu", "cs_gemm.cu", "cs_gemm_pair.cu", "cs_chain.cu", "cs_small.cu", "cs_layers.cu", "cs_attn.cu", "cs_attn_tc.cu", "cs_attn_tcw.cu", "cs_api.cu", "cs_drafted.cu", "cs_paged.cu", "cs_paged_attn.cu", "cs_paged_attn_tc.cu"]
 
 
 def native_path() -> str:

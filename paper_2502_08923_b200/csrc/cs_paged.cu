@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(kThreads, 2)
 k_heads(HeadsArgs a) {
   CS_PDL_PROLOGUE();
   constexpr int kLanes = DH / 16, kPer = 32 / kLanes, kW = sizeof(S) == 4 ? 8 : 4;    // lanes of a head, heads of a unit, words of a chunk
-  constexpr int kFlight = sizeof(S) == 4 ? 2 : 3;
+  constexpr int kFlight = sizeof(S) == 4 ? 2 : 4;
   __shared__ int s_seq[kWarps], s_pos[kWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = lane % kLanes, sub = lane / kLanes;
   const long long row0 = (long long)blockIdx.x * (kWarps / a.warps_per_row), row = row0 + warp / a.warps_per_row;
@@ -298,7 +298,7 @@ cudaError_t launch_heads(HeadsArgs a, int rows, int head_dim, cudaStream_t st) {
   const int per = 512 / head_dim, units = cs_ceil_div(a.n_q, per) + cs_ceil_div(a.n_k, per) + cs_ceil_div(a.n_v, per);
   a.n_rows = rows;
   a.warps_per_row = 8;
-  while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)rows * a.warps_per_row > 2 * 148 * 32)) a.warps_per_row /= 2;
+  while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)rows * a.warps_per_row > 148 * 64)) a.warps_per_row /= 2;
   const dim3 grid((unsigned)(((long long)rows * a.warps_per_row + kWarps - 1) / kWarps));
   switch (head_dim) {
     case 32: return cs_launch_pdl(k_heads<S, D, 32, kPaged>, grid, dim3(kThreads), 0, st, a);
@@ -440,8 +440,9 @@ cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void
   int dev = 0, sms = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     return refuse(CS_ERR_CUDA, "no device");
-  cs_paged_cache* c = static_cast<cs_paged_cache*>(calloc(1, sizeof(cs_paged_cache)));
+  cs_paged_cache* c = static_cast<cs_paged_cache*>(aligned_alloc(64, (sizeof(cs_paged_cache) + 63) / 64 * 64));   // (operand maps: 64 bytes)
   if (c == nullptr) return refuse(CS_ERR_CAPACITY, "out of host memory");
+  memset(c, 0, sizeof(*c));
   c->cfg = *cfg;
   c->num_sms = sms < kPagedMaxCtas ? sms : kPagedMaxCtas;
   int shift = 0;
@@ -455,6 +456,11 @@ cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void
   const char* wl = getenv("CS_WAIT_LIMIT_US");
   const long long us = wl != nullptr ? atoll(wl) : 0;
   c->wait_limit_ns = us > 0 ? (unsigned long long)us * 1000ull : 2000000000ull;
+  if (cfg->head_dim != 32 && cs_paged_tc_maps(c) != CS_OK) {
+    snprintf(t_paged_err, sizeof(t_paged_err), "cs_paged_create: %s", c->err);
+    free(c);
+    return CS_ERR_CUDA;
+  }
   const cudaError_t e = cudaMemsetAsync(ws, 0, l.parts, static_cast<cudaStream_t>(stream));
   if (e != cudaSuccess) {
     free(c);
@@ -541,12 +547,14 @@ cs_status cs_paged_attention(cs_paged_cache* c, const cs_blocks* blocks, const v
   a.scale = scale; a.scale_log2e = (float)(1.4426950408889634 * (double)scale);
   a.parts = c->parts; a.parts_ml = c->parts_ml; a.counters = c->counters; a.status = c->status;
   a.wait_ns = c->wait_limit_ns;
+  // 16 query rows per KV head are a tile of the kernel for few rows, which takes heads of 32 whatever their rows
+  const bool few = c->cfg.head_dim == 32 || (long long)blocks->rows * a.group <= 16ll * blocks->n_seqs;
   for (int b = 0; b < blocks->n_seqs; b += kPagedMaxSeqs) {      // (a launch's plan holds so many)
     PagedAttnArgs p = a;
     p.blk.n_seqs = blocks->n_seqs - b < kPagedMaxSeqs ? blocks->n_seqs - b : kPagedMaxSeqs;
     p.blk.start += b; p.blk.len += b; p.blk.kv_len += b;
     p.blk.table += (long long)b * blocks->table_width;
-    const cs_status r = cs_launch_paged_few(c, p, static_cast<cudaStream_t>(stream));
+    const cs_status r = few ? cs_launch_paged_few(c, p, static_cast<cudaStream_t>(stream)) : cs_launch_paged_tc(c, p, static_cast<cudaStream_t>(stream));
     if (r != CS_OK) return r;
   }
   return CS_OK;

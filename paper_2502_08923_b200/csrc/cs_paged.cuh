@@ -54,6 +54,8 @@ struct PagedAttnArgs {
 };
 
 cs_status cs_launch_paged_few(cs_paged_cache* c, const PagedAttnArgs& a, cudaStream_t st);
+cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& a, cudaStream_t st);
+cs_status cs_paged_tc_maps(cs_paged_cache* c);   // the pools' operand maps
 
 #ifdef __CUDACC__
 namespace {
@@ -209,6 +211,29 @@ __device__ __forceinline__ PagedPiece paged_piece(const PagedAttnArgs& a, const 
   o.n_tiles = (int)min((long long)tiles - rest, end - at);
   o.whole = o.n_tiles == tiles;
   return o;
+}
+// The piece after one, if the CTA's run goes on behind it.
+__device__ __forceinline__ bool paged_next(const PagedAttnArgs& a, const PagedPlan& plan, PagedPiece& p, long long end) {
+  const long long at = p.item_at + p.item_tiles;
+  if (at >= end) return false;
+  if (p.rg + 1 < paged_row_groups(a, p.len)) ++p.rg;
+  else {
+    p.rg = 0;
+    if (++p.head == a.kv.n_kv_heads) {
+      p.head = 0;
+      do ++p.seq; while (plan.before[p.seq + 1] <= at);
+      p.start = plan.start[p.seq]; p.len = plan.len[p.seq]; p.kv = plan.kv[p.seq];
+    }
+  }
+  // (rows x heads stay below 2^31)
+  const int r0 = p.rg * a.item_rows / a.group, r1 = min(p.len - 1, (p.rg * a.item_rows + a.item_rows - 1) / a.group);
+  paged_range(a.mask, a.window, p.len, p.kv, r0, r1, p.lo, p.hi);
+  p.tile0 = p.hi > p.lo ? p.lo / kPagedTile : 0;
+  p.item_tiles = p.hi > p.lo ? (p.hi + kPagedTile - 1) / kPagedTile - p.tile0 : 1;
+  p.item_at = at;
+  p.n_tiles = (int)min((long long)p.item_tiles, end - at);
+  p.whole = p.n_tiles == p.item_tiles;
+  return true;
 }
 // the CTA (of n) whose run holds tile x of a line of `total`
 __device__ __forceinline__ int paged_owner(long long x, long long total, int n) { return (int)(((x + 1) * n - 1) / total); }

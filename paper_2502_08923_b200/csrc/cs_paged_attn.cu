@@ -81,29 +81,6 @@ k_paged_few(PagedAttnArgs a) {
   const uint32_t my_ring = (uint32_t)__cvta_generic_to_shared(ring) + (uint32_t)(warp * kStages * 2 * kSliceBytes);
   const uint8_t* my_ring_p = ring + warp * kStages * 2 * kSliceBytes;
 
-  // ---- the piece after one, if the run goes on behind it
-  auto next_piece = [&](PagedPiece& p) -> bool {
-    const long long at = p.item_at + p.item_tiles;
-    if (at >= run1) return false;
-    if (p.rg + 1 < paged_row_groups(a, p.len)) ++p.rg;
-    else {
-      p.rg = 0;
-      if (++p.head == a.kv.n_kv_heads) {
-        p.head = 0;
-        do ++p.seq; while (plan.before[p.seq + 1] <= at);
-        p.start = plan.start[p.seq]; p.len = plan.len[p.seq]; p.kv = plan.kv[p.seq];
-      }
-    }
-    const int r0 = p.rg * kRows / a.group, r1 = min(p.len - 1, (p.rg * kRows + kRows - 1) / a.group);
-    paged_range(a.mask, a.window, p.len, p.kv, r0, r1, p.lo, p.hi);
-    p.tile0 = p.hi > p.lo ? p.lo / kPagedTile : 0;
-    p.item_tiles = p.hi > p.lo ? (p.hi + kPagedTile - 1) / kPagedTile - p.tile0 : 1;
-    p.item_at = at;
-    p.n_tiles = (int)min((long long)p.item_tiles, run1 - at);
-    p.whole = p.n_tiles == p.item_tiles;
-    return true;
-  };
-
   // ---- the fetching side: runs kStages slices ahead, across pieces
   PagedPiece f = paged_piece(a, plan, run0, run1, lane);
   PagedPiece p = f;
@@ -132,7 +109,7 @@ k_paged_few(PagedAttnArgs a) {
       if (++f_stage == kStages) f_stage = 0;
       if (++f_tile == f.n_tiles) {
         f_tile = 0;
-        f_more = next_piece(f);
+        f_more = paged_next(a, plan, f, run1);
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -359,7 +336,7 @@ k_paged_few(PagedAttnArgs a) {
                      PagedType<T>::pack(acc[4] * inv, acc[5] * inv), PagedType<T>::pack(acc[6] * inv, acc[7] * inv));
       if (a.lse != nullptr && c8 == 0) a.lse[r] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
     }
-    more = next_piece(p);
+    more = paged_next(a, plan, p, run1);
     if (more) __syncthreads();                   // (the exchange rows are free again)
   }
   asm volatile("cp.async.wait_all;" ::: "memory");

@@ -1,0 +1,639 @@
+// Attention of tall blocks over a paged KV cache on the 5th-generation tensor cores (Sec. 3.2; App. B.2), head sizes 64 and 128.
+//
+// The mathematics is that of cs_paged_attn.cu.  Query rows (row of the block x head of the group) are the M = 128 of both products, so that TMEM
+// lane = query row and one thread has a whole row of scores:
+//     S [128 x 128 keys] = Q K_tile^T      (both from shared memory)
+//     O [128 x D]       += P V_tile        (P in tensor memory, over the scores it comes from; V as it lies in the cache, MN-major)
+// A CTA (one per SM, persistent, runs of tiles as cs_paged.cuh deals them out) has two slots of S/P and O columns, each with a warpgroup for its softmax, so
+// that the tensor cores work on one slot while the other's weights are made.  An item of more than 128 rows fills both slots with
+// different rows over the same tiles (each K and V tile is fetched once for 256 rows); of fewer, the slots take the tiles
+// in turn and are added up at the end, from tensor memory.
+//
+// Steps s = 0, 1, ... alternate between the slots.  The MMA warp issues S(0) S(1), then P V(s) and S(s + 2) for every s: S(s + 2) overwrites P(s), which the products'
+// order keeps.  A slot's scores being there means that its product before is done, so a softmax that moves its reference point may
+// rescale O at once.  The reference point moves only past 2^8 (softmax does not depend on it, and weights up to 2^8 are as exact as weights up
+// to 1), which leaves rescaling to a few tiles.  Weights are rounded once, to the cache's type, on their way into the second product; their sum is
+// taken before.
+//
+// Warps 0-7 softmax, 8 issues MMAs, 9 and 10 fetch K and V tiles (a copy per page and 64 dims, page-table entries 32 at a time), 11 fetches queries.
+//
+// Keys no row of the item sees may hold anything: their scores are masked, their V rows set to zero in shared memory.  Tiles that some rows see and
+// others do not are looked through for values that are not finite (0 x inf is not 0): those are set to zero as well, and what
+// they do to the rows that see them is added where the results are written.
+//
+// Every wait is bounded: on expiry the CTA flags CS_DEV_TIMEOUT, stops issuing, walks through its barriers, drains what is in flight, frees its TMEM and returns.
+#include <type_traits>
+
+#include "cs_paged.cuh"
+#include "cs_tcgen.cuh"
+
+namespace {
+
+constexpr int kThreads = 384, kMmaWarp = 8, kKWarp = 9, kQWarp = 11;   // (10: V)
+constexpr int kM = 128;                                            // query rows of a slot
+constexpr uint32_t kSCol = 0, kOCol = 256, kTmemCols = 512;        // slot x 128 columns each
+template <int DH> constexpr int kTileBytes = kPagedTile * DH * 2;  // of K, of V, and of a slot's queries
+template <int DH> constexpr int kStages = DH == 128 ? 4 : 8;
+constexpr int kCtl = 512;
+template <int DH> constexpr int kTcSmem = 1024 + (kStages<DH> + 2) * kTileBytes<DH> + kCtl + 2 * kM * 8 + (int)sizeof(PagedPlan);
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2, int c3) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+               ::"r"(dst), "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+__device__ __forceinline__ void umma_ta(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+               ::"r"(tmem_d), "r"(tmem_a), "l"(bdesc), "r"(idesc), "r"(acc) : "memory");
+}
+#define CS_R32(v) "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]), \
+  "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]), "=f"(v[16]), "=f"(v[17]), "=f"(v[18]), "=f"(v[19]), "=f"(v[20]), "=f"(v[21]), "=f"(v[22]), "=f"(v[23]), \
+  "=f"(v[24]), "=f"(v[25]), "=f"(v[26]), "=f"(v[27]), "=f"(v[28]), "=f"(v[29]), "=f"(v[30]), "=f"(v[31])
+// 32 columns of this thread's lane; valid after ld_wait and ld_valid
+__device__ __forceinline__ void ld32(uint32_t taddr, float* v) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : CS_R32(v) : "r"(taddr));
+}
+__device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void ld_valid(float* v) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 8)
+    asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]), "+f"(v[i + 6]), "+f"(v[i + 7])::"memory");
+}
+__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t* v) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
+        "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+        "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
+}
+__device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* v) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+               ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
+                 "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
+}
+__device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pack2(float lo, float hi) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
+}
+__device__ __forceinline__ void unpack2(f32x2 r, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(r)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+  return d;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+__device__ __forceinline__ void store32b(void* dst, const uint32_t* v) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+// barrier of the eight softmax warps
+__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+
+template <typename T>
+__device__ __forceinline__ uint32_t odd_halves(uint32_t w) {      // bits of the halves that are not finite
+  constexpr uint32_t e = std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;
+  return ((w & e) == e ? 0xffffu : 0u) | (((w >> 16) & e) == e ? 0xffff0000u : 0u);
+}
+
+template <typename T, int DH>
+__global__ void __launch_bounds__(kThreads, 1)
+k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmQ, PagedAttnArgs a, int q_box_bytes) {
+  constexpr int kTB = kTileBytes<DH>, kNS = kStages<DH>, kHalves = DH / 64, kHalf = kPagedTile * 128;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* ring = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));   // [stage][64 dims][128 keys][128 B]
+  uint8_t* sq = ring + kNS * kTB;                                       // [slot][64 dims][128 rows][128 B]
+  uint64_t* bars = reinterpret_cast<uint64_t*>(sq + 2 * kTB);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kNS + 16);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  volatile int* s_odd = reinterpret_cast<volatile int*>(tmem_slot + 2);      // values that are not finite were taken out (by the parity of the piece)
+  int* s_last = reinterpret_cast<int*>(tmem_slot + 4);
+  float2* s_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(bars) + kCtl);      // [slot][128 rows]
+  PagedPlan& plan = *reinterpret_cast<PagedPlan*>(s_ml + 2 * kM);
+  const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8 * kNS, b_s = b_empty + 8 * kNS, b_p = b_s + 16, b_o = b_p + 16, b_qfull = b_o + 16, b_qfree = b_qfull + 8,
+                 b_drain = b_qfree + 8;
+  const int tid = threadIdx.x, warp = (int)uniform(tid >> 5), lane = tid & 31;
+
+  CS_PDL_PROLOGUE();
+  if (tid == 0) {
+    for (int s = 0; s < kNS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_empty + 8 * s, 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(b_s + 8 * s, 1); mbar_init(b_p + 8 * s, 4); mbar_init(b_o + 8 * s, 1); }
+    mbar_init(b_qfull, 1); mbar_init(b_qfree, 1); mbar_init(b_drain, 1);
+    *s_abort = 0; s_odd[0] = 0; s_odd[1] = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kMmaWarp) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(kTmemCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  fence_before();
+  paged_plan(a, plan);                            // (ends with a barrier)
+  fence_after();
+  const uint32_t tmem = uniform(*tmem_slot);
+  const long long total = plan.before[a.blk.n_seqs];
+  const int n_cta = (int)min((long long)gridDim.x, total), cta = blockIdx.x;
+  const long long run0 = cta < n_cta ? total * cta / n_cta : 0, run1 = cta < n_cta ? total * (cta + 1) / n_cta : 0;
+
+  // Bounded waits.  Once one has run out all others return at once.
+  auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
+    if (mbar_try_wait(bar, parity)) return true;
+    unsigned long long t0 = 0;
+    for (uint32_t it = 0;; ++it) {
+      if (mbar_try_wait(bar, parity)) return true;
+      if ((it & 15u) == 15u) {
+        if (*s_abort) return false;
+        const unsigned long long now = globaltimer_ns();
+        if (t0 == 0) t0 = now;
+        else if (now - t0 > a.wait_ns) {
+          *s_abort = 1;
+          atomicOr(a.status, CS_DEV_TIMEOUT);
+          return false;
+        }
+      }
+    }
+  };
+  auto wait_warp = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, wait(bar, parity)); };
+  const int slot_rows = a.item_rows / 2;          // query rows of a slot
+  auto two_slots = [&](const PagedPiece& p) { return p.len * a.group - p.rg * a.item_rows > slot_rows; };
+  // Order of the ring: K and V tiles in turn where the slots share them, else K0 K1 V0 K2 V1 ... (entry of step s, of n steps)
+  auto k_entry = [](bool both, int s) { return both ? s & ~1 : s < 2 ? s : 2 * s - 1; };
+  auto v_entry = [](bool both, int s, int n) { return both ? s | 1 : s + min(s + 2, n); };
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (run1 > run0) {
+      PagedPiece p = paged_piece(a, plan, run0, run1, lane);
+      uint32_t base = 0, piece = 0;               // ring entries before this piece; pieces
+      bool ok = true;
+      if (warp == kMmaWarp) {
+        // ---------------------------------------------------------------- MMA issuer
+        constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u;
+        constexpr uint32_t idesc_s = (1u << 4) | kType | ((uint32_t)(kPagedTile >> 3) << 17) | ((uint32_t)(kM >> 4) << 24);
+        constexpr uint32_t idesc_o = (1u << 4) | kType | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(kM >> 4) << 24);   // B (= V) is MN-major
+        const uint64_t dq0 = desc_kmajor(smem_u32(sq)), dk0 = desc_kmajor(smem_u32(ring)), dv0 = desc_mnmajor(smem_u32(ring), kHalf);
+        uint32_t p_phase[2] = {0, 0};
+        for (bool more = true; more && ok;) {
+          const bool both = two_slots(p);
+          const int n = both ? 2 * p.n_tiles : p.n_tiles;
+          ok = wait_warp(b_qfull, piece & 1);
+          auto scores = [&](int s) {
+            const uint32_t e = base + k_entry(both, s), st = e % kNS;
+            if (!(both && (s & 1))) ok = wait_warp(b_full + 8 * st, (e / kNS) & 1);
+            if (!ok) return;
+            fence_after();
+            if (elect_one()) {
+              const uint64_t dk = dk0 + st * (kTB >> 4), dq = dq0 + (both && (s & 1) ? kTB >> 4 : 0);
+#pragma unroll
+              for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                  umma_bf16(tmem + kSCol + (s & 1) * 128, dq + h * (kHalf >> 4) + 2 * k, dk + h * (kHalf >> 4) + 2 * k, idesc_s, (h | k) ? 1u : 0u);
+              if (!both || (s & 1)) umma_commit(b_empty + 8 * st);
+              umma_commit(b_s + 8 * (s & 1));
+              if (s == n - 1) umma_commit(b_qfree);
+            }
+          };
+          if (ok) scores(0);
+          if (ok && n > 1) scores(1);
+          for (int s = 0; s < n && ok; ++s) {
+            const uint32_t e = base + v_entry(both, s, n), st = e % kNS;
+            ok = wait_warp(b_full + 8 * st, (e / kNS) & 1) && wait_warp(b_p + 8 * (s & 1), p_phase[s & 1]);
+            if (!ok) break;
+            p_phase[s & 1] ^= 1;
+            fence_after();
+            if (elect_one()) {
+              const uint64_t dv = dv0 + st * (kTB >> 4);
+#pragma unroll
+              for (int k = 0; k < 8; ++k)           // 16 keys per instruction
+                umma_ta(tmem + kOCol + (s & 1) * 128, tmem + kSCol + (s & 1) * 128 + k * 8, dv + k * (2048 >> 4), idesc_o, (s > 1 || k > 0) ? 1u : 0u);
+              if (!both || (s & 1)) umma_commit(b_empty + 8 * st);
+              if (s >= n - 2) umma_commit(b_o + 8 * (s & 1));
+            }
+            if (s + 2 < n) scores(s + 2);
+          }
+          base += 2 * p.n_tiles;
+          ++piece;
+          more = paged_next(a, plan, p, run1);
+        }
+        if (!ok) {                                   // what was issued must be done before its memory goes away
+          if (elect_one()) umma_commit(b_drain);
+          __syncwarp();
+          const unsigned long long t0 = globaltimer_ns();
+          while (!mbar_try_wait(b_drain, 0) && globaltimer_ns() - t0 < a.wait_ns) {}
+        }
+      } else if (warp == kQWarp) {
+        // ---------------------------------------------------------------- queries
+        for (bool more = true; more && ok;) {
+          const bool both = two_slots(p);
+          if (piece > 0) ok = wait_warp(b_qfree, (piece - 1) & 1);
+          if (!ok) break;
+          if (elect_one()) {
+            mbar_expect_tx(b_qfull, (uint32_t)(q_box_bytes * kHalves * (both ? 2 : 1)));
+            for (int s = 0; s < (both ? 2 : 1); ++s)
+              for (int h = 0; h < kHalves; ++h)
+                tma_load_3d(smem_u32(sq) + s * kTB + h * kHalf, &tmQ, b_qfull, 64 * h, p.head * a.group, p.start + (p.rg * a.item_rows + s * slot_rows) / a.group);
+          }
+          ++piece;
+          more = paged_next(a, plan, p, run1);
+        }
+        // a copy that nobody waited for must land before the shared memory goes away
+        const unsigned long long t0 = globaltimer_ns();
+        while (!mbar_try_wait(b_qfull, (piece - 1) & 1) && globaltimer_ns() - t0 < a.wait_ns) {}
+      } else {
+        // ---------------------------------------------------------------- K tiles, V tiles
+        const bool is_k = warp == kKWarp;
+        const CUtensorMap* tm = is_k ? &tmK : &tmV;
+        const int rows = min(a.kv.page_size, kPagedTile), per_tile = kPagedTile / rows, shift = a.kv.page_shift;
+        uint32_t last_e[kNS], asked = 0;             // (bit per stage: a copy was started there)
+#pragma unroll
+        for (int i = 0; i < kNS; ++i) last_e[i] = 0;
+        for (bool more = true; more && ok;) {
+          const bool both = two_slots(p);
+          const int n = both ? 2 * p.n_tiles : p.n_tiles, inc = both ? 2 : 1;
+          int entry = 0, first = -64;                // this lane's page-table entry, and of which page the first lane has one
+          const int* table = a.blk.table + (long long)p.seq * a.blk.table_width;
+          for (int s = 0; s < n && ok; s += inc) {
+            const uint32_t e = base + (is_k ? k_entry(both, s) : v_entry(both, s, n)), st = e % kNS;
+            const int key0 = (p.tile0 + s / inc) * kPagedTile, page0 = key0 >> shift;
+            // pages of the tile that hold keys of the item
+            const int pa = max(key0, p.lo), pz = min(key0 + kPagedTile, p.hi);
+            int j0 = 0, j1 = 0;
+            if (pz > pa) { j0 = (pa >> shift) - page0; j1 = ((pz - 1) >> shift) - page0 + 1; }
+            if (page0 < first || page0 + per_tile > first + 32) {
+              first = page0;
+              const int page = first + lane;
+              entry = -1;
+              if (((long long)(page + 1) << shift) > p.lo && ((long long)page << shift) < p.hi) entry = __ldcg(table + page);
+            }
+            ok = wait_warp(b_empty + 8 * st, ((e / kNS) & 1) ^ 1);
+            if (!ok) break;
+            if (elect_one()) mbar_expect_tx(b_full + 8 * st, (uint32_t)((j1 - j0) * rows * 128 * kHalves));
+            __syncwarp();
+            for (int j = j0; j < j1; ++j) {
+              int page = (int)__shfl_sync(0xffffffffu, entry, page0 + j - first);
+              if ((unsigned)page >= (unsigned)a.kv.n_pages) {      // (a page behind the last one reads as zeros)
+                page = a.kv.n_pages;
+                if (lane == 0) atomicOr(a.status, CS_DEV_BADARG);
+              }
+              const int slot = (key0 + j * rows) & (a.kv.page_size - 1);
+              if (elect_one()) {
+                const uint32_t dst = smem_u32(ring) + st * kTB + j * rows * 128;
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h) tma_load_4d(dst + h * kHalf, tm, b_full + 8 * st, 64 * h, slot, p.head, page);
+              }
+            }
+            asked |= 1u << st;
+#pragma unroll
+            for (int i = 0; i < kNS; ++i) if (i == (int)st) last_e[i] = e;
+          }
+          base += 2 * p.n_tiles;
+          more = paged_next(a, plan, p, run1);
+        }
+        if (!ok) {                                   // copies that nobody will consume must land before the shared memory goes away
+#pragma unroll
+          for (int i = 0; i < kNS; ++i) {
+            const unsigned long long t0 = globaltimer_ns();
+            if (asked >> i & 1u)
+              while (!mbar_try_wait(b_full + 8 * i, (last_e[i] / kNS) & 1) && globaltimer_ns() - t0 < a.wait_ns) {}
+          }
+        }
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    // ------------------------------------------------------------------ softmax and results: one thread per query row
+    if (run1 > run0) {
+      PagedPiece p = paged_piece(a, plan, run0, run1, lane);
+      const int slot = warp >> 2, row = tid & 127, G = a.group;
+      const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_col = lanes + kSCol + slot * 128, o_col = lanes + kOCol + slot * 128;
+      uint32_t base = 0, s_phase = 0, o_phase[2] = {0, 0}, piece = 0;
+      for (bool more = true; more; ++piece) {
+        const bool both = two_slots(p);
+        const int n = both ? 2 * p.n_tiles : p.n_tiles, first_row = p.rg * a.item_rows + (both ? slot * slot_rows : 0);
+        const int mrow = first_row + row;
+        const bool live = row < slot_rows && mrow < p.len * G;
+        int lo = 0, hi = 0, all_lo, all_hi, x;
+        if (live) paged_range(a.mask, a.window, p.len, p.kv, mrow / G, mrow / G, lo, hi);
+        const int last_row = min(p.len * G, (p.rg + 1) * a.item_rows) - 1;
+        paged_range(a.mask, a.window, p.len, p.kv, p.rg * a.item_rows / G, p.rg * a.item_rows / G, x, all_hi);   // keys that all rows of the item see
+        paged_range(a.mask, a.window, p.len, p.kv, last_row / G, last_row / G, all_lo, x);
+        const bool some = __any_sync(0xffffffffu, live);       // (a warp without rows leaves its lanes to chance: nobody reads them)
+        const unsigned span = hi > lo ? hi - lo : 0;
+        float m = -INFINITY;
+        f32x2 l2 = pack2(0.f, 0.f);
+        const f32x2 sc2 = pack2(a.scale_log2e, a.scale_log2e);
+
+        for (int s = slot; s < n; s += 2) {
+          const int key0 = (p.tile0 + (both ? s >> 1 : s)) * kPagedTile;
+          const bool mixed = key0 < all_lo || key0 + kPagedTile > all_hi;
+          bool ok = wait(b_s + 8 * slot, s_phase);
+          s_phase ^= 1;
+          ok = __all_sync(0xffffffffu, ok);
+          fence_after();
+          if (some && ok) {
+            float v[128];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) ld32(s_col + 32 * c, v + 32 * c);
+            ld_wait();
+#pragma unroll
+            for (int c = 0; c < 4; ++c) ld_valid(v + 32 * c);
+            if (mixed) {
+              const int d = key0 - lo;
+#pragma unroll
+              for (int j = 0; j < 128; ++j) v[j] = (unsigned)(d + j) < span ? v[j] : -INFINITY;
+            }
+            float mx[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+            for (int j = 4; j < 128; j += 8) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) mx[i] = fmaxf(fmaxf(mx[i], v[j + i]), j + 4 + i < 128 ? v[j + 4 + i] : -INFINITY);
+            }
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2e;
+            const bool moves = m == -INFINITY ? top > m : top > m + 8.f;
+            if (__any_sync(0xffffffffu, moves)) {
+              const float corr = !moves ? 1.f : m == -INFINITY ? 0.f : paged_ex2(m - top);
+              if (moves) m = top;
+              float l0, l1;
+              unpack2(l2, l0, l1);
+              l2 = pack2(l0 * corr, l1 * corr);
+              if (s > 1) {
+#pragma unroll
+                for (int c = 0; c < DH / 32; ++c) {
+                  float o[32];
+                  ld32(o_col + 32 * c, o);
+                  ld_wait();
+                  ld_valid(o);
+#pragma unroll
+                  for (int j = 0; j < 32; ++j) o[j] *= corr;
+                  st32(o_col + 32 * c, reinterpret_cast<const uint32_t*>(o));
+                }
+              }
+            }
+            const float nm = m == -INFINITY ? 0.f : -m;
+            const f32x2 nm2 = pack2(nm, nm);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              uint32_t w[16];
+#pragma unroll
+              for (int j = 0; j < 16; ++j) {
+                float x0, x1;
+                unpack2(fma2(pack2(v[32 * c + 2 * j], v[32 * c + 2 * j + 1]), sc2, nm2), x0, x1);
+                x0 = paged_ex2(x0); x1 = paged_ex2(x1);
+                l2 = add2(l2, pack2(x0, x1));
+                w[j] = PagedType<T>::pack(x0, x1);
+              }
+              st16(s_col + 16 * c, w);
+            }
+            st_wait();
+          }
+          if (mixed && ok) {
+            // V rows that no row of the item sees become zeros, and so do values that are not finite where not all rows see them
+            const uint32_t e = base + v_entry(both, s, n), st = e % kNS;
+            if (wait(b_full + 8 * st, (e / kNS) & 1)) {
+              const int key = key0 + row;
+              uint8_t* vrow = ring + st * kTB + row * 128;
+              if (key < p.lo || key >= p.hi) {
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                  for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(vrow + h * kHalf + ((c + lane) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+              } else if (key < all_lo || key >= all_hi) {
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+                  for (int c = 0; c < 8; ++c) {
+                    volatile uint32_t* at = reinterpret_cast<volatile uint32_t*>(vrow + h * kHalf + ((c + lane) & 7) * 16);
+                    uint4 x4 = *reinterpret_cast<const uint4*>(vrow + h * kHalf + ((c + lane) & 7) * 16);
+                    const uint32_t b0 = odd_halves<T>(x4.x), b1 = odd_halves<T>(x4.y), b2 = odd_halves<T>(x4.z), b3 = odd_halves<T>(x4.w);
+                    if (b0 | b1 | b2 | b3) {
+                      s_odd[piece & 1] = 1;          // (before the value goes: whoever finds it gone knows)
+                      __threadfence_block();
+                      at[0] = x4.x & ~b0; at[1] = x4.y & ~b1; at[2] = x4.z & ~b2; at[3] = x4.w & ~b3;
+                    }
+                  }
+              }
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          }
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(b_p + 8 * slot);
+        }
+
+        // ---- results
+        float l0, l1;
+        unpack2(l2, l0, l1);
+        float l = l0 + l1;
+        const bool mine = n > slot, other = n > 1 - slot;          // did this slot, the other slot have a step?
+        if (mine) wait(b_o + 8 * slot, o_phase[slot]);
+        if (!both && other) wait(b_o + 8 * (1 - slot), o_phase[1 - slot]);
+        if (n > 0) o_phase[0] ^= 1;
+        if (n > 1) o_phase[1] ^= 1;
+        fence_after();
+        float k_mine = 1.f, k_other = 0.f;
+        if (!both) {
+          // the slots' rows are the same: each warpgroup adds up half of the columns, from tensor memory
+          s_ml[slot * kM + row] = make_float2(m, l);
+          softmax_sync();
+          const float2 o_ml = s_ml[(1 - slot) * kM + row];
+          const bool nothing = o_ml.x == -INFINITY && o_ml.y == 0.f;
+          const float M = fmaxf(m, o_ml.x);
+          k_mine = m == -INFINITY ? 0.f : paged_ex2(m - M);
+          k_other = o_ml.x == -INFINITY ? 0.f : paged_ex2(o_ml.x - M);
+          l = (m == -INFINITY && l == 0.f ? 0.f : l * k_mine) + (nothing ? 0.f : o_ml.y * k_other);
+          m = M;
+        }
+        const bool odd = s_odd[piece & 1] != 0;
+        const bool good = *s_abort == 0;
+        const int c_first = both ? 0 : slot * (DH / 2), c_last = both ? DH : c_first + DH / 2;
+        const int item_row = (both ? slot * slot_rows : 0) + row;
+        const bool opens = p.item_at >= run0;
+        const long long part = ((long long)cta * 2 + (opens ? 1 : 0)) * kPagedMaxRows + item_row;
+        const long long out_row = (long long)(p.start + (live ? mrow / G : 0)) * a.n_heads + p.head * G + (live ? mrow % G : 0);
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        if (some && good) {
+          for (int c0 = c_first; c0 < c_last; c0 += 32) {
+            float o[32];
+            if (both) {
+              ld32(o_col + c0, o);
+              ld_wait();
+              ld_valid(o);
+            } else {
+              float o2[32];
+              ld32(lanes + kOCol + slot * 128 + c0, o);
+              ld32(lanes + kOCol + (1 - slot) * 128 + c0, o2);
+              ld_wait();
+              ld_valid(o);
+              ld_valid(o2);
+              // (a slot without steps holds what an earlier item left)
+#pragma unroll
+              for (int j = 0; j < 32; ++j) o[j] = (mine ? o[j] * k_mine : 0.f) + (other ? o2[j] * k_other : 0.f);
+            }
+            if (odd && live) {
+              for (int t = 0; t < p.n_tiles; ++t) {
+                const int key0 = (p.tile0 + t) * kPagedTile;
+                if (key0 >= all_lo && key0 + kPagedTile <= all_hi) continue;
+                for (int key = max(key0, lo); key < min(key0 + kPagedTile, hi); ++key) {
+                  if (key >= all_lo && key < all_hi) continue;
+                  const int page = __ldcg(a.blk.table + (long long)p.seq * a.blk.table_width + (key >> a.kv.page_shift));
+                  if ((unsigned)page >= (unsigned)a.kv.n_pages) continue;
+                  const char* src = a.kv.v + (page * a.kv.page_stride + p.head * a.kv.head_stride + (long long)(key & (a.kv.page_size - 1)) * a.kv.slot_stride + c0) * 2;
+#pragma unroll
+                  for (int j = 0; j < 16; ++j) {
+                    const uint32_t w = __ldcg(reinterpret_cast<const unsigned*>(src) + j), bits = odd_halves<T>(w);
+                    const float2 f = PagedType<T>::unpack(w);
+                    if (bits & 0xffffu) o[2 * j] += f.x;
+                    if (bits >> 16) o[2 * j + 1] += f.y;
+                  }
+                }
+              }
+            }
+            if (live) {
+              if (p.whole) {
+                uint32_t w[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j) w[j] = PagedType<T>::pack(o[2 * j] * inv, o[2 * j + 1] * inv);
+                char* dst = a.out + (out_row * DH + c0) * 2;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(dst + 16 * j) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+              } else {
+                float* dst = a.parts + part * DH + c0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) store32b(dst + 8 * j, reinterpret_cast<const uint32_t*>(o) + 8 * j);
+              }
+            }
+          }
+          if (live && (both || slot == 0)) {
+            if (!p.whole) __stcg(reinterpret_cast<float2*>(a.parts_ml) + part, make_float2(m, l));
+            else if (a.lse != nullptr) a.lse[out_row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+          }
+        }
+        fence_before();
+        if (!p.whole) {
+          // ---- pieces of an item that several CTAs share: the last one to arrive adds them up, in the order of the keys
+          __threadfence();
+          softmax_sync();
+          const int c0 = paged_owner(p.item_at, total, n_cta), c1 = paged_owner(p.item_at + p.item_tiles - 1, total, n_cta);
+          if (tid == 0) {
+            int last = 0;
+            if (good && *s_abort == 0) {
+              last = atomicAdd(a.counters + c0, 1) == c1 - c0;
+              if (last) a.counters[c0] = 0;
+            }
+            *s_last = last;
+          }
+          softmax_sync();
+          if (*s_last) {
+            __threadfence();
+            const int rows = min(a.item_rows, p.len * G - p.rg * a.item_rows);
+            for (int i = tid; i < rows * (DH / 8); i += 256) {
+              const int r = i / (DH / 8), c8 = i % (DH / 8) * 8, mr = p.rg * a.item_rows + r;
+              auto at = [&](int c) { return ((long long)c * 2 + (c == c0 ? 1 : 0)) * kPagedMaxRows + r; };
+              float M = -INFINITY, L = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+              for (int c = c0; c <= c1; ++c) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at(c)).x);
+#pragma unroll 4
+              for (int c = c0; c <= c1; ++c) {
+                const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at(c));
+                const float4 v0 = __ldcg(reinterpret_cast<const float4*>(a.parts + at(c) * DH + c8)), v1 = __ldcg(reinterpret_cast<const float4*>(a.parts + at(c) * DH + c8 + 4));
+                const float k = ml.x == -INFINITY ? 0.f : paged_ex2(ml.x - M);
+                if (ml.x == -INFINITY && ml.y == 0.f) continue;      // (it saw nothing)
+                L = fmaf(k, ml.y, L);
+                acc[0] = fmaf(k, v0.x, acc[0]); acc[1] = fmaf(k, v0.y, acc[1]); acc[2] = fmaf(k, v0.z, acc[2]); acc[3] = fmaf(k, v0.w, acc[3]);
+                acc[4] = fmaf(k, v1.x, acc[4]); acc[5] = fmaf(k, v1.y, acc[5]); acc[6] = fmaf(k, v1.z, acc[6]); acc[7] = fmaf(k, v1.w, acc[7]);
+              }
+              const float iv = L == 0.f ? 0.f : 1.f / L;
+              const long long r_out = (long long)(p.start + mr / G) * a.n_heads + p.head * G + mr % G;
+              *reinterpret_cast<uint4*>(a.out + (r_out * DH + c8) * 2) =
+                  make_uint4(PagedType<T>::pack(acc[0] * iv, acc[1] * iv), PagedType<T>::pack(acc[2] * iv, acc[3] * iv), PagedType<T>::pack(acc[4] * iv, acc[5] * iv),
+                             PagedType<T>::pack(acc[6] * iv, acc[7] * iv));
+              if (a.lse != nullptr && c8 == 0) a.lse[r_out] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+            }
+          }
+        }
+        softmax_sync();                                // both slots' O, the exchange rows and this piece's flag are free again
+        if (tid == 0) s_odd[piece & 1] = 0;
+        base += 2 * p.n_tiles;
+        more = paged_next(a, plan, p, run1);
+      }
+    }
+  }
+  // ---------------------------------------------------------------------- teardown
+  fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encoder() {
+  static EncodeFn fn = []() -> EncodeFn {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    return cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess ? reinterpret_cast<EncodeFn>(p) : nullptr;
+  }();
+  return fn;
+}
+cs_status encode(cs_paged_cache* c, CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+  EncodeFn enc = encoder();
+  const cuuint32_t ones[4] = {1, 1, 1, 1};
+  const CUresult r = enc == nullptr ? CUDA_ERROR_NOT_FOUND
+                                    : enc(tm, c->cfg.dtype == CS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void*>(base), dims, strides, box,
+                                          ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r == CUDA_SUCCESS) return CS_OK;
+  snprintf(c->err, sizeof(c->err), "cuTensorMapEncodeTiled (rank %d) failed with %d", rank, (int)r);
+  return CS_ERR_CUDA;
+}
+
+template <typename T, int DH>
+cs_status launch_tc(cs_paged_cache* c, const PagedAttnArgs& a, const CUtensorMap& tmQ, int q_box_bytes, unsigned bit, cudaStream_t st) {
+  if (!(c->attr_set & bit)) {
+    CS_CUDA_OK(c, cudaFuncSetAttribute(k_paged_tc<T, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem<DH>));
+    c->attr_set |= bit;
+  }
+  CS_CUDA_OK(c, cs_launch_pdl(k_paged_tc<T, DH>, dim3(c->num_sms), dim3(kThreads), kTcSmem<DH>, st, c->tmK, c->tmV, tmQ, a, q_box_bytes));
+  return CS_OK;
+}
+
+}  // namespace
+
+cs_status cs_paged_tc_maps(cs_paged_cache* c) {
+  const cs_paged_config& f = c->cfg;
+  const cuuint64_t dims[4] = {(cuuint64_t)f.head_dim, (cuuint64_t)f.page_size, (cuuint64_t)f.n_kv_heads, (cuuint64_t)f.n_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)f.slot_stride * 2, (cuuint64_t)f.head_stride * 2, (cuuint64_t)f.page_stride * 2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)(f.page_size < kPagedTile ? f.page_size : kPagedTile), 1, 1};
+  const cs_status s = encode(c, &c->tmK, f.k, 4, dims, strides, box);
+  return s != CS_OK ? s : encode(c, &c->tmV, f.v, 4, dims, strides, box);
+}
+
+cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& args, cudaStream_t st) {
+  PagedAttnArgs a = args;
+  const int tokens = kM / a.group;                 // rows of the block in a slot, with all heads of the group
+  a.item_rows = 2 * tokens * a.group;
+  const int box_rows = tokens < a.blk.rows ? tokens : a.blk.rows, dh = c->cfg.head_dim;
+  CUtensorMap tmQ;
+  // (a stride that no second row or head uses may be anything)
+  const cuuint64_t dims[3] = {(cuuint64_t)dh, (cuuint64_t)a.n_heads, (cuuint64_t)a.blk.rows};
+  const cuuint64_t strides[2] = {(cuuint64_t)(a.n_heads > 1 ? a.q_head : dh) * 2, (cuuint64_t)(a.blk.rows > 1 ? a.q_row : (long long)dh * a.n_heads) * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)box_rows};
+  const cs_status s = encode(c, &tmQ, a.q, 3, dims, strides, box);
+  if (s != CS_OK) return s;
+  const int bytes = 128 * a.group * box_rows;
+  const bool bf = c->cfg.dtype == CS_BF16;
+  if (dh == 64) return bf ? launch_tc<__nv_bfloat16, 64>(c, a, tmQ, bytes, 64, st) : launch_tc<__half, 64>(c, a, tmQ, bytes, 128, st);
+  return bf ? launch_tc<__nv_bfloat16, 128>(c, a, tmQ, bytes, 256, st) : launch_tc<__half, 128>(c, a, tmQ, bytes, 512, st);
+}
