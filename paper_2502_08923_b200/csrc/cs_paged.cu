@@ -338,7 +338,7 @@ cs_status check_blocks(const cs_blocks* b) {
 BlocksView view_of(const cs_blocks* b) { return BlocksView{b->start, b->len, b->kv_len, b->page_table, b->n_seqs, b->table_width, b->rows}; }
 
 struct PagedLayout {
-  size_t status, counters, parts, parts_ml, total;
+  size_t status, counters, splits, parts, parts_ml, total;
 };
 PagedLayout layout_of(const cs_paged_config& c) {
   PagedLayout l;
@@ -346,6 +346,7 @@ PagedLayout layout_of(const cs_paged_config& c) {
   auto put = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) & ~(size_t)255; return o; };
   l.status = put(256);
   l.counters = put(kPagedMaxCtas * sizeof(int));
+  l.splits = put(kPagedMaxCtas * sizeof(PagedSplit));
   l.parts = put((size_t)kPagedMaxCtas * 2 * kPagedMaxRows * c.head_dim * 4);
   l.parts_ml = put((size_t)kPagedMaxCtas * 2 * kPagedMaxRows * 8);
   l.total = at;
@@ -451,6 +452,7 @@ cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void
   char* ws = static_cast<char*>(workspace);
   c->status = reinterpret_cast<int*>(ws + l.status);
   c->counters = reinterpret_cast<int*>(ws + l.counters);
+  c->splits = reinterpret_cast<PagedSplit*>(ws + l.splits);
   c->parts = reinterpret_cast<float*>(ws + l.parts);
   c->parts_ml = reinterpret_cast<float*>(ws + l.parts_ml);
   const char* wl = getenv("CS_WAIT_LIMIT_US");
@@ -545,7 +547,7 @@ cs_status cs_paged_attention(cs_paged_cache* c, const cs_blocks* blocks, const v
   a.n_heads = n_heads; a.group = n_heads / c->cfg.n_kv_heads;
   a.mask = mask; a.window = window;
   a.scale = scale; a.scale_log2e = (float)(1.4426950408889634 * (double)scale);
-  a.parts = c->parts; a.parts_ml = c->parts_ml; a.counters = c->counters; a.status = c->status;
+  a.parts = c->parts; a.parts_ml = c->parts_ml; a.counters = c->counters; a.splits = c->splits; a.status = c->status;
   a.wait_ns = c->wait_limit_ns;
   // 16 query rows per KV head are a tile of the kernel for few rows, which takes heads of 32 whatever their rows
   const bool few = c->cfg.head_dim == 32 || (long long)blocks->rows * a.group <= 16ll * blocks->n_seqs;

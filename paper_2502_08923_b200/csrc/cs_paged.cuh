@@ -22,12 +22,19 @@ struct BlocksView {
   int n_seqs, table_width, rows;
 };
 
+// an item whose first tiles are a CTA's last ones: the CTAs behind it, up to `last`, have the rest (-1: none)
+struct PagedSplit {
+  int last, rows;              // query rows
+  int first_row, head, start;  // of the block (row x head of the group), KV head, the block's first row
+};
+
 struct cs_paged_cache {
   cs_paged_config cfg;
   PagedView view;
   CUtensorMap tmK, tmV;        // [page][head][slot][dim], boxes of 64 dims x up to 128 slots (head sizes 64 and 128)
   int* status;                 // device status word
   int* counters;               // pieces of an item that are done, by the CTA that holds its first tile; 0 between launches
+  PagedSplit* splits;          // of the last launch on the tensor cores, by CTA [kPagedMaxCtas]
   float* parts;                // un-normalised pieces [kPagedMaxCtas][2][kPagedMaxRows][head_dim]
   float* parts_ml;             // their (reference point, sum) [kPagedMaxCtas][2][kPagedMaxRows][2]
   int num_sms;
@@ -50,6 +57,7 @@ struct PagedAttnArgs {
   int item_rows;               // query rows (row of the block x head of the group) per work item
   float *parts, *parts_ml;
   int *counters, *status;
+  PagedSplit* splits;
   unsigned long long wait_ns;
 };
 
@@ -78,15 +86,20 @@ __device__ __forceinline__ void paged_range(int mask, int window, int len, int k
 // (sequence, head, row group) make one line of tiles, of which every CTA takes an equal run: CTA i of n the tiles
 // [total * i / n, total * (i + 1) / n).  So no CTA waits for another, none has more than one tile more than the
 // others whatever the lengths are, and at most two items of a CTA are shared with others.
+// (rows x heads stay below 2^31)
 __device__ __forceinline__ int paged_item_tiles(const PagedAttnArgs& a, int len, int kv, int rg) {
-  const int G = a.group, r0 = (int)((long long)rg * a.item_rows / G);
-  const int r1 = (int)min((long long)len - 1, (((long long)rg + 1) * a.item_rows - 1) / G);
+  const unsigned G = a.group;
+  const int r0 = (unsigned)(rg * a.item_rows) / G, r1 = min(len - 1, (int)((unsigned)(rg * a.item_rows + a.item_rows - 1) / G));
   int lo, hi;
   paged_range(a.mask, a.window, len, kv, r0, r1, lo, hi);
   return hi > lo ? (hi + kPagedTile - 1) / kPagedTile - lo / kPagedTile : 1;
 }
 __device__ __forceinline__ int paged_row_groups(const PagedAttnArgs& a, int len) {
-  return (int)(((long long)len * a.group + a.item_rows - 1) / a.item_rows);
+  return (int)((unsigned)(len * a.group + a.item_rows - 1) / (unsigned)a.item_rows);
+}
+// (a 64-bit division is some hundred instructions, and nearly always need not be one)
+__device__ __forceinline__ long long paged_div(long long x, long long y) {
+  return ((x | y) >> 32) == 0 ? (long long)((unsigned)x / (unsigned)y) : x / y;
 }
 
 // a block's items of one KV head, by a whole warp: their tiles together
@@ -106,23 +119,55 @@ struct PagedPlan {                              // in shared memory
   int tall[kPagedMaxSeqs], n_tall;              // sequences whose row groups a warp adds up
 };
 
-// By all threads of a CTA of at least 128 (a multiple of 32).  Ends with a barrier.
+// one sequence's block, left out (length 0) if something is wrong with it
+__device__ __forceinline__ void paged_load_block(const PagedAttnArgs& a, PagedPlan& p, int b, bool report, int& len, int& kv) {
+  const int start = __ldcg(a.blk.start + b);
+  len = __ldcg(a.blk.len + b);
+  kv = __ldcg(a.blk.kv_len + b);
+  const int flag = paged_block_flag(a.blk, a.kv.page_size, a.mask != CS_MASK_PREFIX, start, len, kv);
+  if (flag != 0) {
+    if (report && blockIdx.x == 0) atomicOr(a.status, flag);
+    len = 0;
+  }
+  p.start[b] = start; p.len[b] = len; p.kv[b] = kv;
+}
+
+// By all threads of a CTA (a multiple of 32, 128 at least).  Up to 32 sequences every warp works the plan out for itself - all write the same - and
+// nothing is waited for; else it ends with a barrier.
 __device__ __forceinline__ void paged_plan(const PagedAttnArgs& a, PagedPlan& p) {
   const int tid = threadIdx.x, nt = blockDim.x, warp = tid >> 5, lane = tid & 31, B = a.blk.n_seqs;
+  if (B <= 32) {
+    int len = 0, kv = 0, n = 0;
+    long long t = 0;
+    if (lane < B) {
+      paged_load_block(a, p, lane, warp == 0, len, kv);
+      n = paged_row_groups(a, len);
+      if (n <= 2) for (int g = 0; g < n; ++g) t += paged_item_tiles(a, len, kv, g);
+    }
+    for (unsigned tall = __ballot_sync(0xffffffffu, n > 2); tall != 0; tall &= tall - 1) {
+      const int b = __ffs(tall) - 1;
+      const long long s = paged_block_tiles(a, __shfl_sync(0xffffffffu, len, b), __shfl_sync(0xffffffffu, kv, b), lane);
+      if (lane == b) t = s;
+    }
+    t *= a.kv.n_kv_heads;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long v = __shfl_up_sync(0xffffffffu, t, o);
+      if (lane >= o) t += v;
+    }
+    if (lane < B) p.before[lane + 1] = t;
+    if (lane == 0) p.before[0] = 0;
+    __syncwarp();
+    return;
+  }
   if (tid == 0) p.n_tall = 0;
   __syncthreads();
   for (int b = tid; b < B; b += nt) {
-    const int start = __ldcg(a.blk.start + b), kv = __ldcg(a.blk.kv_len + b);
-    int len = __ldcg(a.blk.len + b);
-    const int flag = paged_block_flag(a.blk, a.kv.page_size, a.mask != CS_MASK_PREFIX, start, len, kv);
-    if (flag != 0) {                            // (left out)
-      if (blockIdx.x == 0) atomicOr(a.status, flag);
-      len = 0;
-    }
-    p.start[b] = start; p.len[b] = len; p.kv[b] = kv;
+    int len, kv;
+    paged_load_block(a, p, b, true, len, kv);
     const int n = paged_row_groups(a, len);
     long long t = 0;
-    if (n <= 4) {
+    if (n <= 2) {
       for (int g = 0; g < n; ++g) t += paged_item_tiles(a, len, kv, g);
     } else {
       p.tall[atomicAdd(&p.n_tall, 1)] = b;
@@ -172,13 +217,15 @@ struct PagedPiece {
 // Piece that begins at tile `at` of the line, by a whole warp (all lanes get it); `end`: where the CTA's run ends.
 __device__ __forceinline__ PagedPiece paged_piece(const PagedAttnArgs& a, const PagedPlan& p, long long at, long long end, int lane) {
   PagedPiece o;
+  // the last sequence that begins at or before it (32 x 32 sequences)
+  const int B = a.blk.n_seqs;
   int b = 0;
-  for (int step = 512; step > 0; step >>= 1)
-    if (b + step <= a.blk.n_seqs - 1 && p.before[b + step] <= at) b += step;
+  if (B > 32) b = 32 * (__popc(__ballot_sync(0xffffffffu, 32 * lane < B && p.before[min(32 * lane, B)] <= at)) - 1);
+  b += __popc(__ballot_sync(0xffffffffu, b + lane < B && p.before[min(b + lane, B)] <= at)) - 1;
   o.seq = b; o.start = p.start[b]; o.len = p.len[b]; o.kv = p.kv[b];
-  const long long all = p.before[b + 1] - p.before[b], per_head = all / a.kv.n_kv_heads;
+  const long long all = p.before[b + 1] - p.before[b], per_head = paged_div(all, a.kv.n_kv_heads);
   long long rest = at - p.before[b];
-  o.head = (int)(rest / per_head);
+  o.head = (int)paged_div(rest, per_head);
   rest -= o.head * per_head;
   // row group: 32 at a time
   const int n = paged_row_groups(a, o.len);
@@ -202,8 +249,7 @@ __device__ __forceinline__ PagedPiece paged_piece(const PagedAttnArgs& a, const 
     rest -= __shfl_sync(0xffffffffu, inc, 31);
   }
   o.rg = g0;
-  const int G = a.group, r0 = (int)((long long)g0 * a.item_rows / G);
-  const int r1 = (int)min((long long)o.len - 1, (((long long)g0 + 1) * a.item_rows - 1) / G);
+  const int r0 = (unsigned)(g0 * a.item_rows) / (unsigned)a.group, r1 = min(o.len - 1, (int)((unsigned)(g0 * a.item_rows + a.item_rows - 1) / (unsigned)a.group));
   paged_range(a.mask, a.window, o.len, o.kv, r0, r1, o.lo, o.hi);
   o.item_tiles = tiles;
   o.item_at = at - rest;
@@ -225,8 +271,7 @@ __device__ __forceinline__ bool paged_next(const PagedAttnArgs& a, const PagedPl
       p.start = plan.start[p.seq]; p.len = plan.len[p.seq]; p.kv = plan.kv[p.seq];
     }
   }
-  // (rows x heads stay below 2^31)
-  const int r0 = p.rg * a.item_rows / a.group, r1 = min(p.len - 1, (p.rg * a.item_rows + a.item_rows - 1) / a.group);
+  const int r0 = (unsigned)(p.rg * a.item_rows) / (unsigned)a.group, r1 = min(p.len - 1, (int)((unsigned)(p.rg * a.item_rows + a.item_rows - 1) / (unsigned)a.group));
   paged_range(a.mask, a.window, p.len, p.kv, r0, r1, p.lo, p.hi);
   p.tile0 = p.hi > p.lo ? p.lo / kPagedTile : 0;
   p.item_tiles = p.hi > p.lo ? (p.hi + kPagedTile - 1) / kPagedTile - p.tile0 : 1;
@@ -236,7 +281,7 @@ __device__ __forceinline__ bool paged_next(const PagedAttnArgs& a, const PagedPl
   return true;
 }
 // the CTA (of n) whose run holds tile x of a line of `total`
-__device__ __forceinline__ int paged_owner(long long x, long long total, int n) { return (int)(((x + 1) * n - 1) / total); }
+__device__ __forceinline__ int paged_owner(long long x, long long total, int n) { return (int)paged_div((x + 1) * n - 1, total); }
 
 // 2^x, hardware approximation (relative error about 2^-22; -inf gives 0)
 __device__ __forceinline__ float paged_ex2(float x) {

@@ -76,7 +76,7 @@ k_paged_few(PagedAttnArgs a) {
   const long long total = plan.before[a.blk.n_seqs];
   const int n_cta = (int)min((long long)gridDim.x, total), cta = blockIdx.x;
   if (cta >= n_cta) return;
-  const long long run0 = total * cta / n_cta, run1 = total * (cta + 1) / n_cta;
+  const long long run0 = paged_div(total * cta, n_cta), run1 = paged_div(total * (cta + 1), n_cta);
 
   const uint32_t my_ring = (uint32_t)__cvta_generic_to_shared(ring) + (uint32_t)(warp * kStages * 2 * kSliceBytes);
   const uint8_t* my_ring_p = ring + warp * kStages * 2 * kSliceBytes;
@@ -312,19 +312,36 @@ k_paged_few(PagedAttnArgs a) {
       if (write && mine) {
         __threadfence();
         M = -INFINITY; L = 0.f;
-        auto at = [&](int c) { return ((long long)c * 2 + (c == c0 ? 1 : 0)) * kPagedMaxRows + row; };
-        for (int c = c0; c <= c1; ++c) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at(c)).x);
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-#pragma unroll 4
-        for (int c = c0; c <= c1; ++c) {
-          const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at(c));
-          const float4 v0 = __ldcg(reinterpret_cast<const float4*>(a.parts + at(c) * DH + c8)), v1 = __ldcg(reinterpret_cast<const float4*>(a.parts + at(c) * DH + c8 + 4));
-          const float k = ml.x == -INFINITY ? 0.f : paged_ex2(ml.x - M);
-          if (ml.x == -INFINITY && ml.y == 0.f) continue;
-          L = fmaf(k, ml.y, L);
-          acc[0] = fmaf(k, v0.x, acc[0]); acc[1] = fmaf(k, v0.y, acc[1]); acc[2] = fmaf(k, v0.z, acc[2]); acc[3] = fmaf(k, v0.w, acc[3]);
-          acc[4] = fmaf(k, v1.x, acc[4]); acc[5] = fmaf(k, v1.y, acc[5]); acc[6] = fmaf(k, v1.z, acc[6]); acc[7] = fmaf(k, v1.w, acc[7]);
+        // (a batch's loads in flight together: one by one 18 pieces took 10 us)
+        constexpr int kBatch = 10;
+        for (int cb = c0; cb <= c1; cb += kBatch) {
+          float2 ml[kBatch];
+          float4 v0[kBatch], v1[kBatch];
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            const long long at = ((long long)min(cb + i, c1) * 2 + (cb + i == c0 ? 1 : 0)) * kPagedMaxRows + row;
+            ml[i] = __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at);
+            v0[i] = __ldcg(reinterpret_cast<const float4*>(a.parts + at * DH + c8));
+            v1[i] = __ldcg(reinterpret_cast<const float4*>(a.parts + at * DH + c8 + 4));
+          }
+          float top = M;
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) top = fmaxf(top, ml[i].x);
+          const float keep = M == -INFINITY ? (L == 0.f ? 0.f : L) : paged_ex2(M - top);     // (L without a maximum is NaN)
+          M = top;
+          L *= keep;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[e] *= keep;
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) {
+            if (cb + i > c1 || (ml[i].x == -INFINITY && ml[i].y == 0.f)) continue;           // (it saw nothing)
+            const float k = ml[i].x == -INFINITY ? 0.f : paged_ex2(ml[i].x - M);
+            L = fmaf(k, ml[i].y, L);
+            acc[0] = fmaf(k, v0[i].x, acc[0]); acc[1] = fmaf(k, v0[i].y, acc[1]); acc[2] = fmaf(k, v0[i].z, acc[2]); acc[3] = fmaf(k, v0[i].w, acc[3]);
+            acc[4] = fmaf(k, v1[i].x, acc[4]); acc[5] = fmaf(k, v1[i].y, acc[5]); acc[6] = fmaf(k, v1[i].z, acc[6]); acc[7] = fmaf(k, v1[i].w, acc[7]);
+          }
         }
       }
     }

@@ -119,7 +119,6 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kNS + 16);
   volatile int* s_abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
   volatile int* s_odd = reinterpret_cast<volatile int*>(tmem_slot + 2);      // values that are not finite were taken out (by the parity of the piece)
-  int* s_last = reinterpret_cast<int*>(tmem_slot + 4);
   float2* s_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(bars) + kCtl);      // [slot][128 rows]
   PagedPlan& plan = *reinterpret_cast<PagedPlan*>(s_ml + 2 * kM);
   const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8 * kNS, b_s = b_empty + 8 * kNS, b_p = b_s + 16, b_o = b_p + 16, b_qfull = b_o + 16, b_qfree = b_qfull + 8,
@@ -139,12 +138,13 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   fence_before();
-  paged_plan(a, plan);                            // (ends with a barrier)
+  paged_plan(a, plan);
+  __syncthreads();
   fence_after();
   const uint32_t tmem = uniform(*tmem_slot);
   const long long total = plan.before[a.blk.n_seqs];
   const int n_cta = (int)min((long long)gridDim.x, total), cta = blockIdx.x;
-  const long long run0 = cta < n_cta ? total * cta / n_cta : 0, run1 = cta < n_cta ? total * (cta + 1) / n_cta : 0;
+  const long long run0 = cta < n_cta ? paged_div(total * cta, n_cta) : 0, run1 = cta < n_cta ? paged_div(total * (cta + 1), n_cta) : 0;
 
   // Bounded waits.  Once one has run out all others return at once.
   auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
@@ -319,6 +319,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       const int slot = warp >> 2, row = tid & 127, G = a.group;
       const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_col = lanes + kSCol + slot * 128, o_col = lanes + kOCol + slot * 128;
       uint32_t base = 0, s_phase = 0, o_phase[2] = {0, 0}, piece = 0;
+      bool split = false;
       for (bool more = true; more; ++piece) {
         const bool both = two_slots(p);
         const int n = both ? 2 * p.n_tiles : p.n_tiles, first_row = p.rg * a.item_rows + (both ? slot * slot_rows : 0);
@@ -521,52 +522,22 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           }
         }
         fence_before();
-        if (!p.whole) {
-          // ---- pieces of an item that several CTAs share: the last one to arrive adds them up, in the order of the keys
-          __threadfence();
-          softmax_sync();
-          const int c0 = paged_owner(p.item_at, total, n_cta), c1 = paged_owner(p.item_at + p.item_tiles - 1, total, n_cta);
-          if (tid == 0) {
-            int last = 0;
-            if (good && *s_abort == 0) {
-              last = atomicAdd(a.counters + c0, 1) == c1 - c0;
-              if (last) a.counters[c0] = 0;
-            }
-            *s_last = last;
-          }
-          softmax_sync();
-          if (*s_last) {
-            __threadfence();
-            const int rows = min(a.item_rows, p.len * G - p.rg * a.item_rows);
-            for (int i = tid; i < rows * (DH / 8); i += 256) {
-              const int r = i / (DH / 8), c8 = i % (DH / 8) * 8, mr = p.rg * a.item_rows + r;
-              auto at = [&](int c) { return ((long long)c * 2 + (c == c0 ? 1 : 0)) * kPagedMaxRows + r; };
-              float M = -INFINITY, L = 0.f, acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-              for (int c = c0; c <= c1; ++c) M = fmaxf(M, __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at(c)).x);
-#pragma unroll 4
-              for (int c = c0; c <= c1; ++c) {
-                const float2 ml = __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at(c));
-                const float4 v0 = __ldcg(reinterpret_cast<const float4*>(a.parts + at(c) * DH + c8)), v1 = __ldcg(reinterpret_cast<const float4*>(a.parts + at(c) * DH + c8 + 4));
-                const float k = ml.x == -INFINITY ? 0.f : paged_ex2(ml.x - M);
-                if (ml.x == -INFINITY && ml.y == 0.f) continue;      // (it saw nothing)
-                L = fmaf(k, ml.y, L);
-                acc[0] = fmaf(k, v0.x, acc[0]); acc[1] = fmaf(k, v0.y, acc[1]); acc[2] = fmaf(k, v0.z, acc[2]); acc[3] = fmaf(k, v0.w, acc[3]);
-                acc[4] = fmaf(k, v1.x, acc[4]); acc[5] = fmaf(k, v1.y, acc[5]); acc[6] = fmaf(k, v1.z, acc[6]); acc[7] = fmaf(k, v1.w, acc[7]);
-              }
-              const float iv = L == 0.f ? 0.f : 1.f / L;
-              const long long r_out = (long long)(p.start + mr / G) * a.n_heads + p.head * G + mr % G;
-              *reinterpret_cast<uint4*>(a.out + (r_out * DH + c8) * 2) =
-                  make_uint4(PagedType<T>::pack(acc[0] * iv, acc[1] * iv), PagedType<T>::pack(acc[2] * iv, acc[3] * iv), PagedType<T>::pack(acc[4] * iv, acc[5] * iv),
-                             PagedType<T>::pack(acc[6] * iv, acc[7] * iv));
-              if (a.lse != nullptr && c8 == 0) a.lse[r_out] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
-            }
-          }
+        if (opens && !p.whole && tid == 0) {               // (the run ends with this item)
+          PagedSplit d;
+          d.last = paged_owner(p.item_at + p.item_tiles - 1, total, n_cta);
+          d.rows = min(a.item_rows, p.len * G - p.rg * a.item_rows);
+          d.first_row = p.rg * a.item_rows; d.head = p.head; d.start = p.start;
+          a.splits[cta] = d;
+          split = true;
         }
         softmax_sync();                                // both slots' O, the exchange rows and this piece's flag are free again
         if (tid == 0) s_odd[piece & 1] = 0;
         base += 2 * p.n_tiles;
         more = paged_next(a, plan, p, run1);
       }
+      if (tid == 0 && (!split || *s_abort)) a.splits[cta].last = -1;
+    } else if (tid == 0) {
+      a.splits[cta].last = -1;
     }
   }
   // ---------------------------------------------------------------------- teardown
@@ -575,6 +546,66 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   if (warp == kMmaWarp) {
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+  }
+}
+
+// Items that several CTAs share: their pieces added up, in the order of the keys.  One warp per row; CTA x of a column handles the item that begins in CTA x of the
+// launch before.  (The last CTA to arrive did this inside the kernel at first: 430 KB through one SM are 5 us with its loads in flight together, 14 without.)
+constexpr int kMergeWarps = 8, kMergeRows = 8;    // CTAs that share an item's rows
+template <typename T, int DH>
+__global__ void __launch_bounds__(kMergeWarps * 32)
+k_paged_merge(PagedAttnArgs a) {
+  CS_PDL_PROLOGUE();
+  constexpr int kBatch = 10, kV = DH / 32;        // columns of a lane
+  const int c0 = blockIdx.x, lane = threadIdx.x & 31;
+  const int c1 = __ldcg(&a.splits[c0].last), rows = __ldcg(&a.splits[c0].rows), first_row = __ldcg(&a.splits[c0].first_row), head = __ldcg(&a.splits[c0].head),
+            start = __ldcg(&a.splits[c0].start);
+  if (c1 < 0) return;
+  for (int r = blockIdx.y * kMergeWarps + (threadIdx.x >> 5); r < rows; r += kMergeWarps * kMergeRows) {
+    float M = -INFINITY, L = 0.f, acc[kV];
+#pragma unroll
+    for (int e = 0; e < kV; ++e) acc[e] = 0.f;
+    for (int cb = c0; cb <= c1; cb += kBatch) {
+      float2 ml[kBatch];
+      float v[kBatch][kV];
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const long long at = ((long long)min(cb + i, c1) * 2 + (cb + i == c0 ? 1 : 0)) * kPagedMaxRows + r;
+        ml[i] = __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at);
+        if constexpr (kV == 4) {
+          const float4 x = __ldcg(reinterpret_cast<const float4*>(a.parts + at * DH) + lane);
+          v[i][0] = x.x; v[i][1] = x.y; v[i][2] = x.z; v[i][3] = x.w;
+        } else {
+          const float2 x = __ldcg(reinterpret_cast<const float2*>(a.parts + at * DH) + lane);
+          v[i][0] = x.x; v[i][1] = x.y;
+        }
+      }
+      float top = M;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) top = fmaxf(top, ml[i].x);
+      const float keep = M == -INFINITY ? (L == 0.f ? 0.f : L) : paged_ex2(M - top);     // (L without a maximum is NaN)
+      M = top;
+      L *= keep;
+#pragma unroll
+      for (int e = 0; e < kV; ++e) acc[e] *= keep;
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        if (cb + i > c1 || (ml[i].x == -INFINITY && ml[i].y == 0.f)) continue;           // (it saw nothing)
+        const float k = ml[i].x == -INFINITY ? 0.f : paged_ex2(ml[i].x - M);
+        L = fmaf(k, ml[i].y, L);
+#pragma unroll
+        for (int e = 0; e < kV; ++e) acc[e] = fmaf(k, v[i][e], acc[e]);
+      }
+    }
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    const int m = first_row + r;
+    const long long row = (long long)(start + m / a.group) * a.n_heads + head * a.group + m % a.group;
+    uint32_t w[kV / 2];
+#pragma unroll
+    for (int e = 0; e < kV / 2; ++e) w[e] = PagedType<T>::pack(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+    if constexpr (kV == 4) *reinterpret_cast<uint2*>(a.out + row * DH * 2 + lane * 8) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t*>(a.out + row * DH * 2 + lane * 4) = w[0];
+    if (a.lse != nullptr && lane == 0) a.lse[row] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
   }
 }
 
@@ -606,6 +637,7 @@ cs_status launch_tc(cs_paged_cache* c, const PagedAttnArgs& a, const CUtensorMap
     c->attr_set |= bit;
   }
   CS_CUDA_OK(c, cs_launch_pdl(k_paged_tc<T, DH>, dim3(c->num_sms), dim3(kThreads), kTcSmem<DH>, st, c->tmK, c->tmV, tmQ, a, q_box_bytes));
+  CS_CUDA_OK(c, cs_launch_pdl(k_paged_merge<T, DH>, dim3(c->num_sms, kMergeRows), dim3(kMergeWarps * 32), 0, st, a));
   return CS_OK;
 }
 
