@@ -523,6 +523,7 @@ size_t cs_paged_workspace_bytes(const cs_paged_config* cfg);
 cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void* workspace, size_t workspace_bytes,
                           void* stream);
 void cs_paged_destroy(cs_paged_cache* cache);
+int cs_paged_head_dim(const cs_paged_cache* cache); /* 0 for NULL */
 const char* cs_paged_last_error(const cs_paged_cache* cache);
 
 /* Waits for `stream`, then returns and clears what the device found wrong: CS_ERR_CAPACITY (a block that does not fit its

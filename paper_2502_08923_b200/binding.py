@@ -1,8 +1,8 @@
 """ctypes binding of libcopyspec.so: same names as the C ABI (include/copyspec.h),
 argument marshalling only.  PyTorch provides device memory and the current stream; every
 step of the path runs in the library's CUDA kernels.  There is no CPU fallback: if the
-library cannot be loaded, every call raises.  (The search call also has its marshalling in native code;
-without that file, which goes by the versions of Python and torch, it takes the way of the other calls.)"""
+library cannot be loaded, every call raises.  (The search call and those around the paged cache also have their marshalling in native code;
+without that file, which goes by the versions of Python and torch, they take the way of the other calls.)"""
 from __future__ import annotations
 
 import ctypes as C
@@ -76,10 +76,11 @@ EXPORTS = ("cs_workspace_bytes", "cs_create", "cs_destroy", "cs_last_error", "cs
            "cs_loop_launches_per_step", "cs_lm_head", "cs_lm_head_static", "cs_gram_index_bytes",
            "cs_gram_index_reset", "cs_gram_index_update", "cs_find_match_indexed", "cs_gram_index_status",
            "cs_rope_table", "cs_qk_norm_rope", "cs_paged_workspace_bytes", "cs_paged_create", "cs_paged_destroy", "cs_paged_last_error",
-           "cs_paged_status", "cs_paged_append", "cs_paged_attention")
+           "cs_paged_status", "cs_paged_append", "cs_paged_attention", "cs_paged_head_dim")
 
 _lib = None
 _search = None      # cs_find_match in native code, for plain arguments
+_native = None      # the module with all that is in native code, or None
 
 
 def lib_path() -> str:
@@ -177,6 +178,8 @@ def load(build_if_missing: bool = True) -> C.CDLL:
     lib.cs_paged_destroy.argtypes = [vp]
     lib.cs_paged_last_error.restype = C.c_char_p
     lib.cs_paged_last_error.argtypes = [vp]
+    lib.cs_paged_head_dim.restype = i
+    lib.cs_paged_head_dim.argtypes = [vp]
     lib.cs_paged_status.restype = i
     lib.cs_paged_status.argtypes = [vp, vp]
     lib.cs_paged_append.restype = i
@@ -190,11 +193,14 @@ def load(build_if_missing: bool = True) -> C.CDLL:
 
 def _native_search():
     """cs_find_match in native code, or, where there is none for this Python and torch, what leaves every call to the general path."""
+    global _native
+    _native = None
     path = _build.native_path()
     try:
         spec = importlib.util.spec_from_file_location(f"{__package__}._native", path)
         module = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(module)
+        _native = module
         return module.find_match
     except ImportError as e:
         warnings.warn(f"the search call's native side does not load, its general path takes all calls: {e}", RuntimeWarning)
@@ -625,6 +631,12 @@ def cs_qk_norm_rope(q, k, pos, rope, q_gain=None, k_gain=None, eps=1e-5, dtype=N
     Returns (q, k) in `dtype` (default: the inputs' type; 16-bit types from fp32 inputs); `out` may supply those tensors, the inputs
     themselves among them."""
     some = q if q is not None else k
+    if out is None and some is not None and (_native or (load() and _native)):
+        got = _native.qk_norm_rope(q, k, pos, rope, q_gain, k_gain, eps, _DTYPE.get(dtype or some.dtype, -1))
+        if got.__class__ is tuple:
+            return got
+        if got is not None:
+            raise CsError(got, "cs_qk_norm_rope")
     if some is None or (q is not None and k is not None and (q.dtype != k.dtype or q.shape[0] != k.shape[0] or q.shape[2:] != k.shape[2:])):
         raise ValueError("q and k must have the same rows, head size and type")
     dtype = dtype or some.dtype
@@ -660,7 +672,7 @@ class PagedCache:
             raise ValueError("heads must be contiguous")
         self.lib = load()
         self.k_pages, self.v_pages = k_pages, v_pages
-        self.dtype = k_pages.dtype
+        self.dtype, self.scale = k_pages.dtype, k_pages.shape[3] ** -0.5
         n, h, s, d = k_pages.shape
         st = k_pages.stride()
         self.c_cfg = CsPagedConfig(k_pages.data_ptr(), v_pages.data_ptr(), st[0], st[1], st[2], n, s, h, d, _DTYPE[self.dtype])
@@ -677,11 +689,12 @@ class PagedCache:
         if rc != CS_OK:
             msg = self.lib.cs_paged_last_error(None)
             raise CsError(rc, "cs_paged_create", msg.decode() if msg else "")
+        self._id = (self.handle.value, _DTYPE[self.dtype])
 
     def close(self):
         if getattr(self, "handle", None):
             self.lib.cs_paged_destroy(self.handle)
-            self.handle = None
+            self.handle, self._id = None, (0, 0)
 
     def __del__(self):
         try:
@@ -703,6 +716,12 @@ class PagedCache:
     def cs_paged_append(self, k, v, block_start, block_len, kv_len, page_table, rope=None, k_gain=None, q=None, q_gain=None, eps=1e-5, q_out=None):
         """Appends the blocks' keys (normed where there is a gain, rotated) and values [rows][Hkv][D] to their pages; with `q`
         [rows][H][D] norms and rotates the block's queries in the same launch and returns them in the cache's type."""
+        if q_out is None and _native is not None:
+            got = _native.paged_append(*self._id, k, v, block_start, block_len, kv_len, page_table, rope, k_gain, q, q_gain, eps)
+            if got.__class__ is tuple:
+                return got[0]
+            if got is not None:
+                self._check(got, "cs_paged_append")
         d = self.k_pages.shape[3]
         if k.dtype != v.dtype or k.shape != v.shape or k.dim() != 3 or k.shape[2] != d or (q is not None and (q.dtype != k.dtype or q.shape[0] != k.shape[0] or q.shape[2] != d)):
             raise ValueError("q, k and v must have the same rows and type and the cache's head size")
@@ -719,6 +738,12 @@ class PagedCache:
         MASK_PREFIX (the cached keys) or MASK_FULL (the cached keys and the whole block); `window` > 0: only the last so many positions up to
         the row's own; `scale`: 1 / sqrt(D) by default.  Returns out [rows][H][D], with `with_lse` (or an `lse` tensor) also log sum exp [rows][H] fp32.
         Rows of no block are left as they were."""
+        if out is None and lse is None and _native is not None:
+            got = _native.paged_attention(*self._id, q, block_start, block_len, kv_len, page_table, mask, window, self.scale if scale is None else scale, with_lse)
+            if got.__class__ is tuple:
+                return got if with_lse else got[0]
+            if got is not None:
+                self._check(got, "cs_paged_attention")
         if q.dtype != self.dtype:
             raise ValueError(f"q must be {self.dtype}, the cache's type")
         ptr, row, head = _rows(q, "q")
@@ -734,7 +759,7 @@ class PagedCache:
         elif lse is not None and (lse.shape != (T, H) or lse.dtype is not torch.float32 or not lse.is_cuda or not lse.is_contiguous()):
             raise ValueError("lse must be a contiguous fp32 CUDA tensor [rows][heads]")
         blocks = self._blocks(block_start, block_len, kv_len, page_table, T)
-        rc = self.lib.cs_paged_attention(self.handle, blocks, ptr, row, head, H, mask, window, D ** -0.5 if scale is None else scale, out.data_ptr(),
+        rc = self.lib.cs_paged_attention(self.handle, blocks, ptr, row, head, H, mask, window, self.scale if scale is None else scale, out.data_ptr(),
                                          None if lse is None else lse.data_ptr(), _stream())
         self._check(rc, "cs_paged_attention")
         return out if lse is None else (out, lse)

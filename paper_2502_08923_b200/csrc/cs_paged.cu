@@ -474,6 +474,8 @@ cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void
 
 void cs_paged_destroy(cs_paged_cache* cache) { free(cache); }
 
+int cs_paged_head_dim(const cs_paged_cache* cache) { return cache != nullptr ? cache->cfg.head_dim : 0; }
+
 const char* cs_paged_last_error(const cs_paged_cache* cache) { return cache != nullptr ? cache->err : t_paged_err; }
 
 cs_status cs_paged_status(cs_paged_cache* c, void* stream) {
@@ -545,6 +547,7 @@ cs_status cs_paged_attention(cs_paged_cache* c, const cs_blocks* blocks, const v
   a.q = static_cast<const char*>(q); a.q_row = q_row_stride; a.q_head = q_head_stride;
   a.out = static_cast<char*>(out); a.lse = lse;
   a.n_heads = n_heads; a.group = n_heads / c->cfg.n_kv_heads;
+  a.by_group = PagedDivisor::by(a.group);
   a.mask = mask; a.window = window;
   a.scale = scale; a.scale_log2e = (float)(1.4426950408889634 * (double)scale);
   a.parts = c->parts; a.parts_ml = c->parts_ml; a.counters = c->counters; a.splits = c->splits; a.status = c->status;

@@ -9,7 +9,7 @@
 static constexpr int kPagedMaxCtas = 160;      // CTAs of an attention launch at most
 static constexpr int kPagedMaxRows = 256;      // query rows (rows x heads of a group) of one work item at most
 static constexpr int kPagedTile = 128;         // keys of a tile, the unit work is dealt out in
-static constexpr int kPagedMaxSeqs = 1024;     // sequences of one attention launch; more are further launches
+static constexpr int kPagedMaxSeqs = 512;      // sequences of one attention launch; more are further launches
 
 struct PagedView {
   char *k, *v;
@@ -43,6 +43,19 @@ struct cs_paged_cache {
   char err[256];
 };
 
+// x / d for 0 <= x < 2^31: the high half of a product, a sum and a shift (Granlund and Montgomery 1994, "Division by invariant integers using multiplication")
+struct PagedDivisor {
+  unsigned mul, shift;
+#ifdef __CUDACC__
+  __device__ __forceinline__ int of(int x) const { return (int)((__umulhi((unsigned)x, mul) + (unsigned)x) >> shift); }
+#endif
+  static PagedDivisor by(unsigned d) {
+    unsigned l = 0;
+    while ((1ull << l) < d) ++l;
+    return PagedDivisor{(unsigned)((((1ull << l) - d) << 32) / d + 1), l};
+  }
+};
+
 // what an attention launch is about
 struct PagedAttnArgs {
   PagedView kv;
@@ -55,6 +68,7 @@ struct PagedAttnArgs {
   int mask, window;
   float scale_log2e, scale;
   int item_rows;               // query rows (row of the block x head of the group) per work item
+  PagedDivisor by_group, by_item_rows;
   float *parts, *parts_ml;
   int *counters, *status;
   PagedSplit* splits;
@@ -88,14 +102,13 @@ __device__ __forceinline__ void paged_range(int mask, int window, int len, int k
 // others whatever the lengths are, and at most two items of a CTA are shared with others.
 // (rows x heads stay below 2^31)
 __device__ __forceinline__ int paged_item_tiles(const PagedAttnArgs& a, int len, int kv, int rg) {
-  const unsigned G = a.group;
-  const int r0 = (unsigned)(rg * a.item_rows) / G, r1 = min(len - 1, (int)((unsigned)(rg * a.item_rows + a.item_rows - 1) / G));
+  const int r0 = a.by_group.of(rg * a.item_rows), r1 = min(len - 1, a.by_group.of(rg * a.item_rows + a.item_rows - 1));
   int lo, hi;
   paged_range(a.mask, a.window, len, kv, r0, r1, lo, hi);
   return hi > lo ? (hi + kPagedTile - 1) / kPagedTile - lo / kPagedTile : 1;
 }
 __device__ __forceinline__ int paged_row_groups(const PagedAttnArgs& a, int len) {
-  return (int)((unsigned)(len * a.group + a.item_rows - 1) / (unsigned)a.item_rows);
+  return a.by_item_rows.of(len * a.group + a.item_rows - 1);
 }
 // (a 64-bit division is some hundred instructions, and nearly always need not be one)
 __device__ __forceinline__ long long paged_div(long long x, long long y) {
@@ -114,6 +127,7 @@ __device__ __forceinline__ long long paged_block_tiles(const PagedAttnArgs& a, i
 
 struct PagedPlan {                              // in shared memory
   long long before[kPagedMaxSeqs + 1];          // tiles of the sequences before this one
+  long long per_head[kPagedMaxSeqs];            // tiles of one of its KV heads
   int start[kPagedMaxSeqs], len[kPagedMaxSeqs], kv[kPagedMaxSeqs];
   long long warp_sum[32];
   int tall[kPagedMaxSeqs], n_tall;              // sequences whose row groups a warp adds up
@@ -149,6 +163,7 @@ __device__ __forceinline__ void paged_plan(const PagedAttnArgs& a, PagedPlan& p)
       const long long s = paged_block_tiles(a, __shfl_sync(0xffffffffu, len, b), __shfl_sync(0xffffffffu, kv, b), lane);
       if (lane == b) t = s;
     }
+    if (lane < B) p.per_head[lane] = t;
     t *= a.kv.n_kv_heads;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -172,13 +187,14 @@ __device__ __forceinline__ void paged_plan(const PagedAttnArgs& a, PagedPlan& p)
     } else {
       p.tall[atomicAdd(&p.n_tall, 1)] = b;
     }
+    p.per_head[b] = t;
     p.before[b + 1] = t * a.kv.n_kv_heads;
   }
   __syncthreads();
   for (int i = warp; i < p.n_tall; i += nt >> 5) {
     const int b = p.tall[i];
     const long long t = paged_block_tiles(a, p.len[b], p.kv[b], lane);
-    if (lane == 0) p.before[b + 1] = t * a.kv.n_kv_heads;
+    if (lane == 0) { p.per_head[b] = t; p.before[b + 1] = t * a.kv.n_kv_heads; }
   }
   if (tid == 0) p.before[0] = 0;
   __syncthreads();
@@ -217,20 +233,20 @@ struct PagedPiece {
 // Piece that begins at tile `at` of the line, by a whole warp (all lanes get it); `end`: where the CTA's run ends.
 __device__ __forceinline__ PagedPiece paged_piece(const PagedAttnArgs& a, const PagedPlan& p, long long at, long long end, int lane) {
   PagedPiece o;
-  // the last sequence that begins at or before it (32 x 32 sequences)
+  // the last sequence that begins at or before it (32 at a time)
   const int B = a.blk.n_seqs;
   int b = 0;
   if (B > 32) b = 32 * (__popc(__ballot_sync(0xffffffffu, 32 * lane < B && p.before[min(32 * lane, B)] <= at)) - 1);
   b += __popc(__ballot_sync(0xffffffffu, b + lane < B && p.before[min(b + lane, B)] <= at)) - 1;
   o.seq = b; o.start = p.start[b]; o.len = p.len[b]; o.kv = p.kv[b];
-  const long long all = p.before[b + 1] - p.before[b], per_head = paged_div(all, a.kv.n_kv_heads);
+  const long long per_head = p.per_head[b];
   long long rest = at - p.before[b];
-  o.head = (int)paged_div(rest, per_head);
+  o.head = a.kv.n_kv_heads <= 32 ? __popc(__ballot_sync(0xffffffffu, lane < a.kv.n_kv_heads && (lane + 1) * per_head <= rest)) : (int)paged_div(rest, per_head);
   rest -= o.head * per_head;
   // row group: 32 at a time
   const int n = paged_row_groups(a, o.len);
-  int g0 = 0, tiles = 0;
-  for (;; g0 += 32) {
+  int g0 = 0, tiles = (int)per_head;
+  for (; n > 1; g0 += 32) {
     const int t = g0 + lane < n ? paged_item_tiles(a, o.len, o.kv, g0 + lane) : 0;
     int inc = t;
 #pragma unroll
@@ -249,7 +265,7 @@ __device__ __forceinline__ PagedPiece paged_piece(const PagedAttnArgs& a, const 
     rest -= __shfl_sync(0xffffffffu, inc, 31);
   }
   o.rg = g0;
-  const int r0 = (unsigned)(g0 * a.item_rows) / (unsigned)a.group, r1 = min(o.len - 1, (int)((unsigned)(g0 * a.item_rows + a.item_rows - 1) / (unsigned)a.group));
+  const int r0 = a.by_group.of(g0 * a.item_rows), r1 = min(o.len - 1, a.by_group.of(g0 * a.item_rows + a.item_rows - 1));
   paged_range(a.mask, a.window, o.len, o.kv, r0, r1, o.lo, o.hi);
   o.item_tiles = tiles;
   o.item_at = at - rest;
@@ -271,7 +287,7 @@ __device__ __forceinline__ bool paged_next(const PagedAttnArgs& a, const PagedPl
       p.start = plan.start[p.seq]; p.len = plan.len[p.seq]; p.kv = plan.kv[p.seq];
     }
   }
-  const int r0 = (unsigned)(p.rg * a.item_rows) / (unsigned)a.group, r1 = min(p.len - 1, (int)((unsigned)(p.rg * a.item_rows + a.item_rows - 1) / (unsigned)a.group));
+  const int r0 = a.by_group.of(p.rg * a.item_rows), r1 = min(p.len - 1, a.by_group.of(p.rg * a.item_rows + a.item_rows - 1));
   paged_range(a.mask, a.window, p.len, p.kv, r0, r1, p.lo, p.hi);
   p.tile0 = p.hi > p.lo ? p.lo / kPagedTile : 0;
   p.item_tiles = p.hi > p.lo ? (p.hi + kPagedTile - 1) / kPagedTile - p.tile0 : 1;

@@ -82,53 +82,63 @@ k_paged_few(PagedAttnArgs a) {
   const uint8_t* my_ring_p = ring + warp * kStages * 2 * kSliceBytes;
 
   // ---- the fetching side: runs kStages slices ahead, across pieces
-  PagedPiece f = paged_piece(a, plan, run0, run1, lane);
-  PagedPiece p = f;
+  PagedPiece p = paged_piece(a, plan, run0, run1, lane), f = p;
   int f_tile = 0, f_entry = 0, f_stage = 0;
   bool f_more = true;
+  // page-table entries of this warp's slices of the next 32 tiles, one per lane: asked for a slice before the first is needed
+  auto entries = [&]() {
+    const int k = (f.tile0 + f_tile + lane) * kPagedTile + warp * kSlice;
+    f_entry = k < f.hi && k + kSlice > f.lo ? __ldcg(a.blk.table + (long long)f.seq * a.blk.table_width + (k >> a.kv.page_shift)) : 0;
+  };
+  const long long lane_off = (lane / CPR * a.kv.slot_stride + lane % CPR * 8) * 2, hop = 32 / CPR * a.kv.slot_stride * 2;   // this lane's chunks of a slice, bytes
+  entries();
   auto fetch = [&]() {
     if (f_more) {
       const int key0 = (f.tile0 + f_tile) * kPagedTile + warp * kSlice;
-      if ((f_tile & 31) == 0) {                  // page-table entries of this warp's slices of the next 32 tiles, one per lane
-        const int k = key0 + lane * kPagedTile;
-        f_entry = k < f.hi && k + kSlice > f.lo ? __ldcg(a.blk.table + (long long)f.seq * a.blk.table_width + (k >> a.kv.page_shift)) : 0;
-      }
       const int page = __shfl_sync(0xffffffffu, f_entry, f_tile & 31);
-      const bool exists = (unsigned)page < (unsigned)a.kv.n_pages, used = key0 < f.hi && key0 + kSlice > f.lo;
+      const bool used = key0 < f.hi && key0 + kSlice > f.lo, exists = (unsigned)page < (unsigned)a.kv.n_pages;
       if (used && !exists && lane == 0) atomicOr(a.status, CS_DEV_BADARG);
-      const long long off = exists ? page * a.kv.page_stride + f.head * a.kv.head_stride + (long long)(key0 & (a.kv.page_size - 1)) * a.kv.slot_stride : 0;
       const uint32_t dst = my_ring + (uint32_t)(f_stage * 2 * kSliceBytes);
+      if (used && exists) {
+        const long long off = (page * a.kv.page_stride + f.head * a.kv.head_stride + (long long)(key0 & (a.kv.page_size - 1)) * a.kv.slot_stride) * 2 + lane_off;
+        const char *k = a.kv.k + off, *v = a.kv.v + off;
+        const bool all = key0 >= f.lo && key0 + kSlice <= f.hi;
 #pragma unroll
-      for (int i = 0; i < kIter; ++i) {
-        const int j = (i * 32 + lane) / CPR, c = (i * 32 + lane) % CPR;
-        const bool on = used && exists && key0 + j >= f.lo && key0 + j < f.hi;
-        const long long e = (on ? off + j * a.kv.slot_stride + c * 8 : 0) * 2;
-        cp16(dst + at_chunk<DH>(j, c), a.kv.k + e, on);
-        cp16(dst + kSliceBytes + at_chunk<DH>(j, c), a.kv.v + e, on);
+        for (int i = 0; i < kIter; ++i) {
+          const int j = (i * 32 + lane) / CPR, c = lane % CPR;
+          const bool on = all || (key0 + j >= f.lo && key0 + j < f.hi);
+          cp16(dst + at_chunk<DH>(j, c), on ? k + i * hop : a.kv.k, on);
+          cp16(dst + kSliceBytes + at_chunk<DH>(j, c), on ? v + i * hop : a.kv.v, on);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kIter; ++i) {
+          cp16(dst + (i * 32 + lane) * 16, a.kv.k, false);
+          cp16(dst + kSliceBytes + (i * 32 + lane) * 16, a.kv.v, false);
+        }
       }
       if (++f_stage == kStages) f_stage = 0;
       if (++f_tile == f.n_tiles) {
         f_tile = 0;
         f_more = paged_next(a, plan, f, run1);
       }
+      if ((f_tile & 31) == 0 && f_more) entries();
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
 #pragma unroll
   for (int s = 0; s < kStages; ++s) fetch();
 
-  int stage = 0;
-  for (bool more = true; more;) {
-    // ---- queries and what each of this thread's two rows attends to
-    const int G = a.group;
-    uint32_t qf[kSteps][4];
-    int lo[2], hi[2];
-    int all_lo = 0, all_hi = 0x7fffffff;         // keys every live row of the item sees
+  const int G = a.group;
+  uint32_t qf[kSteps][4];
+  int lo[2], hi[2], all_lo, all_hi;              // what this thread's two rows attend to; keys every live row of the item sees
+  auto queries = [&](const PagedPiece& p) {
+    all_lo = 0; all_hi = 0x7fffffff;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int m = p.rg * kRows + g + 8 * h;
       const bool live = m < p.len * G;
-      const int r = live ? m / G : 0, head = p.head * G + (live ? m % G : 0);
+      const int r = live ? a.by_group.of(m) : 0, head = p.head * G + (live ? m - r * G : 0);
       if (live) {
         paged_range(a.mask, a.window, p.len, p.kv, r, r, lo[h], hi[h]);
         all_lo = max(all_lo, lo[h]);
@@ -145,7 +155,13 @@ k_paged_few(PagedAttnArgs a) {
     }
     all_lo = __reduce_max_sync(0xffffffffu, all_lo);
     all_hi = __reduce_min_sync(0xffffffffu, all_hi);
+  };
+  queries(p);
 
+  // items shared with other CTAs, at most two: the run's first and its last
+  struct Shared { int c0, c1, start, len, rg, head; } shared[2] = {{-1, 0, 0, 0, 0, 0}, {-1, 0, 0, 0, 0, 0}};
+  int stage = 0;
+  for (bool more = true; more;) {
     float o[DH / 8][4];
 #pragma unroll
     for (int n = 0; n < DH / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
@@ -260,7 +276,7 @@ k_paged_few(PagedAttnArgs a) {
       fetch();
     }
 
-    // ---- the warps' results meet: a row's sixteenth, eighth or quarter per thread
+    // ---- the warps' results meet: eight columns of a row per thread
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
@@ -270,11 +286,13 @@ k_paged_few(PagedAttnArgs a) {
       for (int n = 0; n < DH / 8; ++n) *reinterpret_cast<float2*>(dst + 8 * n) = make_float2(o[n][2 * h], o[n][2 * h + 1]);
       if (t == 0) s_ml[warp * kRows + g + 8 * h] = make_float2(m[h], l[h]);
     }
+    PagedPiece next = p;
+    more = paged_next(a, plan, next, run1);
+    if (more) queries(next);                     // (on their way while the results of this piece are written)
     __syncthreads();
     const int row = tid / CPR, c8 = tid % CPR * 8, mrow = p.rg * kRows + row;
-    const bool mine = row < kRows && mrow < p.len * G;
-    float acc[8], M = -INFINITY, L = 0.f;
-    if (mine) {
+    if (row < kRows && mrow < p.len * G) {
+      float acc[8], M = -INFINITY, L = 0.f;
       for (int w = 0; w < kWarps; ++w) M = fmaxf(M, s_ml[w * kRows + row].x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] = 0.f;
@@ -288,75 +306,90 @@ k_paged_few(PagedAttnArgs a) {
         acc[0] = fmaf(k, v0.x, acc[0]); acc[1] = fmaf(k, v0.y, acc[1]); acc[2] = fmaf(k, v0.z, acc[2]); acc[3] = fmaf(k, v0.w, acc[3]);
         acc[4] = fmaf(k, v1.x, acc[4]); acc[5] = fmaf(k, v1.y, acc[5]); acc[6] = fmaf(k, v1.z, acc[6]); acc[7] = fmaf(k, v1.w, acc[7]);
       }
-    }
-    bool write = p.whole;
-    if (!p.whole) {
-      const bool opens = p.item_at >= run0;
-      const long long slot = (long long)cta * 2 + (opens ? 1 : 0);
-      if (mine) {
-        float* dst = a.parts + (slot * kPagedMaxRows + row) * DH + c8;
+      if (p.whole) {
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        const int r = a.by_group.of(mrow);
+        const long long at = (long long)(p.start + r) * a.n_heads + p.head * G + (mrow - r * G);
+        *reinterpret_cast<uint4*>(a.out + (at * DH + c8) * 2) =
+            make_uint4(PagedType<T>::pack(acc[0] * inv, acc[1] * inv), PagedType<T>::pack(acc[2] * inv, acc[3] * inv),
+                       PagedType<T>::pack(acc[4] * inv, acc[5] * inv), PagedType<T>::pack(acc[6] * inv, acc[7] * inv));
+        if (a.lse != nullptr && c8 == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+      } else {
+        const long long at = ((long long)cta * 2 + (p.item_at >= run0 ? 1 : 0)) * kPagedMaxRows + row;
+        float* dst = a.parts + at * DH + c8;
         __stcg(reinterpret_cast<float4*>(dst), make_float4(acc[0], acc[1], acc[2], acc[3]));
         __stcg(reinterpret_cast<float4*>(dst + 4), make_float4(acc[4], acc[5], acc[6], acc[7]));
-        if (c8 == 0) __stcg(reinterpret_cast<float2*>(a.parts_ml) + slot * kPagedMaxRows + row, make_float2(M, L));
-      }
-      __threadfence();
-      __syncthreads();
-      const int c0 = paged_owner(p.item_at, total, n_cta), c1 = paged_owner(p.item_at + p.item_tiles - 1, total, n_cta);
-      if (tid == 0) {
-        const int last = atomicAdd(a.counters + c0, 1) == c1 - c0;
-        if (last) a.counters[c0] = 0;
-        *s_last = last;
-      }
-      __syncthreads();
-      write = *s_last != 0;
-      if (write && mine) {
-        __threadfence();
-        M = -INFINITY; L = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] = 0.f;
-        // (a batch's loads in flight together: one by one 18 pieces took 10 us)
-        constexpr int kBatch = 10;
-        for (int cb = c0; cb <= c1; cb += kBatch) {
-          float2 ml[kBatch];
-          float4 v0[kBatch], v1[kBatch];
-#pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            const long long at = ((long long)min(cb + i, c1) * 2 + (cb + i == c0 ? 1 : 0)) * kPagedMaxRows + row;
-            ml[i] = __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at);
-            v0[i] = __ldcg(reinterpret_cast<const float4*>(a.parts + at * DH + c8));
-            v1[i] = __ldcg(reinterpret_cast<const float4*>(a.parts + at * DH + c8 + 4));
-          }
-          float top = M;
-#pragma unroll
-          for (int i = 0; i < kBatch; ++i) top = fmaxf(top, ml[i].x);
-          const float keep = M == -INFINITY ? (L == 0.f ? 0.f : L) : paged_ex2(M - top);     // (L without a maximum is NaN)
-          M = top;
-          L *= keep;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) acc[e] *= keep;
-#pragma unroll
-          for (int i = 0; i < kBatch; ++i) {
-            if (cb + i > c1 || (ml[i].x == -INFINITY && ml[i].y == 0.f)) continue;           // (it saw nothing)
-            const float k = ml[i].x == -INFINITY ? 0.f : paged_ex2(ml[i].x - M);
-            L = fmaf(k, ml[i].y, L);
-            acc[0] = fmaf(k, v0[i].x, acc[0]); acc[1] = fmaf(k, v0[i].y, acc[1]); acc[2] = fmaf(k, v0[i].z, acc[2]); acc[3] = fmaf(k, v0[i].w, acc[3]);
-            acc[4] = fmaf(k, v1[i].x, acc[4]); acc[5] = fmaf(k, v1[i].y, acc[5]); acc[6] = fmaf(k, v1[i].z, acc[6]); acc[7] = fmaf(k, v1[i].w, acc[7]);
-          }
-        }
+        if (c8 == 0) __stcg(reinterpret_cast<float2*>(a.parts_ml) + at, make_float2(M, L));
       }
     }
-    if (write && mine) {
-      const float inv = L == 0.f ? 0.f : 1.f / L;
-      const long long r = (long long)(p.start + mrow / G) * a.n_heads + p.head * G + mrow % G;
-      *reinterpret_cast<uint4*>(a.out + (r * DH + c8) * 2) =
-          make_uint4(PagedType<T>::pack(acc[0] * inv, acc[1] * inv), PagedType<T>::pack(acc[2] * inv, acc[3] * inv),
-                     PagedType<T>::pack(acc[4] * inv, acc[5] * inv), PagedType<T>::pack(acc[6] * inv, acc[7] * inv));
-      if (a.lse != nullptr && c8 == 0) a.lse[r] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    if (!p.whole) {
+      const Shared s = {paged_owner(p.item_at, total, n_cta), paged_owner(p.item_at + p.item_tiles - 1, total, n_cta), p.start, p.len, p.rg, p.head};
+      if (p.item_at < run0) shared[0] = s;
+      else shared[1] = s;
     }
-    more = paged_next(a, plan, p, run1);
+    p = next;
     if (more) __syncthreads();                   // (the exchange rows are free again)
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
+
+  // ---- shared items: the CTA that arrives last adds the pieces up, in the order of the keys.  (Both at the end of the run: arriving takes 1.5 us of waiting for
+  // writes and the counter, during which the next piece's keys would not be fetched.)
+  if (shared[0].c0 < 0 && shared[1].c0 < 0) return;
+  __threadfence();
+  __syncthreads();
+  if (tid < 2) {
+    const int c0 = tid == 0 ? shared[0].c0 : shared[1].c0, c1 = tid == 0 ? shared[0].c1 : shared[1].c1;
+    int last = 0;
+    if (c0 >= 0) {
+      last = atomicAdd(a.counters + c0, 1) == c1 - c0;
+      if (last) a.counters[c0] = 0;
+    }
+    s_last[tid] = last;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int which = 0; which < 2; ++which) {
+    if (!s_last[which]) continue;
+    __threadfence();
+    const Shared s = which == 0 ? shared[0] : shared[1];
+    const int rows = min(kRows, s.len * G - s.rg * kRows);
+    for (int i = tid; i < rows * (DH / 4); i += kThreads) {
+      const int row = i / (DH / 4), c4 = i % (DH / 4) * 4;
+      float M = -INFINITY, L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+      // (a batch's loads in flight together: one by one 18 pieces took 10 us)
+      constexpr int kBatch = 20;
+      for (int cb = s.c0; cb <= s.c1; cb += kBatch) {
+        float2 ml[kBatch];
+        float4 v[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+          const long long at = ((long long)min(cb + j, s.c1) * 2 + (cb + j == s.c0 ? 1 : 0)) * kPagedMaxRows + row;
+          ml[j] = __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at);
+          v[j] = __ldcg(reinterpret_cast<const float4*>(a.parts + at * DH + c4));
+        }
+        float top = M;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) top = fmaxf(top, ml[j].x);
+        const float keep = M == -INFINITY ? (L == 0.f ? 0.f : L) : paged_ex2(M - top);     // (L without a maximum is NaN)
+        M = top;
+        L *= keep;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[e] *= keep;
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+          if (cb + j > s.c1 || (ml[j].x == -INFINITY && ml[j].y == 0.f)) continue;         // (it saw nothing)
+          const float k = ml[j].x == -INFINITY ? 0.f : paged_ex2(ml[j].x - M);
+          L = fmaf(k, ml[j].y, L);
+          acc[0] = fmaf(k, v[j].x, acc[0]); acc[1] = fmaf(k, v[j].y, acc[1]); acc[2] = fmaf(k, v[j].z, acc[2]); acc[3] = fmaf(k, v[j].w, acc[3]);
+        }
+      }
+      const float inv = L == 0.f ? 0.f : 1.f / L;
+      const int mrow = s.rg * kRows + row, r = a.by_group.of(mrow);
+      const long long at = (long long)(s.start + r) * a.n_heads + s.head * G + (mrow - r * G);
+      *reinterpret_cast<uint2*>(a.out + (at * DH + c4) * 2) = make_uint2(PagedType<T>::pack(acc[0] * inv, acc[1] * inv), PagedType<T>::pack(acc[2] * inv, acc[3] * inv));
+      if (a.lse != nullptr && c4 == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    }
+  }
 }
 
 template <typename T, int DH>
@@ -374,6 +407,7 @@ cs_status launch_few(cs_paged_cache* c, const PagedAttnArgs& a, unsigned bit, cu
 cs_status cs_launch_paged_few(cs_paged_cache* c, const PagedAttnArgs& args, cudaStream_t st) {
   PagedAttnArgs a = args;
   a.item_rows = kRows;
+  a.by_item_rows = PagedDivisor::by(kRows);
   const bool bf = c->cfg.dtype == CS_BF16;
   switch (c->cfg.head_dim) {
     case 32: return bf ? launch_few<__nv_bfloat16, 32>(c, a, 1, st) : launch_few<__half, 32>(c, a, 2, st);

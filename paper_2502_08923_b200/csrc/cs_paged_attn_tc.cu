@@ -656,6 +656,7 @@ cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& args, cudaS
   PagedAttnArgs a = args;
   const int tokens = kM / a.group;                 // rows of the block in a slot, with all heads of the group
   a.item_rows = 2 * tokens * a.group;
+  a.by_item_rows = PagedDivisor::by(a.item_rows);
   const int box_rows = tokens < a.blk.rows ? tokens : a.blk.rows, dh = c->cfg.head_dim;
   CUtensorMap tmQ;
   // (a stride that no second row or head uses may be anything)
