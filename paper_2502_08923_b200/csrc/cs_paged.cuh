@@ -68,6 +68,7 @@ struct PagedAttnArgs {
   int mask, window;
   float scale_log2e, scale;
   int item_rows;               // query rows (row of the block x head of the group) per work item
+  int item_cost;               // what an item costs beside its tiles, in tiles
   PagedDivisor by_group, by_item_rows;
   float *parts, *parts_ml;
   int *counters, *status;
@@ -97,15 +98,16 @@ __device__ __forceinline__ void paged_range(int mask, int window, int len, int k
 
 // Work is dealt out in key tiles.  An item is one (sequence, KV head, group of item_rows query rows); its tiles are the
 // kPagedTile-aligned ones its rows attend to, one at least (a row without keys is written too).  Items in the order
-// (sequence, head, row group) make one line of tiles, of which every CTA takes an equal run: CTA i of n the tiles
-// [total * i / n, total * (i + 1) / n).  So no CTA waits for another, none has more than one tile more than the
-// others whatever the lengths are, and at most two items of a CTA are shared with others.
-// (rows x heads stay below 2^31)
-__device__ __forceinline__ int paged_item_tiles(const PagedAttnArgs& a, int len, int kv, int rg) {
+// (sequence, head, row group) make one line, of which every CTA takes an equal run: CTA i of n the places
+// [total * i / n, total * (i + 1) / n).  So no CTA waits for another, none has more to do than the others whatever the
+// lengths are, and at most two items of a CTA are shared with others.  An item takes item_cost places, in front of one for each
+// tile: changing from one to the next costs time as well (64 single tokens over 500 - 4,097 keys of the 8B shape, nothing / two places for it: FIG_COST us).
+// places of an item in the line (rows x heads stay below 2^31)
+__device__ __forceinline__ int paged_item_places(const PagedAttnArgs& a, int len, int kv, int rg) {
   const int r0 = a.by_group.of(rg * a.item_rows), r1 = min(len - 1, a.by_group.of(rg * a.item_rows + a.item_rows - 1));
   int lo, hi;
   paged_range(a.mask, a.window, len, kv, r0, r1, lo, hi);
-  return hi > lo ? (hi + kPagedTile - 1) / kPagedTile - lo / kPagedTile : 1;
+  return a.item_cost + (hi > lo ? (hi + kPagedTile - 1) / kPagedTile - lo / kPagedTile : 1);
 }
 __device__ __forceinline__ int paged_row_groups(const PagedAttnArgs& a, int len) {
   return a.by_item_rows.of(len * a.group + a.item_rows - 1);
@@ -115,19 +117,19 @@ __device__ __forceinline__ long long paged_div(long long x, long long y) {
   return ((x | y) >> 32) == 0 ? (long long)((unsigned)x / (unsigned)y) : x / y;
 }
 
-// a block's items of one KV head, by a whole warp: their tiles together
+// a block's items of one KV head, by a whole warp: their places together
 __device__ __forceinline__ long long paged_block_tiles(const PagedAttnArgs& a, int len, int kv, int lane) {
   const int n = paged_row_groups(a, len);
   long long sum = 0;
-  for (int g = lane; g < n; g += 32) sum += paged_item_tiles(a, len, kv, g);
+  for (int g = lane; g < n; g += 32) sum += paged_item_places(a, len, kv, g);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   return sum;
 }
 
 struct PagedPlan {                              // in shared memory
-  long long before[kPagedMaxSeqs + 1];          // tiles of the sequences before this one
-  long long per_head[kPagedMaxSeqs];            // tiles of one of its KV heads
+  long long before[kPagedMaxSeqs + 1];          // places of the sequences before this one
+  long long per_head[kPagedMaxSeqs];            // places of one of its KV heads
   int start[kPagedMaxSeqs], len[kPagedMaxSeqs], kv[kPagedMaxSeqs];
   long long warp_sum[32];
   int tall[kPagedMaxSeqs], n_tall;              // sequences whose row groups a warp adds up
@@ -156,7 +158,7 @@ __device__ __forceinline__ void paged_plan(const PagedAttnArgs& a, PagedPlan& p)
     if (lane < B) {
       paged_load_block(a, p, lane, warp == 0, len, kv);
       n = paged_row_groups(a, len);
-      if (n <= 2) for (int g = 0; g < n; ++g) t += paged_item_tiles(a, len, kv, g);
+      if (n <= 2) for (int g = 0; g < n; ++g) t += paged_item_places(a, len, kv, g);
     }
     for (unsigned tall = __ballot_sync(0xffffffffu, n > 2); tall != 0; tall &= tall - 1) {
       const int b = __ffs(tall) - 1;
@@ -183,7 +185,7 @@ __device__ __forceinline__ void paged_plan(const PagedAttnArgs& a, PagedPlan& p)
     const int n = paged_row_groups(a, len);
     long long t = 0;
     if (n <= 2) {
-      for (int g = 0; g < n; ++g) t += paged_item_tiles(a, len, kv, g);
+      for (int g = 0; g < n; ++g) t += paged_item_places(a, len, kv, g);
     } else {
       p.tall[atomicAdd(&p.n_tall, 1)] = b;
     }
@@ -226,11 +228,11 @@ struct PagedPiece {
   int lo, hi;                  // keys the item's rows attend to between them
   int tile0, n_tiles;          // first tile (absolute: key / kPagedTile) and how many are this CTA's
   int item_tiles;
-  long long item_at;           // where the item's tiles begin in the line
-  bool whole;
+  long long item_at;           // where the item begins in the line
+  bool opens, whole;           // has the item's first tile; has all of them
 };
 
-// Piece that begins at tile `at` of the line, by a whole warp (all lanes get it); `end`: where the CTA's run ends.
+// Piece that begins at place `at` of the line, by a whole warp (all lanes get it); `end`: where the CTA's run ends.  It may be empty: n_tiles 0.
 __device__ __forceinline__ PagedPiece paged_piece(const PagedAttnArgs& a, const PagedPlan& p, long long at, long long end, int lane) {
   PagedPiece o;
   // the last sequence that begins at or before it (32 at a time)
@@ -245,9 +247,9 @@ __device__ __forceinline__ PagedPiece paged_piece(const PagedAttnArgs& a, const 
   rest -= o.head * per_head;
   // row group: 32 at a time
   const int n = paged_row_groups(a, o.len);
-  int g0 = 0, tiles = (int)per_head;
+  int g0 = 0, places = (int)per_head;
   for (; n > 1; g0 += 32) {
-    const int t = g0 + lane < n ? paged_item_tiles(a, o.len, o.kv, g0 + lane) : 0;
+    const int t = g0 + lane < n ? paged_item_places(a, o.len, o.kv, g0 + lane) : 0;
     int inc = t;
 #pragma unroll
     for (int s = 1; s < 32; s <<= 1) {
@@ -257,8 +259,8 @@ __device__ __forceinline__ PagedPiece paged_piece(const PagedAttnArgs& a, const 
     const unsigned ends_behind = __ballot_sync(0xffffffffu, (long long)inc > rest);
     if (ends_behind != 0 || g0 + 32 >= n) {
       const int l = ends_behind != 0 ? __ffs(ends_behind) - 1 : 0;
-      tiles = __shfl_sync(0xffffffffu, t, l);
-      rest -= __shfl_sync(0xffffffffu, inc, l) - tiles;
+      places = __shfl_sync(0xffffffffu, t, l);
+      rest -= __shfl_sync(0xffffffffu, inc, l) - places;
       g0 += l;
       break;
     }
@@ -267,17 +269,19 @@ __device__ __forceinline__ PagedPiece paged_piece(const PagedAttnArgs& a, const 
   o.rg = g0;
   const int r0 = a.by_group.of(g0 * a.item_rows), r1 = min(o.len - 1, a.by_group.of(g0 * a.item_rows + a.item_rows - 1));
   paged_range(a.mask, a.window, o.len, o.kv, r0, r1, o.lo, o.hi);
-  o.item_tiles = tiles;
+  o.item_tiles = places - a.item_cost;
   o.item_at = at - rest;
-  o.tile0 = (o.hi > o.lo ? o.lo / kPagedTile : 0) + (int)rest;
-  o.n_tiles = (int)min((long long)tiles - rest, end - at);
-  o.whole = o.n_tiles == tiles;
+  const int skip = max(0, (int)rest - a.item_cost);            // tiles that the CTAs before have
+  o.tile0 = (o.hi > o.lo ? o.lo / kPagedTile : 0) + skip;
+  o.n_tiles = (int)min((long long)(o.item_tiles - skip), max(0ll, end - o.item_at - a.item_cost - skip));
+  o.opens = skip == 0;
+  o.whole = o.n_tiles == o.item_tiles;
   return o;
 }
 // The piece after one, if the CTA's run goes on behind it.
 __device__ __forceinline__ bool paged_next(const PagedAttnArgs& a, const PagedPlan& plan, PagedPiece& p, long long end) {
-  const long long at = p.item_at + p.item_tiles;
-  if (at >= end) return false;
+  const long long at = p.item_at + p.item_tiles + a.item_cost;
+  if (at + a.item_cost >= end) return false;
   if (p.rg + 1 < paged_row_groups(a, p.len)) ++p.rg;
   else {
     p.rg = 0;
@@ -292,12 +296,16 @@ __device__ __forceinline__ bool paged_next(const PagedAttnArgs& a, const PagedPl
   p.tile0 = p.hi > p.lo ? p.lo / kPagedTile : 0;
   p.item_tiles = p.hi > p.lo ? (p.hi + kPagedTile - 1) / kPagedTile - p.tile0 : 1;
   p.item_at = at;
-  p.n_tiles = (int)min((long long)p.item_tiles, end - at);
+  p.n_tiles = (int)min((long long)p.item_tiles, end - at - a.item_cost);
+  p.opens = true;
   p.whole = p.n_tiles == p.item_tiles;
   return true;
 }
-// the CTA (of n) whose run holds tile x of a line of `total`
+// The CTA (of n) whose run holds place x of a line of `total`; the first and the last one of an item's CTAs.
 __device__ __forceinline__ int paged_owner(long long x, long long total, int n) { return (int)paged_div((x + 1) * n - 1, total); }
+
+__device__ __forceinline__ int paged_first_cta(const PagedAttnArgs& a, const PagedPiece& p, long long total, int n) { return paged_owner(p.item_at + a.item_cost, total, n); }
+__device__ __forceinline__ int paged_last_cta(const PagedAttnArgs& a, const PagedPiece& p, long long total, int n) { return paged_owner(p.item_at + a.item_cost + p.item_tiles - 1, total, n); }
 
 // 2^x, hardware approximation (relative error about 2^-22; -inf gives 0)
 __device__ __forceinline__ float paged_ex2(float x) {

@@ -26,7 +26,8 @@ namespace {
 
 constexpr int kWarps = 8, kThreads = kWarps * 32, kSlice = 16, kRows = 16;
 template <int DH> constexpr int kFewStages = DH == 128 ? 2 : 4;
-template <int DH> constexpr int kFewSmem = kWarps * kFewStages<DH> * 2 * kSlice * DH * 2 + kWarps * kRows * (DH + 8) * 4 + kWarps * kRows * 8 + (int)sizeof(PagedPlan) + 16;
+template <int DH> constexpr int kFewSmem = kWarps * kFewStages<DH> * 2 * kSlice * DH * 2 + kWarps * kRows * (DH + 8) * 4 + kWarps * kRows * 8 +
+                                         (kFewStages<DH> + 1) * kRows * DH * 2 + (int)sizeof(PagedPlan) + 16;
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool on) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
@@ -68,7 +69,8 @@ k_paged_few(PagedAttnArgs a) {
   uint8_t* ring = smem;                                                                  // [warp][stage][K, V][16 keys][DH]
   float* s_o = reinterpret_cast<float*>(ring + kWarps * kStages * 2 * kSliceBytes);        // [warp][16 rows][kLd]
   float2* s_ml = reinterpret_cast<float2*>(s_o + kWarps * kRows * kLd);                      // [warp][16 rows]
-  PagedPlan& plan = *reinterpret_cast<PagedPlan*>(s_ml + kWarps * kRows);
+  uint8_t* s_q = reinterpret_cast<uint8_t*>(s_ml + kWarps * kRows);                          // [kStages + 1][16 rows][DH]: queries of the pieces being fetched
+  PagedPlan& plan = *reinterpret_cast<PagedPlan*>(s_q + (kStages + 1) * kRows * DH * 2);
   int* s_last = reinterpret_cast<int*>(&plan + 1);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
 
@@ -83,7 +85,20 @@ k_paged_few(PagedAttnArgs a) {
 
   // ---- the fetching side: runs kStages slices ahead, across pieces
   PagedPiece p = paged_piece(a, plan, run0, run1, lane), f = p;
-  int f_tile = 0, f_entry = 0, f_stage = 0;
+  if (p.n_tiles == 0) return;                    // (a run may hold nothing but the place an item begins with)
+  const int G = a.group;
+  int f_tile = 0, f_entry = 0, f_stage = 0, f_q = 0, q_at = 0;
+  // Queries go through shared memory, with the fetched piece: two rows by every warp.  (Loaded where the piece begins they waited behind all keys in flight: 2.5 us.)
+  auto queries = [&]() {
+    const int row = lane / CPR + warp * 2, c = lane % CPR, m = f.rg * kRows + row, r = a.by_group.of(m);
+    if (lane < 2 * CPR) {
+      const bool live = m < f.len * G;
+      const char* src = a.q + (live ? (f.start + r) * a.q_row + (f.head * G + m - r * G) * a.q_head + c * 8 : 0) * 2;
+      cp16((uint32_t)__cvta_generic_to_shared(s_q) + (uint32_t)(f_q * kRows * DH * 2) + at_chunk<DH>(row, c), src, live);
+    }
+    if (++f_q == kStages + 1) f_q = 0;
+  };
+  queries();
   bool f_more = true;
   // page-table entries of this warp's slices of the next 32 tiles, one per lane: asked for a slice before the first is needed
   auto entries = [&]() {
@@ -121,6 +136,7 @@ k_paged_few(PagedAttnArgs a) {
       if (++f_tile == f.n_tiles) {
         f_tile = 0;
         f_more = paged_next(a, plan, f, run1);
+        if (f_more) queries();
       }
       if ((f_tile & 31) == 0 && f_more) entries();
     }
@@ -129,39 +145,36 @@ k_paged_few(PagedAttnArgs a) {
 #pragma unroll
   for (int s = 0; s < kStages; ++s) fetch();
 
-  const int G = a.group;
   uint32_t qf[kSteps][4];
   int lo[2], hi[2], all_lo, all_hi;              // what this thread's two rows attend to; keys every live row of the item sees
-  auto queries = [&](const PagedPiece& p) {
+  auto begin = [&]() {
     all_lo = 0; all_hi = 0x7fffffff;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int m = p.rg * kRows + g + 8 * h;
-      const bool live = m < p.len * G;
-      const int r = live ? a.by_group.of(m) : 0, head = p.head * G + (live ? m - r * G : 0);
-      if (live) {
+      lo[h] = hi[h] = 0;
+      if (m < p.len * G) {
+        const int r = a.by_group.of(m);
         paged_range(a.mask, a.window, p.len, p.kv, r, r, lo[h], hi[h]);
         all_lo = max(all_lo, lo[h]);
         all_hi = min(all_hi, hi[h]);
-      } else {
-        lo[h] = hi[h] = 0;
-      }
-      const char* src = a.q + ((long long)(p.start + r) * a.q_row + head * a.q_head) * 2 + 4 * t;
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        qf[s][h] = live ? __ldcg(reinterpret_cast<const unsigned*>(src + 32 * s)) : 0u;
-        qf[s][h + 2] = live ? __ldcg(reinterpret_cast<const unsigned*>(src + 32 * s + 16)) : 0u;
       }
     }
     all_lo = __reduce_max_sync(0xffffffffu, all_lo);
     all_hi = __reduce_min_sync(0xffffffffu, all_hi);
+    const uint32_t q = (uint32_t)__cvta_generic_to_shared(s_q) + (uint32_t)(q_at * kRows * DH * 2);
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) ldm4(q + at_chunk<DH>((lane & 7) + (((lane >> 3) & 1) << 3), 2 * s + (lane >> 4)), qf[s]);
+    if (++q_at == kStages + 1) q_at = 0;
   };
-  queries(p);
+  asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
+  __syncthreads();
 
   // items shared with other CTAs, at most two: the run's first and its last
   struct Shared { int c0, c1, start, len, rg, head; } shared[2] = {{-1, 0, 0, 0, 0, 0}, {-1, 0, 0, 0, 0, 0}};
   int stage = 0;
   for (bool more = true; more;) {
+    begin();                                     // (its queries came with the last slice of the piece before, or the first of all)
     float o[DH / 8][4];
 #pragma unroll
     for (int n = 0; n < DH / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
@@ -288,7 +301,6 @@ k_paged_few(PagedAttnArgs a) {
     }
     PagedPiece next = p;
     more = paged_next(a, plan, next, run1);
-    if (more) queries(next);                     // (on their way while the results of this piece are written)
     __syncthreads();
     const int row = tid / CPR, c8 = tid % CPR * 8, mrow = p.rg * kRows + row;
     if (row < kRows && mrow < p.len * G) {
@@ -315,7 +327,7 @@ k_paged_few(PagedAttnArgs a) {
                        PagedType<T>::pack(acc[4] * inv, acc[5] * inv), PagedType<T>::pack(acc[6] * inv, acc[7] * inv));
         if (a.lse != nullptr && c8 == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
       } else {
-        const long long at = ((long long)cta * 2 + (p.item_at >= run0 ? 1 : 0)) * kPagedMaxRows + row;
+        const long long at = ((long long)cta * 2 + (p.opens ? 1 : 0)) * kPagedMaxRows + row;
         float* dst = a.parts + at * DH + c8;
         __stcg(reinterpret_cast<float4*>(dst), make_float4(acc[0], acc[1], acc[2], acc[3]));
         __stcg(reinterpret_cast<float4*>(dst + 4), make_float4(acc[4], acc[5], acc[6], acc[7]));
@@ -323,9 +335,9 @@ k_paged_few(PagedAttnArgs a) {
       }
     }
     if (!p.whole) {
-      const Shared s = {paged_owner(p.item_at, total, n_cta), paged_owner(p.item_at + p.item_tiles - 1, total, n_cta), p.start, p.len, p.rg, p.head};
-      if (p.item_at < run0) shared[0] = s;
-      else shared[1] = s;
+      const Shared s = {paged_first_cta(a, p, total, n_cta), paged_last_cta(a, p, total, n_cta), p.start, p.len, p.rg, p.head};
+      if (p.opens) shared[1] = s;
+      else shared[0] = s;
     }
     p = next;
     if (more) __syncthreads();                   // (the exchange rows are free again)
@@ -352,42 +364,60 @@ k_paged_few(PagedAttnArgs a) {
     if (!s_last[which]) continue;
     __threadfence();
     const Shared s = which == 0 ? shared[0] : shared[1];
-    const int rows = min(kRows, s.len * G - s.rg * kRows);
-    for (int i = tid; i < rows * (DH / 4); i += kThreads) {
-      const int row = i / (DH / 4), c4 = i % (DH / 4) * 4;
-      float M = -INFINITY, L = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-      // (a batch's loads in flight together: one by one 18 pieces took 10 us)
-      constexpr int kBatch = 20;
-      for (int cb = s.c0; cb <= s.c1; cb += kBatch) {
-        float2 ml[kBatch];
-        float4 v[kBatch];
+    // The pieces come into the ring, all in flight together, and are added up from there.  (Through registers it is either one piece after the other, 10 us
+    // for 18, or a body of some thousand instructions that nobody has run yet: 5 us.)
+    const int rows = min(kRows, s.len * G - s.rg * kRows), fit = kWarps * kStages * 2 * kSliceBytes / (rows * DH * 4);
+    constexpr int kTasks = (kRows * DH / 4 + kThreads - 1) / kThreads;      // (row, four columns) of a thread
+    const uint32_t s_parts = (uint32_t)__cvta_generic_to_shared(ring), s_pml = (uint32_t)__cvta_generic_to_shared(s_o);
+    float M[kTasks], L[kTasks], acc[kTasks][4];
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-          const long long at = ((long long)min(cb + j, s.c1) * 2 + (cb + j == s.c0 ? 1 : 0)) * kPagedMaxRows + row;
-          ml[j] = __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at);
-          v[j] = __ldcg(reinterpret_cast<const float4*>(a.parts + at * DH + c4));
-        }
-        float top = M;
+    for (int k = 0; k < kTasks; ++k) { M[k] = -INFINITY; L[k] = 0.f; acc[k][0] = acc[k][1] = acc[k][2] = acc[k][3] = 0.f; }
+#pragma unroll 1
+    for (int cb = s.c0; cb <= s.c1; cb += fit) {
+      const int n = min(fit, s.c1 - cb + 1);
+#pragma unroll 1
+      for (int i = warp; i < n * rows; i += kWarps) {
+        const int piece = i / rows, row = i - piece * rows;
+        const long long at = ((long long)(cb + piece) * 2 + (cb + piece == s.c0 ? 1 : 0)) * kPagedMaxRows + row;
+        if (lane < DH / 4) cp16(s_parts + (uint32_t)((i * (DH / 4) + lane) * 16), a.parts + at * DH + lane * 4, true);
+        if (lane == 0 && (row & 1) == 0) cp16(s_pml + (uint32_t)((piece * kRows + row) * 8), a.parts_ml + at * 2, true);     // (two rows)
+      }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncthreads();
 #pragma unroll
-        for (int j = 0; j < kBatch; ++j) top = fmaxf(top, ml[j].x);
-        const float keep = M == -INFINITY ? (L == 0.f ? 0.f : L) : paged_ex2(M - top);     // (L without a maximum is NaN)
-        M = top;
-        L *= keep;
+      for (int k = 0; k < kTasks; ++k) {
+        const int row = (tid + k * kThreads) / (DH / 4), c4 = (tid + k * kThreads) % (DH / 4);
+        if (row >= rows) continue;
+        const float2* ml = reinterpret_cast<const float2*>(s_o) + row;
+        float top = M[k];
+#pragma unroll 1
+        for (int j = 0; j < n; ++j) top = fmaxf(top, ml[j * kRows].x);
+        const float keep = M[k] == -INFINITY ? (L[k] == 0.f ? 0.f : L[k]) : paged_ex2(M[k] - top);     // (L without a maximum is NaN)
+        M[k] = top;
+        L[k] *= keep;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[e] *= keep;
-#pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-          if (cb + j > s.c1 || (ml[j].x == -INFINITY && ml[j].y == 0.f)) continue;         // (it saw nothing)
-          const float k = ml[j].x == -INFINITY ? 0.f : paged_ex2(ml[j].x - M);
-          L = fmaf(k, ml[j].y, L);
-          acc[0] = fmaf(k, v[j].x, acc[0]); acc[1] = fmaf(k, v[j].y, acc[1]); acc[2] = fmaf(k, v[j].z, acc[2]); acc[3] = fmaf(k, v[j].w, acc[3]);
+        for (int e = 0; e < 4; ++e) acc[k][e] *= keep;
+#pragma unroll 2
+        for (int j = 0; j < n; ++j) {
+          const float2 x = ml[j * kRows];
+          if (x.x == -INFINITY && x.y == 0.f) continue;                    // (it saw nothing)
+          const float w = x.x == -INFINITY ? 0.f : paged_ex2(x.x - top);
+          const float4 v = reinterpret_cast<const float4*>(ring)[(j * rows + row) * (DH / 4) + c4];
+          L[k] = fmaf(w, x.y, L[k]);
+          acc[k][0] = fmaf(w, v.x, acc[k][0]); acc[k][1] = fmaf(w, v.y, acc[k][1]); acc[k][2] = fmaf(w, v.z, acc[k][2]); acc[k][3] = fmaf(w, v.w, acc[k][3]);
         }
       }
-      const float inv = L == 0.f ? 0.f : 1.f / L;
+      __syncthreads();                           // (the ring is free again)
+    }
+#pragma unroll
+    for (int k = 0; k < kTasks; ++k) {
+      const int row = (tid + k * kThreads) / (DH / 4), c4 = (tid + k * kThreads) % (DH / 4) * 4;
+      if (row >= rows) continue;
+      const float inv = L[k] == 0.f ? 0.f : 1.f / L[k];
       const int mrow = s.rg * kRows + row, r = a.by_group.of(mrow);
       const long long at = (long long)(s.start + r) * a.n_heads + s.head * G + (mrow - r * G);
-      *reinterpret_cast<uint2*>(a.out + (at * DH + c4) * 2) = make_uint2(PagedType<T>::pack(acc[0] * inv, acc[1] * inv), PagedType<T>::pack(acc[2] * inv, acc[3] * inv));
-      if (a.lse != nullptr && c4 == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+      *reinterpret_cast<uint2*>(a.out + (at * DH + c4) * 2) = make_uint2(PagedType<T>::pack(acc[k][0] * inv, acc[k][1] * inv), PagedType<T>::pack(acc[k][2] * inv, acc[k][3] * inv));
+      if (a.lse != nullptr && c4 == 0) a.lse[at] = L[k] == 0.f ? -INFINITY : (M[k] + log2f(L[k])) * 0.6931471805599453f;
     }
   }
 }
@@ -408,6 +438,7 @@ cs_status cs_launch_paged_few(cs_paged_cache* c, const PagedAttnArgs& args, cuda
   PagedAttnArgs a = args;
   a.item_rows = kRows;
   a.by_item_rows = PagedDivisor::by(kRows);
+  a.item_cost = 1;
   const bool bf = c->cfg.dtype == CS_BF16;
   switch (c->cfg.head_dim) {
     case 32: return bf ? launch_few<__nv_bfloat16, 32>(c, a, 1, st) : launch_few<__half, 32>(c, a, 2, st);

@@ -146,6 +146,9 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   const int n_cta = (int)min((long long)gridDim.x, total), cta = blockIdx.x;
   const long long run0 = cta < n_cta ? paged_div(total * cta, n_cta) : 0, run1 = cta < n_cta ? paged_div(total * (cta + 1), n_cta) : 0;
 
+  const PagedPiece piece0 = run1 > run0 ? paged_piece(a, plan, run0, run1, lane) : PagedPiece{};
+  const bool work = run1 > run0 && piece0.n_tiles > 0;         // (a run may hold nothing but the place an item begins with)
+
   // Bounded waits.  Once one has run out all others return at once.
   auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
     if (mbar_try_wait(bar, parity)) return true;
@@ -173,8 +176,8 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (run1 > run0) {
-      PagedPiece p = paged_piece(a, plan, run0, run1, lane);
+    if (work) {
+      PagedPiece p = piece0;
       uint32_t base = 0, piece = 0;               // ring entries before this piece; pieces
       bool ok = true;
       if (warp == kMmaWarp) {
@@ -314,8 +317,8 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     // ------------------------------------------------------------------ softmax and results: one thread per query row
-    if (run1 > run0) {
-      PagedPiece p = paged_piece(a, plan, run0, run1, lane);
+    if (work) {
+      PagedPiece p = piece0;
       const int slot = warp >> 2, row = tid & 127, G = a.group;
       const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_col = lanes + kSCol + slot * 128, o_col = lanes + kOCol + slot * 128;
       uint32_t base = 0, s_phase = 0, o_phase[2] = {0, 0}, piece = 0;
@@ -460,8 +463,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         const bool good = *s_abort == 0;
         const int c_first = both ? 0 : slot * (DH / 2), c_last = both ? DH : c_first + DH / 2;
         const int item_row = (both ? slot * slot_rows : 0) + row;
-        const bool opens = p.item_at >= run0;
-        const long long part = ((long long)cta * 2 + (opens ? 1 : 0)) * kPagedMaxRows + item_row;
+        const long long part = ((long long)cta * 2 + (p.opens ? 1 : 0)) * kPagedMaxRows + item_row;
         const long long out_row = (long long)(p.start + (live ? mrow / G : 0)) * a.n_heads + p.head * G + (live ? mrow % G : 0);
         const float inv = l == 0.f ? 0.f : 1.f / l;
         if (some && good) {
@@ -522,9 +524,9 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           }
         }
         fence_before();
-        if (opens && !p.whole && tid == 0) {               // (the run ends with this item)
+        if (p.opens && !p.whole && tid == 0) {               // (the run ends with this item)
           PagedSplit d;
-          d.last = paged_owner(p.item_at + p.item_tiles - 1, total, n_cta);
+          d.last = paged_last_cta(a, p, total, n_cta);
           d.rows = min(a.item_rows, p.len * G - p.rg * a.item_rows);
           d.first_row = p.rg * a.item_rows; d.head = p.head; d.start = p.start;
           a.splits[cta] = d;
@@ -657,6 +659,7 @@ cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& args, cudaS
   const int tokens = kM / a.group;                 // rows of the block in a slot, with all heads of the group
   a.item_rows = 2 * tokens * a.group;
   a.by_item_rows = PagedDivisor::by(a.item_rows);
+  a.item_cost = 1;
   const int box_rows = tokens < a.blk.rows ? tokens : a.blk.rows, dh = c->cfg.head_dim;
   CUtensorMap tmQ;
   // (a stride that no second row or head uses may be anything)
