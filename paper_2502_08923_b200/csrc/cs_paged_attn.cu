@@ -369,42 +369,61 @@ k_paged_few(PagedAttnArgs a) {
     const int rows = min(kRows, s.len * G - s.rg * kRows), fit = kWarps * kStages * 2 * kSliceBytes / (rows * DH * 4);
     constexpr int kTasks = (kRows * DH / 4 + kThreads - 1) / kThreads;      // (row, four columns) of a thread
     const uint32_t s_parts = (uint32_t)__cvta_generic_to_shared(ring), s_pml = (uint32_t)__cvta_generic_to_shared(s_o);
-    float M[kTasks], L[kTasks], acc[kTasks][4];
+    float2* pml = reinterpret_cast<float2*>(s_o);      // [piece][16 rows]: reference point, then weight; sum
+    float acc[kTasks][4];
 #pragma unroll
-    for (int k = 0; k < kTasks; ++k) { M[k] = -INFINITY; L[k] = 0.f; acc[k][0] = acc[k][1] = acc[k][2] = acc[k][3] = 0.f; }
+    for (int k = 0; k < kTasks; ++k) acc[k][0] = acc[k][1] = acc[k][2] = acc[k][3] = 0.f;
+    if (tid < kRows) s_ml[tid] = make_float2(-INFINITY, 0.f);              // a row's reference point and sum so far
 #pragma unroll 1
     for (int cb = s.c0; cb <= s.c1; cb += fit) {
       const int n = min(fit, s.c1 - cb + 1);
 #pragma unroll 1
-      for (int i = warp; i < n * rows; i += kWarps) {
-        const int piece = i / rows, row = i - piece * rows;
-        const long long at = ((long long)(cb + piece) * 2 + (cb + piece == s.c0 ? 1 : 0)) * kPagedMaxRows + row;
-        if (lane < DH / 4) cp16(s_parts + (uint32_t)((i * (DH / 4) + lane) * 16), a.parts + at * DH + lane * 4, true);
-        if (lane == 0 && (row & 1) == 0) cp16(s_pml + (uint32_t)((piece * kRows + row) * 8), a.parts_ml + at * 2, true);     // (two rows)
+      for (int i = warp; i < n; i += kWarps) {
+        const long long at = ((long long)(cb + i) * 2 + (cb + i == s.c0 ? 1 : 0)) * kPagedMaxRows;
+        const float* src = a.parts + at * DH + lane * 4;
+        const uint32_t dst = s_parts + (uint32_t)((i * rows * (DH / 4) + lane) * 16);
+        if (2 * lane < rows) cp16(s_pml + (uint32_t)((i * kRows + 2 * lane) * 8), a.parts_ml + (at + 2 * lane) * 2, true);
+#pragma unroll 4
+        for (int j = lane; j < rows * (DH / 4); j += 32) cp16(dst + (uint32_t)((j - lane) * 16), src + (j - lane) * 4, true);
       }
       asm volatile("cp.async.wait_all;" ::: "memory");
+      __syncthreads();
+#pragma unroll 1
+      for (int row = warp; row < rows; row += kWarps) {
+        const float2 old = s_ml[row];
+        float top = old.x, sum = 0.f;
+        for (int j = lane; j < n; j += 32) top = fmaxf(top, pml[j * kRows + row].x);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        for (int j = lane; j < n; j += 32) {
+          const float2 x = pml[j * kRows + row];
+          const float w = x.x == -INFINITY ? 0.f : paged_ex2(x.x - top);
+          sum += x.x == -INFINITY && x.y == 0.f ? 0.f : w * x.y;           // (without a maximum, but a sum: NaN)
+          pml[j * kRows + row].x = w;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) {
+          const float keep = old.x == -INFINITY ? 1.f : paged_ex2(old.x - top);
+          s_ml[row] = make_float2(top, old.y * keep + sum);
+          s_ml[kRows + row].x = keep;
+        }
+      }
       __syncthreads();
 #pragma unroll
       for (int k = 0; k < kTasks; ++k) {
         const int row = (tid + k * kThreads) / (DH / 4), c4 = (tid + k * kThreads) % (DH / 4);
         if (row >= rows) continue;
-        const float2* ml = reinterpret_cast<const float2*>(s_o) + row;
-        float top = M[k];
-#pragma unroll 1
-        for (int j = 0; j < n; ++j) top = fmaxf(top, ml[j * kRows].x);
-        const float keep = M[k] == -INFINITY ? (L[k] == 0.f ? 0.f : L[k]) : paged_ex2(M[k] - top);     // (L without a maximum is NaN)
-        M[k] = top;
-        L[k] *= keep;
+        const float keep = s_ml[kRows + row].x;
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[k][e] *= keep;
-#pragma unroll 2
+        const float4* v = reinterpret_cast<const float4*>(ring) + row * (DH / 4) + c4;
+#pragma unroll 4
         for (int j = 0; j < n; ++j) {
-          const float2 x = ml[j * kRows];
-          if (x.x == -INFINITY && x.y == 0.f) continue;                    // (it saw nothing)
-          const float w = x.x == -INFINITY ? 0.f : paged_ex2(x.x - top);
-          const float4 v = reinterpret_cast<const float4*>(ring)[(j * rows + row) * (DH / 4) + c4];
-          L[k] = fmaf(w, x.y, L[k]);
-          acc[k][0] = fmaf(w, v.x, acc[k][0]); acc[k][1] = fmaf(w, v.y, acc[k][1]); acc[k][2] = fmaf(w, v.z, acc[k][2]); acc[k][3] = fmaf(w, v.w, acc[k][3]);
+          const float2 x = pml[j * kRows + row];
+          const float4 y = v[j * rows * (DH / 4)];
+          if (x.x == 0.f && x.y == 0.f) continue;                          // (a piece that saw nothing)
+          acc[k][0] = fmaf(x.x, y.x, acc[k][0]); acc[k][1] = fmaf(x.x, y.y, acc[k][1]); acc[k][2] = fmaf(x.x, y.z, acc[k][2]); acc[k][3] = fmaf(x.x, y.w, acc[k][3]);
         }
       }
       __syncthreads();                           // (the ring is free again)
@@ -413,12 +432,14 @@ k_paged_few(PagedAttnArgs a) {
     for (int k = 0; k < kTasks; ++k) {
       const int row = (tid + k * kThreads) / (DH / 4), c4 = (tid + k * kThreads) % (DH / 4) * 4;
       if (row >= rows) continue;
-      const float inv = L[k] == 0.f ? 0.f : 1.f / L[k];
+      const float2 ml = s_ml[row];
+      const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;
       const int mrow = s.rg * kRows + row, r = a.by_group.of(mrow);
       const long long at = (long long)(s.start + r) * a.n_heads + s.head * G + (mrow - r * G);
       *reinterpret_cast<uint2*>(a.out + (at * DH + c4) * 2) = make_uint2(PagedType<T>::pack(acc[k][0] * inv, acc[k][1] * inv), PagedType<T>::pack(acc[k][2] * inv, acc[k][3] * inv));
-      if (a.lse != nullptr && c4 == 0) a.lse[at] = L[k] == 0.f ? -INFINITY : (M[k] + log2f(L[k])) * 0.6931471805599453f;
+      if (a.lse != nullptr && c4 == 0) a.lse[at] = ml.y == 0.f ? -INFINITY : (ml.x + log2f(ml.y)) * 0.6931471805599453f;
     }
+    __syncthreads();
   }
 }
 
@@ -438,7 +459,7 @@ cs_status cs_launch_paged_few(cs_paged_cache* c, const PagedAttnArgs& args, cuda
   PagedAttnArgs a = args;
   a.item_rows = kRows;
   a.by_item_rows = PagedDivisor::by(kRows);
-  a.item_cost = 1;
+  a.item_cost = 2;
   const bool bf = c->cfg.dtype == CS_BF16;
   switch (c->cfg.head_dim) {
     case 32: return bf ? launch_few<__nv_bfloat16, 32>(c, a, 1, st) : launch_few<__half, 32>(c, a, 2, st);
