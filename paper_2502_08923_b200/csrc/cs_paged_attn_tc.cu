@@ -17,9 +17,9 @@
 //
 // Warps 0-7 softmax, 8 issues MMAs, 9 and 10 fetch K and V tiles (a copy per page and 64 dims, page-table entries 32 at a time), 11 fetches queries.
 //
-// Keys no row of the item sees may hold anything: their scores are masked, their V rows set to zero in shared memory.  Tiles that some rows see and
-// others do not are looked through for values that are not finite (0 x inf is not 0): those are set to zero as well, and what
-// they do to the rows that see them is added where the results are written.
+// Keys no row of the item sees may hold anything: their scores are masked, their V rows set to zero in shared memory.  A value that is not finite at a key that some rows
+// of the item see and others do not reaches the others' sums too (0 x inf is not 0): a row whose result is not finite is looked at again where it is written
+// (mend_row).  (Tiles of such keys were looked through ahead of the product at first, which made them three times as long as others.)
 //
 // Every wait is bounded: on expiry the CTA flags CS_DEV_TIMEOUT, stops issuing, walks through its barriers, drains what is in flight, frees its TMEM and returns.
 #include <type_traits>
@@ -35,7 +35,8 @@ constexpr uint32_t kSCol = 0, kOCol = 256, kTmemCols = 512;        // slot x 128
 template <int DH> constexpr int kTileBytes = kPagedTile * DH * 2;  // of K, of V, and of a slot's queries
 template <int DH> constexpr int kStages = DH == 128 ? 4 : 8;
 constexpr int kCtl = 512;
-template <int DH> constexpr int kTcSmem = 1024 + (kStages<DH> + 2) * kTileBytes<DH> + kCtl + 2 * kM * 8 + (int)sizeof(PagedPlan);
+constexpr int kPieces = 4;         // descriptors of pieces (published at most two ahead of the products, of which the softmax may be one behind)
+template <int DH> constexpr int kTcSmem = 1024 + (kStages<DH> + 2) * kTileBytes<DH> + kCtl + 2 * kM * 8 + kPieces * 64 + (int)sizeof(PagedPlan);
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2, int c3) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
@@ -56,20 +57,16 @@ __device__ __forceinline__ void ld32(uint32_t taddr, float* v) {
       "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
       : CS_R32(v) : "r"(taddr));
 }
+__device__ __forceinline__ void ld16(uint32_t taddr, float* v) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]), "=f"(v[4]), "=f"(v[5]), "=f"(v[6]), "=f"(v[7]), "=f"(v[8]), "=f"(v[9]), "=f"(v[10]), "=f"(v[11]),
+                 "=f"(v[12]), "=f"(v[13]), "=f"(v[14]), "=f"(v[15]) : "r"(taddr));
+}
 __device__ __forceinline__ void ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void ld_valid(float* v) {
 #pragma unroll
   for (int i = 0; i < 32; i += 8)
     asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]), "+f"(v[i + 6]), "+f"(v[i + 7])::"memory");
-}
-__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t* v) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
-        "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
-        "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
 }
 __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -99,38 +96,108 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
 __device__ __forceinline__ void store32b(void* dst, const uint32_t* v) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
-// barrier of the eight softmax warps
-__device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
+// barrier of a slot's four softmax warps that also ORs a predicate
+__device__ __forceinline__ bool slot_any(int slot, bool pred) {
+  uint32_t out;
+  asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %2, 0;\nbar.red.or.pred q, %1, 128, p;\nselp.u32 %0, 1, 0, q;\n}" : "=r"(out) : "r"(slot + 1), "r"((uint32_t)pred) : "memory");
+  return out != 0;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// Weights 2^(score scale - m) of 32 keys, rounded to T, to tensor memory, and their sum.  (The 16-a-clock unit behind ex2 is busy for half of the loop's
+// time.  A polynomial in packed arithmetic for a quarter to three eighths of them was no faster in short runs and 2 - 4 % slower at the power cap.)
+template <typename T>
+__device__ __forceinline__ void weights(const float* v, uint32_t taddr, f32x2 sc2, f32x2 nm2, f32x2& l2) {
+  uint32_t w[16];
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    float x0, x1;
+    unpack2(fma2(pack2(v[2 * j], v[2 * j + 1]), sc2, nm2), x0, x1);
+    x0 = paged_ex2(x0);
+    x1 = paged_ex2(x1);
+    l2 = add2(l2, pack2(x0, x1));
+    w[j] = PagedType<T>::pack(x0, x1);
+  }
+  st16(taddr, w);
+}
 
 template <typename T>
-__device__ __forceinline__ uint32_t odd_halves(uint32_t w) {      // bits of the halves that are not finite
-  constexpr uint32_t e = std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;
-  return ((w & e) == e ? 0xffffu : 0u) | (((w >> 16) & e) == e ? 0xffff0000u : 0u);
+__device__ __forceinline__ float value_at(const char* base, long long element) {
+  if constexpr (std::is_same<T, __nv_bfloat16>::value) return __bfloat162float(__ushort_as_bfloat16(__ldcg(reinterpret_cast<const unsigned short*>(base) + element)));
+  else return __half2float(__ushort_as_half(__ldcg(reinterpret_cast<const unsigned short*>(base) + element)));
+}
+
+// What the roles need to know of a piece; worked out by one warp and left in shared memory, since the softmax threads have no register to spare (what they
+// spill lies beyond L1, which shared memory leaves next to nothing of: 350 bytes of it made the tile loop a third slower).
+struct TcPiece {
+  int start, len, kv, seq, head, rg;
+  int lo, hi, all_lo, all_hi;      // keys that some row of the item attends to, that all do
+  int tile0, steps;                // steps 0: there is no further piece
+  int both, opens, whole, last;    // both slots have rows of their own; has the item's first tile; all; the CTA with the last
+};
+
+// A row whose output is not finite, 32 columns of it: if a value that is not finite lies at a key that the row does not see but others of the item do, the product took it
+// in (0 x inf is not 0), and the row's sum is worked out again from the keys it does see, term by term.  `dst`: fp32 (part of an item, scale 1) or T.
+template <typename T, int DH>
+__device__ __noinline__ void mend_row(const PagedAttnArgs& a, const TcPiece& p, int n_tiles, int lo, int hi, long long q_at, float m, float scale_by, int c0, void* dst, bool part) {
+  const int first = max(p.lo, p.tile0 * kPagedTile), last = min(p.hi, (p.tile0 + n_tiles) * kPagedTile);
+  const int* table = a.blk.table + (long long)p.seq * a.blk.table_width;
+  auto at = [&](int key) -> long long {                    // element of the pools, -1: no such page
+    const int page = __ldcg(table + (key >> a.kv.page_shift));
+    return (unsigned)page < (unsigned)a.kv.n_pages ? page * a.kv.page_stride + p.head * a.kv.head_stride + (long long)(key & (a.kv.page_size - 1)) * a.kv.slot_stride : -1;
+  };
+  bool tainted = false;
+  for (int key = first; key < last && !tainted; ++key) {
+    if (key >= lo && key < hi) { key = min(hi, last) - 1; continue; }
+    const long long e = at(key);
+    for (int d = 0; d < 32 && e >= 0; ++d) tainted |= !(fabsf(value_at<T>(a.kv.v, e + c0 + d)) < INFINITY);
+  }
+  if (!tainted) return;
+  for (int d0 = 0; d0 < 32; d0 += 8) {
+    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int key = max(first, lo); key < min(last, hi); ++key) {
+      const long long e = at(key);
+      float s = 0.f;
+      for (int d = 0; d < DH && e >= 0; ++d) s = fmaf(value_at<T>(a.q, q_at + d), value_at<T>(a.kv.k, e + d), s);
+      const float w = paged_ex2(fmaf(s, a.scale_log2e, m == -INFINITY ? 0.f : -m));
+#pragma unroll
+      for (int d = 0; d < 8; ++d) o[d] = fmaf(w, e >= 0 ? value_at<T>(a.kv.v, e + c0 + d0 + d) : 0.f, o[d]);
+    }
+    for (int d = 0; d < 8; ++d) {
+      if (part) reinterpret_cast<float*>(dst)[d0 + d] = o[d];
+      else reinterpret_cast<unsigned short*>(dst)[d0 + d] = (unsigned short)PagedType<T>::pack(o[d] * scale_by, 0.f);
+    }
+  }
 }
 
 template <typename T, int DH>
 __global__ void __launch_bounds__(kThreads, 1)
-k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmQ, PagedAttnArgs a, int q_box_bytes) {
+k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ PagedAttnArgs a, int q_box_bytes) {
   constexpr int kTB = kTileBytes<DH>, kNS = kStages<DH>, kHalves = DH / 64, kHalf = kPagedTile * 128;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));   // [stage][64 dims][128 keys][128 B]
   uint8_t* sq = ring + kNS * kTB;                                       // [slot][64 dims][128 rows][128 B]
   uint64_t* bars = reinterpret_cast<uint64_t*>(sq + 2 * kTB);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kNS + 16);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kNS + 18);
   volatile int* s_abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  volatile int* s_odd = reinterpret_cast<volatile int*>(tmem_slot + 2);      // values that are not finite were taken out (by the parity of the piece)
   float2* s_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(bars) + kCtl);      // [slot][128 rows]
-  PagedPlan& plan = *reinterpret_cast<PagedPlan*>(s_ml + 2 * kM);
-  const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8 * kNS, b_s = b_empty + 8 * kNS, b_p = b_s + 16, b_o = b_p + 16, b_qfull = b_o + 16, b_qfree = b_qfull + 8,
-                 b_drain = b_qfree + 8;
+  TcPiece* s_piece = reinterpret_cast<TcPiece*>(s_ml + 2 * kM);
+  PagedPlan& plan = *reinterpret_cast<PagedPlan*>(s_piece + kPieces);
+  const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8 * kNS, b_s = b_empty + 8 * kNS, b_p = b_s + 16, b_p2 = b_p + 16, b_o = b_p2 + 16, b_qfull = b_o + 16, b_qfree = b_qfull + 8,
+                 b_drain = b_qfree + 8, b_piece = b_drain + 8, b_ml = b_piece + 8 * kPieces, b_read = b_ml + 8;
   const int tid = threadIdx.x, warp = (int)uniform(tid >> 5), lane = tid & 31;
 
   CS_PDL_PROLOGUE();
   if (tid == 0) {
     for (int s = 0; s < kNS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_empty + 8 * s, 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(b_s + 8 * s, 1); mbar_init(b_p + 8 * s, 4); mbar_init(b_o + 8 * s, 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(b_s + 8 * s, 1); mbar_init(b_p + 8 * s, 4); mbar_init(b_p2 + 8 * s, 4); mbar_init(b_o + 8 * s, 1); }
     mbar_init(b_qfull, 1); mbar_init(b_qfree, 1); mbar_init(b_drain, 1);
-    *s_abort = 0; s_odd[0] = 0; s_odd[1] = 0;
+    for (int s = 0; s < kPieces; ++s) mbar_init(b_piece + 8 * s, 1);
+    mbar_init(b_ml, 8); mbar_init(b_read, 8);
+    *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kMmaWarp) {
@@ -145,9 +212,6 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   const long long total = plan.before[a.blk.n_seqs];
   const int n_cta = (int)min((long long)gridDim.x, total), cta = blockIdx.x;
   const long long run0 = cta < n_cta ? paged_div(total * cta, n_cta) : 0, run1 = cta < n_cta ? paged_div(total * (cta + 1), n_cta) : 0;
-
-  const PagedPiece piece0 = run1 > run0 ? paged_piece(a, plan, run0, run1, lane) : PagedPiece{};
-  const bool work = run1 > run0 && piece0.n_tiles > 0;         // (a run may hold nothing but the place an item begins with)
 
   // Bounded waits.  Once one has run out all others return at once.
   auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
@@ -169,378 +233,398 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   };
   auto wait_warp = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, wait(bar, parity)); };
   const int slot_rows = a.item_rows / 2;          // query rows of a slot
-  auto two_slots = [&](const PagedPiece& p) { return p.len * a.group - p.rg * a.item_rows > slot_rows; };
+  // the next piece, once it is known (by a warp; false: a wait has run out)
+  auto known = [&](uint32_t piece) -> bool { return wait_warp(b_piece + 8 * (piece % kPieces), (piece / kPieces) & 1) && !__any_sync(0xffffffffu, *s_abort != 0); };
   // Order of the ring: K and V tiles in turn where the slots share them, else K0 K1 V0 K2 V1 ... (entry of step s, of n steps)
   auto k_entry = [](bool both, int s) { return both ? s & ~1 : s < 2 ? s : 2 * s - 1; };
   auto v_entry = [](bool both, int s, int n) { return both ? s | 1 : s + min(s + 2, n); };
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (work) {
-      PagedPiece p = piece0;
-      uint32_t base = 0, piece = 0;               // ring entries before this piece; pieces
-      bool ok = true;
-      if (warp == kMmaWarp) {
-        // ---------------------------------------------------------------- MMA issuer
-        constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u;
-        constexpr uint32_t idesc_s = (1u << 4) | kType | ((uint32_t)(kPagedTile >> 3) << 17) | ((uint32_t)(kM >> 4) << 24);
-        constexpr uint32_t idesc_o = (1u << 4) | kType | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(kM >> 4) << 24);   // B (= V) is MN-major
-        const uint64_t dq0 = desc_kmajor(smem_u32(sq)), dk0 = desc_kmajor(smem_u32(ring)), dv0 = desc_mnmajor(smem_u32(ring), kHalf);
-        uint32_t p_phase[2] = {0, 0};
-        for (bool more = true; more && ok;) {
-          const bool both = two_slots(p);
-          const int n = both ? 2 * p.n_tiles : p.n_tiles;
-          ok = wait_warp(b_qfull, piece & 1);
-          auto scores = [&](int s) {
-            const uint32_t e = base + k_entry(both, s), st = e % kNS;
-            if (!(both && (s & 1))) ok = wait_warp(b_full + 8 * st, (e / kNS) & 1);
-            if (!ok) return;
-            fence_after();
-            if (elect_one()) {
-              const uint64_t dk = dk0 + st * (kTB >> 4), dq = dq0 + (both && (s & 1) ? kTB >> 4 : 0);
-#pragma unroll
-              for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                  umma_bf16(tmem + kSCol + (s & 1) * 128, dq + h * (kHalf >> 4) + 2 * k, dk + h * (kHalf >> 4) + 2 * k, idesc_s, (h | k) ? 1u : 0u);
-              if (!both || (s & 1)) umma_commit(b_empty + 8 * st);
-              umma_commit(b_s + 8 * (s & 1));
-              if (s == n - 1) umma_commit(b_qfree);
-            }
-          };
-          if (ok) scores(0);
-          if (ok && n > 1) scores(1);
-          for (int s = 0; s < n && ok; ++s) {
-            const uint32_t e = base + v_entry(both, s, n), st = e % kNS;
-            ok = wait_warp(b_full + 8 * st, (e / kNS) & 1) && wait_warp(b_p + 8 * (s & 1), p_phase[s & 1]);
-            if (!ok) break;
-            p_phase[s & 1] ^= 1;
-            fence_after();
-            if (elect_one()) {
-              const uint64_t dv = dv0 + st * (kTB >> 4);
-#pragma unroll
-              for (int k = 0; k < 8; ++k)           // 16 keys per instruction
-                umma_ta(tmem + kOCol + (s & 1) * 128, tmem + kSCol + (s & 1) * 128 + k * 8, dv + k * (2048 >> 4), idesc_o, (s > 1 || k > 0) ? 1u : 0u);
-              if (!both || (s & 1)) umma_commit(b_empty + 8 * st);
-              if (s >= n - 2) umma_commit(b_o + 8 * (s & 1));
-            }
-            if (s + 2 < n) scores(s + 2);
-          }
-          base += 2 * p.n_tiles;
-          ++piece;
-          more = paged_next(a, plan, p, run1);
-        }
-        if (!ok) {                                   // what was issued must be done before its memory goes away
-          if (elect_one()) umma_commit(b_drain);
-          __syncwarp();
-          const unsigned long long t0 = globaltimer_ns();
-          while (!mbar_try_wait(b_drain, 0) && globaltimer_ns() - t0 < a.wait_ns) {}
-        }
-      } else if (warp == kQWarp) {
-        // ---------------------------------------------------------------- queries
-        for (bool more = true; more && ok;) {
-          const bool both = two_slots(p);
-          if (piece > 0) ok = wait_warp(b_qfree, (piece - 1) & 1);
-          if (!ok) break;
+    uint32_t base = 0, piece = 0;                 // ring entries before this piece; pieces
+    bool ok = true;
+    if (warp == kMmaWarp) {
+      // ------------------------------------------------------------------ MMA issuer
+      constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u;
+      constexpr uint32_t idesc_s = (1u << 4) | kType | ((uint32_t)(kPagedTile >> 3) << 17) | ((uint32_t)(kM >> 4) << 24);
+      constexpr uint32_t idesc_o = (1u << 4) | kType | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(kM >> 4) << 24);   // B (= V) is MN-major
+      const uint64_t dq0 = desc_kmajor(smem_u32(sq)), dk0 = desc_kmajor(smem_u32(ring)), dv0 = desc_mnmajor(smem_u32(ring), kHalf);
+      uint32_t p_phase[2] = {0, 0};
+      for (;; ++piece) {
+        ok = known(piece);
+        if (!ok) break;
+        const TcPiece& d = s_piece[piece % kPieces];
+        const int n = (int)uniform((uint32_t)d.steps);
+        const bool both = uniform((uint32_t)d.both) != 0;
+        if (n == 0) break;
+        ok = wait_warp(b_qfull, piece & 1);
+        auto scores = [&](int s) {
+          const uint32_t e = base + k_entry(both, s), st = e % kNS;
+          if (!(both && (s & 1))) ok = wait_warp(b_full + 8 * st, (e / kNS) & 1);
+          if (!ok) return;
+          fence_after();
           if (elect_one()) {
-            mbar_expect_tx(b_qfull, (uint32_t)(q_box_bytes * kHalves * (both ? 2 : 1)));
-            for (int s = 0; s < (both ? 2 : 1); ++s)
-              for (int h = 0; h < kHalves; ++h)
-                tma_load_3d(smem_u32(sq) + s * kTB + h * kHalf, &tmQ, b_qfull, 64 * h, p.head * a.group, p.start + (p.rg * a.item_rows + s * slot_rows) / a.group);
+            const uint64_t dk = dk0 + st * (kTB >> 4), dq = dq0 + (both && (s & 1) ? kTB >> 4 : 0);
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                umma_bf16(tmem + kSCol + (s & 1) * 128, dq + h * (kHalf >> 4) + 2 * k, dk + h * (kHalf >> 4) + 2 * k, idesc_s, (h | k) ? 1u : 0u);
+            umma_commit(b_s + 8 * (s & 1));
+            if (!both || (s & 1)) umma_commit(b_empty + 8 * st);
+            if (s == n - 1) umma_commit(b_qfree);
           }
-          ++piece;
-          more = paged_next(a, plan, p, run1);
-        }
-        // a copy that nobody waited for must land before the shared memory goes away
-        const unsigned long long t0 = globaltimer_ns();
-        while (!mbar_try_wait(b_qfull, (piece - 1) & 1) && globaltimer_ns() - t0 < a.wait_ns) {}
-      } else {
-        // ---------------------------------------------------------------- K tiles, V tiles
-        const bool is_k = warp == kKWarp;
-        const CUtensorMap* tm = is_k ? &tmK : &tmV;
-        const int rows = min(a.kv.page_size, kPagedTile), per_tile = kPagedTile / rows, shift = a.kv.page_shift;
-        uint32_t last_e[kNS], asked = 0;             // (bit per stage: a copy was started there)
+        };
+        if (ok) scores(0);
+        if (ok && n > 1) scores(1);
+        for (int s = 0; s < n && ok; ++s) {
+          const uint32_t e = base + v_entry(both, s, n), st = e % kNS;
+          ok = wait_warp(b_full + 8 * st, (e / kNS) & 1) && wait_warp(b_p + 8 * (s & 1), p_phase[s & 1]);
+          if (!ok) break;
+          const uint64_t dv = dv0 + st * (kTB >> 4);
+          const uint32_t acc = tmem + kOCol + (s & 1) * 128, w = tmem + kSCol + (s & 1) * 128;
+          fence_after();
+          if (elect_one()) {
 #pragma unroll
-        for (int i = 0; i < kNS; ++i) last_e[i] = 0;
-        for (bool more = true; more && ok;) {
-          const bool both = two_slots(p);
-          const int n = both ? 2 * p.n_tiles : p.n_tiles, inc = both ? 2 : 1;
-          int entry = 0, first = -64;                // this lane's page-table entry, and of which page the first lane has one
-          const int* table = a.blk.table + (long long)p.seq * a.blk.table_width;
-          for (int s = 0; s < n && ok; s += inc) {
-            const uint32_t e = base + (is_k ? k_entry(both, s) : v_entry(both, s, n)), st = e % kNS;
-            const int key0 = (p.tile0 + s / inc) * kPagedTile, page0 = key0 >> shift;
-            // pages of the tile that hold keys of the item
-            const int pa = max(key0, p.lo), pz = min(key0 + kPagedTile, p.hi);
-            int j0 = 0, j1 = 0;
-            if (pz > pa) { j0 = (pa >> shift) - page0; j1 = ((pz - 1) >> shift) - page0 + 1; }
-            if (page0 < first || page0 + per_tile > first + 32) {
-              first = page0;
-              const int page = first + lane;
-              entry = -1;
-              if (((long long)(page + 1) << shift) > p.lo && ((long long)page << shift) < p.hi) entry = __ldcg(table + page);
-            }
-            ok = wait_warp(b_empty + 8 * st, ((e / kNS) & 1) ^ 1);
-            if (!ok) break;
-            if (elect_one()) mbar_expect_tx(b_full + 8 * st, (uint32_t)((j1 - j0) * rows * 128 * kHalves));
-            __syncwarp();
-            for (int j = j0; j < j1; ++j) {
-              int page = (int)__shfl_sync(0xffffffffu, entry, page0 + j - first);
-              if ((unsigned)page >= (unsigned)a.kv.n_pages) {      // (a page behind the last one reads as zeros)
-                page = a.kv.n_pages;
-                if (lane == 0) atomicOr(a.status, CS_DEV_BADARG);
-              }
-              const int slot = (key0 + j * rows) & (a.kv.page_size - 1);
-              if (elect_one()) {
-                const uint32_t dst = smem_u32(ring) + st * kTB + j * rows * 128;
-#pragma unroll
-                for (int h = 0; h < kHalves; ++h) tma_load_4d(dst + h * kHalf, tm, b_full + 8 * st, 64 * h, slot, p.head, page);
-              }
-            }
-            asked |= 1u << st;
-#pragma unroll
-            for (int i = 0; i < kNS; ++i) if (i == (int)st) last_e[i] = e;
+            for (int k = 0; k < 4; ++k) umma_ta(acc, w + k * 8, dv + k * (2048 >> 4), idesc_o, (s > 1 || k > 0) ? 1u : 0u);   // 16 keys per instruction
           }
-          base += 2 * p.n_tiles;
-          more = paged_next(a, plan, p, run1);
-        }
-        if (!ok) {                                   // copies that nobody will consume must land before the shared memory goes away
+          ok = wait_warp(b_p2 + 8 * (s & 1), p_phase[s & 1]);
+          if (!ok) break;
+          p_phase[s & 1] ^= 1;
+          fence_after();
+          if (elect_one()) {
 #pragma unroll
-          for (int i = 0; i < kNS; ++i) {
-            const unsigned long long t0 = globaltimer_ns();
-            if (asked >> i & 1u)
-              while (!mbar_try_wait(b_full + 8 * i, (last_e[i] / kNS) & 1) && globaltimer_ns() - t0 < a.wait_ns) {}
+            for (int k = 4; k < 8; ++k) umma_ta(acc, w + k * 8, dv + k * (2048 >> 4), idesc_o, 1u);
+            if (!both || (s & 1)) umma_commit(b_empty + 8 * st);
+            if (s >= n - 2) umma_commit(b_o + 8 * (s & 1));
           }
+          if (s + 2 < n) scores(s + 2);
         }
+        base += both ? n : 2 * n;
+        if (!ok) break;
       }
+      if (!ok) {                                   // what was issued must be done before its memory goes away
+        if (elect_one()) umma_commit(b_drain);
+        __syncwarp();
+        const unsigned long long t0 = globaltimer_ns();
+        while (!mbar_try_wait(b_drain, 0) && globaltimer_ns() - t0 < a.wait_ns) {}
+      }
+    } else if (warp == kQWarp) {
+      // ------------------------------------------------------------------ pieces and queries
+      PagedPiece p;
+      p.n_tiles = 0;
+      if (run1 > run0) p = paged_piece(a, plan, run0, run1, lane);
+      bool more = p.n_tiles > 0;                   // (a run may hold nothing but the place an item begins with)
+      for (;; ++piece) {
+        const bool both = more && p.len * a.group - p.rg * a.item_rows > slot_rows;
+        if (lane == 0) {
+          TcPiece d;
+          d.steps = more ? (both ? 2 * p.n_tiles : p.n_tiles) : 0;
+          if (more) {
+            int x;
+            const int last_row = min(p.len * a.group, (p.rg + 1) * a.item_rows) - 1, r0 = a.by_group.of(p.rg * a.item_rows), r1 = a.by_group.of(last_row);
+            paged_range(a.mask, a.window, p.len, p.kv, r0, r0, x, d.all_hi);
+            paged_range(a.mask, a.window, p.len, p.kv, r1, r1, d.all_lo, x);
+            d.start = p.start; d.len = p.len; d.kv = p.kv; d.seq = p.seq; d.head = p.head; d.rg = p.rg;
+            d.lo = p.lo; d.hi = p.hi; d.tile0 = p.tile0; d.both = both; d.opens = p.opens; d.whole = p.whole;
+            d.last = p.whole ? cta : paged_last_cta(a, p, total, n_cta);
+          }
+          s_piece[piece % kPieces] = d;
+          mbar_arrive(b_piece + 8 * (piece % kPieces));
+        }
+        __syncwarp();
+        if (!more) break;
+        if (piece > 0) ok = wait_warp(b_qfree, (piece - 1) & 1);
+        if (!ok) break;
+        if (elect_one()) {
+          mbar_expect_tx(b_qfull, (uint32_t)(q_box_bytes * kHalves * (both ? 2 : 1)));
+          for (int s = 0; s < (both ? 2 : 1); ++s)
+            for (int h = 0; h < kHalves; ++h)
+              tma_load_3d(smem_u32(sq) + s * kTB + h * kHalf, &tmQ, b_qfull, 64 * h, p.head * a.group, p.start + a.by_group.of(p.rg * a.item_rows + s * slot_rows));
+        }
+        more = paged_next(a, plan, p, run1);
+      }
+      if (!ok) {
+        // (every role meets a last piece, and a copy that nobody waited for must land before the shared memory goes away)
+        const unsigned long long t0 = globaltimer_ns();
+        while (piece > 0 && !mbar_try_wait(b_qfull, (piece - 1) & 1) && globaltimer_ns() - t0 < a.wait_ns) {}
+      }
+    } else {
+      // ------------------------------------------------------------------ K tiles, V tiles
+      const bool is_k = warp == kKWarp;
+      const CUtensorMap* tm = is_k ? &tmK : &tmV;
+      const int rows = min(a.kv.page_size, kPagedTile), per_tile = kPagedTile / rows, shift = a.kv.page_shift;
+      uint32_t asked = 0;                          // entries this warp has started copies for, + 1
+      for (;; ++piece) {
+        if (!known(piece)) break;
+        const TcPiece& d = s_piece[piece % kPieces];
+        const int n = (int)uniform((uint32_t)d.steps), tile0 = (int)uniform((uint32_t)d.tile0), head = (int)uniform((uint32_t)d.head), lo = (int)uniform((uint32_t)d.lo),
+                  hi = (int)uniform((uint32_t)d.hi), seq = (int)uniform((uint32_t)d.seq);
+        const bool both = uniform((uint32_t)d.both) != 0;
+        if (n == 0) break;
+        const int inc = both ? 2 : 1;
+        int entry = 0, first = -64;                // this lane's page-table entry, and of which page the first lane has one
+        const int* table = a.blk.table + (long long)seq * a.blk.table_width;
+        for (int s = 0; s < n && ok; s += inc) {
+          const uint32_t e = base + (is_k ? k_entry(both, s) : v_entry(both, s, n)), st = e % kNS;
+          const int key0 = (tile0 + (both ? s >> 1 : s)) * kPagedTile, page0 = key0 >> shift;
+          // pages of the tile that hold keys of the item
+          const int pa = max(key0, lo), pz = min(key0 + kPagedTile, hi);
+          int j0 = 0, j1 = 0;
+          if (pz > pa) { j0 = (pa >> shift) - page0; j1 = ((pz - 1) >> shift) - page0 + 1; }
+          if (page0 < first || page0 + per_tile > first + 32) {
+            first = page0;
+            const int page = first + lane;
+            entry = -1;
+            if (((long long)(page + 1) << shift) > lo && ((long long)page << shift) < hi) entry = __ldcg(table + page);
+          }
+          ok = wait_warp(b_empty + 8 * st, ((e / kNS) & 1) ^ 1);
+          if (!ok) break;
+          if (elect_one()) mbar_expect_tx(b_full + 8 * st, (uint32_t)((j1 - j0) * rows * 128 * kHalves));
+          __syncwarp();
+          for (int j = j0; j < j1; ++j) {
+            int page = (int)__shfl_sync(0xffffffffu, entry, page0 + j - first);
+            if ((unsigned)page >= (unsigned)a.kv.n_pages) {      // (a page behind the last one reads as zeros)
+              page = a.kv.n_pages;
+              if (lane == 0) atomicOr(a.status, CS_DEV_BADARG);
+            }
+            const int slot = (key0 + j * rows) & (a.kv.page_size - 1);
+            if (elect_one()) {
+              const uint32_t dst = smem_u32(ring) + st * kTB + j * rows * 128;
+#pragma unroll
+              for (int h = 0; h < kHalves; ++h) tma_load_4d(dst + h * kHalf, tm, b_full + 8 * st, 64 * h, slot, head, page);
+            }
+          }
+          asked = e + 1;
+        }
+        base += both ? n : 2 * n;
+        if (!ok) break;
+      }
+      if (*s_abort)                                // copies that nobody will consume must land before the shared memory goes away
+        for (uint32_t e = asked > kNS ? asked - kNS : 0; e < asked; ++e) {
+          // (entries of the other warp's are waited for as well; one that was never started runs into the limit)
+          const unsigned long long t0 = globaltimer_ns();
+          while (!mbar_try_wait(b_full + 8 * (e % kNS), (e / kNS) & 1) && globaltimer_ns() - t0 < a.wait_ns) {}
+        }
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-    // ------------------------------------------------------------------ softmax and results: one thread per query row
-    if (work) {
-      PagedPiece p = piece0;
-      const int slot = warp >> 2, row = tid & 127, G = a.group;
-      const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_col = lanes + kSCol + slot * 128, o_col = lanes + kOCol + slot * 128;
-      uint32_t base = 0, s_phase = 0, o_phase[2] = {0, 0}, piece = 0;
-      bool split = false;
-      for (bool more = true; more; ++piece) {
-        const bool both = two_slots(p);
-        const int n = both ? 2 * p.n_tiles : p.n_tiles, first_row = p.rg * a.item_rows + (both ? slot * slot_rows : 0);
-        const int mrow = first_row + row;
-        const bool live = row < slot_rows && mrow < p.len * G;
-        int lo = 0, hi = 0, all_lo, all_hi, x;
-        if (live) paged_range(a.mask, a.window, p.len, p.kv, mrow / G, mrow / G, lo, hi);
-        const int last_row = min(p.len * G, (p.rg + 1) * a.item_rows) - 1;
-        paged_range(a.mask, a.window, p.len, p.kv, p.rg * a.item_rows / G, p.rg * a.item_rows / G, x, all_hi);   // keys that all rows of the item see
-        paged_range(a.mask, a.window, p.len, p.kv, last_row / G, last_row / G, all_lo, x);
-        const bool some = __any_sync(0xffffffffu, live);       // (a warp without rows leaves its lanes to chance: nobody reads them)
-        const unsigned span = hi > lo ? hi - lo : 0;
-        float m = -INFINITY;
-        f32x2 l2 = pack2(0.f, 0.f);
-        const f32x2 sc2 = pack2(a.scale_log2e, a.scale_log2e);
+    // -------------------------------------------------------------------- softmax and results: one thread per query row
+    const int slot = warp >> 2, row = tid & 127, G = a.group;
+    const bool out_32 = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;      // (rows are multiples of 32 bytes)
+    const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_col = lanes + kSCol + slot * 128, o_col = lanes + kOCol + slot * 128;
+    uint32_t base = 0, s_phase = 0, o_phase[2] = {0, 0}, piece = 0, turns = 0;     // (turns: pieces whose tiles the slots took in turn)
+    bool split = false;
+    for (;; ++piece) {
+      if (slot_any(slot, !known(piece))) break;
+      const TcPiece& p = s_piece[piece % kPieces];
+      const int n = p.steps;
+      if (n == 0) break;
+      const bool both = p.both != 0;
+      const int mrow = p.rg * a.item_rows + (both ? slot * slot_rows : 0) + row;
+      const bool live = row < slot_rows && mrow < p.len * G;
+      const bool some = __any_sync(0xffffffffu, live);         // (a warp without rows leaves its lanes to chance: nobody reads them)
+      int lo = 0, hi = 0;
+      if (live) {
+        const int r = a.by_group.of(mrow);
+        paged_range(a.mask, a.window, p.len, p.kv, r, r, lo, hi);
+      }
+      float m = live ? -INFINITY : 0.f;
+      f32x2 l2 = pack2(0.f, 0.f);
+      const f32x2 sc2 = pack2(a.scale_log2e, a.scale_log2e);
+      const int tile0 = p.tile0, all_lo = p.all_lo, all_hi = p.all_hi;
 
-        for (int s = slot; s < n; s += 2) {
-          const int key0 = (p.tile0 + (both ? s >> 1 : s)) * kPagedTile;
-          const bool mixed = key0 < all_lo || key0 + kPagedTile > all_hi;
-          bool ok = wait(b_s + 8 * slot, s_phase);
-          s_phase ^= 1;
-          ok = __all_sync(0xffffffffu, ok);
-          fence_after();
-          if (some && ok) {
-            float v[128];
+      for (int s = slot; s < n; s += 2) {
+        const int key0 = (tile0 + (both ? s >> 1 : s)) * kPagedTile;
+        const bool mixed = key0 < all_lo || key0 + kPagedTile > all_hi;
+        bool ok = wait(b_s + 8 * slot, s_phase);
+        s_phase ^= 1;
+        ok = __all_sync(0xffffffffu, ok);
+        fence_after();
+        float v[128];
+        if (some && ok) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) ld32(s_col + 32 * c, v + 32 * c);
-            ld_wait();
+          for (int c = 0; c < 4; ++c) ld32(s_col + 32 * c, v + 32 * c);
+          ld_wait();
 #pragma unroll
-            for (int c = 0; c < 4; ++c) ld_valid(v + 32 * c);
-            if (mixed) {
-              const int d = key0 - lo;
-#pragma unroll
-              for (int j = 0; j < 128; ++j) v[j] = (unsigned)(d + j) < span ? v[j] : -INFINITY;
-            }
-            float mx[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-            for (int j = 4; j < 128; j += 8) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) mx[i] = fmaxf(fmaxf(mx[i], v[j + i]), j + 4 + i < 128 ? v[j + 4 + i] : -INFINITY);
-            }
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2e;
-            const bool moves = m == -INFINITY ? top > m : top > m + 8.f;
-            if (__any_sync(0xffffffffu, moves)) {
-              const float corr = !moves ? 1.f : m == -INFINITY ? 0.f : paged_ex2(m - top);
-              if (moves) m = top;
-              float l0, l1;
-              unpack2(l2, l0, l1);
-              l2 = pack2(l0 * corr, l1 * corr);
-              if (s > 1) {
-#pragma unroll
-                for (int c = 0; c < DH / 32; ++c) {
-                  float o[32];
-                  ld32(o_col + 32 * c, o);
-                  ld_wait();
-                  ld_valid(o);
-#pragma unroll
-                  for (int j = 0; j < 32; ++j) o[j] *= corr;
-                  st32(o_col + 32 * c, reinterpret_cast<const uint32_t*>(o));
-                }
-              }
-            }
-            const float nm = m == -INFINITY ? 0.f : -m;
-            const f32x2 nm2 = pack2(nm, nm);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-              uint32_t w[16];
-#pragma unroll
-              for (int j = 0; j < 16; ++j) {
-                float x0, x1;
-                unpack2(fma2(pack2(v[32 * c + 2 * j], v[32 * c + 2 * j + 1]), sc2, nm2), x0, x1);
-                x0 = paged_ex2(x0); x1 = paged_ex2(x1);
-                l2 = add2(l2, pack2(x0, x1));
-                w[j] = PagedType<T>::pack(x0, x1);
-              }
-              st16(s_col + 16 * c, w);
-            }
-            st_wait();
-          }
-          if (mixed && ok) {
-            // V rows that no row of the item sees become zeros, and so do values that are not finite where not all rows see them
+          for (int c = 0; c < 4; ++c) ld_valid(v + 32 * c);
+        }
+        if (mixed && ok) {
+          if (key0 < p.lo || key0 + kPagedTile > p.hi) {
+            // V rows that no row of the item sees become zeros (whatever lies there: its weight is 0, but 0 x inf is not)
             const uint32_t e = base + v_entry(both, s, n), st = e % kNS;
-            if (wait(b_full + 8 * st, (e / kNS) & 1)) {
-              const int key = key0 + row;
+            if (wait(b_full + 8 * st, (e / kNS) & 1) && (key0 + row < p.lo || key0 + row >= p.hi)) {
               uint8_t* vrow = ring + st * kTB + row * 128;
-              if (key < p.lo || key >= p.hi) {
 #pragma unroll
-                for (int h = 0; h < kHalves; ++h)
+              for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-                  for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(vrow + h * kHalf + ((c + lane) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-              } else if (key < all_lo || key >= all_hi) {
-#pragma unroll
-                for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-                  for (int c = 0; c < 8; ++c) {
-                    volatile uint32_t* at = reinterpret_cast<volatile uint32_t*>(vrow + h * kHalf + ((c + lane) & 7) * 16);
-                    uint4 x4 = *reinterpret_cast<const uint4*>(vrow + h * kHalf + ((c + lane) & 7) * 16);
-                    const uint32_t b0 = odd_halves<T>(x4.x), b1 = odd_halves<T>(x4.y), b2 = odd_halves<T>(x4.z), b3 = odd_halves<T>(x4.w);
-                    if (b0 | b1 | b2 | b3) {
-                      s_odd[piece & 1] = 1;          // (before the value goes: whoever finds it gone knows)
-                      __threadfence_block();
-                      at[0] = x4.x & ~b0; at[1] = x4.y & ~b1; at[2] = x4.z & ~b2; at[3] = x4.w & ~b3;
-                    }
-                  }
-              }
+                for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(vrow + h * kHalf + ((c + lane) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
           }
+          // a bit for each of 32 keys that the row sees
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int from = min(max(lo - key0 - 32 * c, 0), 32), to = min(max(hi - key0 - 32 * c, 0), 32);
+            const uint32_t bits = (to == 32 ? 0xffffffffu : (1u << to) - 1u) & ~(from == 32 ? 0xffffffffu : (1u << from) - 1u);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[32 * c + j] = bits & (1u << j) ? v[32 * c + j] : -INFINITY;
+          }
+        }
+        if (some && ok) {
+          float mx[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+          for (int j = 4; j < 124; j += 8) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], v[j + i], v[j + 4 + i]);
+          }
+          const float top = max3(max3(mx[0], mx[1], v[124]), max3(mx[2], mx[3], v[125]), max3(v[126], v[127], v[127])) * a.scale_log2e;
+          const bool moves = live && (m == -INFINITY ? top > m : top > m + 8.f);
+          if (__any_sync(0xffffffffu, moves)) {
+            const float corr = !moves ? 1.f : m == -INFINITY ? 0.f : paged_ex2(m - top);
+            if (moves) m = top;
+            float l0, l1;
+            unpack2(l2, l0, l1);
+            l2 = pack2(l0 * corr, l1 * corr);
+            if (s > 1) {
+#pragma unroll 1
+              for (int c = 0; c < DH / 16; ++c) {      // (sixteen columns at a time: all scores are in registers)
+                float o[16];
+                ld16(o_col + 16 * c, o);
+                ld_wait();
+                asm volatile("" : "+f"(o[0]), "+f"(o[1]), "+f"(o[2]), "+f"(o[3]), "+f"(o[4]), "+f"(o[5]), "+f"(o[6]), "+f"(o[7])::"memory");
+                asm volatile("" : "+f"(o[8]), "+f"(o[9]), "+f"(o[10]), "+f"(o[11]), "+f"(o[12]), "+f"(o[13]), "+f"(o[14]), "+f"(o[15])::"memory");
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[j] *= corr;
+                st16(o_col + 16 * c, reinterpret_cast<const uint32_t*>(o));
+              }
+            }
+          }
+          const float nm = m == -INFINITY ? 0.f : -m;
+          const f32x2 nm2 = pack2(nm, nm);
+          weights<T>(v, s_col, sc2, nm2, l2);
+          weights<T>(v + 32, s_col + 16, sc2, nm2, l2);
+          st_wait();
           fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(b_p + 8 * slot);
+          if (lane == 0) mbar_arrive(b_p + 8 * slot);      // (the products with the first 64 keys may begin)
+          weights<T>(v + 64, s_col + 32, sc2, nm2, l2);
+          weights<T>(v + 96, s_col + 48, sc2, nm2, l2);
+          st_wait();
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(b_p2 + 8 * slot);
+        } else {
+          fence_before();
+          __syncwarp();
+          if (lane == 0) { mbar_arrive(b_p + 8 * slot); mbar_arrive(b_p2 + 8 * slot); }
         }
-
-        // ---- results
-        float l0, l1;
-        unpack2(l2, l0, l1);
-        float l = l0 + l1;
-        const bool mine = n > slot, other = n > 1 - slot;          // did this slot, the other slot have a step?
-        if (mine) wait(b_o + 8 * slot, o_phase[slot]);
-        if (!both && other) wait(b_o + 8 * (1 - slot), o_phase[1 - slot]);
-        if (n > 0) o_phase[0] ^= 1;
-        if (n > 1) o_phase[1] ^= 1;
-        fence_after();
-        float k_mine = 1.f, k_other = 0.f;
-        if (!both) {
-          // the slots' rows are the same: each warpgroup adds up half of the columns, from tensor memory
-          s_ml[slot * kM + row] = make_float2(m, l);
-          softmax_sync();
-          const float2 o_ml = s_ml[(1 - slot) * kM + row];
-          const bool nothing = o_ml.x == -INFINITY && o_ml.y == 0.f;
-          const float M = fmaxf(m, o_ml.x);
-          k_mine = m == -INFINITY ? 0.f : paged_ex2(m - M);
-          k_other = o_ml.x == -INFINITY ? 0.f : paged_ex2(o_ml.x - M);
-          l = (m == -INFINITY && l == 0.f ? 0.f : l * k_mine) + (nothing ? 0.f : o_ml.y * k_other);
-          m = M;
-        }
-        const bool odd = s_odd[piece & 1] != 0;
-        const bool good = *s_abort == 0;
-        const int c_first = both ? 0 : slot * (DH / 2), c_last = both ? DH : c_first + DH / 2;
-        const int item_row = (both ? slot * slot_rows : 0) + row;
-        const long long part = ((long long)cta * 2 + (p.opens ? 1 : 0)) * kPagedMaxRows + item_row;
-        const long long out_row = (long long)(p.start + (live ? mrow / G : 0)) * a.n_heads + p.head * G + (live ? mrow % G : 0);
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        if (some && good) {
-          for (int c0 = c_first; c0 < c_last; c0 += 32) {
-            float o[32];
-            if (both) {
-              ld32(o_col + c0, o);
-              ld_wait();
-              ld_valid(o);
-            } else {
-              float o2[32];
-              ld32(lanes + kOCol + slot * 128 + c0, o);
-              ld32(lanes + kOCol + (1 - slot) * 128 + c0, o2);
-              ld_wait();
-              ld_valid(o);
-              ld_valid(o2);
-              // (a slot without steps holds what an earlier item left)
-#pragma unroll
-              for (int j = 0; j < 32; ++j) o[j] = (mine ? o[j] * k_mine : 0.f) + (other ? o2[j] * k_other : 0.f);
-            }
-            if (odd && live) {
-              for (int t = 0; t < p.n_tiles; ++t) {
-                const int key0 = (p.tile0 + t) * kPagedTile;
-                if (key0 >= all_lo && key0 + kPagedTile <= all_hi) continue;
-                for (int key = max(key0, lo); key < min(key0 + kPagedTile, hi); ++key) {
-                  if (key >= all_lo && key < all_hi) continue;
-                  const int page = __ldcg(a.blk.table + (long long)p.seq * a.blk.table_width + (key >> a.kv.page_shift));
-                  if ((unsigned)page >= (unsigned)a.kv.n_pages) continue;
-                  const char* src = a.kv.v + (page * a.kv.page_stride + p.head * a.kv.head_stride + (long long)(key & (a.kv.page_size - 1)) * a.kv.slot_stride + c0) * 2;
-#pragma unroll
-                  for (int j = 0; j < 16; ++j) {
-                    const uint32_t w = __ldcg(reinterpret_cast<const unsigned*>(src) + j), bits = odd_halves<T>(w);
-                    const float2 f = PagedType<T>::unpack(w);
-                    if (bits & 0xffffu) o[2 * j] += f.x;
-                    if (bits >> 16) o[2 * j + 1] += f.y;
-                  }
-                }
-              }
-            }
-            if (live) {
-              if (p.whole) {
-                uint32_t w[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) w[j] = PagedType<T>::pack(o[2 * j] * inv, o[2 * j + 1] * inv);
-                char* dst = a.out + (out_row * DH + c0) * 2;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(dst + 16 * j) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-              } else {
-                float* dst = a.parts + part * DH + c0;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) store32b(dst + 8 * j, reinterpret_cast<const uint32_t*>(o) + 8 * j);
-              }
-            }
-          }
-          if (live && (both || slot == 0)) {
-            if (!p.whole) __stcg(reinterpret_cast<float2*>(a.parts_ml) + part, make_float2(m, l));
-            else if (a.lse != nullptr) a.lse[out_row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-          }
-        }
-        fence_before();
-        if (p.opens && !p.whole && tid == 0) {               // (the run ends with this item)
-          PagedSplit d;
-          d.last = paged_last_cta(a, p, total, n_cta);
-          d.rows = min(a.item_rows, p.len * G - p.rg * a.item_rows);
-          d.first_row = p.rg * a.item_rows; d.head = p.head; d.start = p.start;
-          a.splits[cta] = d;
-          split = true;
-        }
-        softmax_sync();                                // both slots' O, the exchange rows and this piece's flag are free again
-        if (tid == 0) s_odd[piece & 1] = 0;
-        base += 2 * p.n_tiles;
-        more = paged_next(a, plan, p, run1);
       }
-      if (tid == 0 && (!split || *s_abort)) a.splits[cta].last = -1;
-    } else if (tid == 0) {
-      a.splits[cta].last = -1;
+
+      // ---- results
+      float l0, l1;
+      unpack2(l2, l0, l1);
+      float l = l0 + l1;
+      const bool mine = n > slot, other = n > 1 - slot;        // did this slot, the other slot have a step?
+      if (mine) wait(b_o + 8 * slot, o_phase[slot]);
+      if (!both && other) wait(b_o + 8 * (1 - slot), o_phase[1 - slot]);
+      if (n > 0) o_phase[0] ^= 1;
+      if (n > 1) o_phase[1] ^= 1;
+      fence_after();
+      float k_mine = 1.f, k_other = 0.f;
+      if (!both) {
+        // the slots' rows are the same: each warpgroup adds up half of the columns, from tensor memory
+        s_ml[slot * kM + row] = make_float2(m, l);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_ml);
+        wait(b_ml, turns & 1);
+        const float2 o_ml = s_ml[(1 - slot) * kM + row];
+        const bool nothing = o_ml.x == -INFINITY && o_ml.y == 0.f;
+        const float M = fmaxf(m, o_ml.x);
+        k_mine = m == -INFINITY ? 0.f : paged_ex2(m - M);
+        k_other = o_ml.x == -INFINITY ? 0.f : paged_ex2(o_ml.x - M);
+        l = (m == -INFINITY && l == 0.f ? 0.f : l * k_mine) + (nothing ? 0.f : o_ml.y * k_other);
+        m = M;
+      }
+      const bool good = *s_abort == 0;
+      const int c_first = both ? 0 : slot * (DH / 2), c_last = both ? DH : c_first + DH / 2;
+      const long long part = ((long long)cta * 2 + (p.opens ? 1 : 0)) * kPagedMaxRows + (both ? slot * slot_rows : 0) + row;
+      const int r = live ? a.by_group.of(mrow) : 0, head = p.head * G + (live ? mrow - r * G : 0);
+      const long long out_row = (long long)(p.start + r) * a.n_heads + head;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      const bool whole = p.whole != 0;
+      if (some && good) {
+#pragma unroll 1
+        for (int c0 = c_first; c0 < c_last; c0 += 32) {
+          float o[32];
+          ld32(o_col + c0, o);
+          if (both) {
+            ld_wait();
+            ld_valid(o);
+          } else {
+            float o2[32];
+            ld32(lanes + kOCol + (1 - slot) * 128 + c0, o2);
+            ld_wait();
+            ld_valid(o);
+            ld_valid(o2);
+            // (a slot without steps holds what an earlier item left)
+#pragma unroll
+            for (int j = 0; j < 32; ++j) o[j] = (mine ? o[j] * k_mine : 0.f) + (other ? o2[j] * k_other : 0.f);
+          }
+          if (live) {
+            f32x2 z = pack2(0.f, 0.f);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) z = fma2(pack2(o[2 * j], o[2 * j + 1]), pack2(0.f, 0.f), z);      // (NaN if one is not finite)
+            void* dst;
+            if (whole) {
+              uint32_t w[16];
+#pragma unroll
+              for (int j = 0; j < 16; ++j) w[j] = PagedType<T>::pack(o[2 * j] * inv, o[2 * j + 1] * inv);
+              dst = a.out + (out_row * DH + c0) * 2;
+              if (out_32) {
+                store32b(dst, w);
+                store32b(reinterpret_cast<char*>(dst) + 32, w + 8);
+              } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(reinterpret_cast<char*>(dst) + 16 * j) = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+              }
+            } else {
+              dst = a.parts + part * DH + c0;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) store32b(reinterpret_cast<float*>(dst) + 8 * j, reinterpret_cast<const uint32_t*>(o) + 8 * j);
+            }
+            float z0, z1;
+            unpack2(z, z0, z1);
+            if (!(z0 + z1 == 0.f))
+              mend_row<T, DH>(a, p, both ? n >> 1 : n, lo, hi, (long long)(p.start + r) * a.q_row + head * a.q_head, m, inv, c0, dst, !whole);
+          }
+          __syncwarp();
+        }
+        if (live && (both || slot == 0)) {
+          if (!whole) __stcg(reinterpret_cast<float2*>(a.parts_ml) + part, make_float2(m, l));
+          else if (a.lse != nullptr) a.lse[out_row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+        }
+      }
+      fence_before();
+      if (p.opens && !whole && tid == 0) {               // (the run ends with this item)
+        PagedSplit d;
+        d.last = p.last;
+        d.rows = min(a.item_rows, p.len * G - p.rg * a.item_rows);
+        d.first_row = p.rg * a.item_rows; d.head = p.head; d.start = p.start;
+        a.splits[cta] = d;
+        split = true;
+      }
+      if (!both) {                                       // both warpgroups have read both slots' O and the exchange rows
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b_read);
+        wait(b_read, turns & 1);
+        ++turns;
+        __syncwarp();
+      }
+      base += both ? n : 2 * n;
     }
+    if (tid == 0 && (!split || *s_abort)) a.splits[cta].last = -1;
   }
   // ---------------------------------------------------------------------- teardown
   fence_before();
@@ -572,7 +656,11 @@ k_paged_merge(PagedAttnArgs a) {
       float v[kBatch][kV];
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
-        const long long at = ((long long)min(cb + i, c1) * 2 + (cb + i == c0 ? 1 : 0)) * kPagedMaxRows + r;
+        ml[i] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int e = 0; e < kV; ++e) v[i][e] = 0.f;
+        if (cb + i > c1) continue;
+        const long long at = ((long long)(cb + i) * 2 + (cb + i == c0 ? 1 : 0)) * kPagedMaxRows + r;
         ml[i] = __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at);
         if constexpr (kV == 4) {
           const float4 x = __ldcg(reinterpret_cast<const float4*>(a.parts + at * DH) + lane);
@@ -592,7 +680,7 @@ k_paged_merge(PagedAttnArgs a) {
       for (int e = 0; e < kV; ++e) acc[e] *= keep;
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
-        if (cb + i > c1 || (ml[i].x == -INFINITY && ml[i].y == 0.f)) continue;           // (it saw nothing)
+        if (ml[i].x == -INFINITY && ml[i].y == 0.f) continue;                            // (it saw nothing)
         const float k = ml[i].x == -INFINITY ? 0.f : paged_ex2(ml[i].x - M);
         L = fmaf(k, ml[i].y, L);
 #pragma unroll
