@@ -635,23 +635,61 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   }
 }
 
-// Items that several CTAs share: their pieces added up, in the order of the keys.  One warp per row; CTA x of a column handles the item that begins in CTA x of the
-// launch before.  (The last CTA to arrive did this inside the kernel at first: 430 KB through one SM are 5 us with its loads in flight together, 14 without.)
-constexpr int kMergeWarps = 8, kMergeRows = 8;    // CTAs that share an item's rows
+// Items that several CTAs share: their pieces added up, in the order of the keys.  All their rows are dealt out over all warps.  (The last CTA to arrive did this inside
+// the kernel at first: 430 KB through one SM, 5 us with its loads in flight together and 14 without.)
+constexpr int kMergeWarps = 8, kMergeCtas = 3;    // CTAs per SM
 template <typename T, int DH>
-__global__ void __launch_bounds__(kMergeWarps * 32)
-k_paged_merge(PagedAttnArgs a) {
+__global__ void __launch_bounds__(kMergeWarps * 32, kMergeCtas)
+k_paged_merge(PagedAttnArgs a, int n_cta) {
   CS_PDL_PROLOGUE();
-  constexpr int kBatch = 10, kV = DH / 32;        // columns of a lane
-  const int c0 = blockIdx.x, lane = threadIdx.x & 31;
-  const int c1 = __ldcg(&a.splits[c0].last), rows = __ldcg(&a.splits[c0].rows), first_row = __ldcg(&a.splits[c0].first_row), head = __ldcg(&a.splits[c0].head),
-            start = __ldcg(&a.splits[c0].start);
-  if (c1 < 0) return;
-  for (int r = blockIdx.y * kMergeWarps + (threadIdx.x >> 5); r < rows; r += kMergeWarps * kMergeRows) {
+  constexpr int kBatch = 8, kV = DH / 32, kPerLane = kPagedMaxCtas / 32;        // columns of a lane; splits of a lane
+  __shared__ PagedSplit s_split[kPagedMaxCtas];
+  __shared__ int s_before[kPagedMaxCtas];         // rows of the items before
+  __shared__ float2 s_ml[kMergeWarps];
+  __shared__ __align__(16) float s_o[kMergeWarps][DH];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  if (tid < kPagedMaxCtas) {
+    PagedSplit d;
+    d.last = -1; d.rows = 0;
+    if (tid < n_cta) {
+      const int* src = reinterpret_cast<const int*>(a.splits + tid);
+      d.last = __ldcg(src); d.rows = __ldcg(src + 1); d.first_row = __ldcg(src + 2); d.head = __ldcg(src + 3); d.start = __ldcg(src + 4);
+      if (d.last < 0) d.rows = 0;
+    }
+    s_split[tid] = d;
+  }
+  __syncthreads();
+  // (every warp adds up for itself, all the same)
+  int mine[kPerLane], sum = 0;
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) { mine[i] = sum; sum += s_split[lane * kPerLane + i].rows; }
+  int inc = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += v;
+  }
+  const int total = __shfl_sync(0xffffffffu, inc, 31);
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    mine[i] += inc - sum;
+    s_before[lane * kPerLane + i] = mine[i];
+  }
+  __syncwarp();
+  // A warp per row; where there are fewer rows than CTAs a CTA per row, its warps with an eighth of the pieces each.
+  const bool together = total <= (int)gridDim.x;
+  const int hop = together ? kMergeWarps : 1;
+  for (int g = together ? blockIdx.x : blockIdx.x * kMergeWarps + warp; g < total; g += gridDim.x * (together ? 1 : kMergeWarps)) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) n += mine[i] <= g;
+    const int c0 = (int)__reduce_add_sync(0xffffffffu, (unsigned)n) - 1;            // the last item that begins at or before it (those without rows come first)
+    const PagedSplit d = s_split[c0];
+    const int r = g - s_before[c0], c1 = d.last;
     float M = -INFINITY, L = 0.f, acc[kV];
 #pragma unroll
     for (int e = 0; e < kV; ++e) acc[e] = 0.f;
-    for (int cb = c0; cb <= c1; cb += kBatch) {
+    for (int cb = c0 + (together ? warp : 0); cb <= c1; cb += kBatch * hop) {
       float2 ml[kBatch];
       float v[kBatch][kV];
 #pragma unroll
@@ -659,8 +697,9 @@ k_paged_merge(PagedAttnArgs a) {
         ml[i] = make_float2(-INFINITY, 0.f);
 #pragma unroll
         for (int e = 0; e < kV; ++e) v[i][e] = 0.f;
-        if (cb + i > c1) continue;
-        const long long at = ((long long)(cb + i) * 2 + (cb + i == c0 ? 1 : 0)) * kPagedMaxRows + r;
+        const int c = cb + i * hop;
+        if (c > c1) continue;
+        const long long at = ((long long)c * 2 + (c == c0 ? 1 : 0)) * kPagedMaxRows + r;
         ml[i] = __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at);
         if constexpr (kV == 4) {
           const float4 x = __ldcg(reinterpret_cast<const float4*>(a.parts + at * DH) + lane);
@@ -687,9 +726,29 @@ k_paged_merge(PagedAttnArgs a) {
         for (int e = 0; e < kV; ++e) acc[e] = fmaf(k, v[i][e], acc[e]);
       }
     }
+    if (together) {
+      s_ml[warp] = make_float2(M, L);
+#pragma unroll
+      for (int e = 0; e < kV; ++e) s_o[warp][lane * kV + e] = acc[e];
+      __syncthreads();
+      if (warp > 0) return;                      // (a row is all that a CTA has)
+      for (int w = 0; w < kMergeWarps; ++w) M = fmaxf(M, s_ml[w].x);
+      L = 0.f;
+#pragma unroll
+      for (int e = 0; e < kV; ++e) acc[e] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kMergeWarps; ++w) {
+        const float2 x = s_ml[w];
+        if (x.x == -INFINITY && x.y == 0.f) continue;
+        const float k = x.x == -INFINITY ? 0.f : paged_ex2(x.x - M);
+        L = fmaf(k, x.y, L);
+#pragma unroll
+        for (int e = 0; e < kV; ++e) acc[e] = fmaf(k, s_o[w][lane * kV + e], acc[e]);
+      }
+    }
     const float inv = L == 0.f ? 0.f : 1.f / L;
-    const int m = first_row + r;
-    const long long row = (long long)(start + m / a.group) * a.n_heads + head * a.group + m % a.group;
+    const int m = d.first_row + r, q = a.by_group.of(m);
+    const long long row = (long long)(d.start + q) * a.n_heads + d.head * a.group + (m - q * a.group);
     uint32_t w[kV / 2];
 #pragma unroll
     for (int e = 0; e < kV / 2; ++e) w[e] = PagedType<T>::pack(acc[2 * e] * inv, acc[2 * e + 1] * inv);
@@ -727,7 +786,7 @@ cs_status launch_tc(cs_paged_cache* c, const PagedAttnArgs& a, const CUtensorMap
     c->attr_set |= bit;
   }
   CS_CUDA_OK(c, cs_launch_pdl(k_paged_tc<T, DH>, dim3(c->num_sms), dim3(kThreads), kTcSmem<DH>, st, c->tmK, c->tmV, tmQ, a, q_box_bytes));
-  CS_CUDA_OK(c, cs_launch_pdl(k_paged_merge<T, DH>, dim3(c->num_sms, kMergeRows), dim3(kMergeWarps * 32), 0, st, a));
+  CS_CUDA_OK(c, cs_launch_pdl(k_paged_merge<T, DH>, dim3(c->num_sms * kMergeCtas), dim3(kMergeWarps * 32), 0, st, a, c->num_sms));
   return CS_OK;
 }
 
@@ -747,7 +806,7 @@ cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& args, cudaS
   const int tokens = kM / a.group;                 // rows of the block in a slot, with all heads of the group
   a.item_rows = 2 * tokens * a.group;
   a.by_item_rows = PagedDivisor::by(a.item_rows);
-  a.item_cost = 1;
+  a.item_cost = 2;
   const int box_rows = tokens < a.blk.rows ? tokens : a.blk.rows, dh = c->cfg.head_dim;
   CUtensorMap tmQ;
   // (a stride that no second row or head uses may be anything)
