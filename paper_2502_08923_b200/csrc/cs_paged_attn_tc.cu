@@ -213,21 +213,17 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   const int n_cta = (int)min((long long)gridDim.x, total), cta = blockIdx.x;
   const long long run0 = cta < n_cta ? paged_div(total * cta, n_cta) : 0, run1 = cta < n_cta ? paged_div(total * (cta + 1), n_cta) : 0;
 
-  // Bounded waits.  Once one has run out all others return at once.
+  // Bounded waits, in few instructions (see the MMA issuer).  Once one has run out all others return.
   auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
     if (mbar_try_wait(bar, parity)) return true;
-    unsigned long long t0 = 0;
-    for (uint32_t it = 0;; ++it) {
+    const unsigned long long t0 = globaltimer_ns();
+    for (;;) {
       if (mbar_try_wait(bar, parity)) return true;
-      if ((it & 15u) == 15u) {
-        if (*s_abort) return false;
-        const unsigned long long now = globaltimer_ns();
-        if (t0 == 0) t0 = now;
-        else if (now - t0 > a.wait_ns) {
-          *s_abort = 1;
-          atomicOr(a.status, CS_DEV_TIMEOUT);
-          return false;
-        }
+      if (*s_abort) return false;
+      if (globaltimer_ns() - t0 > a.wait_ns) {
+        *s_abort = 1;
+        atomicOr(a.status, CS_DEV_TIMEOUT);
+        return false;
       }
     }
   };
@@ -249,7 +245,10 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       constexpr uint32_t idesc_s = (1u << 4) | kType | ((uint32_t)(kPagedTile >> 3) << 17) | ((uint32_t)(kM >> 4) << 24);
       constexpr uint32_t idesc_o = (1u << 4) | kType | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(kM >> 4) << 24);   // B (= V) is MN-major
       const uint64_t dq0 = desc_kmajor(smem_u32(sq)), dk0 = desc_kmajor(smem_u32(ring)), dv0 = desc_mnmajor(smem_u32(ring), kHalf);
-      uint32_t p_phase[2] = {0, 0};
+      // One lane runs a piece's steps by itself, and every instruction counts: this warp comes by once in 900 clocks, when the softmax warps have filled the instruction cache with
+      // their unrolled loops, so that its instructions are fetched anew each time.  (All lanes with votes, ring places worked out from the step, waits in
+      // line: 900 clocks a step of its own, and the tensor cores waited for it.)
+      uint32_t p_phase = 0;                       // bit s: of slot s
       for (;; ++piece) {
         ok = known(piece);
         if (!ok) break;
@@ -258,48 +257,52 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         const bool both = uniform((uint32_t)d.both) != 0;
         if (n == 0) break;
         ok = wait_warp(b_qfull, piece & 1);
-        auto scores = [&](int s) {
-          const uint32_t e = base + k_entry(both, s), st = e % kNS;
-          if (!(both && (s & 1))) ok = wait_warp(b_full + 8 * st, (e / kNS) & 1);
-          if (!ok) return;
-          fence_after();
-          if (elect_one()) {
-            const uint64_t dk = dk0 + st * (kTB >> 4), dq = dq0 + (both && (s & 1) ? kTB >> 4 : 0);
+        if (!ok) break;
+        fence_after();
+        bool fine = true;
+        if (elect_one()) {
+          uint32_t at = base, k_at = 0, v_at = 0;   // next ring entry, in the order of first use; entries of the K and V tile at hand
+          auto scores = [&](int s) {
+            if (!both || !(s & 1)) {
+              k_at = at++;
+              if (!wait(b_full + 8 * (k_at % kNS), (k_at / kNS) & 1)) { fine = false; return; }
+            }
+            const uint64_t dk = dk0 + (k_at % kNS) * (kTB >> 4), dq = dq0 + (both && (s & 1) ? kTB >> 4 : 0);
+            const uint32_t acc = tmem + kSCol + (s & 1) * 128;
 #pragma unroll
             for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                umma_bf16(tmem + kSCol + (s & 1) * 128, dq + h * (kHalf >> 4) + 2 * k, dk + h * (kHalf >> 4) + 2 * k, idesc_s, (h | k) ? 1u : 0u);
+              for (int k = 0; k < 4; ++k) umma_bf16(acc, dq + h * (kHalf >> 4) + 2 * k, dk + h * (kHalf >> 4) + 2 * k, idesc_s, (h | k) ? 1u : 0u);
             umma_commit(b_s + 8 * (s & 1));
-            if (!both || (s & 1)) umma_commit(b_empty + 8 * st);
+            if (!both || (s & 1)) umma_commit(b_empty + 8 * (k_at % kNS));
             if (s == n - 1) umma_commit(b_qfree);
-          }
-        };
-        if (ok) scores(0);
-        if (ok && n > 1) scores(1);
-        for (int s = 0; s < n && ok; ++s) {
-          const uint32_t e = base + v_entry(both, s, n), st = e % kNS;
-          ok = wait_warp(b_full + 8 * st, (e / kNS) & 1) && wait_warp(b_p + 8 * (s & 1), p_phase[s & 1]);
-          if (!ok) break;
-          const uint64_t dv = dv0 + st * (kTB >> 4);
-          const uint32_t acc = tmem + kOCol + (s & 1) * 128, w = tmem + kSCol + (s & 1) * 128;
-          fence_after();
-          if (elect_one()) {
+          };
+          scores(0);
+          if (fine && n > 1) scores(1);
+          for (int s = 0; s < n && fine; ++s) {
+            const uint32_t slot = s & 1;
+            if (!both || !slot) {
+              v_at = at++;
+              if (!wait(b_full + 8 * (v_at % kNS), (v_at / kNS) & 1)) { fine = false; break; }
+            }
+            if (!wait(b_p + 8 * slot, p_phase >> slot & 1)) { fine = false; break; }
+            fence_after();
+            const uint64_t dv = dv0 + (v_at % kNS) * (kTB >> 4);
+            const uint32_t acc = tmem + kOCol + slot * 128, w = tmem + kSCol + slot * 128;
 #pragma unroll
             for (int k = 0; k < 4; ++k) umma_ta(acc, w + k * 8, dv + k * (2048 >> 4), idesc_o, (s > 1 || k > 0) ? 1u : 0u);   // 16 keys per instruction
-          }
-          ok = wait_warp(b_p2 + 8 * (s & 1), p_phase[s & 1]);
-          if (!ok) break;
-          p_phase[s & 1] ^= 1;
-          fence_after();
-          if (elect_one()) {
+            if (!wait(b_p2 + 8 * slot, p_phase >> slot & 1)) { fine = false; break; }
+            p_phase ^= 1u << slot;
+            fence_after();
 #pragma unroll
             for (int k = 4; k < 8; ++k) umma_ta(acc, w + k * 8, dv + k * (2048 >> 4), idesc_o, 1u);
-            if (!both || (s & 1)) umma_commit(b_empty + 8 * st);
-            if (s >= n - 2) umma_commit(b_o + 8 * (s & 1));
+            if (!both || slot) umma_commit(b_empty + 8 * (v_at % kNS));
+            if (s >= n - 2) umma_commit(b_o + 8 * slot);
+            if (s + 2 < n) scores(s + 2);
           }
-          if (s + 2 < n) scores(s + 2);
         }
+        ok = __all_sync(0xffffffffu, fine);
+        p_phase = __reduce_xor_sync(0xffffffffu, elect_one() ? p_phase : 0u);
         base += both ? n : 2 * n;
         if (!ok) break;
       }
@@ -441,6 +444,19 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         s_phase ^= 1;
         ok = __all_sync(0xffffffffu, ok);
         fence_after();
+        if (mixed && ok && (key0 < p.lo || key0 + kPagedTile > p.hi)) {
+          // V rows that no row of the item sees become zeros (whatever lies there: its weight is 0, but 0 x inf is not)
+          const uint32_t e = base + v_entry(both, s, n), st = e % kNS;
+          if (wait(b_full + 8 * st, (e / kNS) & 1) && (key0 + row < p.lo || key0 + row >= p.hi)) {
+            uint8_t* vrow = ring + st * kTB + row * 128;
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+              for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(vrow + h * kHalf + ((c + lane) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+        }
         float v[128];
         if (some && ok) {
 #pragma unroll
@@ -450,19 +466,6 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           for (int c = 0; c < 4; ++c) ld_valid(v + 32 * c);
         }
         if (mixed && ok) {
-          if (key0 < p.lo || key0 + kPagedTile > p.hi) {
-            // V rows that no row of the item sees become zeros (whatever lies there: its weight is 0, but 0 x inf is not)
-            const uint32_t e = base + v_entry(both, s, n), st = e % kNS;
-            if (wait(b_full + 8 * st, (e / kNS) & 1) && (key0 + row < p.lo || key0 + row >= p.hi)) {
-              uint8_t* vrow = ring + st * kTB + row * 128;
-#pragma unroll
-              for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-                for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(vrow + h * kHalf + ((c + lane) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-          }
           // a bit for each of 32 keys that the row sees
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
