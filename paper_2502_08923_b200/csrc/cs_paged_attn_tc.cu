@@ -36,7 +36,7 @@ template <int DH> constexpr int kTileBytes = kPagedTile * DH * 2;  // of K, of V
 template <int DH> constexpr int kStages = DH == 128 ? 4 : 8;
 constexpr int kCtl = 512;
 constexpr int kPieces = 4;         // descriptors of pieces (published at most two ahead of the products, of which the softmax may be one behind)
-template <int DH> constexpr int kTcSmem = 1024 + (kStages<DH> + 2) * kTileBytes<DH> + kCtl + 2 * kM * 12 + kPieces * 64 + (int)sizeof(PagedPlan);
+template <int DH> constexpr int kTcSmem = 1024 + (kStages<DH> + 2) * kTileBytes<DH> + kCtl + 2 * kM * 8 + kPieces * 64 + (int)sizeof(PagedPlan);
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2, int c3) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
@@ -68,29 +68,10 @@ __device__ __forceinline__ void ld_valid(float* v) {
   for (int i = 0; i < 32; i += 8)
     asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]), "+f"(v[i + 6]), "+f"(v[i + 7])::"memory");
 }
-__device__ __forceinline__ void st32(uint32_t taddr, const uint32_t* v) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-      "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
-      ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
-        "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
-        "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]) : "memory");
-}
 __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* v) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
                ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
                  "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
-}
-__device__ __forceinline__ void scale16(uint32_t taddr, float by) {      // sixteen columns of a lane multiplied
-  float o[16];
-  ld16(taddr, o);
-  ld_wait();
-  asm volatile("" : "+f"(o[0]), "+f"(o[1]), "+f"(o[2]), "+f"(o[3]), "+f"(o[4]), "+f"(o[5]), "+f"(o[6]), "+f"(o[7])::"memory");
-  asm volatile("" : "+f"(o[8]), "+f"(o[9]), "+f"(o[10]), "+f"(o[11]), "+f"(o[12]), "+f"(o[13]), "+f"(o[14]), "+f"(o[15])::"memory");
-#pragma unroll
-  for (int j = 0; j < 16; ++j) o[j] *= by;
-  st16(taddr, reinterpret_cast<const uint32_t*>(o));
 }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -126,9 +107,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// Weights 2^(score scale - m) of 32 keys, rounded to T, and their sum.
+// Weights 2^(score scale - m) of 32 keys, rounded to T, to tensor memory, and their sum.  (The 16-a-clock unit behind ex2 is busy for half of the loop's
+// time.  A polynomial in packed arithmetic for a quarter to three eighths of them was no faster in short runs and 2 - 4 % slower at the power cap.)
 template <typename T>
-__device__ __forceinline__ void weights(const float* v, uint32_t* w, f32x2 sc2, f32x2 nm2, f32x2& l2) {
+__device__ __forceinline__ void weights(const float* v, uint32_t taddr, f32x2 sc2, f32x2 nm2, f32x2& l2) {
+  uint32_t w[16];
 #pragma unroll
   for (int j = 0; j < 16; ++j) {
     float x0, x1;
@@ -138,6 +121,7 @@ __device__ __forceinline__ void weights(const float* v, uint32_t* w, f32x2 sc2, 
     l2 = add2(l2, pack2(x0, x1));
     w[j] = PagedType<T>::pack(x0, x1);
   }
+  st16(taddr, w);
 }
 
 template <typename T>
@@ -200,17 +184,16 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kNS + 18);
   volatile int* s_abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float2* s_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(bars) + kCtl);      // [slot][128 rows]
-  float* s_later = reinterpret_cast<float*>(s_ml + 2 * kM);
-  TcPiece* s_piece = reinterpret_cast<TcPiece*>(s_later + 2 * kM);
+  TcPiece* s_piece = reinterpret_cast<TcPiece*>(s_ml + 2 * kM);
   PagedPlan& plan = *reinterpret_cast<PagedPlan*>(s_piece + kPieces);
-  const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8 * kNS, b_s = b_empty + 8 * kNS, b_p = b_s + 16, b_o = b_p + 16, b_qfull = b_o + 16, b_qfree = b_qfull + 8,
+  const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8 * kNS, b_s = b_empty + 8 * kNS, b_p = b_s + 16, b_p2 = b_p + 16, b_o = b_p2 + 16, b_qfull = b_o + 16, b_qfree = b_qfull + 8,
                  b_drain = b_qfree + 8, b_piece = b_drain + 8, b_ml = b_piece + 8 * kPieces, b_read = b_ml + 8;
   const int tid = threadIdx.x, warp = (int)uniform(tid >> 5), lane = tid & 31;
 
   CS_PDL_PROLOGUE();
   if (tid == 0) {
     for (int s = 0; s < kNS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_empty + 8 * s, 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(b_s + 8 * s, 1); mbar_init(b_p + 8 * s, 4); mbar_init(b_o + 8 * s, 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(b_s + 8 * s, 1); mbar_init(b_p + 8 * s, 4); mbar_init(b_p2 + 8 * s, 4); mbar_init(b_o + 8 * s, 1); }
     mbar_init(b_qfull, 1); mbar_init(b_qfree, 1); mbar_init(b_drain, 1);
     for (int s = 0; s < kPieces; ++s) mbar_init(b_piece + 8 * s, 1);
     mbar_init(b_ml, 8); mbar_init(b_read, 8);
@@ -306,9 +289,13 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
             fence_after();
             const uint64_t dv = dv0 + (v_at % kNS) * (kTB >> 4);
             const uint32_t acc = tmem + kOCol + slot * 128, w = tmem + kSCol + slot * 128;
-            p_phase ^= 1u << slot;
 #pragma unroll
-            for (int k = 0; k < 8; ++k) umma_ta(acc, w + k * 8, dv + k * (2048 >> 4), idesc_o, (s > 1 || k > 0) ? 1u : 0u);   // 16 keys per instruction
+            for (int k = 0; k < 4; ++k) umma_ta(acc, w + k * 8, dv + k * (2048 >> 4), idesc_o, (s > 1 || k > 0) ? 1u : 0u);   // 16 keys per instruction
+            if (!wait(b_p2 + 8 * slot, p_phase >> slot & 1)) { fine = false; break; }
+            p_phase ^= 1u << slot;
+            fence_after();
+#pragma unroll
+            for (int k = 4; k < 8; ++k) umma_ta(acc, w + k * 8, dv + k * (2048 >> 4), idesc_o, 1u);
             if (!both || slot) umma_commit(b_empty + 8 * (v_at % kNS));
             if (s >= n - 2) umma_commit(b_o + 8 * slot);
             if (s + 2 < n) scores(s + 2);
@@ -445,10 +432,10 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         const int r = a.by_group.of(mrow);
         paged_range(a.mask, a.window, p.len, p.kv, r, r, lo, hi);
       }
-      float m = live ? -INFINITY : 0.f, l = 0.f, later = 1.f;  // reference point, sum, what O is still to be multiplied by
+      float m = live ? -INFINITY : 0.f;
+      f32x2 l2 = pack2(0.f, 0.f);
       const f32x2 sc2 = pack2(a.scale_log2e, a.scale_log2e);
       const int tile0 = p.tile0, all_lo = p.all_lo, all_hi = p.all_hi;
-      constexpr float kMost = std::is_same<T, __half>::value ? 32768.f : 1.152921504606846976e18f;      // 2^15: no weight rounds to infinity; 2^60
 
       for (int s = slot; s < n; s += 2) {
         const int key0 = (tile0 + (both ? s >> 1 : s)) * kPagedTile;
@@ -470,107 +457,98 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
         }
+        float v[128];
         if (some && ok) {
-          if (s > 1 && __any_sync(0xffffffffu, later != 1.f)) {      // (the scores are there, so the product before is done)
-#pragma unroll 1
-            for (int c = 0; c < DH / 16; ++c) scale16(o_col + 16 * c, later);
-            later = 1.f;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) ld32(s_col + 32 * c, v + 32 * c);
+          ld_wait();
+#pragma unroll
+          for (int c = 0; c < 4; ++c) ld_valid(v + 32 * c);
+        }
+        if (mixed && ok) {
+          // a bit for each of 32 keys that the row sees
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int from = min(max(lo - key0 - 32 * c, 0), 32), to = min(max(hi - key0 - 32 * c, 0), 32);
+            const uint32_t bits = (to == 32 ? 0xffffffffu : (1u << to) - 1u) & ~(from == 32 ? 0xffffffffu : (1u << from) - 1u);
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[32 * c + j] = bits & (1u << j) ? v[32 * c + j] : -INFINITY;
           }
-          uint32_t w[64];
-          f32x2 sum2;
-          float sum;
-          for (bool again = false;;) {
-            float v[128];
+        }
+        if (some && ok) {
+          float mx[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) ld32(s_col + 32 * c, v + 32 * c);
-            ld_wait();
+          for (int j = 4; j < 124; j += 8) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) ld_valid(v + 32 * c);
-            if (mixed) {
-              // a bit for each of 32 keys that the row sees
+            for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], v[j + i], v[j + 4 + i]);
+          }
+          const float top = max3(max3(mx[0], mx[1], v[124]), max3(mx[2], mx[3], v[125]), max3(v[126], v[127], v[127])) * a.scale_log2e;
+          const bool moves = live && (m == -INFINITY ? top > m : top > m + 8.f);
+          if (__any_sync(0xffffffffu, moves)) {
+            const float corr = !moves ? 1.f : m == -INFINITY ? 0.f : paged_ex2(m - top);
+            if (moves) m = top;
+            float l0, l1;
+            unpack2(l2, l0, l1);
+            l2 = pack2(l0 * corr, l1 * corr);
+            if (s > 1) {
+#pragma unroll 1
+              for (int c = 0; c < DH / 16; ++c) {      // (sixteen columns at a time: all scores are in registers)
+                float o[16];
+                ld16(o_col + 16 * c, o);
+                ld_wait();
+                asm volatile("" : "+f"(o[0]), "+f"(o[1]), "+f"(o[2]), "+f"(o[3]), "+f"(o[4]), "+f"(o[5]), "+f"(o[6]), "+f"(o[7])::"memory");
+                asm volatile("" : "+f"(o[8]), "+f"(o[9]), "+f"(o[10]), "+f"(o[11]), "+f"(o[12]), "+f"(o[13]), "+f"(o[14]), "+f"(o[15])::"memory");
 #pragma unroll
-              for (int c = 0; c < 4; ++c) {
-                const int from = min(max(lo - key0 - 32 * c, 0), 32), to = min(max(hi - key0 - 32 * c, 0), 32);
-                const uint32_t bits = (to == 32 ? 0xffffffffu : (1u << to) - 1u) & ~(from == 32 ? 0xffffffffu : (1u << from) - 1u);
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[32 * c + j] = bits & (1u << j) ? v[32 * c + j] : -INFINITY;
+                for (int j = 0; j < 16; ++j) o[j] *= corr;
+                st16(o_col + 16 * c, reinterpret_cast<const uint32_t*>(o));
               }
             }
-            if (again || __any_sync(0xffffffffu, m == -INFINITY)) {
-              float mx[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-              for (int j = 4; j < 124; j += 8) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], v[j + i], v[j + 4 + i]);
-              }
-              const float top = max3(max3(mx[0], mx[1], v[124]), max3(mx[2], mx[3], v[125]), max3(v[126], v[127], v[127])) * a.scale_log2e;
-              if (live && top > m) {
-                const float corr = m == -INFINITY ? 0.f : paged_ex2(m - top);
-                m = top;
-                l *= corr;
-                later = corr;
-              }
-              if (s > 1 && __any_sync(0xffffffffu, later != 1.f)) {
-#pragma unroll 1
-                for (int c = 0; c < DH / 16; ++c) scale16(o_col + 16 * c, later);
-              }
-              later = 1.f;
-            }
-            const float nm = m == -INFINITY ? 0.f : -m;
-            const f32x2 nm2 = pack2(nm, nm);
-            sum2 = pack2(0.f, 0.f);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) weights<T>(v + 32 * c, w + 16 * c, sc2, nm2, sum2);
-            float s0, s1;
-            unpack2(sum2, s0, s1);
-            sum = s0 + s1;
-            if (again || !__any_sync(0xffffffffu, live && !(sum < kMost))) break;
-            again = true;                        // (some row's scores have left the reference point far behind: once more, from their maximum)
           }
-          st32(s_col, w);
-          st32(s_col + 32, w + 32);
+          const float nm = m == -INFINITY ? 0.f : -m;
+          const f32x2 nm2 = pack2(nm, nm);
+          weights<T>(v, s_col, sc2, nm2, l2);
+          weights<T>(v + 32, s_col + 16, sc2, nm2, l2);
           st_wait();
           fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(b_p + 8 * slot);
-          l += sum;
-          if (live && sum > 256.f && sum < kMost) {                 // the reference point follows, by whole powers of two; O when its product is done
-            const int e = (int)(__float_as_uint(sum) >> 23) - 127;
-            const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-            m += (float)e;
-            l *= down;
-            later = down;
-          }
+          if (lane == 0) mbar_arrive(b_p + 8 * slot);      // (the products with the first 64 keys may begin)
+          weights<T>(v + 64, s_col + 32, sc2, nm2, l2);
+          weights<T>(v + 96, s_col + 48, sc2, nm2, l2);
+          st_wait();
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(b_p2 + 8 * slot);
         } else {
           fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(b_p + 8 * slot);
+          if (lane == 0) { mbar_arrive(b_p + 8 * slot); mbar_arrive(b_p2 + 8 * slot); }
         }
       }
 
       // ---- results
+      float l0, l1;
+      unpack2(l2, l0, l1);
+      float l = l0 + l1;
       const bool mine = n > slot, other = n > 1 - slot;        // did this slot, the other slot have a step?
       if (mine) wait(b_o + 8 * slot, o_phase[slot]);
       if (!both && other) wait(b_o + 8 * (1 - slot), o_phase[1 - slot]);
       if (n > 0) o_phase[0] ^= 1;
       if (n > 1) o_phase[1] ^= 1;
       fence_after();
-      float k_mine = later, k_other = 0.f;
+      float k_mine = 1.f, k_other = 0.f;
       if (!both) {
         // the slots' rows are the same: each warpgroup adds up half of the columns, from tensor memory
         s_ml[slot * kM + row] = make_float2(m, l);
-        s_later[slot * kM + row] = later;
         __syncwarp();
         if (lane == 0) mbar_arrive(b_ml);
         wait(b_ml, turns & 1);
         const float2 o_ml = s_ml[(1 - slot) * kM + row];
         const bool nothing = o_ml.x == -INFINITY && o_ml.y == 0.f;
         const float M = fmaxf(m, o_ml.x);
-        const float w_mine = m == -INFINITY ? 0.f : paged_ex2(m - M), w_other = o_ml.x == -INFINITY ? 0.f : paged_ex2(o_ml.x - M);
-        l = (m == -INFINITY && l == 0.f ? 0.f : l * w_mine) + (nothing ? 0.f : o_ml.y * w_other);
+        k_mine = m == -INFINITY ? 0.f : paged_ex2(m - M);
+        k_other = o_ml.x == -INFINITY ? 0.f : paged_ex2(o_ml.x - M);
+        l = (m == -INFINITY && l == 0.f ? 0.f : l * k_mine) + (nothing ? 0.f : o_ml.y * k_other);
         m = M;
-        k_mine = w_mine * later;
-        k_other = w_other * s_later[(1 - slot) * kM + row];
       }
       const bool good = *s_abort == 0;
       const int c_first = both ? 0 : slot * (DH / 2), c_last = both ? DH : c_first + DH / 2;
@@ -587,8 +565,6 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           if (both) {
             ld_wait();
             ld_valid(o);
-#pragma unroll
-            for (int j = 0; j < 32; ++j) o[j] *= k_mine;
           } else {
             float o2[32];
             ld32(lanes + kOCol + (1 - slot) * 128 + c0, o2);
