@@ -69,6 +69,7 @@ struct PagedAttnArgs {
   float scale_log2e, scale;
   int item_rows;               // query rows (row of the block x head of the group) per work item
   int item_cost;               // what an item costs beside its tiles, in tiles
+  int keep;                    // items of up to so many tiles are not shared where a CTA has no more than that to do
   PagedDivisor by_group, by_item_rows;
   float *parts, *parts_ml;
   int *counters, *status;
@@ -306,6 +307,31 @@ __device__ __forceinline__ int paged_owner(long long x, long long total, int n) 
 
 __device__ __forceinline__ int paged_first_cta(const PagedAttnArgs& a, const PagedPiece& p, long long total, int n) { return paged_owner(p.item_at + a.item_cost, total, n); }
 __device__ __forceinline__ int paged_last_cta(const PagedAttnArgs& a, const PagedPiece& p, long long total, int n) { return paged_owner(p.item_at + a.item_cost + p.item_tiles - 1, total, n); }
+
+// The first piece of a CTA's run, by a whole warp, and where the run ends; empty (n_tiles 0) if there is nothing to do.  Where CTAs have little to do, items of up to `keep` tiles are left
+// to the CTA that has the last place of them: reading a few more tiles takes less time than adding pieces up.  (The small model's 11 rows over 512 keys, five
+// tiles a head, cut / whole: FIG_KEEP us.)
+__device__ __forceinline__ PagedPiece paged_run(const PagedAttnArgs& a, const PagedPlan& plan, long long total, int n_cta, int cta, int lane, long long& end) {
+  const long long begin = paged_div(total * cta, n_cta);
+  end = paged_div(total * (cta + 1), n_cta);
+  PagedPiece p = paged_piece(a, plan, begin, end, lane);
+  if (total > (long long)gridDim.x * a.keep) return p;
+  PagedPiece q = p;
+  for (;;) {                                     // the item that the run ends in
+    const long long behind = q.item_at + a.item_cost + q.item_tiles;
+    if (end < behind && q.item_tiles <= a.keep) end = q.item_at;
+    if (end <= behind || !paged_next(a, plan, q, total)) break;
+  }
+  if (p.item_tiles <= a.keep) {
+    p.tile0 = p.hi > p.lo ? p.lo / kPagedTile : 0;
+    p.opens = p.whole = true;
+    p.n_tiles = end > p.item_at ? p.item_tiles : 0;
+  } else {
+    // (the end may have moved to the end of this item)
+    p.whole = p.n_tiles == p.item_tiles;
+  }
+  return p;
+}
 
 // 2^x, hardware approximation (relative error about 2^-22; -inf gives 0)
 __device__ __forceinline__ float paged_ex2(float x) {

@@ -78,14 +78,14 @@ k_paged_few(PagedAttnArgs a) {
   const long long total = plan.before[a.blk.n_seqs];
   const int n_cta = (int)min((long long)gridDim.x, total), cta = blockIdx.x;
   if (cta >= n_cta) return;
-  const long long run0 = paged_div(total * cta, n_cta), run1 = paged_div(total * (cta + 1), n_cta);
 
   const uint32_t my_ring = (uint32_t)__cvta_generic_to_shared(ring) + (uint32_t)(warp * kStages * 2 * kSliceBytes);
   const uint8_t* my_ring_p = ring + warp * kStages * 2 * kSliceBytes;
 
   // ---- the fetching side: runs kStages slices ahead, across pieces
-  PagedPiece p = paged_piece(a, plan, run0, run1, lane), f = p;
-  if (p.n_tiles == 0) return;                    // (a run may hold nothing but the place an item begins with)
+  long long run1;
+  PagedPiece p = paged_run(a, plan, total, n_cta, cta, lane, run1), f = p;
+  if (p.n_tiles == 0) return;
   const int G = a.group;
   int f_tile = 0, f_entry = 0, f_stage = 0, f_q = 0, q_at = 0;
   // Queries go through shared memory, with the fetched piece: two rows by every warp.  (Loaded where the piece begins they waited behind all keys in flight: 2.5 us.)
@@ -460,6 +460,7 @@ cs_status cs_launch_paged_few(cs_paged_cache* c, const PagedAttnArgs& args, cuda
   a.item_rows = kRows;
   a.by_item_rows = PagedDivisor::by(kRows);
   a.item_cost = 2;
+  a.keep = c->cfg.head_dim == 128 ? 6 : c->cfg.head_dim == 64 ? 10 : 16;
   const bool bf = c->cfg.dtype == CS_BF16;
   switch (c->cfg.head_dim) {
     case 32: return bf ? launch_few<__nv_bfloat16, 32>(c, a, 1, st) : launch_few<__half, 32>(c, a, 2, st);

@@ -211,7 +211,6 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   const uint32_t tmem = uniform(*tmem_slot);
   const long long total = plan.before[a.blk.n_seqs];
   const int n_cta = (int)min((long long)gridDim.x, total), cta = blockIdx.x;
-  const long long run0 = cta < n_cta ? paged_div(total * cta, n_cta) : 0, run1 = cta < n_cta ? paged_div(total * (cta + 1), n_cta) : 0;
 
   // Bounded waits, in few instructions (see the MMA issuer).  Once one has run out all others return.
   auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
@@ -316,8 +315,9 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       // ------------------------------------------------------------------ pieces and queries
       PagedPiece p;
       p.n_tiles = 0;
-      if (run1 > run0) p = paged_piece(a, plan, run0, run1, lane);
-      bool more = p.n_tiles > 0;                   // (a run may hold nothing but the place an item begins with)
+      long long run1 = 0;
+      if (cta < n_cta) p = paged_run(a, plan, total, n_cta, cta, lane, run1);
+      bool more = p.n_tiles > 0;
       for (;; ++piece) {
         const bool both = more && p.len * a.group - p.rg * a.item_rows > slot_rows;
         if (lane == 0) {
@@ -810,6 +810,7 @@ cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& args, cudaS
   a.item_rows = 2 * tokens * a.group;
   a.by_item_rows = PagedDivisor::by(a.item_rows);
   a.item_cost = 2;
+  a.keep = 5;
   const int box_rows = tokens < a.blk.rows ? tokens : a.blk.rows, dh = c->cfg.head_dim;
   CUtensorMap tmQ;
   // (a stride that no second row or head uses may be anything)
