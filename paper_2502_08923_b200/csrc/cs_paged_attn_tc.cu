@@ -31,7 +31,13 @@ namespace {
 
 constexpr int kThreads = 384, kMmaWarp = 8, kKWarp = 9, kQWarp = 11;   // (10: V)
 constexpr int kM = 128;                                            // query rows of a slot
-constexpr uint32_t kSCol = 0, kOCol = 256, kTmemCols = 512;        // slot x 128 columns each
+// Tensor memory: scores of slot s at 128 s, output from 256 on.  With heads of 128 that is all there is, and weights lie over the scores they come from; with heads of 64
+// they have 64 columns of their own, and a slot's next scores are made while the softmax is at work on the last ones, which it has in registers.
+constexpr uint32_t kTmemCols = 512;
+template <int DH> constexpr bool kApart = DH == 64;
+constexpr uint32_t kOCol = 256;
+template <int DH> constexpr uint32_t kPCol = kApart<DH> ? 384 : 0;
+template <int DH> constexpr uint32_t kPStep = kApart<DH> ? 64 : 128;
 template <int DH> constexpr int kTileBytes = kPagedTile * DH * 2;  // of K, of V, and of a slot's queries
 template <int DH> constexpr int kStages = DH == 128 ? 4 : 8;
 constexpr int kCtl = 512;
@@ -181,19 +187,19 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   uint8_t* ring = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));   // [stage][64 dims][128 keys][128 B]
   uint8_t* sq = ring + kNS * kTB;                                       // [slot][64 dims][128 rows][128 B]
   uint64_t* bars = reinterpret_cast<uint64_t*>(sq + 2 * kTB);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kNS + 18);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kNS + 20);
   volatile int* s_abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float2* s_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(bars) + kCtl);      // [slot][128 rows]
   TcPiece* s_piece = reinterpret_cast<TcPiece*>(s_ml + 2 * kM);
   PagedPlan& plan = *reinterpret_cast<PagedPlan*>(s_piece + kPieces);
-  const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8 * kNS, b_s = b_empty + 8 * kNS, b_p = b_s + 16, b_p2 = b_p + 16, b_o = b_p2 + 16, b_qfull = b_o + 16, b_qfree = b_qfull + 8,
+  const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8 * kNS, b_s = b_empty + 8 * kNS, b_p = b_s + 16, b_p2 = b_p + 16, b_o = b_p2 + 16, b_taken = b_o + 16, b_qfull = b_taken + 16, b_qfree = b_qfull + 8,
                  b_drain = b_qfree + 8, b_piece = b_drain + 8, b_ml = b_piece + 8 * kPieces, b_read = b_ml + 8;
   const int tid = threadIdx.x, warp = (int)uniform(tid >> 5), lane = tid & 31;
 
   CS_PDL_PROLOGUE();
   if (tid == 0) {
     for (int s = 0; s < kNS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_empty + 8 * s, 1); }
-    for (int s = 0; s < 2; ++s) { mbar_init(b_s + 8 * s, 1); mbar_init(b_p + 8 * s, 4); mbar_init(b_p2 + 8 * s, 4); mbar_init(b_o + 8 * s, 1); }
+    for (int s = 0; s < 2; ++s) { mbar_init(b_s + 8 * s, 1); mbar_init(b_p + 8 * s, 4); mbar_init(b_p2 + 8 * s, 4); mbar_init(b_o + 8 * s, 1); mbar_init(b_taken + 8 * s, 4); }
     mbar_init(b_qfull, 1); mbar_init(b_qfree, 1); mbar_init(b_drain, 1);
     for (int s = 0; s < kPieces; ++s) mbar_init(b_piece + 8 * s, 1);
     mbar_init(b_ml, 8); mbar_init(b_read, 8);
@@ -230,9 +236,16 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   const int slot_rows = a.item_rows / 2;          // query rows of a slot
   // the next piece, once it is known (by a warp; false: a wait has run out)
   auto known = [&](uint32_t piece) -> bool { return wait_warp(b_piece + 8 * (piece % kPieces), (piece / kPieces) & 1) && !__any_sync(0xffffffffu, *s_abort != 0); };
-  // Order of the ring: K and V tiles in turn where the slots share them, else K0 K1 V0 K2 V1 ... (entry of step s, of n steps)
-  auto k_entry = [](bool both, int s) { return both ? s & ~1 : s < 2 ? s : 2 * s - 1; };
-  auto v_entry = [](bool both, int s, int n) { return both ? s | 1 : s + min(s + 2, n); };
+  // Order of the ring, that of first use: where the slots share tiles K0 V0 K1 V1 .., else K0 K1 V0 K2 V1 ..; with scores made ahead (kApart) K0 K1 V0 K2 V1 .. and
+  // K0 K1 K2 V0 K3 V1 ..  (Entry of step s, of n steps.)
+  auto k_entry = [](bool both, int s) {
+    const int i = both ? s >> 1 : s, ahead = (both ? 1 : 2) + (kApart<DH> ? 1 : 0);      // K tiles in front of the first V tile
+    return i < ahead ? i : 2 * i - ahead + 1;
+  };
+  auto v_entry = [](bool both, int s, int n) {
+    const int i = both ? s >> 1 : s, tiles = both ? n >> 1 : n, ahead = (both ? 1 : 2) + (kApart<DH> ? 1 : 0);
+    return i + min(i + ahead, tiles);
+  };
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
@@ -247,7 +260,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       // One lane runs a piece's steps by itself, and every instruction counts: this warp comes by once in 900 clocks, when the softmax warps have filled the instruction cache with
       // their unrolled loops, so that its instructions are fetched anew each time.  (All lanes with votes, ring places worked out from the step, waits in
       // line: 900 clocks a step of its own, and the tensor cores waited for it.)
-      uint32_t p_phase = 0;                       // bit s: of slot s
+      uint32_t p_phase = 0, t_phase = 0;          // bit s: of slot s
       for (;; ++piece) {
         ok = known(piece);
         if (!ok) break;
@@ -267,7 +280,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
               if (!wait(b_full + 8 * (k_at % kNS), (k_at / kNS) & 1)) { fine = false; return; }
             }
             const uint64_t dk = dk0 + (k_at % kNS) * (kTB >> 4), dq = dq0 + (both && (s & 1) ? kTB >> 4 : 0);
-            const uint32_t acc = tmem + kSCol + (s & 1) * 128;
+            const uint32_t acc = tmem + (s & 1) * 128;
 #pragma unroll
             for (int h = 0; h < kHalves; ++h)
 #pragma unroll
@@ -280,6 +293,13 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           if (fine && n > 1) scores(1);
           for (int s = 0; s < n && fine; ++s) {
             const uint32_t slot = s & 1;
+            if (kApart<DH> && s + 2 < n) {
+              if (!wait(b_taken + 8 * slot, t_phase >> slot & 1)) { fine = false; break; }      // (the softmax has the scores in registers)
+              fence_after();
+              scores(s + 2);
+              if (!fine) break;
+            }
+            if (kApart<DH>) t_phase ^= 1u << slot;
             if (!both || !slot) {
               v_at = at++;
               if (!wait(b_full + 8 * (v_at % kNS), (v_at / kNS) & 1)) { fine = false; break; }
@@ -287,7 +307,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
             if (!wait(b_p + 8 * slot, p_phase >> slot & 1)) { fine = false; break; }
             fence_after();
             const uint64_t dv = dv0 + (v_at % kNS) * (kTB >> 4);
-            const uint32_t acc = tmem + kOCol + slot * 128, w = tmem + kSCol + slot * 128;
+            const uint32_t acc = tmem + kOCol + slot * DH, w = tmem + kPCol<DH> + slot * kPStep<DH>;
 #pragma unroll
             for (int k = 0; k < 4; ++k) umma_ta(acc, w + k * 8, dv + k * (2048 >> 4), idesc_o, (s > 1 || k > 0) ? 1u : 0u);   // 16 keys per instruction
             if (!wait(b_p2 + 8 * slot, p_phase >> slot & 1)) { fine = false; break; }
@@ -296,12 +316,13 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
 #pragma unroll
             for (int k = 4; k < 8; ++k) umma_ta(acc, w + k * 8, dv + k * (2048 >> 4), idesc_o, 1u);
             if (!both || slot) umma_commit(b_empty + 8 * (v_at % kNS));
-            if (s >= n - 2) umma_commit(b_o + 8 * slot);
-            if (s + 2 < n) scores(s + 2);
+            umma_commit(b_o + 8 * slot);
+            if (!kApart<DH> && s + 2 < n) scores(s + 2);
           }
         }
         ok = __all_sync(0xffffffffu, fine);
         p_phase = __reduce_xor_sync(0xffffffffu, elect_one() ? p_phase : 0u);
+        t_phase = __reduce_xor_sync(0xffffffffu, elect_one() ? t_phase : 0u);
         base += both ? n : 2 * n;
         if (!ok) break;
       }
@@ -415,8 +436,9 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     // -------------------------------------------------------------------- softmax and results: one thread per query row
     const int slot = warp >> 2, row = tid & 127, G = a.group;
     const bool out_32 = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;      // (rows are multiples of 32 bytes)
-    const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_col = lanes + kSCol + slot * 128, o_col = lanes + kOCol + slot * 128;
-    uint32_t base = 0, s_phase = 0, o_phase[2] = {0, 0}, piece = 0, turns = 0;     // (turns: pieces whose tiles the slots took in turn)
+    const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_col = lanes + slot * 128, o_col = lanes + kOCol + slot * DH, p_col = lanes + kPCol<DH> + slot * kPStep<DH>;
+    uint32_t base = 0, s_phase = 0, piece = 0, turns = 0;      // (turns: pieces whose tiles the slots took in turn)
+    uint32_t o_mine = 0, o_other = 0;                          // products of this slot, of the other one, so far
     bool split = false;
     for (;; ++piece) {
       if (slot_any(slot, !known(piece))) break;
@@ -465,6 +487,11 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
 #pragma unroll
           for (int c = 0; c < 4; ++c) ld_valid(v + 32 * c);
         }
+        if constexpr (kApart<DH>) {
+          fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(b_taken + 8 * slot);
+        }
         if (mixed && ok) {
           // a bit for each of 32 keys that the row sees
 #pragma unroll
@@ -483,6 +510,14 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
             for (int i = 0; i < 4; ++i) mx[i] = max3(mx[i], v[j + i], v[j + 4 + i]);
           }
           const float top = max3(max3(mx[0], mx[1], v[124]), max3(mx[2], mx[3], v[125]), max3(v[126], v[127], v[127])) * a.scale_log2e;
+          // (O and the weights' columns: the product before must be done.  With scores over the weights they would not be there otherwise.)
+          if constexpr (kApart<DH>) {
+            if (s > 1) {
+              wait(b_o + 8 * slot, (o_mine - 1) & 1);
+              __syncwarp();
+              fence_after();
+            }
+          }
           const bool moves = live && (m == -INFINITY ? top > m : top > m + 8.f);
           if (__any_sync(0xffffffffu, moves)) {
             const float corr = !moves ? 1.f : m == -INFINITY ? 0.f : paged_ex2(m - top);
@@ -506,23 +541,26 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           }
           const float nm = m == -INFINITY ? 0.f : -m;
           const f32x2 nm2 = pack2(nm, nm);
-          weights<T>(v, s_col, sc2, nm2, l2);
-          weights<T>(v + 32, s_col + 16, sc2, nm2, l2);
+          weights<T>(v, p_col, sc2, nm2, l2);
+          weights<T>(v + 32, p_col + 16, sc2, nm2, l2);
           st_wait();
           fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(b_p + 8 * slot);      // (the products with the first 64 keys may begin)
-          weights<T>(v + 64, s_col + 32, sc2, nm2, l2);
-          weights<T>(v + 96, s_col + 48, sc2, nm2, l2);
+          weights<T>(v + 64, p_col + 32, sc2, nm2, l2);
+          weights<T>(v + 96, p_col + 48, sc2, nm2, l2);
           st_wait();
           fence_before();
           __syncwarp();
           if (lane == 0) mbar_arrive(b_p2 + 8 * slot);
         } else {
+          // (nor may a warp without rows run ahead: its arrivals would count for the step before)
+          if constexpr (kApart<DH>) { if (s > 1) wait(b_o + 8 * slot, (o_mine - 1) & 1); }
           fence_before();
           __syncwarp();
           if (lane == 0) { mbar_arrive(b_p + 8 * slot); mbar_arrive(b_p2 + 8 * slot); }
         }
+        ++o_mine;
       }
 
       // ---- results
@@ -530,10 +568,9 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       unpack2(l2, l0, l1);
       float l = l0 + l1;
       const bool mine = n > slot, other = n > 1 - slot;        // did this slot, the other slot have a step?
-      if (mine) wait(b_o + 8 * slot, o_phase[slot]);
-      if (!both && other) wait(b_o + 8 * (1 - slot), o_phase[1 - slot]);
-      if (n > 0) o_phase[0] ^= 1;
-      if (n > 1) o_phase[1] ^= 1;
+      o_other += (n + slot) >> 1;
+      if (mine) wait(b_o + 8 * slot, (o_mine - 1) & 1);
+      if (!both && other) wait(b_o + 8 * (1 - slot), (o_other - 1) & 1);
       fence_after();
       float k_mine = 1.f, k_other = 0.f;
       if (!both) {
@@ -567,7 +604,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
             ld_valid(o);
           } else {
             float o2[32];
-            ld32(lanes + kOCol + (1 - slot) * 128 + c0, o2);
+            ld32(lanes + kOCol + (1 - slot) * DH + c0, o2);
             ld_wait();
             ld_valid(o);
             ld_valid(o2);
@@ -771,12 +808,12 @@ EncodeFn encoder() {
   }();
   return fn;
 }
-cs_status encode(cs_paged_cache* c, CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+cs_status encode(cs_paged_cache* c, CUtensorMap* tm, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box, CUtensorMapL2promotion promote) {
   EncodeFn enc = encoder();
   const cuuint32_t ones[4] = {1, 1, 1, 1};
   const CUresult r = enc == nullptr ? CUDA_ERROR_NOT_FOUND
                                     : enc(tm, c->cfg.dtype == CS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void*>(base), dims, strides, box,
-                                          ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                                          ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, promote, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r == CUDA_SUCCESS) return CS_OK;
   snprintf(c->err, sizeof(c->err), "cuTensorMapEncodeTiled (rank %d) failed with %d", rank, (int)r);
   return CS_ERR_CUDA;
@@ -800,8 +837,10 @@ cs_status cs_paged_tc_maps(cs_paged_cache* c) {
   const cuuint64_t dims[4] = {(cuuint64_t)f.head_dim, (cuuint64_t)f.page_size, (cuuint64_t)f.n_kv_heads, (cuuint64_t)f.n_pages};
   const cuuint64_t strides[3] = {(cuuint64_t)f.slot_stride * 2, (cuuint64_t)f.head_stride * 2, (cuuint64_t)f.page_stride * 2};
   const cuuint32_t box[4] = {64, (cuuint32_t)(f.page_size < kPagedTile ? f.page_size : kPagedTile), 1, 1};
-  const cs_status s = encode(c, &c->tmK, f.k, 4, dims, strides, box);
-  return s != CS_OK ? s : encode(c, &c->tmV, f.v, 4, dims, strides, box);
+  // (rows of 128 bytes between those of other heads: 256 bytes at a time would fetch those as well, FIG_PROMOTE)
+  const CUtensorMapL2promotion promote = f.head_dim == 64 && f.slot_stride != 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B;
+  const cs_status s = encode(c, &c->tmK, f.k, 4, dims, strides, box, promote);
+  return s != CS_OK ? s : encode(c, &c->tmV, f.v, 4, dims, strides, box, promote);
 }
 
 cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& args, cudaStream_t st) {
@@ -817,7 +856,7 @@ cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& args, cudaS
   const cuuint64_t dims[3] = {(cuuint64_t)dh, (cuuint64_t)a.n_heads, (cuuint64_t)a.blk.rows};
   const cuuint64_t strides[2] = {(cuuint64_t)(a.n_heads > 1 ? a.q_head : dh) * 2, (cuuint64_t)(a.blk.rows > 1 ? a.q_row : (long long)dh * a.n_heads) * 2};
   const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)box_rows};
-  const cs_status s = encode(c, &tmQ, a.q, 3, dims, strides, box);
+  const cs_status s = encode(c, &tmQ, a.q, 3, dims, strides, box, CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
   if (s != CS_OK) return s;
   const int bytes = 128 * a.group * box_rows;
   const bool bf = c->cfg.dtype == CS_BF16;
