@@ -675,14 +675,47 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   }
 }
 
-// Items that several CTAs share: their pieces added up, in the order of the keys.  All their rows are dealt out over all warps.  (The last CTA to arrive did this inside
-// the kernel at first: 430 KB through one SM, 5 us with its loads in flight together and 14 without.)
+// Items that several CTAs share: their pieces added up, in the order of the keys, by a launch of its own.  (The last CTA to arrive did this inside the kernel at first: 430 KB through
+// one SM, 5 us with its loads in flight together and 14 without.)  Bound by latencies: a list, a search, the pieces.  All rows are dealt out over all warps, two at a
+// time for each (one at a time 148 items of 256 rows took 11 us for FIG_MERGE now); where there are few rows a CTA has one at a time, its warps an eighth of the pieces each.
 constexpr int kMergeWarps = 8, kMergeCtas = 3;    // CTAs per SM
+
+// where output row `g` of the line of all split rows is kept, and by whom
+struct MergeRow {
+  int c0, c1, r;
+};
+struct MergeSum {
+  float M, L;
+};
+template <int kV>
+__device__ __forceinline__ void load_part(const PagedAttnArgs& a, int dh, int c, const MergeRow& w, int lane, float2& ml, float (&v)[kV]) {
+  const long long at = ((long long)c * 2 + (c == w.c0 ? 1 : 0)) * kPagedMaxRows + w.r;
+  ml = __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at);
+  const float* src = a.parts + at * dh + lane * kV;
+  if constexpr (kV == 4) {
+    const float4 x = __ldcg(reinterpret_cast<const float4*>(src));
+    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+  } else {
+    const float2 x = __ldcg(reinterpret_cast<const float2*>(src));
+    v[0] = x.x; v[1] = x.y;
+  }
+}
+// a piece to a sum with its own reference point
+template <int kV>
+__device__ __forceinline__ void add_part(MergeSum& s, float (&acc)[kV], float2 ml, const float (&v)[kV]) {
+  if (ml.x == -INFINITY && ml.y == 0.f) return;                  // (it saw nothing)
+  const float top = fmaxf(s.M, ml.x), keep = s.M == -INFINITY ? (s.L == 0.f ? 0.f : s.L) : paged_ex2(s.M - top), k = ml.x == -INFINITY ? 0.f : paged_ex2(ml.x - top);   // (a sum without a maximum is NaN)
+  s.M = top;
+  s.L = fmaf(k, ml.y, s.L * keep);
+#pragma unroll
+  for (int e = 0; e < kV; ++e) acc[e] = fmaf(k, v[e], acc[e] * keep);
+}
+
 template <typename T, int DH>
 __global__ void __launch_bounds__(kMergeWarps * 32, kMergeCtas)
 k_paged_merge(PagedAttnArgs a, int n_cta) {
   CS_PDL_PROLOGUE();
-  constexpr int kBatch = 8, kV = DH / 32, kPerLane = kPagedMaxCtas / 32;        // columns of a lane; splits of a lane
+  constexpr int kV = DH / 32, kPerLane = kPagedMaxCtas / 32;     // columns of a lane; splits of a lane
   __shared__ PagedSplit s_split[kPagedMaxCtas];
   __shared__ int s_before[kPagedMaxCtas];         // rows of the items before
   __shared__ float2 s_ml[kMergeWarps];
@@ -716,85 +749,94 @@ k_paged_merge(PagedAttnArgs a, int n_cta) {
     s_before[lane * kPerLane + i] = mine[i];
   }
   __syncwarp();
-  // A warp per row; where there are fewer rows than CTAs a CTA per row, its warps with an eighth of the pieces each.
-  const bool together = total <= (int)gridDim.x;
-  const int hop = together ? kMergeWarps : 1;
-  for (int g = together ? blockIdx.x : blockIdx.x * kMergeWarps + warp; g < total; g += gridDim.x * (together ? 1 : kMergeWarps)) {
+  auto find = [&](int g) -> MergeRow {
     int n = 0;
 #pragma unroll
     for (int i = 0; i < kPerLane; ++i) n += mine[i] <= g;
     const int c0 = (int)__reduce_add_sync(0xffffffffu, (unsigned)n) - 1;            // the last item that begins at or before it (those without rows come first)
-    const PagedSplit d = s_split[c0];
-    const int r = g - s_before[c0], c1 = d.last;
-    float M = -INFINITY, L = 0.f, acc[kV];
+    return MergeRow{c0, s_split[c0].last, g - s_before[c0]};
+  };
+  auto write = [&](const MergeRow& w, const MergeSum& s, const float (&acc)[kV]) {
+    const PagedSplit& d = s_split[w.c0];
+    const float inv = s.L == 0.f ? 0.f : 1.f / s.L;
+    const int m = d.first_row + w.r, q = a.by_group.of(m);
+    const long long row = (long long)(d.start + q) * a.n_heads + d.head * a.group + (m - q * a.group);
+    uint32_t x[kV / 2];
 #pragma unroll
-    for (int e = 0; e < kV; ++e) acc[e] = 0.f;
-    for (int cb = c0 + (together ? warp : 0); cb <= c1; cb += kBatch * hop) {
-      float2 ml[kBatch];
-      float v[kBatch][kV];
+    for (int e = 0; e < kV / 2; ++e) x[e] = PagedType<T>::pack(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+    if constexpr (kV == 4) *reinterpret_cast<uint2*>(a.out + row * DH * 2 + lane * 8) = make_uint2(x[0], x[1]);
+    else *reinterpret_cast<uint32_t*>(a.out + row * DH * 2 + lane * 4) = x[0];
+    if (a.lse != nullptr && lane == 0) a.lse[row] = s.L == 0.f ? -INFINITY : (s.M + log2f(s.L)) * 0.6931471805599453f;
+  };
+
+  if (total <= 2 * (int)gridDim.x) {
+    for (int g = blockIdx.x; g < total; g += gridDim.x) {
+      const MergeRow w = find(g);
+      MergeSum s{-INFINITY, 0.f};
+      float acc[kV] = {};
+      constexpr int kBatch = 4;
+      for (int cb = w.c0 + warp; cb <= w.c1; cb += kBatch * kMergeWarps) {
+        float2 ml[kBatch];
+        float v[kBatch][kV];
 #pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        ml[i] = make_float2(-INFINITY, 0.f);
+        for (int i = 0; i < kBatch; ++i)
+          if (cb + i * kMergeWarps <= w.c1) load_part<kV>(a, DH, cb + i * kMergeWarps, w, lane, ml[i], v[i]);
 #pragma unroll
-        for (int e = 0; e < kV; ++e) v[i][e] = 0.f;
-        const int c = cb + i * hop;
-        if (c > c1) continue;
-        const long long at = ((long long)c * 2 + (c == c0 ? 1 : 0)) * kPagedMaxRows + r;
-        ml[i] = __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at);
-        if constexpr (kV == 4) {
-          const float4 x = __ldcg(reinterpret_cast<const float4*>(a.parts + at * DH) + lane);
-          v[i][0] = x.x; v[i][1] = x.y; v[i][2] = x.z; v[i][3] = x.w;
-        } else {
-          const float2 x = __ldcg(reinterpret_cast<const float2*>(a.parts + at * DH) + lane);
-          v[i][0] = x.x; v[i][1] = x.y;
-        }
+        for (int i = 0; i < kBatch; ++i)
+          if (cb + i * kMergeWarps <= w.c1) add_part<kV>(s, acc, ml[i], v[i]);
       }
-      float top = M;
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) top = fmaxf(top, ml[i].x);
-      const float keep = M == -INFINITY ? (L == 0.f ? 0.f : L) : paged_ex2(M - top);     // (L without a maximum is NaN)
-      M = top;
-      L *= keep;
-#pragma unroll
-      for (int e = 0; e < kV; ++e) acc[e] *= keep;
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        if (ml[i].x == -INFINITY && ml[i].y == 0.f) continue;                            // (it saw nothing)
-        const float k = ml[i].x == -INFINITY ? 0.f : paged_ex2(ml[i].x - M);
-        L = fmaf(k, ml[i].y, L);
-#pragma unroll
-        for (int e = 0; e < kV; ++e) acc[e] = fmaf(k, v[i][e], acc[e]);
-      }
-    }
-    if (together) {
-      s_ml[warp] = make_float2(M, L);
+      s_ml[warp] = make_float2(s.M, s.L);
 #pragma unroll
       for (int e = 0; e < kV; ++e) s_o[warp][lane * kV + e] = acc[e];
       __syncthreads();
-      if (warp > 0) return;                      // (a row is all that a CTA has)
-      for (int w = 0; w < kMergeWarps; ++w) M = fmaxf(M, s_ml[w].x);
-      L = 0.f;
+      if (warp == 0) {
+        s = MergeSum{-INFINITY, 0.f};
 #pragma unroll
-      for (int e = 0; e < kV; ++e) acc[e] = 0.f;
+        for (int e = 0; e < kV; ++e) acc[e] = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < kMergeWarps; ++i) {
+          float v[kV];
 #pragma unroll
-      for (int w = 0; w < kMergeWarps; ++w) {
-        const float2 x = s_ml[w];
-        if (x.x == -INFINITY && x.y == 0.f) continue;
-        const float k = x.x == -INFINITY ? 0.f : paged_ex2(x.x - M);
-        L = fmaf(k, x.y, L);
-#pragma unroll
-        for (int e = 0; e < kV; ++e) acc[e] = fmaf(k, s_o[w][lane * kV + e], acc[e]);
+          for (int e = 0; e < kV; ++e) v[e] = s_o[i][lane * kV + e];
+          add_part<kV>(s, acc, s_ml[i], v);
+        }
+        write(w, s, acc);
       }
+      __syncthreads();
     }
-    const float inv = L == 0.f ? 0.f : 1.f / L;
-    const int m = d.first_row + r, q = a.by_group.of(m);
-    const long long row = (long long)(d.start + q) * a.n_heads + d.head * a.group + (m - q * a.group);
-    uint32_t w[kV / 2];
+    return;
+  }
+  constexpr int kAtOnce = 2, kPieces2 = 3;
+  for (int g = (blockIdx.x * kMergeWarps + warp) * kAtOnce; g < total; g += gridDim.x * kMergeWarps * kAtOnce) {
+    MergeRow w[kAtOnce];
+    MergeSum s[kAtOnce];
+    float acc[kAtOnce][kV];
+    int most = 0;
 #pragma unroll
-    for (int e = 0; e < kV / 2; ++e) w[e] = PagedType<T>::pack(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-    if constexpr (kV == 4) *reinterpret_cast<uint2*>(a.out + row * DH * 2 + lane * 8) = make_uint2(w[0], w[1]);
-    else *reinterpret_cast<uint32_t*>(a.out + row * DH * 2 + lane * 4) = w[0];
-    if (a.lse != nullptr && lane == 0) a.lse[row] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    for (int j = 0; j < kAtOnce; ++j) {
+      w[j] = find(min(g + j, total - 1));
+      s[j] = MergeSum{-INFINITY, 0.f};
+      most = max(most, w[j].c1 - w[j].c0);
+#pragma unroll
+      for (int e = 0; e < kV; ++e) acc[j][e] = 0.f;
+    }
+    for (int i = 0; i <= most; i += kPieces2) {
+      float2 ml[kAtOnce][kPieces2];
+      float v[kAtOnce][kPieces2][kV];
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+        for (int k = 0; k < kPieces2; ++k)
+          if (w[j].c0 + i + k <= w[j].c1) load_part<kV>(a, DH, w[j].c0 + i + k, w[j], lane, ml[j][k], v[j][k]);
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+        for (int k = 0; k < kPieces2; ++k)
+          if (w[j].c0 + i + k <= w[j].c1) add_part<kV>(s[j], acc[j], ml[j][k], v[j][k]);
+    }
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j)
+      if (g + j < total) write(w[j], s[j], acc[j]);
   }
 }
 
