@@ -196,8 +196,12 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
                  b_drain = b_qfree + 8, b_piece = b_drain + 8, b_ml = b_piece + 8 * kPieces, b_read = b_ml + 8;
   const int tid = threadIdx.x, warp = (int)uniform(tid >> 5), lane = tid & 31;
 
-  CS_PDL_PROLOGUE();
+  // (nothing of this depends on the kernel before, so it is done while that one ends)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (tid == 0) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmK) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmV) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmQ) : "memory");
     for (int s = 0; s < kNS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_empty + 8 * s, 1); }
     for (int s = 0; s < 2; ++s) { mbar_init(b_s + 8 * s, 1); mbar_init(b_p + 8 * s, 4); mbar_init(b_p2 + 8 * s, 4); mbar_init(b_o + 8 * s, 1); mbar_init(b_taken + 8 * s, 4); }
     mbar_init(b_qfull, 1); mbar_init(b_qfree, 1); mbar_init(b_drain, 1);
@@ -211,6 +215,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   fence_before();
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   paged_plan(a, plan);
   __syncthreads();
   fence_after();
