@@ -555,6 +555,11 @@ cs_status cs_paged_attention(cs_paged_cache* cache, const cs_blocks* blocks, con
                              int64_t q_head_stride, int n_heads, cs_mask mask, int window, float scale, void* out,
                              float* lse, void* stream);
 
+/* Test hook for the bounded waits (no counterpart in the paper): the next cs_paged_attention of this handle that runs on the tensor cores leaves out the copy of every CTA's
+ * tile-th K tile, so that the products wait for it until the wait limit (CS_WAIT_LIMIT_US at cs_paged_create) and the CTA gives up: copies and
+ * products in flight end, nothing is written, cs_paged_status reports CS_ERR_TIMEOUT.  Calls of few rows have no such waits.  tile < 0 clears it. */
+cs_status cs_paged_debug_drop_tile(cs_paged_cache* cache, int tile);
+
 #ifdef __cplusplus
 }
 #endif

@@ -76,7 +76,7 @@ EXPORTS = ("cs_workspace_bytes", "cs_create", "cs_destroy", "cs_last_error", "cs
            "cs_loop_launches_per_step", "cs_lm_head", "cs_lm_head_static", "cs_gram_index_bytes",
            "cs_gram_index_reset", "cs_gram_index_update", "cs_find_match_indexed", "cs_gram_index_status",
            "cs_rope_table", "cs_qk_norm_rope", "cs_paged_workspace_bytes", "cs_paged_create", "cs_paged_destroy", "cs_paged_last_error",
-           "cs_paged_status", "cs_paged_append", "cs_paged_attention", "cs_paged_head_dim")
+           "cs_paged_status", "cs_paged_append", "cs_paged_attention", "cs_paged_head_dim", "cs_paged_debug_drop_tile")
 
 _lib = None
 _search = None      # cs_find_match in native code, for plain arguments
@@ -178,6 +178,8 @@ def load(build_if_missing: bool = True) -> C.CDLL:
     lib.cs_paged_destroy.argtypes = [vp]
     lib.cs_paged_last_error.restype = C.c_char_p
     lib.cs_paged_last_error.argtypes = [vp]
+    lib.cs_paged_debug_drop_tile.restype = i
+    lib.cs_paged_debug_drop_tile.argtypes = [vp, i]
     lib.cs_paged_head_dim.restype = i
     lib.cs_paged_head_dim.argtypes = [vp]
     lib.cs_paged_status.restype = i
@@ -767,3 +769,6 @@ class PagedCache:
     def cs_paged_status(self):
         """Waits for the stream; what the device found wrong since the last call (CS_OK: nothing)."""
         return self.lib.cs_paged_status(self.handle, _stream())
+
+    def cs_paged_debug_drop_tile(self, tile):
+        self._check(self.lib.cs_paged_debug_drop_tile(self.handle, tile), "cs_paged_debug_drop_tile")

@@ -444,6 +444,7 @@ cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void
   cs_paged_cache* c = static_cast<cs_paged_cache*>(aligned_alloc(64, (sizeof(cs_paged_cache) + 63) / 64 * 64));   // (operand maps: 64 bytes)
   if (c == nullptr) return refuse(CS_ERR_CAPACITY, "out of host memory");
   memset(c, 0, sizeof(*c));
+  c->drop = -1;
   c->cfg = *cfg;
   c->num_sms = sms < kPagedMaxCtas ? sms : kPagedMaxCtas;
   int shift = 0;
@@ -493,6 +494,12 @@ cs_status cs_paged_status(cs_paged_cache* c, void* stream) {
   if (bits & CS_DEV_SMEM) return fail(c, CS_ERR_CUDA, "a kernel found its shared memory too small");
   if (bits & CS_DEV_CAPACITY) return fail(c, CS_ERR_CAPACITY, "a block does not fit its row of the page table, or the rotation table is too short");
   return fail(c, CS_ERR_ARG, "a length is negative, rows lie outside the tensors, or a page does not exist");
+}
+
+cs_status cs_paged_debug_drop_tile(cs_paged_cache* c, int tile) {
+  if (c == nullptr) return CS_ERR_ARG;
+  c->drop = tile < 0 ? -1 : tile;
+  return CS_OK;
 }
 
 cs_status cs_paged_append(cs_paged_cache* c, const cs_blocks* blocks, const cs_heads* k, const cs_heads* v, const cs_heads* q, cs_dtype in,
@@ -552,8 +559,13 @@ cs_status cs_paged_attention(cs_paged_cache* c, const cs_blocks* blocks, const v
   a.scale = scale; a.scale_log2e = (float)(1.4426950408889634 * (double)scale);
   a.parts = c->parts; a.parts_ml = c->parts_ml; a.counters = c->counters; a.splits = c->splits; a.status = c->status;
   a.wait_ns = c->wait_limit_ns;
+  a.drop = -1;
   // 16 query rows per KV head are a tile of the kernel for few rows, which takes heads of 32 whatever their rows
   const bool few = c->cfg.head_dim == 32 || (long long)blocks->rows * a.group <= 16ll * blocks->n_seqs;
+  if (!few) {
+    a.drop = c->drop;
+    c->drop = -1;
+  }
   for (int b = 0; b < blocks->n_seqs; b += kPagedMaxSeqs) {      // (a launch's plan holds so many)
     PagedAttnArgs p = a;
     p.blk.n_seqs = blocks->n_seqs - b < kPagedMaxSeqs ? blocks->n_seqs - b : kPagedMaxSeqs;

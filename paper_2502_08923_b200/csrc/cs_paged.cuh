@@ -40,6 +40,7 @@ struct cs_paged_cache {
   int num_sms;
   unsigned attr_set;           // shared-memory opt-ins made, a bit per kernel instance
   unsigned long long wait_limit_ns;
+  int drop;                    // test hook: the next tall launch leaves out this K tile of every CTA (-1 = none)
   char err[256];
 };
 
@@ -75,6 +76,7 @@ struct PagedAttnArgs {
   int *counters, *status;
   PagedSplit* splits;
   unsigned long long wait_ns;
+  int drop;
 };
 
 cs_status cs_launch_paged_few(cs_paged_cache* c, const PagedAttnArgs& a, cudaStream_t st);

@@ -384,6 +384,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       const CUtensorMap* tm = is_k ? &tmK : &tmV;
       const int rows = min(a.kv.page_size, kPagedTile), per_tile = kPagedTile / rows, shift = a.kv.page_shift;
       uint32_t asked = 0;                          // entries this warp has started copies for, + 1
+      int tile_no = 0;
       for (;; ++piece) {
         if (!known(piece)) break;
         const TcPiece& d = s_piece[piece % kPieces];
@@ -409,6 +410,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           }
           ok = wait_warp(b_empty + 8 * st, ((e / kNS) & 1) ^ 1);
           if (!ok) break;
+          if (is_k && tile_no++ == a.drop) continue;             // (test hook: these keys never arrive)
           if (elect_one()) mbar_expect_tx(b_full + 8 * st, (uint32_t)((j1 - j0) * rows * 128 * kHalves));
           __syncwarp();
           for (int j = j0; j < j1; ++j) {
