@@ -459,7 +459,7 @@ cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void
   const char* wl = getenv("CS_WAIT_LIMIT_US");
   const long long us = wl != nullptr ? atoll(wl) : 0;
   c->wait_limit_ns = us > 0 ? (unsigned long long)us * 1000ull : 2000000000ull;
-  if (cfg->head_dim != 32 && cs_paged_tc_maps(c) != CS_OK) {
+  if (cs_paged_tc_maps(c) != CS_OK) {
     snprintf(t_paged_err, sizeof(t_paged_err), "cs_paged_create: %s", c->err);
     free(c);
     return CS_ERR_CUDA;
@@ -560,8 +560,8 @@ cs_status cs_paged_attention(cs_paged_cache* c, const cs_blocks* blocks, const v
   a.parts = c->parts; a.parts_ml = c->parts_ml; a.counters = c->counters; a.splits = c->splits; a.status = c->status;
   a.wait_ns = c->wait_limit_ns;
   a.drop = -1;
-  // 16 query rows per KV head are a tile of the kernel for few rows, which takes heads of 32 whatever their rows
-  const bool few = c->cfg.head_dim == 32 || (long long)blocks->rows * a.group <= 16ll * blocks->n_seqs;
+  // 16 query rows per KV head are a tile of the kernel for few rows
+  const bool few = (long long)blocks->rows * a.group <= 16ll * blocks->n_seqs;
   if (!few) {
     a.drop = c->drop;
     c->drop = -1;

@@ -1,4 +1,4 @@
-// Attention of tall blocks over a paged KV cache on the 5th-generation tensor cores (Sec. 3.2; App. B.2), head sizes 64 and 128.
+// Attention of tall blocks over a paged KV cache on the 5th-generation tensor cores (Sec. 3.2; App. B.2).
 //
 // The mathematics is that of cs_paged_attn.cu.  Query rows (row of the block x head of the group) are the M = 128 of both products, so that TMEM
 // lane = query row and one thread has a whole row of scores:
@@ -31,19 +31,24 @@ namespace {
 
 constexpr int kThreads = 384, kMmaWarp = 8, kKWarp = 9, kQWarp = 11;   // (10: V)
 constexpr int kM = 128;                                            // query rows of a slot
-// Tensor memory: scores of slot s at 128 s, output from 256 on.  With heads of 128 that is all there is, and weights lie over the scores they come from; with heads of 64
+// Tensor memory: scores of slot s at 128 s, output from 256 on.  With heads of 128 that is all there is, and weights lie over the scores they come from; with smaller heads
 // they have 64 columns of their own, and a slot's next scores are made while the softmax is at work on the last ones, which it has in registers.
 constexpr uint32_t kTmemCols = 512;
-template <int DH> constexpr bool kApart = DH == 64;
+template <int DH> constexpr bool kApart = DH <= 64;
 constexpr uint32_t kOCol = 256;
 template <int DH> constexpr uint32_t kPCol = kApart<DH> ? 384 : 0;
 template <int DH> constexpr uint32_t kPStep = kApart<DH> ? 64 : 128;
 template <int DH> constexpr int kTileBytes = kPagedTile * DH * 2;  // of K, of V, and of a slot's queries
 template <int DH> constexpr int kStages = DH == 128 ? 4 : 8;
+template <int DH> constexpr int kRowBytes = DH == 32 ? 64 : 128;    // of a row in shared memory, swizzled over so many bytes; heads of 128 are two halves one behind the other
 constexpr int kCtl = 512;
 constexpr int kPieces = 4;         // descriptors of pieces (published at most two ahead of the products, of which the softmax may be one behind)
 template <int DH> constexpr int kTcSmem = 1024 + (kStages<DH> + 2) * kTileBytes<DH> + kCtl + 2 * kM * 8 + kPieces * 64 + (int)sizeof(PagedPlan);
 
+// Operand descriptors as in cs_tcgen.cuh, for rows of 128 or (heads of 32) 64 bytes: eight of them a group, and the swizzle as wide
+template <int kRow> __device__ __forceinline__ uint64_t desc_rows(uint32_t saddr, uint32_t lbo) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(8 * kRow >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)(kRow == 128 ? 2 : 4) << 61);
+}
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2, int c3) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                ::"r"(dst), "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
@@ -182,7 +187,7 @@ __device__ __noinline__ void mend_row(const PagedAttnArgs& a, const TcPiece& p, 
 template <typename T, int DH>
 __global__ void __launch_bounds__(kThreads, 1)
 k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ PagedAttnArgs a, int q_box_bytes) {
-  constexpr int kTB = kTileBytes<DH>, kNS = kStages<DH>, kHalves = DH / 64, kHalf = kPagedTile * 128;
+  constexpr int kTB = kTileBytes<DH>, kNS = kStages<DH>, kRow = kRowBytes<DH>, kHalves = DH == 128 ? 2 : 1, kHalf = kPagedTile * 128;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));   // [stage][64 dims][128 keys][128 B]
   uint8_t* sq = ring + kNS * kTB;                                       // [slot][64 dims][128 rows][128 B]
@@ -261,7 +266,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u;
       constexpr uint32_t idesc_s = (1u << 4) | kType | ((uint32_t)(kPagedTile >> 3) << 17) | ((uint32_t)(kM >> 4) << 24);
       constexpr uint32_t idesc_o = (1u << 4) | kType | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(kM >> 4) << 24);   // B (= V) is MN-major
-      const uint64_t dq0 = desc_kmajor(smem_u32(sq)), dk0 = desc_kmajor(smem_u32(ring)), dv0 = desc_mnmajor(smem_u32(ring), kHalf);
+      const uint64_t dq0 = desc_rows<kRow>(smem_u32(sq), 16), dk0 = desc_rows<kRow>(smem_u32(ring), 16), dv0 = desc_rows<kRow>(smem_u32(ring), kHalf);
       // One lane runs a piece's steps by itself, and every instruction counts: this warp comes by once in 900 clocks, when the softmax warps have filled the instruction cache with
       // their unrolled loops, so that its instructions are fetched anew each time.  (All lanes with votes, ring places worked out from the step, waits in
       // line: 900 clocks a step of its own, and the tensor cores waited for it.)
@@ -289,7 +294,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
 #pragma unroll
             for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-              for (int k = 0; k < 4; ++k) umma_bf16(acc, dq + h * (kHalf >> 4) + 2 * k, dk + h * (kHalf >> 4) + 2 * k, idesc_s, (h | k) ? 1u : 0u);
+              for (int k = 0; k < kRow / 32; ++k) umma_bf16(acc, dq + h * (kHalf >> 4) + 2 * k, dk + h * (kHalf >> 4) + 2 * k, idesc_s, (h | k) ? 1u : 0u);
             umma_commit(b_s + 8 * (s & 1));
             if (!both || (s & 1)) umma_commit(b_empty + 8 * (k_at % kNS));
             if (s == n - 1) umma_commit(b_qfree);
@@ -314,12 +319,12 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
             const uint64_t dv = dv0 + (v_at % kNS) * (kTB >> 4);
             const uint32_t acc = tmem + kOCol + slot * DH, w = tmem + kPCol<DH> + slot * kPStep<DH>;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) umma_ta(acc, w + k * 8, dv + k * (2048 >> 4), idesc_o, (s > 1 || k > 0) ? 1u : 0u);   // 16 keys per instruction
+            for (int k = 0; k < 4; ++k) umma_ta(acc, w + k * 8, dv + k * (16 * kRow >> 4), idesc_o, (s > 1 || k > 0) ? 1u : 0u);   // 16 keys per instruction
             if (!wait(b_p2 + 8 * slot, p_phase >> slot & 1)) { fine = false; break; }
             p_phase ^= 1u << slot;
             fence_after();
 #pragma unroll
-            for (int k = 4; k < 8; ++k) umma_ta(acc, w + k * 8, dv + k * (2048 >> 4), idesc_o, 1u);
+            for (int k = 4; k < 8; ++k) umma_ta(acc, w + k * 8, dv + k * (16 * kRow >> 4), idesc_o, 1u);
             if (!both || slot) umma_commit(b_empty + 8 * (v_at % kNS));
             umma_commit(b_o + 8 * slot);
             if (!kApart<DH> && s + 2 < n) scores(s + 2);
@@ -411,7 +416,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           ok = wait_warp(b_empty + 8 * st, ((e / kNS) & 1) ^ 1);
           if (!ok) break;
           if (is_k && tile_no++ == a.drop) continue;             // (test hook: these keys never arrive)
-          if (elect_one()) mbar_expect_tx(b_full + 8 * st, (uint32_t)((j1 - j0) * rows * 128 * kHalves));
+          if (elect_one()) mbar_expect_tx(b_full + 8 * st, (uint32_t)((j1 - j0) * rows * kRow * kHalves));
           __syncwarp();
           for (int j = j0; j < j1; ++j) {
             int page = (int)__shfl_sync(0xffffffffu, entry, page0 + j - first);
@@ -421,7 +426,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
             }
             const int slot = (key0 + j * rows) & (a.kv.page_size - 1);
             if (elect_one()) {
-              const uint32_t dst = smem_u32(ring) + st * kTB + j * rows * 128;
+              const uint32_t dst = smem_u32(ring) + st * kTB + j * rows * kRow;
 #pragma unroll
               for (int h = 0; h < kHalves; ++h) tma_load_4d(dst + h * kHalf, tm, b_full + 8 * st, 64 * h, slot, head, page);
             }
@@ -477,11 +482,11 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           // V rows that no row of the item sees become zeros (whatever lies there: its weight is 0, but 0 x inf is not)
           const uint32_t e = base + v_entry(both, s, n), st = e % kNS;
           if (wait(b_full + 8 * st, (e / kNS) & 1) && (key0 + row < p.lo || key0 + row >= p.hi)) {
-            uint8_t* vrow = ring + st * kTB + row * 128;
+            uint8_t* vrow = ring + st * kTB + row * kRow;
 #pragma unroll
             for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-              for (int c = 0; c < 8; ++c) *reinterpret_cast<uint4*>(vrow + h * kHalf + ((c + lane) & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+              for (int c = 0; c < kRow / 16; ++c) *reinterpret_cast<uint4*>(vrow + h * kHalf + ((c + lane) & (kRow / 16 - 1)) * 16) = make_uint4(0u, 0u, 0u, 0u);
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
@@ -595,7 +600,8 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         m = M;
       }
       const bool good = *s_abort == 0;
-      const int c_first = both ? 0 : slot * (DH / 2), c_last = both ? DH : c_first + DH / 2;
+      // (32 columns at a time; heads of 32 have no half for the second warpgroup)
+      const int c_first = both || DH == 32 ? 0 : slot * (DH / 2), c_last = both ? DH : DH == 32 ? (slot == 0 ? 32 : 0) : c_first + DH / 2;
       const long long part = ((long long)cta * 2 + (p.opens ? 1 : 0)) * kPagedMaxRows + (both ? slot * slot_rows : 0) + row;
       const int r = live ? a.by_group.of(mrow) : 0, head = p.head * G + (live ? mrow - r * G : 0);
       const long long out_row = (long long)(p.start + r) * a.n_heads + head;
@@ -702,9 +708,11 @@ __device__ __forceinline__ void load_part(const PagedAttnArgs& a, int dh, int c,
   if constexpr (kV == 4) {
     const float4 x = __ldcg(reinterpret_cast<const float4*>(src));
     v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
-  } else {
+  } else if constexpr (kV == 2) {
     const float2 x = __ldcg(reinterpret_cast<const float2*>(src));
     v[0] = x.x; v[1] = x.y;
+  } else {
+    v[0] = __ldcg(src);
   }
 }
 // a piece to a sum with its own reference point
@@ -768,11 +776,10 @@ k_paged_merge(PagedAttnArgs a, int n_cta) {
     const float inv = s.L == 0.f ? 0.f : 1.f / s.L;
     const int m = d.first_row + w.r, q = a.by_group.of(m);
     const long long row = (long long)(d.start + q) * a.n_heads + d.head * a.group + (m - q * a.group);
-    uint32_t x[kV / 2];
-#pragma unroll
-    for (int e = 0; e < kV / 2; ++e) x[e] = PagedType<T>::pack(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-    if constexpr (kV == 4) *reinterpret_cast<uint2*>(a.out + row * DH * 2 + lane * 8) = make_uint2(x[0], x[1]);
-    else *reinterpret_cast<uint32_t*>(a.out + row * DH * 2 + lane * 4) = x[0];
+    if constexpr (kV == 4)
+      *reinterpret_cast<uint2*>(a.out + row * DH * 2 + lane * 8) = make_uint2(PagedType<T>::pack(acc[0] * inv, acc[1] * inv), PagedType<T>::pack(acc[2] * inv, acc[3] * inv));
+    else if constexpr (kV == 2) *reinterpret_cast<uint32_t*>(a.out + row * DH * 2 + lane * 4) = PagedType<T>::pack(acc[0] * inv, acc[1] * inv);
+    else *reinterpret_cast<unsigned short*>(a.out + row * DH * 2 + lane * 2) = (unsigned short)PagedType<T>::pack(acc[0] * inv, 0.f);
     if (a.lse != nullptr && lane == 0) a.lse[row] = s.L == 0.f ? -INFINITY : (s.M + log2f(s.L)) * 0.6931471805599453f;
   };
 
@@ -862,7 +869,7 @@ cs_status encode(cs_paged_cache* c, CUtensorMap* tm, const void* base, int rank,
   const cuuint32_t ones[4] = {1, 1, 1, 1};
   const CUresult r = enc == nullptr ? CUDA_ERROR_NOT_FOUND
                                     : enc(tm, c->cfg.dtype == CS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, rank, const_cast<void*>(base), dims, strides, box,
-                                          ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, promote, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                                          ones, CU_TENSOR_MAP_INTERLEAVE_NONE, box[0] == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, promote, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r == CUDA_SUCCESS) return CS_OK;
   snprintf(c->err, sizeof(c->err), "cuTensorMapEncodeTiled (rank %d) failed with %d", rank, (int)r);
   return CS_ERR_CUDA;
@@ -885,9 +892,11 @@ cs_status cs_paged_tc_maps(cs_paged_cache* c) {
   const cs_paged_config& f = c->cfg;
   const cuuint64_t dims[4] = {(cuuint64_t)f.head_dim, (cuuint64_t)f.page_size, (cuuint64_t)f.n_kv_heads, (cuuint64_t)f.n_pages};
   const cuuint64_t strides[3] = {(cuuint64_t)f.slot_stride * 2, (cuuint64_t)f.head_stride * 2, (cuuint64_t)f.page_stride * 2};
-  const cuuint32_t box[4] = {64, (cuuint32_t)(f.page_size < kPagedTile ? f.page_size : kPagedTile), 1, 1};
+  const cuuint32_t box[4] = {f.head_dim == 32 ? 32u : 64u, (cuuint32_t)(f.page_size < kPagedTile ? f.page_size : kPagedTile), 1, 1};
   // (rows of 128 bytes between those of other heads: 256 bytes at a time would fetch those as well, FIG_PROMOTE)
-  const CUtensorMapL2promotion promote = f.head_dim == 64 && f.slot_stride != 64 ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B : CU_TENSOR_MAP_L2_PROMOTION_L2_256B;
+  const CUtensorMapL2promotion promote = f.slot_stride == f.head_dim || f.head_dim == 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B
+                                         : f.head_dim == 64                             ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B
+                                                                                        : CU_TENSOR_MAP_L2_PROMOTION_L2_64B;
   const cs_status s = encode(c, &c->tmK, f.k, 4, dims, strides, box, promote);
   return s != CS_OK ? s : encode(c, &c->tmV, f.v, 4, dims, strides, box, promote);
 }
@@ -904,11 +913,12 @@ cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& args, cudaS
   // (a stride that no second row or head uses may be anything)
   const cuuint64_t dims[3] = {(cuuint64_t)dh, (cuuint64_t)a.n_heads, (cuuint64_t)a.blk.rows};
   const cuuint64_t strides[2] = {(cuuint64_t)(a.n_heads > 1 ? a.q_head : dh) * 2, (cuuint64_t)(a.blk.rows > 1 ? a.q_row : (long long)dh * a.n_heads) * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)a.group, (cuuint32_t)box_rows};
+  const cuuint32_t box[3] = {dh == 32 ? 32u : 64u, (cuuint32_t)a.group, (cuuint32_t)box_rows};
   const cs_status s = encode(c, &tmQ, a.q, 3, dims, strides, box, CU_TENSOR_MAP_L2_PROMOTION_L2_128B);
   if (s != CS_OK) return s;
-  const int bytes = 128 * a.group * box_rows;
+  const int bytes = (dh == 32 ? 64 : 128) * a.group * box_rows;
   const bool bf = c->cfg.dtype == CS_BF16;
+  if (dh == 32) return bf ? launch_tc<__nv_bfloat16, 32>(c, a, tmQ, bytes, 1024, st) : launch_tc<__half, 32>(c, a, tmQ, bytes, 2048, st);
   if (dh == 64) return bf ? launch_tc<__nv_bfloat16, 64>(c, a, tmQ, bytes, 64, st) : launch_tc<__half, 64>(c, a, tmQ, bytes, 128, st);
   return bf ? launch_tc<__nv_bfloat16, 128>(c, a, tmQ, bytes, 256, st) : launch_tc<__half, 128>(c, a, tmQ, bytes, 512, st);
 }
