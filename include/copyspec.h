@@ -546,7 +546,7 @@ cs_status cs_paged_append(cs_paged_cache* cache, const cs_blocks* blocks, const 
  *   out[row][h] = softmax_j(scale * q[row][h] . K_j) V_j,  lse[row][h] = log sum_j exp(scale * q[row][h] . K_j)
  * over the keys the mask leaves, query head h with KV head h / (n_heads / n_kv_heads).  Blocks of any height, one token
  * or a prompt's chunk, side by side.  q and out [rows][n_heads][head_dim] in the cache's type, q by strides (elements,
- * multiples of 8; base 16-byte aligned), out contiguous and 16-byte aligned; lse fp32 [rows][n_heads] or NULL.  A row that no key is left for, or whose
+ * multiples of 8; base 16-byte aligned), out contiguous, 16-byte aligned and apart from q; lse fp32 [rows][n_heads] or NULL.  A row that no key is left for, or whose
  * scores are all -inf, gets zeros and lse -inf.  Keys and values outside the range that a row of its block attends to are
  * never looked at, whatever they hold; non-finite values at positions that a row does not attend to do not reach it.
  * n_heads a multiple of n_kv_heads, at most 128 per KV head.  scale > 0; window >= 0.  Async.

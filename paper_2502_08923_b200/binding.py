@@ -668,15 +668,16 @@ class PagedCache:
     def __init__(self, k_pages, v_pages, workspace=None):
         if not k_pages.is_cuda or k_pages.dim() != 4 or k_pages.dtype not in (torch.bfloat16, torch.float16):
             raise ValueError("k_pages must be a CUDA tensor [n_pages][heads][page_size][head_dim] of bf16 or fp16")
-        if v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype or v_pages.device != k_pages.device or v_pages.stride() != k_pages.stride():
+        n, h, s, d = k_pages.shape
+        # (a stride that no second page or head uses may be anything)
+        st, sv = ((t.stride(0) if n > 1 else h * s * d, t.stride(1) if h > 1 else s * d, t.stride(2), t.stride(3)) for t in (k_pages, v_pages))
+        if v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype or v_pages.device != k_pages.device or sv != st:
             raise ValueError("v_pages must have k_pages' shape, strides, type and device")
-        if k_pages.stride(3) != 1:
+        if st[3] != 1:
             raise ValueError("heads must be contiguous")
         self.lib = load()
         self.k_pages, self.v_pages = k_pages, v_pages
         self.dtype, self.scale = k_pages.dtype, k_pages.shape[3] ** -0.5
-        n, h, s, d = k_pages.shape
-        st = k_pages.stride()
         self.c_cfg = CsPagedConfig(k_pages.data_ptr(), v_pages.data_ptr(), st[0], st[1], st[2], n, s, h, d, _DTYPE[self.dtype])
         with torch.cuda.device(k_pages.device):
             if workspace is None:

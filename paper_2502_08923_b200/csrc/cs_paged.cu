@@ -460,7 +460,7 @@ cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void
   const long long us = wl != nullptr ? atoll(wl) : 0;
   c->wait_limit_ns = us > 0 ? (unsigned long long)us * 1000ull : 2000000000ull;
   if (cs_paged_tc_maps(c) != CS_OK) {
-    snprintf(t_paged_err, sizeof(t_paged_err), "cs_paged_create: %s", c->err);
+    snprintf(t_paged_err, sizeof(t_paged_err), "cs_paged_create: %.200s", c->err);
     free(c);
     return CS_ERR_CUDA;
   }
@@ -560,8 +560,9 @@ cs_status cs_paged_attention(cs_paged_cache* c, const cs_blocks* blocks, const v
   a.parts = c->parts; a.parts_ml = c->parts_ml; a.counters = c->counters; a.splits = c->splits; a.status = c->status;
   a.wait_ns = c->wait_limit_ns;
   a.drop = -1;
-  // 16 query rows per KV head are a tile of the kernel for few rows
-  const bool few = (long long)blocks->rows * a.group <= 16ll * blocks->n_seqs;
+  // 16 query rows per KV head are a tile of the kernel for few rows (on tensor cores / by it, us: 11 rows of the 8B shape over 1,024 keys 15.0 / 13.0, over 4,096 16.2 / 18.3, over
+  // 16,384 26.4 / 40.4; 16 x 5 over 1,024 28.8 / 36.2); queries that repeat one row have no operand map
+  const bool few = (long long)blocks->rows * a.group <= 16ll * blocks->n_seqs || (blocks->rows > 1 && q_row_stride <= 0) || (n_heads > 1 && q_head_stride <= 0);
   if (!few) {
     a.drop = c->drop;
     c->drop = -1;

@@ -98,6 +98,19 @@ def test_rows_of_projections():
     assert torch.equal(only[:3], out[:3])
 
 
+@pytest.mark.parametrize("lens", [[1], [3], [90]])
+def test_one_page_one_head_one_row_repeated(lens):
+    """Strides that nothing uses may be anything, and queries may be one row for all."""
+    case = Case(lens, [100], 4, 1, 64, page=256, seed=7, spare=0)
+    assert case.kp.shape[:2] == (1, 1)
+    strange = [torch.as_strided(p, p.shape, (3, 5, p.stride(2), 1)) for p in (case.kp, case.vp)]
+    run(case, cs.PagedCache(*strange))
+    case.q = case.q[:1].expand(case.rows, 4, 64)
+    run(case, cs.PagedCache(*strange))
+    case.q = case.q[:, :1].expand(case.rows, 4, 64)
+    run(case, cs.PagedCache(*strange))
+
+
 @pytest.mark.parametrize("D", [32, 64, 128])
 @pytest.mark.parametrize("lens", [[11], [150]])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])

@@ -9,7 +9,7 @@ from paged_helpers import Case, check_attention
 pytestmark = pytest.mark.gpu
 
 
-@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("D", [32, 64, 128])
 @pytest.mark.parametrize("lens,cached,tile", [([40], [300], 0), ([40], [1500], 2), ([300, 1, 70], [900, 40, 500], 1), ([200], [2000], 5)])
 def test_gives_up_and_recovers(D, lens, cached, tile, monkeypatch):
     monkeypatch.setenv("CS_WAIT_LIMIT_US", "2000")
