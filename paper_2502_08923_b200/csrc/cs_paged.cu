@@ -2,12 +2,13 @@
 //
 // For a row at position p and a head x of D elements, h = rot_dim / 2, c_i = cos(p w_i), s_i = sin(p w_i) from a table:
 //     u = x rsqrt(mean(x^2) + eps) gain,   y_i = u_i c_i - u_{i+h} s_i,   y_{i+h} = u_{i+h} c_i + u_i s_i   (i < h).
-// A lane holds eight neighbouring elements (16 bytes of the 16-bit types), a head is D / 8 lanes.  An element's partner is h away, so it lies in the
-// same place of another lane of the head: one exchange of the raw words.  With A = gain_i c_i and B = -/+ gain_{partner} s_i the rest is
-// y = r (x A + partner B), r the head's reciprocal norm (a reduction over its lanes).
+// A lane holds eight elements of a head's first half and their eight partners (16 bytes each of the 16-bit types; behind rot_dim two neighbouring chunks), a head is D / 16 lanes.  With C = gain cos and
+// S = gain sin, worked out once per row for the queries and once for the keys, an element is r (x0 C - x1 S), r the head's reciprocal norm (a
+// reduction over its lanes), and nothing is exchanged.  Warps take a row each, or 2, 4 or 8 share one where there are few; four units of 32 / (D / 16) heads are in flight.
 //
-// One CTA per row, all of its heads (queries, keys, values) in one go with the loads of up to four heads per lane in flight: bound by HBM
-// where there are many rows, by launch and two dependent loads (whose block is the row's, which page) where there are few.
+// Bound by HBM where there are many rows: 8,192 of the 8B shape 34.4 us (172 MB, 5.0 TB/s of the 6.5 that a copy reaches), an append of 6k rows 32.8 us (150 MB, 4.6).  With an
+// element's partner in another lane, fetched by shuffles, and the factors worked out for each head 61 us, with twice as many warps a row 40.  Few rows: launch and a chain of
+// loads (whose block is the row's, which page, its rotation): 2.4 - 4.3 us.
 #include "cs_paged.cuh"
 
 namespace {
@@ -297,6 +298,8 @@ template <typename S, typename D, bool kPaged>
 cudaError_t launch_heads(HeadsArgs a, int rows, int head_dim, cudaStream_t st) {
   const int per = 512 / head_dim, units = cs_ceil_div(a.n_q, per) + cs_ceil_div(a.n_k, per) + cs_ceil_div(a.n_v, per);
   a.n_rows = rows;
+  // as many warps a row as it takes to give every SM of 148 some 64, each with a unit at least (8,192 rows of the 8B shape with one / two / four: 36.6 / 40.4 / 56.0 us, what is worked out per
+  // row is worked out by each; 11 rows with one take three times as long as with eight)
   a.warps_per_row = 8;
   while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)rows * a.warps_per_row > 148 * 64)) a.warps_per_row /= 2;
   const dim3 grid((unsigned)(((long long)rows * a.warps_per_row + kWarps - 1) / kWarps));

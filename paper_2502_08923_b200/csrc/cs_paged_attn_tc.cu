@@ -9,8 +9,8 @@
 // different rows over the same tiles (each K and V tile is fetched once for 256 rows); of fewer, the slots take the tiles
 // in turn and are added up at the end, from tensor memory.
 //
-// Steps s = 0, 1, ... alternate between the slots.  The MMA warp issues S(0) S(1), then P V(s) and S(s + 2) for every s: S(s + 2) overwrites P(s), which the products'
-// order keeps.  A slot's scores being there means that its product before is done, so a softmax that moves its reference point may
+// Steps s = 0, 1, ... alternate between the slots.  With heads of 128 the MMA warp issues S(0) S(1), then P V(s) and S(s + 2) for every s: S(s + 2) overwrites P(s), which the
+// products' order keeps.  (Smaller heads leave room for weights beside the scores: S(s + 2) goes ahead of P V(s), see kApart; 1,184 rows over 8,192 keys 158 -> 148 us.)  A slot's scores being there means that its product before is done, so a softmax that moves its reference point may
 // rescale O at once.  The reference point moves only past 2^8 (softmax does not depend on it, and weights up to 2^8 are as exact as weights up
 // to 1), which leaves rescaling to a few tiles.  Weights are rounded once, to the cache's type, on their way into the second product; their sum is
 // taken before.
@@ -22,6 +22,14 @@
 // (mend_row).  (Tiles of such keys were looked through ahead of the product at first, which made them three times as long as others.)
 //
 // Every wait is bounded: on expiry the CTA flags CS_DEV_TIMEOUT, stops issuing, walks through its barriers, drains what is in flight, frees its TMEM and returns.
+//
+// What bounds it.  Long chunks: 3,350 clocks for a pair of 128 x 128 tiles with heads of 128, of which the products take 2,048 at their peak rate; a slot's chain is scores into registers
+// 190, maxima 300, weights 1,200 (ex2, 16 a clock, is 1,024 of it), into tensor memory 200, product 512, next scores 512, hand-overs 400.  A 2,048-row chunk behind 30,720
+// keys of the 8B shape: 0.94 ms in short runs (1.13 PFLOP/s), 1.09 ms at the power cap (1.49 GHz, 990 W).  Few rows over long caches: HBM, 4.1 TB/s of 6.5 (8 x 21
+// rows of heads of 64 over 16,384 keys 66 us), less what a run begins and ends with; 11 rows over 4,096 keys 16 us, a chain of latencies (plan and piece 1.5, page entries,
+// first tiles 3, one step 1.8, results 1.4, sums of pieces 5).
+// Tried and not kept: maxima left out, with reference points that follow the sums (3,350 -> 3,400 clocks: they hide behind ex2); a quarter of the exponentials by a polynomial in
+// packed arithmetic (-2 % of the clocks, +1 % of the time at the power cap); products with the first 64 keys only when all weights are there (no slower by themselves).
 #include <type_traits>
 
 #include "cs_paged.cuh"
@@ -690,7 +698,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
 
 // Items that several CTAs share: their pieces added up, in the order of the keys, by a launch of its own.  (The last CTA to arrive did this inside the kernel at first: 430 KB through
 // one SM, 5 us with its loads in flight together and 14 without.)  Bound by latencies: a list, a search, the pieces.  All rows are dealt out over all warps, two at a
-// time for each (one at a time 148 items of 256 rows took 11 us for FIG_MERGE now); where there are few rows a CTA has one at a time, its warps an eighth of the pieces each.
+// time for each (a 2,048-row prompt of the 8B shape, whose 148 CTAs share nearly every item: 69.7 us with one row at a time, 64.3 with two); where there are few rows a CTA has one at a time, its warps an eighth of the pieces each.
 constexpr int kMergeWarps = 8, kMergeCtas = 3;    // CTAs per SM
 
 // where output row `g` of the line of all split rows is kept, and by whom
@@ -893,7 +901,7 @@ cs_status cs_paged_tc_maps(cs_paged_cache* c) {
   const cuuint64_t dims[4] = {(cuuint64_t)f.head_dim, (cuuint64_t)f.page_size, (cuuint64_t)f.n_kv_heads, (cuuint64_t)f.n_pages};
   const cuuint64_t strides[3] = {(cuuint64_t)f.slot_stride * 2, (cuuint64_t)f.head_stride * 2, (cuuint64_t)f.page_stride * 2};
   const cuuint32_t box[4] = {f.head_dim == 32 ? 32u : 64u, (cuuint32_t)(f.page_size < kPagedTile ? f.page_size : kPagedTile), 1, 1};
-  // (rows of 128 bytes between those of other heads: 256 bytes at a time would fetch those as well, FIG_PROMOTE)
+  // (rows of 128 bytes between those of other heads: 256 bytes at a time would fetch those as well: 8 x 21 rows over 16,384 keys, heads of 64, 78 / 67 us)
   const CUtensorMapL2promotion promote = f.slot_stride == f.head_dim || f.head_dim == 128 ? CU_TENSOR_MAP_L2_PROMOTION_L2_256B
                                          : f.head_dim == 64                             ? CU_TENSOR_MAP_L2_PROMOTION_L2_128B
                                                                                         : CU_TENSOR_MAP_L2_PROMOTION_L2_64B;
@@ -906,8 +914,8 @@ cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& args, cudaS
   const int tokens = kM / a.group;                 // rows of the block in a slot, with all heads of the group
   a.item_rows = 2 * tokens * a.group;
   a.by_item_rows = PagedDivisor::by(a.item_rows);
-  a.item_cost = 2;
-  a.keep = 5;
+  a.item_cost = 2;                                 // (one: the three windowed chunks 111 us instead of 109)
+  a.keep = 5;                                      // (a step takes 0.9 us, adding pieces up 5)
   const int box_rows = tokens < a.blk.rows ? tokens : a.blk.rows, dh = c->cfg.head_dim;
   CUtensorMap tmQ;
   // (a stride that no second row or head uses may be anything)

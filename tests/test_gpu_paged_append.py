@@ -208,6 +208,24 @@ def test_on_another_stream():
     check_attention(case, out, lse, *case.attention())
 
 
+def test_without_the_native_side(monkeypatch):
+    """The calls' general path, which stands in where the native module does not load, gives the same bits."""
+    case = Case([4, 60], [30, 130], 8, 2, 64, seed=16)
+    qkv = torch.randn(case.rows, 12, 64, device="cuda").to(BF)
+    rope, pos, (qg, kg) = cs.cs_rope_table(200, 64), torch.arange(case.rows, device="cuda", dtype=torch.int32), gains(64, BF)
+    got = []
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(cs, "_native", None)
+        cache = cs.PagedCache(case.kp, case.vp)
+        q = cache.cs_paged_append(qkv[:, 8:10], qkv[:, 10:], *case.blocks(), rope, kg, q=qkv[:, :8], q_gain=qg)
+        out, lse = cache.cs_paged_attention(q, *case.blocks(), with_lse=True)
+        got.append([q, out, lse, case.kp.clone(), *cs.cs_qk_norm_rope(qkv[:, :8], qkv[:, 8:10], pos, rope, qg, kg), cs.cs_qk_norm_rope(None, qkv[:, 8:10].float(), pos, rope, None, kg, dtype=BF)[1]])
+        assert cache.cs_paged_append(qkv[:, 8:10], qkv[:, 10:], *case.blocks()) is None and cache.cs_paged_status() == cs.CS_OK
+    for a, b in zip(*got):
+        assert torch.equal(a.view(torch.int16) if a.dtype is BF else a, b.view(torch.int16) if b.dtype is BF else b)
+
+
 def test_refusals():
     case = Case([2], [20], 4, 2, 64, seed=1)
     cache = cs.PagedCache(case.kp, case.vp)
