@@ -222,16 +222,26 @@ k_heads(HeadsArgs a) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) g0[j] = g1[j] = 1.f;
           }
-          const float4* r = reinterpret_cast<const float4*>(a.rope + (long long)pos * a.rot_dim + c0 * 8);
-          const bool in_table = (unsigned)pos < (unsigned)a.n_positions;
+          if (!rotated) {
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const float4 one = make_float4(1.f, 1.f, 1.f, 1.f), none = make_float4(nan_f(), nan_f(), nan_f(), nan_f());
-            const float4 x = !rotated ? one : in_table ? r[j] : none, y = !rotated ? one : in_table ? r[2 * half + j] : none;
-            C0[2 * j] = pack2(g0[4 * j] * x.x, g0[4 * j + 1] * x.y); C0[2 * j + 1] = pack2(g0[4 * j + 2] * x.z, g0[4 * j + 3] * x.w);
-            C1[2 * j] = pack2(g1[4 * j] * x.x, g1[4 * j + 1] * x.y); C1[2 * j + 1] = pack2(g1[4 * j + 2] * x.z, g1[4 * j + 3] * x.w);
-            S0[2 * j] = pack2(g0[4 * j] * y.x, g0[4 * j + 1] * y.y); S0[2 * j + 1] = pack2(g0[4 * j + 2] * y.z, g0[4 * j + 3] * y.w);
-            S1[2 * j] = pack2(-g1[4 * j] * y.x, -g1[4 * j + 1] * y.y); S1[2 * j + 1] = pack2(-g1[4 * j + 2] * y.z, -g1[4 * j + 3] * y.w);
+            for (int j = 0; j < 4; ++j) { C0[j] = pack2(g0[2 * j], g0[2 * j + 1]); C1[j] = pack2(g1[2 * j], g1[2 * j + 1]); }
+          } else {
+            float4 cs[2], sn[2];
+            if ((unsigned)pos < (unsigned)a.n_positions) {
+              const float4* r = reinterpret_cast<const float4*>(a.rope + (long long)pos * a.rot_dim + c0 * 8);
+              cs[0] = r[0]; cs[1] = r[1]; sn[0] = r[2 * half]; sn[1] = r[2 * half + 1];
+            } else {
+              cs[0] = cs[1] = sn[0] = sn[1] = make_float4(nan_f(), nan_f(), nan_f(), nan_f());
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              const f32x2 x = pack2(cs[j].x, cs[j].y), y = pack2(cs[j].z, cs[j].w), sx = pack2(sn[j].x, sn[j].y), sy = pack2(sn[j].z, sn[j].w);
+              const f32x2 ga = pack2(g0[4 * j], g0[4 * j + 1]), gb = pack2(g0[4 * j + 2], g0[4 * j + 3]), ha = pack2(g1[4 * j], g1[4 * j + 1]), hb = pack2(g1[4 * j + 2], g1[4 * j + 3]);
+              C0[2 * j] = mul2(ga, x); C0[2 * j + 1] = mul2(gb, y);
+              C1[2 * j] = mul2(ha, x); C1[2 * j + 1] = mul2(hb, y);
+              S0[2 * j] = mul2(ga, sx); S0[2 * j + 1] = mul2(gb, sy);
+              S1[2 * j] = mul2(pack2(-g1[4 * j], -g1[4 * j + 1]), sx); S1[2 * j + 1] = mul2(pack2(-g1[4 * j + 2], -g1[4 * j + 3]), sy);
+            }
           }
         }
       }
