@@ -4,11 +4,12 @@
 //     u = x rsqrt(mean(x^2) + eps) gain,   y_i = u_i c_i - u_{i+h} s_i,   y_{i+h} = u_{i+h} c_i + u_i s_i   (i < h).
 // A lane holds eight elements of a head's first half and their eight partners (16 bytes each of the 16-bit types; behind rot_dim two neighbouring chunks), a head is D / 16 lanes.  With C = gain cos and
 // S = gain sin, worked out once per row for the queries and once for the keys, an element is r (x0 C - x1 S), r the head's reciprocal norm (a
-// reduction over its lanes), and nothing is exchanged.  Warps take a row each, or 2, 4 or 8 share one where there are few; four units of 32 / (D / 16) heads are in flight.
+// reduction over its lanes), and nothing is exchanged.  Warps take a row each, or 2, 4 or 8 share one where there are few; three units of 32 / (D / 16) heads are in flight, in
+// a ring of shared memory for each warp (in registers instead, four of them, 16 warps fit on an SM and not 20, and the setup is there four times: 34 us for the 30 below).
 //
-// Bound by HBM where there are many rows: 8,192 of the 8B shape 34.4 us (172 MB, 5.0 TB/s of the 6.5 that a copy reaches), an append of 6k rows 32.8 us (150 MB, 4.6).  With an
-// element's partner in another lane, fetched by shuffles, and the factors worked out for each head 61 us, with twice as many warps a row 40.  Few rows: launch and a chain of
-// loads (whose block is the row's, which page, its rotation): 2.4 - 4.3 us.
+// Bound by HBM where there are many rows: 8,192 of the 8B shape 30.0 us (172 MB, 5.7 TB/s of the 6.5 that a copy reaches), an append of 6k rows 30.4 us (150 MB, 4.9).  With an
+// element's partner in another lane, fetched by shuffles, and the factors worked out for each head 61 us.  Few rows: launch and a chain of loads (whose block is the row's, which
+// page and, at the same time, its rotation): 2.4 - 4.5 us.
 #include "cs_paged.cuh"
 
 namespace {
@@ -51,14 +52,10 @@ __device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
   return d;
 }
 
-template <typename T> __device__ __forceinline__ void load8(const char* p, uint32_t (&w)[sizeof(T) == 4 ? 8 : 4]) {
-  const uint4 a = __ldcg(reinterpret_cast<const uint4*>(p));
-  w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-  if constexpr (sizeof(T) == 4) {
-    const uint4 b = __ldcg(reinterpret_cast<const uint4*>(p) + 1);
-    w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-  }
+__device__ __forceinline__ void fetch16(uint32_t dst, const char* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void fetch_drain() { asm volatile("cp.async.wait_all;" ::: "memory"); }   // before a warp leaves
 template <typename T, int N> __device__ __forceinline__ void widen(const uint32_t (&w)[N], f32x2 (&f)[4]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -104,14 +101,16 @@ template <typename T> __device__ __forceinline__ void gain8(const char* g, int c
 }
 
 template <typename S, typename D, int DH, bool kPaged>
-__global__ void __launch_bounds__(kThreads, 2)
+__global__ void __maxnreg__(96)
 k_heads(HeadsArgs a) {
   CS_PDL_PROLOGUE();
   constexpr int kLanes = DH / 16, kPer = 32 / kLanes, kW = sizeof(S) == 4 ? 8 : 4;    // lanes of a head, heads of a unit, words of a chunk
-  constexpr int kFlight = sizeof(S) == 4 ? 2 : 4;
+  constexpr int kSlots = sizeof(S) == 4 ? 2 : 4, kPieces = kW / 2;                    // slots of a warp's ring; 16-byte pieces of a lane's two chunks
+  __shared__ uint4 s_ring[kWarps][kSlots][kPieces][32];
   __shared__ int s_seq[kWarps], s_pos[kWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = lane % kLanes, sub = lane / kLanes;
-  const long long row0 = (long long)blockIdx.x * (kWarps / a.warps_per_row), row = row0 + warp / a.warps_per_row;
+  const int n_here = (int)(blockDim.x >> 5) / a.warps_per_row;
+  const long long row0 = (long long)blockIdx.x * n_here, row = row0 + warp / a.warps_per_row;
   // a row's units: up to kPer neighbouring heads, of queries, then keys, then values
   const int uq = (a.n_q + kPer - 1) / kPer, uk = uq + (a.n_k + kPer - 1) / kPer, units = row < a.n_rows ? uk + (a.n_v + kPer - 1) / kPer : 0;
   const int step = a.warps_per_row, u0 = warp % step;
@@ -120,12 +119,12 @@ k_heads(HeadsArgs a) {
   const bool rotated = pair < half;
   const int c0 = rotated ? pair : 2 * pair, c1 = rotated ? pair + half : c0 + 1;
 
-  // Fetching runs kFlight units ahead of the rest.
-  uint32_t w[kFlight][2][kW];
+  // Fetching runs kSlots - 1 units ahead of the rest.  A lane reads from the ring only what it fetched itself.
   int fu = u0, f_end = 0, f_h = 0, f_n = 0;      // next unit, where its kind's units end, this lane's head of it, the kind's heads
-  const char* f_p = nullptr;
+  const char* f_p = a.q;
   long long f_step = 0;
-  auto fetch = [&](uint32_t (&d)[2][kW]) {
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(&s_ring[warp][0][0][lane]);
+  auto fetch = [&](int slot) {
     if (fu >= f_end && fu < units) {             // (the same in the whole warp)
       const int kind = fu < uq ? 0 : fu < uk ? 1 : 2;
       const long long rs = kind == 0 ? a.q_row : kind == 1 ? a.k_row : a.v_row, hs = kind == 0 ? a.q_head : kind == 1 ? a.k_head : a.v_head;
@@ -136,26 +135,24 @@ k_heads(HeadsArgs a) {
       f_step = step * kPer * hs * (long long)sizeof(S);
     }
     if (fu < units && f_h < f_n) {
-      load8<S>(f_p, d[0]);
-      load8<S>(f_p + (c1 - c0) * 8 * (int)sizeof(S), d[1]);
-    } else {
+      const uint32_t d = ring + slot * (kPieces * 512);
+      const char* p1 = f_p + (c1 - c0) * 8 * (int)sizeof(S);
 #pragma unroll
-      for (int j = 0; j < kW; ++j) d[0][j] = d[1][j] = 0u;
+      for (int j = 0; j < kPieces / 2; ++j) { fetch16(d + j * 512, f_p + j * 16); fetch16(d + (kPieces / 2 + j) * 512, p1 + j * 16); }
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
     fu += step; f_h += step * kPer; f_p += f_step;
   };
 #pragma unroll
-  for (int i = 0; i < kFlight; ++i) fetch(w[i]);   // (whose row it is, and where it goes, takes three loads in a row: these are under way meanwhile)
+  for (int i = 0; i < kSlots - 1; ++i) fetch(i); // (whose row it is, and where it goes, takes three loads in a row: these are under way meanwhile)
 
   int pos = 0;
-  long long at = 0;                              // element of the pools where this row's slot of head 0 begins
-  bool stored = true;
+  int page = 0;                                  // (not looked at before the first factors have been asked for)
   if constexpr (kPaged) {
     // the blocks these rows belong to
     if (threadIdx.x < kWarps) s_seq[threadIdx.x] = -1;
     __syncthreads();
-    const int n_here = kWarps / a.warps_per_row;
-    for (int b = threadIdx.x; b < a.blk.n_seqs; b += kThreads) {
+    for (int b = threadIdx.x; b < a.blk.n_seqs; b += (int)blockDim.x) {
       const int start = __ldcg(a.blk.start + b), len = __ldcg(a.blk.len + b), kv = __ldcg(a.blk.kv_len + b);
       const int flag = paged_block_flag(a.blk, a.kv.page_size, true, start, len, kv);
       if (flag != 0) {
@@ -167,16 +164,17 @@ k_heads(HeadsArgs a) {
     }
     __syncthreads();
     const int b = s_seq[warp / a.warps_per_row];
-    if (b < 0 || row >= a.n_rows) return;
+    if (b < 0 || row >= a.n_rows) {
+      fetch_drain();
+      return;
+    }
     pos = s_pos[warp / a.warps_per_row];
     if (a.rot_dim > 0 && pos >= a.n_positions) {
       if (lane == 0) atomicOr(a.status, CS_DEV_CAPACITY);
+      fetch_drain();
       return;
     }
-    const int page = __ldcg(a.blk.table + (long long)b * a.blk.table_width + (pos >> a.kv.page_shift));
-    stored = (unsigned)page < (unsigned)a.kv.n_pages;
-    if (stored) at = page * a.kv.page_stride + (long long)(pos & (a.kv.page_size - 1)) * a.kv.slot_stride;
-    else if (lane == 0) atomicOr(a.status, CS_DEV_BADARG);
+    page = __ldcg(a.blk.table + (long long)b * a.blk.table_width + (pos >> a.kv.page_shift));
   } else {
     if (row >= a.n_rows) return;
     if (a.rot_dim > 0) pos = __ldcg(a.pos + row);
@@ -185,70 +183,76 @@ k_heads(HeadsArgs a) {
   // y0 = r (x0 C0 - x1 S1), y1 = r (x1 C1 + x0 S0), C = gain cos, S = gain sin: worked out once for the queries and once for the keys.  (Table
   // and gains are read through L1: all warps of a row want the same.)
   f32x2 C0[4], C1[4], S0[4], S1[4];
-  int end = 0, h = 0, n = 0;
-  bool norm = false, plain = false;              // (values are neither normed nor rotated)
-  char* dst = nullptr;
-  long long dst_step = 0;
-  for (int ub = u0; ub < units; ub += kFlight * step) {
+  int slot = 0;
+  for (int u = u0; u < units;) {
+    const int kind = u < uq ? 0 : u < uk ? 1 : 2;
+    const int n = kind == 0 ? a.n_q : kind == 1 ? a.n_k : a.n_v, end = kind == 0 ? uq : kind == 1 ? uk : units;
+    const bool plain = kind == 2;                // (values are neither normed nor rotated)
+    const char* gain = kind == 0 ? a.q_gain : kind == 1 ? a.k_gain : nullptr;
+    const bool norm = gain != nullptr;
+    if (!plain) {
+      float g0[8], g1[8];
+      if (norm) {
+        gain8<D>(gain, c0, g0);
+        gain8<D>(gain, c1, g1);
+      } else {
 #pragma unroll
-    for (int i = 0; i < kFlight; ++i) {
-      const int u = ub + i * step;
-      if (u >= units) break;                     // (the same in the whole warp)
-      if (u >= end) {
-        const int kind = u < uq ? 0 : u < uk ? 1 : 2;
-        h = (u - (kind == 0 ? 0 : kind == 1 ? uq : uk)) * kPer + sub;
-        n = kind == 0 ? a.n_q : kind == 1 ? a.n_k : a.n_v;
-        end = kind == 0 ? uq : kind == 1 ? uk : units;
-        plain = kind == 2;
-        if (kind == 0) {
-          dst = a.yq + (row * a.yq_row + h * a.yq_head + c0 * 8) * (long long)sizeof(D);
-          dst_step = step * kPer * a.yq_head * (long long)sizeof(D);
-        } else if constexpr (kPaged) {
-          dst = (kind == 1 ? a.kv.k : a.kv.v) + (at + h * a.kv.head_stride + c0 * 8) * (long long)sizeof(D);
-          dst_step = step * kPer * a.kv.head_stride * (long long)sizeof(D);
-          if (!stored) n = 0;
+        for (int j = 0; j < 8; ++j) g0[j] = g1[j] = 1.f;
+      }
+      if (!rotated) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { C0[j] = pack2(g0[2 * j], g0[2 * j + 1]); C1[j] = pack2(g1[2 * j], g1[2 * j + 1]); }
+      } else {
+        float4 cs[2], sn[2];
+        if ((unsigned)pos < (unsigned)a.n_positions) {
+          const float4* r = reinterpret_cast<const float4*>(a.rope + (long long)pos * a.rot_dim + c0 * 8);
+          cs[0] = r[0]; cs[1] = r[1]; sn[0] = r[2 * half]; sn[1] = r[2 * half + 1];
         } else {
-          dst = a.yk + (row * a.yk_row + h * a.yk_head + c0 * 8) * (long long)sizeof(D);
-          dst_step = step * kPer * a.yk_head * (long long)sizeof(D);
+          cs[0] = cs[1] = sn[0] = sn[1] = make_float4(nan_f(), nan_f(), nan_f(), nan_f());
         }
-        const char* gain = kind == 0 ? a.q_gain : kind == 1 ? a.k_gain : nullptr;
-        norm = gain != nullptr;
-        if (!plain) {
-          float g0[8], g1[8];
-          if (norm) {
-            gain8<D>(gain, c0, g0);
-            gain8<D>(gain, c1, g1);
-          } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) g0[j] = g1[j] = 1.f;
-          }
-          if (!rotated) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) { C0[j] = pack2(g0[2 * j], g0[2 * j + 1]); C1[j] = pack2(g1[2 * j], g1[2 * j + 1]); }
-          } else {
-            float4 cs[2], sn[2];
-            if ((unsigned)pos < (unsigned)a.n_positions) {
-              const float4* r = reinterpret_cast<const float4*>(a.rope + (long long)pos * a.rot_dim + c0 * 8);
-              cs[0] = r[0]; cs[1] = r[1]; sn[0] = r[2 * half]; sn[1] = r[2 * half + 1];
-            } else {
-              cs[0] = cs[1] = sn[0] = sn[1] = make_float4(nan_f(), nan_f(), nan_f(), nan_f());
-            }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-              const f32x2 x = pack2(cs[j].x, cs[j].y), y = pack2(cs[j].z, cs[j].w), sx = pack2(sn[j].x, sn[j].y), sy = pack2(sn[j].z, sn[j].w);
-              const f32x2 ga = pack2(g0[4 * j], g0[4 * j + 1]), gb = pack2(g0[4 * j + 2], g0[4 * j + 3]), ha = pack2(g1[4 * j], g1[4 * j + 1]), hb = pack2(g1[4 * j + 2], g1[4 * j + 3]);
-              C0[2 * j] = mul2(ga, x); C0[2 * j + 1] = mul2(gb, y);
-              C1[2 * j] = mul2(ha, x); C1[2 * j + 1] = mul2(hb, y);
-              S0[2 * j] = mul2(ga, sx); S0[2 * j + 1] = mul2(gb, sy);
-              S1[2 * j] = mul2(pack2(-g1[4 * j], -g1[4 * j + 1]), sx); S1[2 * j + 1] = mul2(pack2(-g1[4 * j + 2], -g1[4 * j + 3]), sy);
-            }
-          }
+        for (int j = 0; j < 2; ++j) {
+          const f32x2 x = pack2(cs[j].x, cs[j].y), y = pack2(cs[j].z, cs[j].w), sx = pack2(sn[j].x, sn[j].y), sy = pack2(sn[j].z, sn[j].w);
+          const f32x2 ga = pack2(g0[4 * j], g0[4 * j + 1]), gb = pack2(g0[4 * j + 2], g0[4 * j + 3]), ha = pack2(g1[4 * j], g1[4 * j + 1]), hb = pack2(g1[4 * j + 2], g1[4 * j + 3]);
+          C0[2 * j] = mul2(ga, x); C0[2 * j + 1] = mul2(gb, y);
+          C1[2 * j] = mul2(ha, x); C1[2 * j + 1] = mul2(hb, y);
+          S0[2 * j] = mul2(ga, sx); S0[2 * j + 1] = mul2(gb, sy);
+          S1[2 * j] = mul2(pack2(-g1[4 * j], -g1[4 * j + 1]), sx); S1[2 * j + 1] = mul2(pack2(-g1[4 * j + 2], -g1[4 * j + 3]), sy);
         }
       }
+    }
+    int h = (u - (kind == 0 ? 0 : kind == 1 ? uq : uk)) * kPer + sub;
+    char* dst;
+    long long dst_step;
+    bool kept = true;
+    if (kind == 0) {
+      dst = a.yq + (row * a.yq_row + h * a.yq_head + c0 * 8) * (long long)sizeof(D);
+      dst_step = step * kPer * a.yq_head * (long long)sizeof(D);
+    } else if constexpr (kPaged) {
+      // the element of the pools where this row's slot of head 0 begins
+      const long long at = page * a.kv.page_stride + (long long)(pos & (a.kv.page_size - 1)) * a.kv.slot_stride;
+      dst = (kind == 1 ? a.kv.k : a.kv.v) + (at + h * a.kv.head_stride + c0 * 8) * (long long)sizeof(D);
+      dst_step = step * kPer * a.kv.head_stride * (long long)sizeof(D);
+      kept = (unsigned)page < (unsigned)a.kv.n_pages;
+      if (!kept && lane == 0) atomicOr(a.status, CS_DEV_BADARG);
+    } else {
+      dst = a.yk + (row * a.yk_row + h * a.yk_head + c0 * 8) * (long long)sizeof(D);
+      dst_step = step * kPer * a.yk_head * (long long)sizeof(D);
+    }
+    for (; u < end; u += step) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 2) : "memory");
+      uint32_t w[2][kW];
+#pragma unroll
+      for (int j = 0; j < kPieces; ++j) {
+        const uint4 v = s_ring[warp][slot][j][lane];
+        uint32_t* d = &w[j / (kPieces / 2)][j % (kPieces / 2) * 4];
+        d[0] = v.x; d[1] = v.y; d[2] = v.z; d[3] = v.w;
+      }
+      fetch((slot + kSlots - 1) % kSlots);       // (into the slot whose unit is done)
+      slot = (slot + 1) % kSlots;
       f32x2 x0[4], x1[4];
-      widen<S>(w[i][0], x0);
-      widen<S>(w[i][1], x1);
-      fetch(w[i]);
+      widen<S>(w[0], x0);
+      widen<S>(w[1], x1);
       if (!plain) {
         if (norm) {
           f32x2 s2 = mul2(x0[0], x0[0]);
@@ -278,7 +282,7 @@ k_heads(HeadsArgs a) {
           for (int j = 0; j < 4; ++j) { x0[j] = mul2(x0[j], C0[j]); x1[j] = mul2(x1[j], C1[j]); }
         }
       }
-      if (h < n) {
+      if (kept && h < n) {
         store8<D>(dst, x0);
         store8<D>(dst + (c1 - c0) * 8 * (int)sizeof(D), x1);
       }
@@ -308,15 +312,16 @@ template <typename S, typename D, bool kPaged>
 cudaError_t launch_heads(HeadsArgs a, int rows, int head_dim, cudaStream_t st) {
   const int per = 512 / head_dim, units = cs_ceil_div(a.n_q, per) + cs_ceil_div(a.n_k, per) + cs_ceil_div(a.n_v, per);
   a.n_rows = rows;
-  // as many warps a row as it takes to give every SM of 148 some 64, each with a unit at least (8,192 rows of the 8B shape with one / two / four: 36.6 / 40.4 / 56.0 us, what is worked out per
-  // row is worked out by each; 11 rows with one take three times as long as with eight)
+  // As many warps a row as run at the same time on 148 SMs (two blocks of 8 warps, or five of 4, on each), each with a unit at least: what is worked out per row is worked out by each of its
+  // warps.  Rows of the 8B shape, us with 8 / 4 / 2 / 1 warps: 256 3.6 / 3.9 / 4.1 / -, 350 6.0 / 4.3 / 4.8 / 5.5, 700 - / 4.7 / 5.6 / 6.5, 2,048 - / 12.9 / 11.2 / 10.2.
   a.warps_per_row = 8;
-  while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)rows * a.warps_per_row > 148 * 64)) a.warps_per_row /= 2;
-  const dim3 grid((unsigned)(((long long)rows * a.warps_per_row + kWarps - 1) / kWarps));
+  while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)rows * a.warps_per_row > 148 * (a.warps_per_row == 8 ? 16 : 20))) a.warps_per_row /= 2;
+  const int warps = a.warps_per_row > 4 ? 8 : 4;
+  const dim3 grid((unsigned)(((long long)rows * a.warps_per_row + warps - 1) / warps)), block(warps * 32);
   switch (head_dim) {
-    case 32: return cs_launch_pdl(k_heads<S, D, 32, kPaged>, grid, dim3(kThreads), 0, st, a);
-    case 64: return cs_launch_pdl(k_heads<S, D, 64, kPaged>, grid, dim3(kThreads), 0, st, a);
-    default: return cs_launch_pdl(k_heads<S, D, 128, kPaged>, grid, dim3(kThreads), 0, st, a);
+    case 32: return cs_launch_pdl(k_heads<S, D, 32, kPaged>, grid, block, 0, st, a);
+    case 64: return cs_launch_pdl(k_heads<S, D, 64, kPaged>, grid, block, 0, st, a);
+    default: return cs_launch_pdl(k_heads<S, D, 128, kPaged>, grid, block, 0, st, a);
   }
 }
 
