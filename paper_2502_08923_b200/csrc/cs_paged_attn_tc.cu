@@ -207,6 +207,9 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   PagedPlan& plan = *reinterpret_cast<PagedPlan*>(s_piece + kPieces);
   const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8 * kNS, b_s = b_empty + 8 * kNS, b_p = b_s + 16, b_p2 = b_p + 16, b_o = b_p2 + 16, b_taken = b_o + 16, b_qfull = b_taken + 16, b_qfree = b_qfull + 8,
                  b_drain = b_qfree + 8, b_piece = b_drain + 8, b_ml = b_piece + 8 * kPieces, b_read = b_ml + 8;
+  // All weights are there.  (Those of the first 64 keys are announced ahead where their product is on the way to the slot's next scores; elsewhere that only costs: 1,184 rows of heads
+  // of 64 over 8,192 keys 141 -> 138 us without.)
+  const uint32_t b_all = kApart<DH> ? b_p : b_p2;
   const int tid = threadIdx.x, warp = (int)uniform(tid >> 5), lane = tid & 31;
 
   // (nothing of this depends on the kernel before, so it is done while that one ends)
@@ -328,9 +331,11 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
             const uint32_t acc = tmem + kOCol + slot * DH, w = tmem + kPCol<DH> + slot * kPStep<DH>;
 #pragma unroll
             for (int k = 0; k < 4; ++k) umma_ta(acc, w + k * 8, dv + k * (16 * kRow >> 4), idesc_o, (s > 1 || k > 0) ? 1u : 0u);   // 16 keys per instruction
-            if (!wait(b_p2 + 8 * slot, p_phase >> slot & 1)) { fine = false; break; }
+            if constexpr (!kApart<DH>) {
+              if (!wait(b_p2 + 8 * slot, p_phase >> slot & 1)) { fine = false; break; }
+              fence_after();
+            }
             p_phase ^= 1u << slot;
-            fence_after();
 #pragma unroll
             for (int k = 4; k < 8; ++k) umma_ta(acc, w + k * 8, dv + k * (16 * kRow >> 4), idesc_o, 1u);
             if (!both || slot) umma_commit(b_empty + 8 * (v_at % kNS));
@@ -563,22 +568,27 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
           const f32x2 nm2 = pack2(nm, nm);
           weights<T>(v, p_col, sc2, nm2, l2);
           weights<T>(v + 32, p_col + 16, sc2, nm2, l2);
-          st_wait();
-          fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(b_p + 8 * slot);      // (the products with the first 64 keys may begin)
+          if constexpr (!kApart<DH>) {
+            st_wait();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(b_p + 8 * slot);    // (the products with the first 64 keys may begin)
+          }
           weights<T>(v + 64, p_col + 32, sc2, nm2, l2);
           weights<T>(v + 96, p_col + 48, sc2, nm2, l2);
           st_wait();
           fence_before();
           __syncwarp();
-          if (lane == 0) mbar_arrive(b_p2 + 8 * slot);
+          if (lane == 0) mbar_arrive(b_all + 8 * slot);
         } else {
           // (nor may a warp without rows run ahead: its arrivals would count for the step before)
           if constexpr (kApart<DH>) { if (s > 1) wait(b_o + 8 * slot, (o_mine - 1) & 1); }
           fence_before();
           __syncwarp();
-          if (lane == 0) { mbar_arrive(b_p + 8 * slot); mbar_arrive(b_p2 + 8 * slot); }
+          if (lane == 0) {
+            if constexpr (!kApart<DH>) mbar_arrive(b_p + 8 * slot);
+            mbar_arrive(b_all + 8 * slot);
+          }
         }
         ++o_mine;
       }
