@@ -105,7 +105,7 @@ __global__ void __maxnreg__(96)
 k_heads(HeadsArgs a) {
   CS_PDL_PROLOGUE();
   constexpr int kLanes = DH / 16, kPer = 32 / kLanes, kW = sizeof(S) == 4 ? 8 : 4;    // lanes of a head, heads of a unit, words of a chunk
-  constexpr int kSlots = sizeof(S) == 4 ? 2 : 4, kPieces = kW / 2;                    // slots of a warp's ring; 16-byte pieces of a lane's two chunks
+  constexpr int kSlots = sizeof(S) == 4 ? 2 : 4, kPieces = kW / 2, kSlotBytes = kPieces * 512;      // slots of a warp's ring; 16-byte pieces of a lane's two chunks
   __shared__ uint4 s_ring[kWarps][kSlots][kPieces][32];
   __shared__ int s_seq[kWarps], s_pos[kWarps];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = lane % kLanes, sub = lane / kLanes;
@@ -123,8 +123,9 @@ k_heads(HeadsArgs a) {
   int fu = u0, f_end = 0, f_h = 0, f_n = 0;      // next unit, where its kind's units end, this lane's head of it, the kind's heads
   const char* f_p = a.q;
   long long f_step = 0;
-  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(&s_ring[warp][0][0][lane]);
-  auto fetch = [&](int slot) {
+  const char* mine = reinterpret_cast<const char*>(&s_ring[warp][0][0][lane]);
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(mine);
+  auto fetch = [&](uint32_t place) {
     if (fu >= f_end && fu < units) {             // (the same in the whole warp)
       const int kind = fu < uq ? 0 : fu < uk ? 1 : 2;
       const long long rs = kind == 0 ? a.q_row : kind == 1 ? a.k_row : a.v_row, hs = kind == 0 ? a.q_head : kind == 1 ? a.k_head : a.v_head;
@@ -135,7 +136,7 @@ k_heads(HeadsArgs a) {
       f_step = step * kPer * hs * (long long)sizeof(S);
     }
     if (fu < units && f_h < f_n) {
-      const uint32_t d = ring + slot * (kPieces * 512);
+      const uint32_t d = ring + place;
       const char* p1 = f_p + (c1 - c0) * 8 * (int)sizeof(S);
 #pragma unroll
       for (int j = 0; j < kPieces / 2; ++j) { fetch16(d + j * 512, f_p + j * 16); fetch16(d + (kPieces / 2 + j) * 512, p1 + j * 16); }
@@ -144,7 +145,7 @@ k_heads(HeadsArgs a) {
     fu += step; f_h += step * kPer; f_p += f_step;
   };
 #pragma unroll
-  for (int i = 0; i < kSlots - 1; ++i) fetch(i); // (whose row it is, and where it goes, takes three loads in a row: these are under way meanwhile)
+  for (int i = 0; i < kSlots - 1; ++i) fetch(i * kSlotBytes); // (whose row it is, and where it goes, takes three loads in a row: these are under way meanwhile)
 
   int pos = 0;
   int page = 0;                                  // (not looked at before the first factors have been asked for)
@@ -183,7 +184,7 @@ k_heads(HeadsArgs a) {
   // y0 = r (x0 C0 - x1 S1), y1 = r (x1 C1 + x0 S0), C = gain cos, S = gain sin: worked out once for the queries and once for the keys.  (Table
   // and gains are read through L1: all warps of a row want the same.)
   f32x2 C0[4], C1[4], S0[4], S1[4];
-  int slot = 0;
+  uint32_t place = 0;                            // of this unit in the ring, bytes
   for (int u = u0; u < units;) {
     const int kind = u < uq ? 0 : u < uk ? 1 : 2;
     const int n = kind == 0 ? a.n_q : kind == 1 ? a.n_k : a.n_v, end = kind == 0 ? uq : kind == 1 ? uk : units;
@@ -244,12 +245,12 @@ k_heads(HeadsArgs a) {
       uint32_t w[2][kW];
 #pragma unroll
       for (int j = 0; j < kPieces; ++j) {
-        const uint4 v = s_ring[warp][slot][j][lane];
+        const uint4 v = *reinterpret_cast<const uint4*>(mine + place + j * 512);
         uint32_t* d = &w[j / (kPieces / 2)][j % (kPieces / 2) * 4];
         d[0] = v.x; d[1] = v.y; d[2] = v.z; d[3] = v.w;
       }
-      fetch((slot + kSlots - 1) % kSlots);       // (into the slot whose unit is done)
-      slot = (slot + 1) % kSlots;
+      fetch((place + (kSlots - 1) * kSlotBytes) % (kSlots * kSlotBytes));      // (into the slot whose unit is done)
+      place = (place + kSlotBytes) % (kSlots * kSlotBytes);
       f32x2 x0[4], x1[4];
       widen<S>(w[0], x0);
       widen<S>(w[1], x1);
