@@ -5,16 +5,16 @@
 // A lane holds eight elements of a head's first half and their eight partners (16 bytes each of the 16-bit types; behind rot_dim two neighbouring chunks), a head is D / 16 lanes.  With C = gain cos and
 // S = gain sin, worked out once per row for the queries and once for the keys, an element is r (x0 C - x1 S), r the head's reciprocal norm (a
 // reduction over its lanes), and nothing is exchanged.  Warps take a row each, or 2, 4 or 8 share one where there are few; three units of 32 / (D / 16) heads are in flight, in
-// a ring of shared memory for each warp (in registers instead, four of them, 16 warps fit on an SM and not 20, and the setup is there four times: 34 us for the 30 below).
+// a ring of shared memory for each warp (in registers instead, four of them, 16 warps fit on an SM and not 20, and the setup is there four times: 34 us for the 29 below).
 //
-// Bound by HBM where there are many rows: 8,192 of the 8B shape 30.0 us (172 MB, 5.7 TB/s of the 6.5 that a copy reaches), an append of 6k rows 30.4 us (150 MB, 4.9).  With an
+// Bound by HBM where there are many rows: 8,192 of the 8B shape 29.3 us (172 MB, 5.9 TB/s of the 6.5 that a copy reaches), an append of 6k rows 29.7 us (150 MB, 5.0).  With an
 // element's partner in another lane, fetched by shuffles, and the factors worked out for each head 61 us.  Few rows: launch and a chain of loads (whose block is the row's, which
-// page and, at the same time, its rotation): 2.4 - 4.5 us.
+// page and, at the same time, its rotation): 2.4 - 4.7 us.
 #include "cs_paged.cuh"
 
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
+constexpr int kThreads = 256;
 
 // what k_heads does with a row
 struct HeadsArgs {
@@ -100,16 +100,16 @@ template <typename T> __device__ __forceinline__ void gain8(const char* g, int c
   }
 }
 
-template <typename S, typename D, int DH, bool kPaged>
-__global__ void __maxnreg__(96)
+template <typename S, typename D, int DH, bool kPaged, int kBlock>
+__global__ void __launch_bounds__(kBlock * 32, kBlock == 8 ? 2 : 5)
 k_heads(HeadsArgs a) {
   CS_PDL_PROLOGUE();
   constexpr int kLanes = DH / 16, kPer = 32 / kLanes, kW = sizeof(S) == 4 ? 8 : 4;    // lanes of a head, heads of a unit, words of a chunk
-  constexpr int kSlots = sizeof(S) == 4 ? 2 : 4, kPieces = kW / 2, kSlotBytes = kPieces * 512;      // slots of a warp's ring; 16-byte pieces of a lane's two chunks
-  __shared__ uint4 s_ring[kWarps][kSlots][kPieces][32];
-  __shared__ int s_seq[kWarps], s_pos[kWarps];
+  constexpr int kSlots = 4, kPieces = kW / 2, kSlotBytes = kPieces * 512;      // slots of a warp's ring; 16-byte pieces of a lane's two chunks
+  __shared__ uint4 s_ring[kBlock][kSlots][kPieces][32];
+  __shared__ int s_seq[kBlock], s_pos[kBlock];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = lane % kLanes, sub = lane / kLanes;
-  const int n_here = (int)(blockDim.x >> 5) / a.warps_per_row;
+  const int n_here = kBlock / a.warps_per_row;
   const long long row0 = (long long)blockIdx.x * n_here, row = row0 + warp / a.warps_per_row;
   // a row's units: up to kPer neighbouring heads, of queries, then keys, then values
   const int uq = (a.n_q + kPer - 1) / kPer, uk = uq + (a.n_k + kPer - 1) / kPer, units = row < a.n_rows ? uk + (a.n_v + kPer - 1) / kPer : 0;
@@ -151,9 +151,9 @@ k_heads(HeadsArgs a) {
   int page = 0;                                  // (not looked at before the first factors have been asked for)
   if constexpr (kPaged) {
     // the blocks these rows belong to
-    if (threadIdx.x < kWarps) s_seq[threadIdx.x] = -1;
+    if (threadIdx.x < kBlock) s_seq[threadIdx.x] = -1;
     __syncthreads();
-    for (int b = threadIdx.x; b < a.blk.n_seqs; b += (int)blockDim.x) {
+    for (int b = threadIdx.x; b < a.blk.n_seqs; b += kBlock * 32) {
       const int start = __ldcg(a.blk.start + b), len = __ldcg(a.blk.len + b), kv = __ldcg(a.blk.kv_len + b);
       const int flag = paged_block_flag(a.blk, a.kv.page_size, true, start, len, kv);
       if (flag != 0) {
@@ -309,21 +309,28 @@ k_rope_table(float* table, int n_positions, int rot_dim, double log_theta) {
 
 thread_local char t_paged_err[256] = "";
 
+template <typename S, typename D, bool kPaged, int kBlock>
+cudaError_t launch_heads_of(const HeadsArgs& a, int head_dim, cudaStream_t st) {
+  const dim3 grid((unsigned)(((long long)a.n_rows * a.warps_per_row + kBlock - 1) / kBlock)), block(kBlock * 32);
+  switch (head_dim) {
+    case 32: return cs_launch_pdl(k_heads<S, D, 32, kPaged, kBlock>, grid, block, 0, st, a);
+    case 64: return cs_launch_pdl(k_heads<S, D, 64, kPaged, kBlock>, grid, block, 0, st, a);
+    default: return cs_launch_pdl(k_heads<S, D, 128, kPaged, kBlock>, grid, block, 0, st, a);
+  }
+}
+
 template <typename S, typename D, bool kPaged>
 cudaError_t launch_heads(HeadsArgs a, int rows, int head_dim, cudaStream_t st) {
   const int per = 512 / head_dim, units = cs_ceil_div(a.n_q, per) + cs_ceil_div(a.n_k, per) + cs_ceil_div(a.n_v, per);
   a.n_rows = rows;
-  // As many warps a row as run at the same time on 148 SMs (two blocks of 8 warps, or five of 4, on each), each with a unit at least: what is worked out per row is worked out by each of its
+  // As many warps a row as run at the same time on 148 SMs (two blocks of 8 warps, or five of 4, on each; 32-bit rows, whose rings are twice as large, take 4 at most), each with a unit at least: what is worked out per row is worked out by each of its
   // warps.  Rows of the 8B shape, us with 8 / 4 / 2 / 1 warps: 256 3.6 / 3.9 / 4.1 / -, 350 6.0 / 4.3 / 4.8 / 5.5, 700 - / 4.7 / 5.6 / 6.5, 2,048 - / 12.9 / 11.2 / 10.2.
-  a.warps_per_row = 8;
+  a.warps_per_row = sizeof(S) == 4 ? 4 : 8;
   while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)rows * a.warps_per_row > 148 * (a.warps_per_row == 8 ? 16 : 20))) a.warps_per_row /= 2;
-  const int warps = a.warps_per_row > 4 ? 8 : 4;
-  const dim3 grid((unsigned)(((long long)rows * a.warps_per_row + warps - 1) / warps)), block(warps * 32);
-  switch (head_dim) {
-    case 32: return cs_launch_pdl(k_heads<S, D, 32, kPaged>, grid, block, 0, st, a);
-    case 64: return cs_launch_pdl(k_heads<S, D, 64, kPaged>, grid, block, 0, st, a);
-    default: return cs_launch_pdl(k_heads<S, D, 128, kPaged>, grid, block, 0, st, a);
+  if constexpr (sizeof(S) == 2) {
+    if (a.warps_per_row == 8) return launch_heads_of<S, D, kPaged, 8>(a, head_dim, st);
   }
+  return launch_heads_of<S, D, kPaged, 4>(a, head_dim, st);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }

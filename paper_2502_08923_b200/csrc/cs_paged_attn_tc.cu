@@ -25,11 +25,13 @@
 //
 // What bounds it.  Long chunks: 3,350 clocks for a pair of 128 x 128 tiles with heads of 128, of which the products take 2,048 at their peak rate; a slot's chain is scores into registers
 // 190, maxima 300, weights 1,200 (ex2, 16 a clock, is 1,024 of it), into tensor memory 200, product 512, next scores 512, hand-overs 400.  A 2,048-row chunk behind 30,720
-// keys of the 8B shape: 0.94 ms in short runs (1.13 PFLOP/s), 1.09 ms at the power cap (1.49 GHz, 990 W).  Few rows over long caches: HBM, 4.1 TB/s of 6.5 (8 x 21
-// rows of heads of 64 over 16,384 keys 66 us), less what a run begins and ends with; 11 rows over 4,096 keys 16 us, a chain of latencies (plan and piece 1.5, page entries,
+// keys of the 8B shape: 0.94 ms in short runs (1.13 PFLOP/s), 1.08 ms at the power cap (1.49 GHz, 990 W).  Heads of 64: 3,700 clocks a pair, all of it the softmax warps' way through their instructions (two warps a scheduler, one
+// instruction in three clocks, no unit above 35 %): 8 x 21 rows over 16,384 keys 65 us, 63.5 without the exponentials, 65 with half of the products, 64 with all pages in L2.  11 rows over 4,096 keys 16 us, a chain of latencies (plan and piece 1.5, page entries,
 // first tiles 3, one step 1.8, results 1.4, sums of pieces 5).
 // Tried and not kept: maxima left out, with reference points that follow the sums (3,350 -> 3,400 clocks: they hide behind ex2); a quarter of the exponentials by a polynomial in
-// packed arithmetic (-2 % of the clocks, +1 % of the time at the power cap); products with the first 64 keys only when all weights are there (no slower by themselves).
+// packed arithmetic (-2 % of the clocks, +1 % of the time at the power cap); products with the first 64 keys only when all weights are there (no slower by themselves); sixteen softmax
+// warps, two to a row with half of the keys each (104 registers; heads of 128 166 -> 180 us for 1,184 rows over 8,192 keys, heads of 64 138 -> 145: a barrier a tile for the common reference
+// point, and no phase shorter for it); slots that keep out of each other's exponentials (141 -> 154); exponentials in blocks of 16 (138 -> 142).
 #include <type_traits>
 
 #include "cs_paged.cuh"
