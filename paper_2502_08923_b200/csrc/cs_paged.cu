@@ -9,7 +9,7 @@
 //
 // Bound by HBM where there are many rows: 8,192 of the 8B shape 29.3 us (172 MB, 5.9 TB/s of the 6.5 that a copy reaches), an append of 6k rows 29.7 us (150 MB, 5.0).  With an
 // element's partner in another lane, fetched by shuffles, and the factors worked out for each head 61 us.  Few rows: launch and a chain of loads (whose block is the row's, which
-// page and, at the same time, its rotation): 2.4 - 4.7 us.
+// page and, at the same time, its rotation): 2.4 - 4.3 us.
 #include "cs_paged.cuh"
 
 namespace {
@@ -105,7 +105,8 @@ __global__ void __launch_bounds__(kBlock * 32, kBlock == 8 ? 2 : 5)
 k_heads(HeadsArgs a) {
   CS_PDL_PROLOGUE();
   constexpr int kLanes = DH / 16, kPer = 32 / kLanes, kW = sizeof(S) == 4 ? 8 : 4;    // lanes of a head, heads of a unit, words of a chunk
-  constexpr int kSlots = 4, kPieces = kW / 2, kSlotBytes = kPieces * 512;      // slots of a warp's ring; 16-byte pieces of a lane's two chunks
+  constexpr bool kWide = sizeof(S) == 4;
+  constexpr int kSlots = kWide && kBlock == 8 ? 2 : 4, kPieces = kW / 2, kSlotBytes = kPieces * 512;      // slots of a warp's ring; 16-byte pieces of a lane's two chunks
   __shared__ uint4 s_ring[kBlock][kSlots][kPieces][32];
   __shared__ int s_seq[kBlock], s_pos[kBlock];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = lane % kLanes, sub = lane / kLanes;
@@ -119,12 +120,14 @@ k_heads(HeadsArgs a) {
   const bool rotated = pair < half;
   const int c0 = rotated ? pair : 2 * pair, c1 = rotated ? pair + half : c0 + 1;
 
-  // Fetching runs kSlots - 1 units ahead of the rest.  A lane reads from the ring only what it fetched itself.
+  // Fetching runs kSlots - 1 units ahead of the rest.  16-bit rows: a lane reads from the ring only what it fetched itself.  32-bit rows lie in the ring as in memory, fetched 16 bytes a
+  // lane side by side (each lane its own 32 bytes in two fetches asked L2 for every sector twice: 8,192 rows of the 8B shape 61.5 us, so 40.6).
   int fu = u0, f_end = 0, f_h = 0, f_n = 0;      // next unit, where its kind's units end, this lane's head of it, the kind's heads
   const char* f_p = a.q;
   long long f_step = 0;
-  const char* mine = reinterpret_cast<const char*>(&s_ring[warp][0][0][lane]);
-  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(mine);
+  const int f_first = kWide ? pair * 16 : c0 * 16;                                         // byte of the head where this lane's first piece begins
+  const char* mine = reinterpret_cast<const char*>(&s_ring[warp][0][0][kWide ? 0 : lane]) + (kWide ? sub * DH * 4 : 0);
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(mine) + (kWide ? pair * 16 : 0);
   auto fetch = [&](uint32_t place) {
     if (fu >= f_end && fu < units) {             // (the same in the whole warp)
       const int kind = fu < uq ? 0 : fu < uk ? 1 : 2;
@@ -132,14 +135,18 @@ k_heads(HeadsArgs a) {
       f_h = (fu - (kind == 0 ? 0 : kind == 1 ? uq : uk)) * kPer + sub;
       f_n = kind == 0 ? a.n_q : kind == 1 ? a.n_k : a.n_v;
       f_end = kind == 0 ? uq : kind == 1 ? uk : units;
-      f_p = (kind == 0 ? a.q : kind == 1 ? a.k : a.v) + (row * rs + f_h * hs + c0 * 8) * (long long)sizeof(S);
+      f_p = (kind == 0 ? a.q : kind == 1 ? a.k : a.v) + (row * rs + f_h * hs) * (long long)sizeof(S) + f_first;
       f_step = step * kPer * hs * (long long)sizeof(S);
     }
     if (fu < units && f_h < f_n) {
       const uint32_t d = ring + place;
-      const char* p1 = f_p + (c1 - c0) * 8 * (int)sizeof(S);
+      if constexpr (kWide) {
 #pragma unroll
-      for (int j = 0; j < kPieces / 2; ++j) { fetch16(d + j * 512, f_p + j * 16); fetch16(d + (kPieces / 2 + j) * 512, p1 + j * 16); }
+        for (int j = 0; j < kPieces; ++j) fetch16(d + j * kLanes * 16, f_p + j * kLanes * 16);
+      } else {
+        fetch16(d, f_p);
+        fetch16(d + 512, f_p + (c1 - c0) * 16);
+      }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
     fu += step; f_h += step * kPer; f_p += f_step;
@@ -242,10 +249,12 @@ k_heads(HeadsArgs a) {
     }
     for (; u < end; u += step) {
       asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 2) : "memory");
+      if constexpr (kWide) __syncwarp();
       uint32_t w[2][kW];
 #pragma unroll
       for (int j = 0; j < kPieces; ++j) {
-        const uint4 v = *reinterpret_cast<const uint4*>(mine + place + j * 512);
+        const int at = kWide ? (j < 2 ? c0 : c1) * 32 + j % 2 * 16 : j * 512;
+        const uint4 v = *reinterpret_cast<const uint4*>(mine + place + at);
         uint32_t* d = &w[j / (kPieces / 2)][j % (kPieces / 2) * 4];
         d[0] = v.x; d[1] = v.y; d[2] = v.z; d[3] = v.w;
       }
@@ -323,14 +332,11 @@ template <typename S, typename D, bool kPaged>
 cudaError_t launch_heads(HeadsArgs a, int rows, int head_dim, cudaStream_t st) {
   const int per = 512 / head_dim, units = cs_ceil_div(a.n_q, per) + cs_ceil_div(a.n_k, per) + cs_ceil_div(a.n_v, per);
   a.n_rows = rows;
-  // As many warps a row as run at the same time on 148 SMs (two blocks of 8 warps, or five of 4, on each; 32-bit rows, whose rings are twice as large, take 4 at most), each with a unit at least: what is worked out per row is worked out by each of its
+  // As many warps a row as run at the same time on 148 SMs (two blocks of 8 warps, or five of 4, on each), each with a unit at least: what is worked out per row is worked out by each of its
   // warps.  Rows of the 8B shape, us with 8 / 4 / 2 / 1 warps: 256 3.6 / 3.9 / 4.1 / -, 350 6.0 / 4.3 / 4.8 / 5.5, 700 - / 4.7 / 5.6 / 6.5, 2,048 - / 12.9 / 11.2 / 10.2.
-  a.warps_per_row = sizeof(S) == 4 ? 4 : 8;
+  a.warps_per_row = 8;
   while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)rows * a.warps_per_row > 148 * (a.warps_per_row == 8 ? 16 : 20))) a.warps_per_row /= 2;
-  if constexpr (sizeof(S) == 2) {
-    if (a.warps_per_row == 8) return launch_heads_of<S, D, kPaged, 8>(a, head_dim, st);
-  }
-  return launch_heads_of<S, D, kPaged, 4>(a, head_dim, st);
+  return a.warps_per_row == 8 ? launch_heads_of<S, D, kPaged, 8>(a, head_dim, st) : launch_heads_of<S, D, kPaged, 4>(a, head_dim, st);
 }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
