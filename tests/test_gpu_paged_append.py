@@ -58,6 +58,33 @@ def test_part_of_a_head_rotated(rot):
         check_rows(got, *norm_rope(q, gain, rope, pos), BF)
 
 
+@pytest.mark.parametrize("src,dst", TYPES)
+@pytest.mark.parametrize("rows", [200, 297, 741, 1481])          # shared by 8, 4, 2 warps, with a warp each
+def test_many_rows_part_rotated(src, dst, rows):
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    x = (2 * torch.randn(rows, 23, 128, generator=g, device="cuda")).to(src)
+    rope = cs.cs_rope_table(2000, 96, 10000.0)
+    pos = torch.randint(0, 2000, (rows,), generator=g, device="cuda", dtype=torch.int32)
+    qg, kg = gains(128, dst)
+    got = cs.cs_qk_norm_rope(x[:, :20], x[:, 20:], pos, rope, qg, kg, dtype=dst)
+    check_rows(got[0], *norm_rope(x[:, :20], qg, rope, pos), dst)
+    check_rows(got[1], *norm_rope(x[:, 20:], kg, rope, pos), dst)
+
+
+@pytest.mark.parametrize("dt", [BF, FP, F32])
+@pytest.mark.parametrize("rows,rot", [(5, 128), (1700, 64)])
+def test_in_place(dt, rows, rot):
+    x = torch.randn(rows, 10, 128, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").to(dt)
+    rope, pos = cs.cs_rope_table(rows, rot), torch.arange(rows, device="cuda", dtype=torch.int32)
+    qg, kg = gains(128, dt)
+    want = [norm_rope(x[:, :7], qg, rope, pos), norm_rope(x[:, 7:9], kg, rope, pos)]
+    rest = x[:, 9].clone()
+    cs.cs_qk_norm_rope(x[:, :7], x[:, 7:9], pos, rope, qg, kg, out=(x[:, :7], x[:, 7:9]))
+    check_rows(x[:, :7], *want[0], dt)
+    check_rows(x[:, 7:9], *want[1], dt)
+    assert torch.equal(x[:, 9], rest)
+
+
 def test_in_place_and_extremes():
     x = torch.randn(9, 12, 64, device="cuda").to(BF)
     x[3, 2] = 0.0                                        # a head of zeros: eps keeps the norm finite
@@ -119,6 +146,13 @@ def append(case, src, norm, H, seed=0, rope=None, gaps=0):
 @pytest.mark.parametrize("norm", [True, False])
 def test_append(D, dt, src, lens, cached, norm):
     append(Case(lens, cached, 8, 2, D, dt, seed=1), src, norm, 8)
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("src", [BF, F32])
+@pytest.mark.parametrize("lens", [[250, 1, 90], [900, 2, 600]])
+def test_append_of_chunks(D, src, lens):
+    append(Case(lens, [30, 0, 601], 32, 8, D, seed=10, gaps=1), src, True, 32)
 
 
 @pytest.mark.parametrize("page", [16, 64, 512])
