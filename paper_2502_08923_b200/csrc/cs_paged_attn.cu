@@ -172,12 +172,15 @@ k_paged_few(PagedAttnArgs a) {
   };
   asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");
   __syncthreads();
+  // A piece's queries are read by every warp (all sixteen rows) before any warp fetches again: of pieces of one tile each the ring holds this one and the kStages behind it, so the next queries
+  // go to this one's place.
+  begin();
+  __syncthreads();
 
   // items shared with other CTAs, at most two: the run's first and its last
   struct Shared { int c0, c1, start, len, rg, head; } shared[2] = {{-1, 0, 0, 0, 0, 0}, {-1, 0, 0, 0, 0, 0}};
   int stage = 0;
   for (bool more = true; more;) {
-    begin();                                     // (its queries came with the last slice of the piece before, or the first of all)
     float o[DH / 8][4];
 #pragma unroll
     for (int n = 0; n < DH / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
@@ -343,7 +346,10 @@ k_paged_few(PagedAttnArgs a) {
       else shared[0] = s;
     }
     p = next;
-    if (more) __syncthreads();                   // (the exchange rows are free again)
+    if (more) {
+      begin();                                   // (its queries came with the last slice of the piece before)
+      __syncthreads();                           // (they are read, and the exchange rows are free again)
+    }
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
 
