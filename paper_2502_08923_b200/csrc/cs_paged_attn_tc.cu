@@ -52,7 +52,9 @@ template <int DH> constexpr int kTileBytes = kPagedTile * DH * 2;  // of K, of V
 template <int DH> constexpr int kStages = DH == 128 ? 4 : 8;
 template <int DH> constexpr int kRowBytes = DH == 32 ? 64 : 128;    // of a row in shared memory, swizzled over so many bytes; heads of 128 are two halves one behind the other
 constexpr int kCtl = 512;
-constexpr int kPieces = 4;         // descriptors of pieces (published at most two ahead of the products, of which the softmax may be one behind)
+// Descriptors of pieces.  A slot that is still at a piece's results holds the others up four pieces on at the latest: the other slot waits for it at the next piece whose tiles the slots take in turn, but the
+// scores of the piece after that may be made (of one tile each, they need neither slot), which frees the queries and makes two more known.
+constexpr int kPieces = 8;
 template <int DH> constexpr int kTcSmem = 1024 + (kStages<DH> + 2) * kTileBytes<DH> + kCtl + 2 * kM * 8 + kPieces * 64 + (int)sizeof(PagedPlan);
 
 // Operand descriptors as in cs_tcgen.cuh, for rows of 128 or (heads of 32) 64 bytes: eight of them a group, and the swizzle as wide
@@ -202,7 +204,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   uint8_t* ring = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));   // [stage][64 dims][128 keys][128 B]
   uint8_t* sq = ring + kNS * kTB;                                       // [slot][64 dims][128 rows][128 B]
   uint64_t* bars = reinterpret_cast<uint64_t*>(sq + 2 * kTB);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kNS + 20);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kNS + 13 + kPieces + 2 + 1);
   volatile int* s_abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float2* s_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(bars) + kCtl);      // [slot][128 rows]
   TcPiece* s_piece = reinterpret_cast<TcPiece*>(s_ml + 2 * kM);

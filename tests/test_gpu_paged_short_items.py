@@ -26,3 +26,20 @@ def test_items_of_one_tile_each(D, H, Hkv, most):
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
     assert cache.cs_paged_status() == cs.CS_OK
     check_attention(case, *first, *case.attention())
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+def test_tall_items_between_items_of_one_tile(D):
+    """On the tensor cores: after an item whose rows fill both slots, items of one tile that one slot has to itself."""
+    g = torch.Generator().manual_seed(D)
+    lens = [60 if b % 4 == 0 else int(torch.randint(1, 6, (1,), generator=g)) for b in range(240)]
+    cached = torch.randint(0, 60, (len(lens),), generator=g).tolist()
+    case = Case(lens, cached, 32, 8, D, seed=D)
+    assert case.rows * 4 > 16 * len(lens)                 # the kernel for tall blocks
+    cache = cs.PagedCache(case.kp, case.vp)
+    first = cache.cs_paged_attention(case.q, *case.blocks(), with_lse=True)
+    for _ in range(30):
+        again = cache.cs_paged_attention(case.q, *case.blocks(), with_lse=True)
+        assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+    assert cache.cs_paged_status() == cs.CS_OK
+    check_attention(case, *first, *case.attention())
