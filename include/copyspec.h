@@ -557,7 +557,7 @@ cs_status cs_paged_attention(cs_paged_cache* cache, const cs_blocks* blocks, con
 
 /* Test hook for the bounded waits (no counterpart in the paper): the next cs_paged_attention of this handle that runs on the tensor cores leaves out the copy of every CTA's
  * tile-th K tile, so that the products wait for it until the wait limit (CS_WAIT_LIMIT_US at cs_paged_create) and the CTA gives up: copies and
- * products in flight end, nothing is written, cs_paged_status reports CS_ERR_TIMEOUT.  Calls of few rows have no such waits.  tile < 0 clears it. */
+ * products in flight end, the rows it had not finished stay as they were (with those of other CTAs that share an item with it), cs_paged_status reports CS_ERR_TIMEOUT.  Calls of few rows have no such waits.  tile < 0 clears it. */
 cs_status cs_paged_debug_drop_tile(cs_paged_cache* cache, int tile);
 
 #ifdef __cplusplus

@@ -22,11 +22,13 @@ struct BlocksView {
   int n_seqs, table_width, rows;
 };
 
-// an item whose first tiles are a CTA's last ones: the CTAs behind it, up to `last`, have the rest (-1: none)
+// What a CTA leaves for the launch that adds pieces up: the item whose first tiles are its last ones; the CTAs behind it, up to `last`, have the rest (kPagedNone: there is no such item,
+// kPagedGaveUp: a wait of this CTA ran out)
 struct PagedSplit {
   int last, rows;              // query rows
   int first_row, head, start;  // of the block (row x head of the group), KV head, the block's first row
 };
+static constexpr int kPagedNone = -1, kPagedGaveUp = -2;
 
 struct cs_paged_cache {
   cs_paged_config cfg;

@@ -21,7 +21,8 @@
 // of the item see and others do not reaches the others' sums too (0 x inf is not 0): a row whose result is not finite is looked at again where it is written
 // (mend_row).  (Tiles of such keys were looked through ahead of the product at first, which made them three times as long as others.)
 //
-// Every wait is bounded: on expiry the CTA flags CS_DEV_TIMEOUT, stops issuing, walks through its barriers, drains what is in flight, frees its TMEM and returns.
+// Every wait is bounded: on expiry the CTA flags CS_DEV_TIMEOUT, stops issuing, walks through its barriers, drains what is in flight, frees its TMEM and returns.  Items that it had not
+// finished, shared ones among them whatever their other CTAs have done, stay unwritten.
 //
 // What bounds it.  Long chunks: 3,350 clocks for a pair of 128 x 128 tiles with heads of 128, of which the products take 2,048 at their peak rate; a slot's chain is scores into registers
 // 190, maxima 300, weights 1,200 (ex2, 16 a clock, is 1,024 of it), into tensor memory 200, product 512, next scores 512, hand-overs 400.  A 2,048-row chunk behind 30,720
@@ -272,6 +273,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     return i + min(i + ahead, tiles);
   };
 
+  bool split = false;                             // (of the first thread: it has announced an item)
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     uint32_t base = 0, piece = 0;                 // ring entries before this piece; pieces
@@ -468,7 +470,6 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_col = lanes + slot * 128, o_col = lanes + kOCol + slot * DH, p_col = lanes + kPCol<DH> + slot * kPStep<DH>;
     uint32_t base = 0, s_phase = 0, piece = 0, turns = 0;      // (turns: pieces whose tiles the slots took in turn)
     uint32_t o_mine = 0, o_other = 0;                          // products of this slot, of the other one, so far
-    bool split = false;
     for (;; ++piece) {
       if (slot_any(slot, !known(piece))) break;
       const TcPiece& p = s_piece[piece % kPieces];
@@ -699,11 +700,11 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       }
       base += both ? n : 2 * n;
     }
-    if (tid == 0 && (!split || *s_abort)) a.splits[cta].last = -1;
   }
   // ---------------------------------------------------------------------- teardown
   fence_before();
   __syncthreads();
+  if (tid == 0 && (!split || *s_abort)) a.splits[cta].last = *s_abort ? kPagedGaveUp : kPagedNone;
   if (warp == kMmaWarp) {
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
@@ -758,33 +759,45 @@ k_paged_merge(PagedAttnArgs a, int n_cta) {
   __shared__ float2 s_ml[kMergeWarps];
   __shared__ __align__(16) float s_o[kMergeWarps][DH];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  constexpr int kGaveUp = 1 << 20;                // more rows than all items can have
   if (tid < kPagedMaxCtas) {
     PagedSplit d;
-    d.last = -1; d.rows = 0;
+    d.last = kPagedNone; d.rows = 0;
     if (tid < n_cta) {
       const int* src = reinterpret_cast<const int*>(a.splits + tid);
       d.last = __ldcg(src); d.rows = __ldcg(src + 1); d.first_row = __ldcg(src + 2); d.head = __ldcg(src + 3); d.start = __ldcg(src + 4);
-      if (d.last < 0) d.rows = 0;
+      if (d.last < 0) d.rows = d.last == kPagedGaveUp ? kGaveUp : 0;
     }
     s_split[tid] = d;
   }
   __syncthreads();
   // (every warp adds up for itself, all the same)
-  int mine[kPerLane], sum = 0;
+  int mine[kPerLane], total;
+  for (;;) {
+    int sum = 0;
 #pragma unroll
-  for (int i = 0; i < kPerLane; ++i) { mine[i] = sum; sum += s_split[lane * kPerLane + i].rows; }
-  int inc = sum;
+    for (int i = 0; i < kPerLane; ++i) { mine[i] = sum; sum += s_split[lane * kPerLane + i].rows; }
+    int inc = sum;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int v = __shfl_up_sync(0xffffffffu, inc, o);
-    if (lane >= o) inc += v;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += v;
+    }
+    total = __shfl_sync(0xffffffffu, inc, 31);
+#pragma unroll
+    for (int i = 0; i < kPerLane; ++i) mine[i] += inc - sum;
+    if (total < kGaveUp) break;
+    // an item that one of its CTAs gave up on stays as it was: a piece is missing, and what lies in its place is an earlier call's
+    __syncthreads();
+    if (tid < n_cta) {
+      bool whole = s_split[tid].last >= 0;
+      for (int c = tid + 1; c <= s_split[tid].last; ++c) whole &= s_split[c].last != kPagedGaveUp;
+      if (!whole) s_split[tid].rows = 0;
+    }
+    __syncthreads();
   }
-  const int total = __shfl_sync(0xffffffffu, inc, 31);
 #pragma unroll
-  for (int i = 0; i < kPerLane; ++i) {
-    mine[i] += inc - sum;
-    s_before[lane * kPerLane + i] = mine[i];
-  }
+  for (int i = 0; i < kPerLane; ++i) s_before[lane * kPerLane + i] = mine[i];
   __syncwarp();
   auto find = [&](int g) -> MergeRow {
     int n = 0;
