@@ -18,8 +18,10 @@
 // Warps 0-7 softmax, 8 issues MMAs, 9 and 10 fetch K and V tiles (a copy per page and 64 dims, page-table entries 32 at a time), 11 fetches queries.
 //
 // Keys no row of the item sees may hold anything: their scores are masked, their V rows set to zero in shared memory.  A value that is not finite at a key that some rows
-// of the item see and others do not reaches the others' sums too (0 x inf is not 0): a row whose result is not finite is looked at again where it is written
-// (mend_row).  (Tiles of such keys were looked through ahead of the product at first, which made them three times as long as others.)
+// of the item see and others do not reaches the others' sums too (0 x inf is not 0).  Looking for such values ahead of every product makes tiles of such keys three times as long.  So that is left to a second pass:
+// where a result is not finite, the CTA goes through that piece once more, with those values left out of the products and added to the rows that see them at the end: one NaN in a 2,048-row chunk behind 30,720 keys makes
+// the call 2.0 ms long instead of 0.91.  (The same instructions run both passes.  A launch of its own for such rows, or a branch of the launch behind, costs calls without any 1 - 10 us for its code
+// alone.)
 //
 // Every wait is bounded: on expiry the CTA flags CS_DEV_TIMEOUT, stops issuing, walks through its barriers, drains what is in flight, frees its TMEM and returns.  Items that it had not
 // finished, shared ones among them whatever their other CTAs have done, stay unwritten.
@@ -52,11 +54,15 @@ template <int DH> constexpr uint32_t kPStep = kApart<DH> ? 64 : 128;
 template <int DH> constexpr int kTileBytes = kPagedTile * DH * 2;  // of K, of V, and of a slot's queries
 template <int DH> constexpr int kStages = DH == 128 ? 4 : 8;
 template <int DH> constexpr int kRowBytes = DH == 32 ? 64 : 128;    // of a row in shared memory, swizzled over so many bytes; heads of 128 are two halves one behind the other
+// Registers of the warpgroups: two of the softmax and one of the others share the 384 x 168 that the block is launched with.  (What the softmax spills it fetches again for every tile: heads of 128 with 72 / 216, 68 bytes spilled,
+// windowed chunks 110 us, with 56 / 224 and none 102; heads of 64 the other way round, 32 bytes and 64 us against 88 and 69.)
+template <int DH> constexpr int kOtherRegs = DH == 128 ? 56 : 72;
+template <int DH> constexpr int kSoftmaxRegs = DH == 128 ? 224 : 216;
 constexpr int kCtl = 512;
 // Descriptors of pieces.  A slot that is still at a piece's results holds the others up four pieces on at the latest: the other slot waits for it at the next piece whose tiles the slots take in turn, but the
 // scores of the piece after that may be made (of one tile each, they need neither slot), which frees the queries and makes two more known.
-constexpr int kPieces = 8;
-template <int DH> constexpr int kTcSmem = 1024 + (kStages<DH> + 2) * kTileBytes<DH> + kCtl + 2 * kM * 8 + kPieces * 64 + (int)sizeof(PagedPlan);
+constexpr int kPieces = 8, kPieceBytes = 72;
+template <int DH> constexpr int kTcSmem = 1024 + (kStages<DH> + 2) * kTileBytes<DH> + kCtl + 2 * kM * 8 + kPieces * kPieceBytes + (int)sizeof(PagedPlan);
 
 // Operand descriptors as in cs_tcgen.cuh, for rows of 128 or (heads of 32) 64 bytes: eight of them a group, and the swizzle as wide
 template <int kRow> __device__ __forceinline__ uint64_t desc_rows(uint32_t saddr, uint32_t lbo) {
@@ -98,6 +104,15 @@ __device__ __forceinline__ void st16(uint32_t taddr, const uint32_t* v) {
                  "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]) : "memory");
 }
 __device__ __forceinline__ void st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// a word of a piece's description, read where it is used: kept in registers across the loop they would spill
+__device__ __forceinline__ int fresh(const int& x) { return *const_cast<const volatile int*>(&x); }
+__device__ __forceinline__ uint32_t flag(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.volatile.shared.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ void set_flag(uint32_t addr, uint32_t v) { asm volatile("st.volatile.shared.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
+__device__ __forceinline__ void or_flag(uint32_t addr, uint32_t v) { asm volatile("red.shared.or.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 typedef unsigned long long f32x2;
@@ -148,12 +163,6 @@ __device__ __forceinline__ void weights(const float* v, uint32_t taddr, f32x2 sc
   st16(taddr, w);
 }
 
-template <typename T>
-__device__ __forceinline__ float value_at(const char* base, long long element) {
-  if constexpr (std::is_same<T, __nv_bfloat16>::value) return __bfloat162float(__ushort_as_bfloat16(__ldcg(reinterpret_cast<const unsigned short*>(base) + element)));
-  else return __half2float(__ushort_as_half(__ldcg(reinterpret_cast<const unsigned short*>(base) + element)));
-}
-
 // What the roles need to know of a piece; worked out by one warp and left in shared memory, since the softmax threads have no register to spare (what they
 // spill lies beyond L1, which shared memory leaves next to nothing of: 350 bytes of it made the tile loop a third slower).
 struct TcPiece {
@@ -161,38 +170,51 @@ struct TcPiece {
   int lo, hi, all_lo, all_hi;      // keys that some row of the item attends to, that all do
   int tile0, steps;                // steps 0: there is no further piece
   int both, opens, whole, last;    // both slots have rows of their own; has the item's first tile; all; the CTA with the last
+  int again;                       // second pass
 };
 
-// A row whose output is not finite, 32 columns of it: if a value that is not finite lies at a key that the row does not see but others of the item do, the product took it
-// in (0 x inf is not 0), and the row's sum is worked out again from the keys it does see, term by term.  `dst`: fp32 (part of an item, scale 1) or T.
-template <typename T, int DH>
-__device__ __noinline__ void mend_row(const PagedAttnArgs& a, const TcPiece& p, int n_tiles, int lo, int hi, long long q_at, float m, float scale_by, int c0, void* dst, bool part) {
-  const int first = max(p.lo, p.tile0 * kPagedTile), last = min(p.hi, (p.tile0 + n_tiles) * kPagedTile);
-  const int* table = a.blk.table + (long long)p.seq * a.blk.table_width;
-  auto at = [&](int key) -> long long {                    // element of the pools, -1: no such page
-    const int page = __ldcg(table + (key >> a.kv.page_shift));
-    return (unsigned)page < (unsigned)a.kv.n_pages ? page * a.kv.page_stride + p.head * a.kv.head_stride + (long long)(key & (a.kv.page_size - 1)) * a.kv.slot_stride : -1;
-  };
-  bool tainted = false;
-  for (int key = first; key < last && !tainted; ++key) {
-    if (key >= lo && key < hi) { key = min(hi, last) - 1; continue; }
-    const long long e = at(key);
-    for (int d = 0; d < 32 && e >= 0; ++d) tainted |= !(fabsf(value_at<T>(a.kv.v, e + c0 + d)) < INFINITY);
-  }
-  if (!tainted) return;
-  for (int d0 = 0; d0 < 32; d0 += 8) {
-    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int key = max(first, lo); key < min(last, hi); ++key) {
-      const long long e = at(key);
-      float s = 0.f;
-      for (int d = 0; d < DH && e >= 0; ++d) s = fmaf(value_at<T>(a.q, q_at + d), value_at<T>(a.kv.k, e + d), s);
-      const float w = paged_ex2(fmaf(s, a.scale_log2e, m == -INFINITY ? 0.f : -m));
+// a word of two 16-bit values with zeros for those that are not finite
+template <typename T>
+__device__ __forceinline__ uint32_t finite_only(uint32_t w) {
+  constexpr uint32_t e = std::is_same<T, __nv_bfloat16>::value ? 0x7f80u : 0x7c00u;
+  return ((w & e) == e ? 0u : w & 0xffffu) | ((w >> 16 & e) == e ? 0u : w & 0xffff0000u);
+}
+
+// In a second pass: 32 columns of a row, as stored (`part`: fp32, else T), get the values that are not finite at keys the row sees and others of its item do not.  (Any positive weight makes the same of them.)
+template <typename T>
+__device__ __noinline__ void add_odd(const PagedAttnArgs& a, const TcPiece& p, int n_tiles, int lo, int hi, int c0, void* dst, bool part) {
+  const int last = min(hi, (p.tile0 + n_tiles) * kPagedTile);
+#pragma unroll 1
+  for (int c = 0; c < 32; c += 32) {
+    float sum[32] = {};
+    for (int key = max(lo, p.tile0 * kPagedTile); key < last; ++key) {
+      if (key >= p.all_lo && key < p.all_hi) {
+        key = p.all_hi - 1;
+        continue;
+      }
+      const int page = __ldcg(a.blk.table + (long long)p.seq * a.blk.table_width + (key >> a.kv.page_shift));
+      if ((unsigned)page >= (unsigned)a.kv.n_pages) continue;
+      const uint4* src = reinterpret_cast<const uint4*>(a.kv.v + (page * a.kv.page_stride + p.head * a.kv.head_stride + (long long)(key & (a.kv.page_size - 1)) * a.kv.slot_stride + c0 + c) * 2);
 #pragma unroll
-      for (int d = 0; d < 8; ++d) o[d] = fmaf(w, e >= 0 ? value_at<T>(a.kv.v, e + c0 + d0 + d) : 0.f, o[d]);
+      for (int j = 0; j < 4; ++j) {
+        const uint4 v = __ldcg(src + j);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float2 x = PagedType<T>::unpack(w[i] ^ finite_only<T>(w[i]));
+          sum[8 * j + 2 * i] += x.x;
+          sum[8 * j + 2 * i + 1] += x.y;
+        }
+      }
     }
-    for (int d = 0; d < 8; ++d) {
-      if (part) reinterpret_cast<float*>(dst)[d0 + d] = o[d];
-      else reinterpret_cast<unsigned short*>(dst)[d0 + d] = (unsigned short)PagedType<T>::pack(o[d] * scale_by, 0.f);
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      if (sum[i] == 0.f) continue;
+      if (part) reinterpret_cast<float*>(dst)[c + i] += sum[i];
+      else {
+        unsigned short* o = reinterpret_cast<unsigned short*>(dst) + c + i;
+        *o = (unsigned short)PagedType<T>::pack(PagedType<T>::unpack(*o).x + sum[i], 0.f);
+      }
     }
   }
 }
@@ -205,13 +227,15 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   uint8_t* ring = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));   // [stage][64 dims][128 keys][128 B]
   uint8_t* sq = ring + kNS * kTB;                                       // [slot][64 dims][128 rows][128 B]
   uint64_t* bars = reinterpret_cast<uint64_t*>(sq + 2 * kTB);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kNS + 13 + kPieces + 2 + 1);
-  volatile int* s_abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * kNS + 13 + kPieces + 2);
   float2* s_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(bars) + kCtl);      // [slot][128 rows]
   TcPiece* s_piece = reinterpret_cast<TcPiece*>(s_ml + 2 * kM);
-  PagedPlan& plan = *reinterpret_cast<PagedPlan*>(s_piece + kPieces);
+  static_assert(sizeof(TcPiece) <= kPieceBytes, "");
+  PagedPlan& plan = *reinterpret_cast<PagedPlan*>(reinterpret_cast<uint8_t*>(s_piece) + kPieces * kPieceBytes);
   const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8 * kNS, b_s = b_empty + 8 * kNS, b_p = b_s + 16, b_p2 = b_p + 16, b_o = b_p2 + 16, b_taken = b_o + 16, b_qfull = b_taken + 16, b_qfree = b_qfull + 8,
                  b_drain = b_qfree + 8, b_piece = b_drain + 8, b_ml = b_piece + 8 * kPieces, b_read = b_ml + 8;
+  // flags, by 32-bit addresses: a wait has run out; an item has been announced; results that are not finite, a bit a piece (the last one for all from there on)
+  const uint32_t f_abort = b_read + 12, f_shares = f_abort + 4, f_odd = f_shares + 4;
   // All weights are there.  (Those of the first 64 keys are announced ahead where their product is on the way to the slot's next scores; elsewhere that only costs: 1,184 rows of heads
   // of 64 over 8,192 keys 141 -> 138 us without.)
   const uint32_t b_all = kApart<DH> ? b_p : b_p2;
@@ -228,7 +252,9 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     mbar_init(b_qfull, 1); mbar_init(b_qfree, 1); mbar_init(b_drain, 1);
     for (int s = 0; s < kPieces; ++s) mbar_init(b_piece + 8 * s, 1);
     mbar_init(b_ml, 8); mbar_init(b_read, 8);
-    *s_abort = 0;
+    set_flag(f_abort, 0);
+    set_flag(f_shares, 0);
+    set_flag(f_odd, 0);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kMmaWarp) {
@@ -250,9 +276,9 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     const unsigned long long t0 = globaltimer_ns();
     for (;;) {
       if (mbar_try_wait(bar, parity)) return true;
-      if (*s_abort) return false;
+      if (flag(f_abort)) return false;
       if (globaltimer_ns() - t0 > a.wait_ns) {
-        *s_abort = 1;
+        set_flag(f_abort, 1);
         atomicOr(a.status, CS_DEV_TIMEOUT);
         return false;
       }
@@ -261,7 +287,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   auto wait_warp = [&](uint32_t bar, uint32_t parity) -> bool { return __all_sync(0xffffffffu, wait(bar, parity)); };
   const int slot_rows = a.item_rows / 2;          // query rows of a slot
   // the next piece, once it is known (by a warp; false: a wait has run out)
-  auto known = [&](uint32_t piece) -> bool { return wait_warp(b_piece + 8 * (piece % kPieces), (piece / kPieces) & 1) && !__any_sync(0xffffffffu, *s_abort != 0); };
+  auto known = [&](uint32_t piece) -> bool { return wait_warp(b_piece + 8 * (piece % kPieces), (piece / kPieces) & 1) && !__any_sync(0xffffffffu, flag(f_abort) != 0); };
   // Order of the ring, that of first use: where the slots share tiles K0 V0 K1 V1 .., else K0 K1 V0 K2 V1 ..; with scores made ahead (kApart) K0 K1 V0 K2 V1 .. and
   // K0 K1 K2 V0 K3 V1 ..  (Entry of step s, of n steps.)
   auto k_entry = [](bool both, int s) {
@@ -273,11 +299,18 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     return i + min(i + ahead, tiles);
   };
 
-  bool split = false;                             // (of the first thread: it has announced an item)
+  // The end of a pass, where all roles meet once, whatever has become of their waits: is there a second one?
+  auto again = [&](bool second) -> bool {
+    uint32_t odd;
+    fence_before();
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %1, 0;\nbar.red.or.pred q, 0, p;\nselp.u32 %0, 1, 0, q;\n}" : "=r"(odd) : "r"(flag(f_odd)) : "memory");
+    fence_after();
+    return !second && odd != 0;
+  };
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs<DH>));
     uint32_t base = 0, piece = 0;                 // ring entries before this piece; pieces
-    bool ok = true;
+    bool ok = true, met = false;
     if (warp == kMmaWarp) {
       // ------------------------------------------------------------------ MMA issuer
       constexpr uint32_t kType = std::is_same<T, __nv_bfloat16>::value ? (1u << 7) | (1u << 10) : 0u;
@@ -294,8 +327,13 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         const TcPiece& d = s_piece[piece % kPieces];
         const int n = (int)uniform((uint32_t)d.steps);
         const bool both = uniform((uint32_t)d.both) != 0;
-        if (n == 0) break;
-        ok = wait_warp(b_qfull, piece & 1);
+        const uint32_t second = uniform((uint32_t)d.again);
+        if (n == 0) {
+          if (again(second)) continue;
+          met = true;
+          break;
+        }
+        ok = wait_warp(b_qfull, (piece - second) & 1);   // (the end of the first pass had no queries)
         if (!ok) break;
         fence_after();
         bool fine = true;
@@ -363,44 +401,55 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       }
     } else if (warp == kQWarp) {
       // ------------------------------------------------------------------ pieces and queries
-      PagedPiece p;
-      p.n_tiles = 0;
-      long long run1 = 0;
-      if (cta < n_cta) p = paged_run(a, plan, total, n_cta, cta, lane, run1);
-      bool more = p.n_tiles > 0;
-      for (;; ++piece) {
-        const bool both = more && p.len * a.group - p.rg * a.item_rows > slot_rows;
-        if (lane == 0) {
-          TcPiece d;
-          d.steps = more ? (both ? 2 * p.n_tiles : p.n_tiles) : 0;
-          if (more) {
-            int x;
-            const int last_row = min(p.len * a.group, (p.rg + 1) * a.item_rows) - 1, r0 = a.by_group.of(p.rg * a.item_rows), r1 = a.by_group.of(last_row);
-            paged_range(a.mask, a.window, p.len, p.kv, r0, r0, x, d.all_hi);
-            paged_range(a.mask, a.window, p.len, p.kv, r1, r1, d.all_lo, x);
-            d.start = p.start; d.len = p.len; d.kv = p.kv; d.seq = p.seq; d.head = p.head; d.rg = p.rg;
-            d.lo = p.lo; d.hi = p.hi; d.tile0 = p.tile0; d.both = both; d.opens = p.opens; d.whole = p.whole;
-            d.last = p.whole ? cta : paged_last_cta(a, p, total, n_cta);
+      uint32_t todo = 0xffffffffu;                 // pieces that the pass has to go through, a bit each (the last one for all from there on)
+      for (uint32_t second = 0; ; ++second, ++piece) {
+        PagedPiece p;
+        p.n_tiles = 0;
+        long long run1 = 0;
+        if (cta < n_cta) p = paged_run(a, plan, total, n_cta, cta, lane, run1);
+        bool more = p.n_tiles > 0;
+        for (uint32_t nth = 0; ; ++piece, ++nth) {
+          for (; more && !(todo >> min(nth, 31u) & 1); ++nth) more = paged_next(a, plan, p, run1);
+          const bool both = more && p.len * a.group - p.rg * a.item_rows > slot_rows;
+          if (lane == 0) {
+            TcPiece d;
+            d.steps = more ? (both ? 2 * p.n_tiles : p.n_tiles) : 0;
+            d.again = second;
+            if (more) {
+              int x;
+              const int last_row = min(p.len * a.group, (p.rg + 1) * a.item_rows) - 1, r0 = a.by_group.of(p.rg * a.item_rows), r1 = a.by_group.of(last_row);
+              paged_range(a.mask, a.window, p.len, p.kv, r0, r0, x, d.all_hi);
+              paged_range(a.mask, a.window, p.len, p.kv, r1, r1, d.all_lo, x);
+              d.start = p.start; d.len = p.len; d.kv = p.kv; d.seq = p.seq; d.head = p.head; d.rg = p.rg;
+              d.lo = p.lo; d.hi = p.hi; d.tile0 = p.tile0; d.both = both; d.opens = p.opens; d.whole = p.whole;
+              d.last = p.whole ? cta : paged_last_cta(a, p, total, n_cta);
+            }
+            s_piece[piece % kPieces] = d;
+            mbar_arrive(b_piece + 8 * (piece % kPieces));
           }
-          s_piece[piece % kPieces] = d;
-          mbar_arrive(b_piece + 8 * (piece % kPieces));
+          __syncwarp();
+          if (!more) break;
+          if (piece - second > 0) ok = wait_warp(b_qfree, (piece - second - 1) & 1);
+          if (!ok) break;
+          if (elect_one()) {
+            mbar_expect_tx(b_qfull, (uint32_t)(q_box_bytes * kHalves * (both ? 2 : 1)));
+            for (int s = 0; s < (both ? 2 : 1); ++s)
+              for (int h = 0; h < kHalves; ++h)
+                tma_load_3d(smem_u32(sq) + s * kTB + h * kHalf, &tmQ, b_qfull, 64 * h, p.head * a.group, p.start + a.by_group.of(p.rg * a.item_rows + s * slot_rows));
+          }
+          more = paged_next(a, plan, p, run1);
         }
-        __syncwarp();
-        if (!more) break;
-        if (piece > 0) ok = wait_warp(b_qfree, (piece - 1) & 1);
-        if (!ok) break;
-        if (elect_one()) {
-          mbar_expect_tx(b_qfull, (uint32_t)(q_box_bytes * kHalves * (both ? 2 : 1)));
-          for (int s = 0; s < (both ? 2 : 1); ++s)
-            for (int h = 0; h < kHalves; ++h)
-              tma_load_3d(smem_u32(sq) + s * kTB + h * kHalf, &tmQ, b_qfull, 64 * h, p.head * a.group, p.start + a.by_group.of(p.rg * a.item_rows + s * slot_rows));
+        if (!ok) {
+          // (every role meets a last piece, and a copy that nobody waited for must land before the shared memory goes away)
+          const unsigned long long t0 = globaltimer_ns();
+          while (piece - second > 0 && !mbar_try_wait(b_qfull, (piece - second - 1) & 1) && globaltimer_ns() - t0 < a.wait_ns) {}
+          break;
         }
-        more = paged_next(a, plan, p, run1);
-      }
-      if (!ok) {
-        // (every role meets a last piece, and a copy that nobody waited for must land before the shared memory goes away)
-        const unsigned long long t0 = globaltimer_ns();
-        while (piece > 0 && !mbar_try_wait(b_qfull, (piece - 1) & 1) && globaltimer_ns() - t0 < a.wait_ns) {}
+        if (!again(second)) {
+          met = true;
+          break;
+        }
+        todo = flag(f_odd);
       }
     } else {
       // ------------------------------------------------------------------ K tiles, V tiles
@@ -415,7 +464,11 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         const int n = (int)uniform((uint32_t)d.steps), tile0 = (int)uniform((uint32_t)d.tile0), head = (int)uniform((uint32_t)d.head), lo = (int)uniform((uint32_t)d.lo),
                   hi = (int)uniform((uint32_t)d.hi), seq = (int)uniform((uint32_t)d.seq);
         const bool both = uniform((uint32_t)d.both) != 0;
-        if (n == 0) break;
+        if (n == 0) {
+          if (again(uniform((uint32_t)d.again))) continue;
+          met = true;
+          break;
+        }
         const int inc = both ? 2 : 1;
         int entry = 0, first = -64;                // this lane's page-table entry, and of which page the first lane has one
         const int* table = a.blk.table + (long long)seq * a.blk.table_width;
@@ -455,56 +508,72 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         base += both ? n : 2 * n;
         if (!ok) break;
       }
-      if (*s_abort)                                // copies that nobody will consume must land before the shared memory goes away
+      if (flag(f_abort))                                // copies that nobody will consume must land before the shared memory goes away
         for (uint32_t e = asked > kNS ? asked - kNS : 0; e < asked; ++e) {
           // (entries of the other warp's are waited for as well; one that was never started runs into the limit)
           const unsigned long long t0 = globaltimer_ns();
           while (!mbar_try_wait(b_full + 8 * (e % kNS), (e / kNS) & 1) && globaltimer_ns() - t0 < a.wait_ns) {}
         }
     }
+    if (!met) again(true);
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs<DH>));
     // -------------------------------------------------------------------- softmax and results: one thread per query row
     const int slot = warp >> 2, row = tid & 127, G = a.group;
     const bool out_32 = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;      // (rows are multiples of 32 bytes)
     const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21), s_col = lanes + slot * 128, o_col = lanes + kOCol + slot * DH, p_col = lanes + kPCol<DH> + slot * kPStep<DH>;
     uint32_t base = 0, s_phase = 0, piece = 0, turns = 0;      // (turns: pieces whose tiles the slots took in turn)
     uint32_t o_mine = 0, o_other = 0;                          // products of this slot, of the other one, so far
+    bool met = false;
     for (;; ++piece) {
       if (slot_any(slot, !known(piece))) break;
       const TcPiece& p = s_piece[piece % kPieces];
       const int n = p.steps;
-      if (n == 0) break;
+      if (n == 0) {
+        if (again(p.again != 0)) continue;
+        met = true;
+        break;
+      }
       const bool both = p.both != 0;
       const int mrow = p.rg * a.item_rows + (both ? slot * slot_rows : 0) + row;
       const bool live = row < slot_rows && mrow < p.len * G;
       const bool some = __any_sync(0xffffffffu, live);         // (a warp without rows leaves its lanes to chance: nobody reads them)
-      int lo = 0, hi = 0;
-      if (live) {
-        const int r = a.by_group.of(mrow);
-        paged_range(a.mask, a.window, p.len, p.kv, r, r, lo, hi);
-      }
+      auto range = [&](int& lo, int& hi) {                     // keys that the row sees  (worked out where they are needed: in registers they would spill)
+        lo = hi = 0;
+        if (live) {
+          const int r = a.by_group.of(mrow);
+          paged_range(a.mask, a.window, fresh(p.len), fresh(p.kv), r, r, lo, hi);
+        }
+      };
       float m = live ? -INFINITY : 0.f;
       f32x2 l2 = pack2(0.f, 0.f);
       const f32x2 sc2 = pack2(a.scale_log2e, a.scale_log2e);
-      const int tile0 = p.tile0, all_lo = p.all_lo, all_hi = p.all_hi;
 
       for (int s = slot; s < n; s += 2) {
-        const int key0 = (tile0 + (both ? s >> 1 : s)) * kPagedTile;
-        const bool mixed = key0 < all_lo || key0 + kPagedTile > all_hi;
+        const int key0 = (fresh(p.tile0) + (both ? s >> 1 : s)) * kPagedTile;
+        const bool mixed = key0 < fresh(p.all_lo) || key0 + kPagedTile > fresh(p.all_hi);
         bool ok = wait(b_s + 8 * slot, s_phase);
         s_phase ^= 1;
         ok = __all_sync(0xffffffffu, ok);
         fence_after();
-        if (mixed && ok && (key0 < p.lo || key0 + kPagedTile > p.hi)) {
-          // V rows that no row of the item sees become zeros (whatever lies there: its weight is 0, but 0 x inf is not)
+        if (mixed && ok && (p.again || key0 < p.lo || key0 + kPagedTile > p.hi)) {
+          // V rows that no row of the item sees become zeros (whatever lies there: its weight is 0, but 0 x inf is not); in a second pass also what is not finite in rows that only some see
           const uint32_t e = base + v_entry(both, s, n), st = e % kNS;
-          if (wait(b_full + 8 * st, (e / kNS) & 1) && (key0 + row < p.lo || key0 + row >= p.hi)) {
+          const bool none = key0 + row < p.lo || key0 + row >= p.hi;
+          if (wait(b_full + 8 * st, (e / kNS) & 1) && (none || (p.again && (key0 + row < p.all_lo || key0 + row >= p.all_hi)))) {
             uint8_t* vrow = ring + st * kTB + row * kRow;
-#pragma unroll
+#pragma unroll 1
             for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-              for (int c = 0; c < kRow / 16; ++c) *reinterpret_cast<uint4*>(vrow + h * kHalf + ((c + lane) & (kRow / 16 - 1)) * 16) = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll 1
+              for (int c = 0; c < kRow / 16; ++c) {
+                uint4* x = reinterpret_cast<uint4*>(vrow + h * kHalf + ((c + lane) & (kRow / 16 - 1)) * 16);
+                uint4 y = make_uint4(0u, 0u, 0u, 0u);
+                if (!none) {
+                  y = *x;
+                  y = make_uint4(finite_only<T>(y.x), finite_only<T>(y.y), finite_only<T>(y.z), finite_only<T>(y.w));
+                }
+                *x = y;
+              }
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
@@ -524,6 +593,8 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         }
         if (mixed && ok) {
           // a bit for each of 32 keys that the row sees
+          int lo, hi;
+          range(lo, hi);
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
             const int from = min(max(lo - key0 - 32 * c, 0), 32), to = min(max(hi - key0 - 32 * c, 0), 32);
@@ -622,7 +693,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         l = (m == -INFINITY && l == 0.f ? 0.f : l * k_mine) + (nothing ? 0.f : o_ml.y * k_other);
         m = M;
       }
-      const bool good = *s_abort == 0;
+      const bool good = flag(f_abort) == 0;
       // (32 columns at a time; heads of 32 have no half for the second warpgroup)
       const int c_first = both || DH == 32 ? 0 : slot * (DH / 2), c_last = both ? DH : DH == 32 ? (slot == 0 ? 32 : 0) : c_first + DH / 2;
       const long long part = ((long long)cta * 2 + (p.opens ? 1 : 0)) * kPagedMaxRows + (both ? slot * slot_rows : 0) + row;
@@ -672,8 +743,12 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
             }
             float z0, z1;
             unpack2(z, z0, z1);
-            if (!(z0 + z1 == 0.f))
-              mend_row<T, DH>(a, p, both ? n >> 1 : n, lo, hi, (long long)(p.start + r) * a.q_row + head * a.q_head, m, inv, c0, dst, !whole);
+            if (!(z0 + z1 == 0.f)) or_flag(f_odd, 1u << min(piece, 31u));
+            if (p.again) {
+              int lo, hi;
+              range(lo, hi);
+              add_odd<T>(a, p, both ? n >> 1 : n, lo, hi, c0, dst, !whole);
+            }
           }
           __syncwarp();
         }
@@ -689,7 +764,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         d.rows = min(a.item_rows, p.len * G - p.rg * a.item_rows);
         d.first_row = p.rg * a.item_rows; d.head = p.head; d.start = p.start;
         a.splits[cta] = d;
-        split = true;
+        set_flag(f_shares, 1);
       }
       if (!both) {                                       // both warpgroups have read both slots' O and the exchange rows
         __syncwarp();
@@ -700,11 +775,10 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       }
       base += both ? n : 2 * n;
     }
+    if (!met) again(true);
   }
-  // ---------------------------------------------------------------------- teardown
-  fence_before();
-  __syncthreads();
-  if (tid == 0 && (!split || *s_abort)) a.splits[cta].last = *s_abort ? kPagedGaveUp : kPagedNone;
+  // ---------------------------------------------------------------------- teardown (all have met)
+  if (tid == 0 && (flag(f_shares) == 0 || flag(f_abort) != 0)) a.splits[cta].last = flag(f_abort) != 0 ? kPagedGaveUp : kPagedNone;
   if (warp == kMmaWarp) {
     fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
