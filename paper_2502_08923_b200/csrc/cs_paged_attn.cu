@@ -11,7 +11,7 @@
 // piece, the last one to arrive (a counter) adds the pieces up in the order of the keys, so results do not depend on who was last.
 // Sixteen query rows (token x head of the group) are the M of m16n8k16; the softmax weights, in the layout the scores come in, are the
 // second product's A operand, as two 16-bit terms (value = hi + lo): the tensor pipe has the room, and the weights stay as
-// exact as the scores.
+// exact as the scores.  In fp16 they are 2^14 times as large, by a reference point that much lower: of weights up to 1 both terms of one below 2^-25 are 0, and tens of thousands of such are more than the type's rounding.
 //
 // Masked keys: scores become -inf.  Keys outside [lo, hi) of the item's rows are never fetched (cp.async fills zeros), so
 // what lies there, freed pages included, does not matter.  Slices that some rows see and others do not are looked through for
@@ -28,6 +28,7 @@
 namespace {
 
 constexpr int kWarps = 8, kThreads = kWarps * 32, kSlice = 16, kRows = 16;
+template <typename T> constexpr float kUp = std::is_same<T, __half>::value ? 14.f : 0.f;      // how far below a row's largest score its reference point is put
 template <int DH> constexpr int kFewStages = DH == 128 ? 2 : 4;
 template <int DH> constexpr int kFewSmem = kWarps * kFewStages<DH> * 2 * kSlice * DH * 2 + kWarps * kRows * (DH + 8) * 4 + kWarps * kRows * 8 +
                                          (kFewStages<DH> + 1) * kRows * DH * 2 + (int)sizeof(PagedPlan) + 16;
@@ -217,7 +218,7 @@ k_paged_few(PagedAttnArgs a) {
         for (int h = 0; h < 2; ++h) {
           float x = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2)) * a.scale_log2e;
+          x = fmaf(fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2)), a.scale_log2e, -kUp<T>);
           nm[h] = fmaxf(m[h], x);
           moves |= nm[h] > m[h];
         }

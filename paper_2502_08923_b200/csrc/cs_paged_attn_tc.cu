@@ -13,7 +13,8 @@
 // products' order keeps.  (Smaller heads leave room for weights beside the scores: S(s + 2) goes ahead of P V(s), see kApart; 1,184 rows over 8,192 keys 158 -> 148 us.)  A slot's scores being there means that its product before is done, so a softmax that moves its reference point may
 // rescale O at once.  The reference point moves only past 2^8 (softmax does not depend on it, and weights up to 2^8 are as exact as weights up
 // to 1), which leaves rescaling to a few tiles.  Weights are rounded once, to the cache's type, on their way into the second product; their sum is
-// taken before.
+// taken before.  In fp16 they are 2^7 (to 2^15) times as large, by a reference point that much lower: those below 2^-25 become 0, and 131,072 of them at 2^-25 of the largest would be 4e-3 of the sum, eight times what the
+// type resolves; below 2^-32 they are 3e-5 at most.
 //
 // Warps 0-7 softmax, 8 issues MMAs, 9 and 10 fetch K and V tiles (a copy per page and 64 dims, page-table entries 32 at a time), 11 fetches queries.
 //
@@ -48,6 +49,7 @@ constexpr int kM = 128;                                            // query rows
 // they have 64 columns of their own, and a slot's next scores are made while the softmax is at work on the last ones, which it has in registers.
 constexpr uint32_t kTmemCols = 512;
 template <int DH> constexpr bool kApart = DH <= 64;
+template <typename T> constexpr float kUp = std::is_same<T, __half>::value ? 7.f : 0.f;      // how far below a row's largest score its reference point is put
 constexpr uint32_t kOCol = 256;
 template <int DH> constexpr uint32_t kPCol = kApart<DH> ? 384 : 0;
 template <int DH> constexpr uint32_t kPStep = kApart<DH> ? 64 : 128;
@@ -619,10 +621,10 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
               fence_after();
             }
           }
-          const bool moves = live && (m == -INFINITY ? top > m : top > m + 8.f);
+          const bool moves = live && (m == -INFINITY ? top > m : top > m + (8.f + kUp<T>));
           if (__any_sync(0xffffffffu, moves)) {
-            const float corr = !moves ? 1.f : m == -INFINITY ? 0.f : paged_ex2(m - top);
-            if (moves) m = top;
+            const float corr = !moves ? 1.f : m == -INFINITY ? 0.f : paged_ex2(m - (top - kUp<T>));
+            if (moves) m = top - kUp<T>;
             float l0, l1;
             unpack2(l2, l0, l1);
             l2 = pack2(l0 * corr, l1 * corr);
