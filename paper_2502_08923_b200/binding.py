@@ -594,6 +594,13 @@ def cs_rope_table(n_positions, rot_dim, theta=10000.0, device="cuda"):
     return table
 
 
+def _on(device, **tensors):
+    """A kernel runs where its first argument is: everything else must be there too."""
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name} is on {t.device}, the call on {device}")
+
+
 def _rows(t, name):
     """(data pointer, row stride, head stride) of a [rows][heads][head_dim] CUDA tensor whose heads are contiguous."""
     if not t.is_cuda or t.dim() != 3 or t.dtype not in _DTYPE or (t.shape[2] > 1 and t.stride(2) != 1):
@@ -646,11 +653,13 @@ def cs_qk_norm_rope(q, k, pos, rope, q_gain=None, k_gain=None, eps=1e-5, dtype=N
         raise ValueError("bf16, fp16 and fp32 are known")
     if rope is not None and (pos is None or pos.shape != some.shape[:1]):
         raise ValueError("pos must have one position per row")
+    _on(some.device, q=q, k=k, pos=pos, rope=rope, q_gain=q_gain, k_gain=k_gain)
     if out is None:
         out = tuple(None if x is None else torch.empty(x.shape, dtype=dtype, device=x.device) for x in (q, k))
     hq, hk = _heads(q, out[0], q_gain, dtype, "q"), _heads(k, out[1], k_gain, dtype, "k")
     table, n, rot = _table(rope)
-    rc = load().cs_qk_norm_rope(hq, hk, some.shape[0], some.shape[2], _DTYPE[some.dtype], _DTYPE[dtype], _i32(pos, "pos"), table, n, rot, eps, _stream())
+    with torch.cuda.device(some.device):
+        rc = load().cs_qk_norm_rope(hq, hk, some.shape[0], some.shape[2], _DTYPE[some.dtype], _DTYPE[dtype], _i32(pos, "pos"), table, n, rot, eps, _stream())
     if rc != CS_OK:
         raise CsError(rc, "cs_qk_norm_rope")
     return out
@@ -692,12 +701,13 @@ class PagedCache:
         if rc != CS_OK:
             msg = self.lib.cs_paged_last_error(None)
             raise CsError(rc, "cs_paged_create", msg.decode() if msg else "")
-        self._id = (self.handle.value, _DTYPE[self.dtype])
+        self.device = k_pages.device
+        self._id = (self.handle.value, _DTYPE[self.dtype], self.device.index)
 
     def close(self):
         if getattr(self, "handle", None):
             self.lib.cs_paged_destroy(self.handle)
-            self.handle, self._id = None, (0, 0)
+            self.handle, self._id = None, (0, 0, -1)
 
     def __del__(self):
         try:
@@ -728,12 +738,15 @@ class PagedCache:
         d = self.k_pages.shape[3]
         if k.dtype != v.dtype or k.shape != v.shape or k.dim() != 3 or k.shape[2] != d or (q is not None and (q.dtype != k.dtype or q.shape[0] != k.shape[0] or q.shape[2] != d)):
             raise ValueError("q, k and v must have the same rows and type and the cache's head size")
+        _on(self.device, k=k, v=v, block_start=block_start, block_len=block_len, kv_len=kv_len, page_table=page_table, rope=rope, k_gain=k_gain, q=q, q_gain=q_gain, q_out=q_out)
         if q is not None and q_out is None:
             q_out = torch.empty(q.shape, dtype=self.dtype, device=q.device)
         hk, hv, hq = _heads(k, None, k_gain, self.dtype, "k"), _heads(v, None, None, self.dtype, "v"), _heads(q, q_out, q_gain, self.dtype, "q")
         blocks = self._blocks(block_start, block_len, kv_len, page_table, k.shape[0])
         table, n, rot = _table(rope)
-        self._check(self.lib.cs_paged_append(self.handle, blocks, hk, hv, hq, _DTYPE[k.dtype], table, n, rot, eps, _stream()), "cs_paged_append")
+        with torch.cuda.device(self.device):
+            rc = self.lib.cs_paged_append(self.handle, blocks, hk, hv, hq, _DTYPE[k.dtype], table, n, rot, eps, _stream())
+        self._check(rc, "cs_paged_append")
         return q_out
 
     def cs_paged_attention(self, q, block_start, block_len, kv_len, page_table, mask=MASK_CAUSAL, window=0, scale=None, out=None, with_lse=False, lse=None):
@@ -749,6 +762,7 @@ class PagedCache:
                 self._check(got, "cs_paged_attention")
         if q.dtype != self.dtype:
             raise ValueError(f"q must be {self.dtype}, the cache's type")
+        _on(self.device, q=q, block_start=block_start, block_len=block_len, kv_len=kv_len, page_table=page_table, out=out, lse=lse)
         ptr, row, head = _rows(q, "q")
         T, H, D = q.shape
         if D != self.k_pages.shape[3]:
@@ -762,14 +776,16 @@ class PagedCache:
         elif lse is not None and (lse.shape != (T, H) or lse.dtype is not torch.float32 or not lse.is_cuda or not lse.is_contiguous()):
             raise ValueError("lse must be a contiguous fp32 CUDA tensor [rows][heads]")
         blocks = self._blocks(block_start, block_len, kv_len, page_table, T)
-        rc = self.lib.cs_paged_attention(self.handle, blocks, ptr, row, head, H, mask, window, self.scale if scale is None else scale, out.data_ptr(),
-                                         None if lse is None else lse.data_ptr(), _stream())
+        with torch.cuda.device(self.device):
+            rc = self.lib.cs_paged_attention(self.handle, blocks, ptr, row, head, H, mask, window, self.scale if scale is None else scale, out.data_ptr(),
+                                             None if lse is None else lse.data_ptr(), _stream())
         self._check(rc, "cs_paged_attention")
         return out if lse is None else (out, lse)
 
     def cs_paged_status(self):
         """Waits for the stream; what the device found wrong since the last call (CS_OK: nothing)."""
-        return self.lib.cs_paged_status(self.handle, _stream())
+        with torch.cuda.device(self.device):
+            return self.lib.cs_paged_status(self.handle, _stream())
 
     def cs_paged_debug_drop_tile(self, tile):
         self._check(self.lib.cs_paged_debug_drop_tile(self.handle, tile), "cs_paged_debug_drop_tile")

@@ -168,13 +168,21 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
-// paged_append(handle, dtype code, k, v, block_start, block_len, kv_len, page_table, rope, k_gain, q, q_gain, eps) -> (q,)
+// the handle of a cache on the current device (the other tensors are), nullptr if it is not one
+cs_paged_cache* cache_of(PyObject* handle, PyObject* device, int64_t head_dim) {
+  long d;
+  if (!PyLong_CheckExact(handle) || !small_int(device, d) || d != c10::cuda::current_device()) return nullptr;
+  cs_paged_cache* const cache = static_cast<cs_paged_cache*>(PyLong_AsVoidPtr(handle));
+  return cache != nullptr && cs_paged_head_dim(cache) == (int)head_dim ? cache : nullptr;
+}
+
+// paged_append(handle, dtype code, device, k, v, block_start, block_len, kv_len, page_table, rope, k_gain, q, q_gain, eps) -> (q,)
 PyObject* paged_append(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   const at::Tensor *q, *k, *v, *rope, *qg, *kg;
   long code;
-  if (n_args != 13 || c10::impl::TorchDispatchModeTLS::any_modes_set() || !PyLong_CheckExact(args[0]) || !small_int(args[1], code) || !tensor_of(args[2], k) || !tensor_of(args[3], v) ||
-      !optional_of(args[8], rope) || !optional_of(args[9], kg) || !optional_of(args[10], q) || !optional_of(args[11], qg) || !PyFloat_CheckExact(args[12]))
+  if (n_args != 14 || c10::impl::TorchDispatchModeTLS::any_modes_set() || !small_int(args[1], code) || !tensor_of(args[3], k) || !tensor_of(args[4], v) ||
+      !optional_of(args[9], rope) || !optional_of(args[10], kg) || !optional_of(args[11], q) || !optional_of(args[12], qg) || !PyFloat_CheckExact(args[13]))
     Py_RETURN_NONE;
   cs_heads hq = {}, hk = {}, hv = {};
   cs_blocks blocks;
@@ -182,14 +190,14 @@ PyObject* paged_append(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   int n, rot;
   const at::ScalarType type = type_of((int)code);
   if (!rows_of(*k, hk) || !rows_of(*v, hv) || k->scalar_type() != v->scalar_type() || k->sizes() != v->sizes() || !gain_of(kg, k->size(2), type, hk) || !table_of(rope, table, n, rot) ||
-      !blocks_of(args + 4, k->size(0), blocks) ||
+      !blocks_of(args + 5, k->size(0), blocks) ||
       (q != nullptr && (!rows_of(*q, hq) || q->scalar_type() != k->scalar_type() || q->size(0) != k->size(0) || q->size(2) != k->size(2) || !gain_of(qg, k->size(2), type, hq))))
     Py_RETURN_NONE;
-  cs_paged_cache* const cache = static_cast<cs_paged_cache*>(PyLong_AsVoidPtr(args[0]));
-  if (cache == nullptr || cs_paged_head_dim(cache) != (int)k->size(2)) Py_RETURN_NONE;
+  cs_paged_cache* const cache = cache_of(args[0], args[2], k->size(2));
+  if (cache == nullptr) Py_RETURN_NONE;
   const at::Tensor yq = q != nullptr ? output_for(*q, type, hq) : at::Tensor();
   void* const stream = c10::cuda::getCurrentCUDAStream().stream();
-  const float eps = (float)PyFloat_AS_DOUBLE(args[12]);
+  const float eps = (float)PyFloat_AS_DOUBLE(args[13]);
   const int in = code_of(k->scalar_type());
   cs_status s;
   Py_BEGIN_ALLOW_THREADS
@@ -203,25 +211,25 @@ PyObject* paged_append(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
-// paged_attention(handle, dtype code, q, block_start, block_len, kv_len, page_table, mask, window, scale, with_lse) -> (out, lse or None)
+// paged_attention(handle, dtype code, device, q, block_start, block_len, kv_len, page_table, mask, window, scale, with_lse) -> (out, lse or None)
 PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   const at::Tensor* q;
   long code, mask, window;
-  if (n_args != 11 || c10::impl::TorchDispatchModeTLS::any_modes_set() || !PyLong_CheckExact(args[0]) || !small_int(args[1], code) || !tensor_of(args[2], q) || !small_int(args[7], mask) ||
-      !small_int(args[8], window) || !PyFloat_CheckExact(args[9]) || !PyBool_Check(args[10]))
+  if (n_args != 12 || c10::impl::TorchDispatchModeTLS::any_modes_set() || !small_int(args[1], code) || !tensor_of(args[3], q) || !small_int(args[8], mask) ||
+      !small_int(args[9], window) || !PyFloat_CheckExact(args[10]) || !PyBool_Check(args[11]))
     Py_RETURN_NONE;
   cs_heads hq = {};
   cs_blocks blocks;
-  if (!rows_of(*q, hq) || code_of(q->scalar_type()) != code || !blocks_of(args + 3, q->size(0), blocks)) Py_RETURN_NONE;
-  cs_paged_cache* const cache = static_cast<cs_paged_cache*>(PyLong_AsVoidPtr(args[0]));
-  if (cache == nullptr || cs_paged_head_dim(cache) != (int)q->size(2)) Py_RETURN_NONE;
-  const bool with_lse = args[10] == Py_True;
+  if (!rows_of(*q, hq) || code_of(q->scalar_type()) != code || !blocks_of(args + 4, q->size(0), blocks)) Py_RETURN_NONE;
+  cs_paged_cache* const cache = cache_of(args[0], args[2], q->size(2));
+  if (cache == nullptr) Py_RETURN_NONE;
+  const bool with_lse = args[11] == Py_True;
   const at::Tensor out = output_for(*q, q->scalar_type(), hq);
   const at::Tensor lse = with_lse ? at::detail::empty_cuda({q->size(0), q->size(1)}, at::kFloat, q->device(), std::nullopt) : at::Tensor();
   void* const stream = c10::cuda::getCurrentCUDAStream().stream();
   float* const lse_p = with_lse ? static_cast<float*>(lse.mutable_data_ptr()) : nullptr;
-  const float scale = (float)PyFloat_AS_DOUBLE(args[9]);
+  const float scale = (float)PyFloat_AS_DOUBLE(args[10]);
   cs_status s;
   Py_BEGIN_ALLOW_THREADS
   s = cs_paged_attention(cache, &blocks, hq.x, hq.row_stride, hq.head_stride, hq.n_heads, (cs_mask)mask, (int)window, scale, hq.y, lse_p, stream);
