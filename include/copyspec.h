@@ -517,11 +517,16 @@ size_t cs_paged_workspace_bytes(const cs_paged_config* cfg);
 
 /* Describes a cache to the calls below.  `cfg` is a host struct (copied); `workspace` is a 256-byte aligned device buffer
  * of at least cs_paged_workspace_bytes(cfg) bytes; both pools and the workspace must outlive the handle.  Clears the
- * workspace's counters and status on `stream` (async).  Work of one handle must stay on one stream at a time; handles of
- * several layers whose work is on one stream may share a workspace, and then share what cs_paged_status says.  Errors: CS_ERR_ARG, CS_ERR_SHAPE, CS_ERR_CAPACITY, CS_ERR_CUDA;
+ * workspace's counters and status on `stream` (async): work on another stream must wait for that, and a workspace that is in use already wants the
+ * next call.  Work of one workspace must stay on one stream at a time.  Errors: CS_ERR_ARG, CS_ERR_SHAPE, CS_ERR_CAPACITY, CS_ERR_CUDA;
  * the text is cs_paged_last_error(NULL). */
 cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void* workspace, size_t workspace_bytes,
                           void* stream);
+
+/* The same for the cache of a further layer whose work is on the stream of `first`'s: its workspace serves both, which then share what cs_paged_status
+ * says.  Nothing is cleared or launched, so it may be made while `first` is at work.  `first` may be destroyed before it.  Errors as above
+ * (CS_ERR_CAPACITY: heads larger than those the workspace was made for). */
+cs_status cs_paged_create_beside(cs_paged_cache** out, const cs_paged_config* cfg, const cs_paged_cache* first);
 void cs_paged_destroy(cs_paged_cache* cache);
 int cs_paged_head_dim(const cs_paged_cache* cache); /* 0 for NULL */
 const char* cs_paged_last_error(const cs_paged_cache* cache);

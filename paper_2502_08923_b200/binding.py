@@ -75,7 +75,7 @@ EXPORTS = ("cs_workspace_bytes", "cs_create", "cs_destroy", "cs_last_error", "cs
            "cs_loop_begin", "cs_loop_steps", "cs_loop_poll", "cs_loop_end", "cs_loop_last_step", "cs_set_stamps", "cs_stamp_layout", "cs_set_match_index",
            "cs_loop_launches_per_step", "cs_lm_head", "cs_lm_head_static", "cs_gram_index_bytes",
            "cs_gram_index_reset", "cs_gram_index_update", "cs_find_match_indexed", "cs_gram_index_status",
-           "cs_rope_table", "cs_qk_norm_rope", "cs_paged_workspace_bytes", "cs_paged_create", "cs_paged_destroy", "cs_paged_last_error",
+           "cs_rope_table", "cs_qk_norm_rope", "cs_paged_workspace_bytes", "cs_paged_create", "cs_paged_create_beside", "cs_paged_destroy", "cs_paged_last_error",
            "cs_paged_status", "cs_paged_append", "cs_paged_attention", "cs_paged_head_dim", "cs_paged_debug_drop_tile")
 
 _lib = None
@@ -174,6 +174,8 @@ def load(build_if_missing: bool = True) -> C.CDLL:
     lib.cs_paged_workspace_bytes.argtypes = [C.POINTER(CsPagedConfig)]
     lib.cs_paged_create.restype = i
     lib.cs_paged_create.argtypes = [C.POINTER(C.c_void_p), C.POINTER(CsPagedConfig), vp, C.c_size_t, vp]
+    lib.cs_paged_create_beside.restype = i
+    lib.cs_paged_create_beside.argtypes = [C.POINTER(C.c_void_p), C.POINTER(CsPagedConfig), vp]
     lib.cs_paged_destroy.restype = None
     lib.cs_paged_destroy.argtypes = [vp]
     lib.cs_paged_last_error.restype = C.c_char_p
@@ -668,7 +670,11 @@ def cs_qk_norm_rope(q, k, pos, rope, q_gain=None, k_gain=None, eps=1e-5, dtype=N
 class PagedCache:
     """One layer's paged KV cache: k_pages and v_pages are the caller's pools [n_pages][Hkv][page_size][D] (bf16 or fp16; any
     order of the strides, the same in both, heads contiguous), kept alive here.  Owns the workspace and the handle; caches of several layers whose work is on one stream
-    may share a workspace (`workspace`: another PagedCache).
+    may share a workspace (`workspace`: another PagedCache), and then what cs_paged_status says.
+
+    Pieces of work that several SMs share meet in the workspace, so the calls of one workspace must be on one stream at a time (or wait for one
+    another): side by side they would mix up each other's results.  A server that overlaps prompts and decoding on two streams makes two caches over the same pools, a
+    workspace each.  The workspace is cleared on the stream that is current here; a first call on another one must wait for it.
 
     Blocks of rows are given by three int32 CUDA tensors [B]: sequence b's block is the rows block_start[b] .. block_start[b] +
     block_len[b] - 1 of the tensors of rows and begins at position kv_len[b]; page_table [B][pages] int32 says where
@@ -689,18 +695,19 @@ class PagedCache:
         self.dtype, self.scale = k_pages.dtype, k_pages.shape[3] ** -0.5
         self.c_cfg = CsPagedConfig(k_pages.data_ptr(), v_pages.data_ptr(), st[0], st[1], st[2], n, s, h, d, _DTYPE[self.dtype])
         with torch.cuda.device(k_pages.device):
+            self.handle, call = C.c_void_p(), "cs_paged_create"
             if workspace is None:
                 nbytes = self.lib.cs_paged_workspace_bytes(C.byref(self.c_cfg))
                 self.workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=k_pages.device)
+                rc = self.lib.cs_paged_create(C.byref(self.handle), C.byref(self.c_cfg), self.workspace.data_ptr(), self.workspace.numel(), _stream())
             else:
-                self.workspace = workspace.workspace
+                self.workspace, call = workspace.workspace, "cs_paged_create_beside"
                 if self.workspace.device != k_pages.device:
                     raise ValueError("the workspace is another device's")
-            self.handle = C.c_void_p()
-            rc = self.lib.cs_paged_create(C.byref(self.handle), C.byref(self.c_cfg), self.workspace.data_ptr(), self.workspace.numel(), _stream())
+                rc = self.lib.cs_paged_create_beside(C.byref(self.handle), C.byref(self.c_cfg), workspace.handle)
         if rc != CS_OK:
             msg = self.lib.cs_paged_last_error(None)
-            raise CsError(rc, "cs_paged_create", msg.decode() if msg else "")
+            raise CsError(rc, call, msg.decode() if msg else "")
         self.device = k_pages.device
         self._id = (self.handle.value, _DTYPE[self.dtype], self.device.index)
 

@@ -454,9 +454,11 @@ size_t cs_paged_workspace_bytes(const cs_paged_config* cfg) {
   return check_config(cfg, &why) == CS_OK ? layout_of(*cfg).total : 0;
 }
 
-cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void* workspace, size_t workspace_bytes, void* stream) {
-  auto refuse = [](cs_status s, const char* text) {
-    snprintf(t_paged_err, sizeof(t_paged_err), "cs_paged_create: %s", text);
+namespace {
+// `clear`: the workspace is nobody's yet
+cs_status create(const char* name, cs_paged_cache** out, const cs_paged_config* cfg, void* workspace, size_t workspace_bytes, bool clear, void* stream) {
+  auto refuse = [&](cs_status s, const char* text) {
+    snprintf(t_paged_err, sizeof(t_paged_err), "%s: %s", name, text);
     return s;
   };
   t_paged_err[0] = 0;
@@ -483,6 +485,8 @@ cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void
   while ((1 << shift) < cfg->page_size) ++shift;
   c->view = PagedView{static_cast<char*>(cfg->k), static_cast<char*>(cfg->v), cfg->page_stride, cfg->head_stride, cfg->slot_stride, cfg->n_pages, cfg->page_size, shift, cfg->n_kv_heads};
   char* ws = static_cast<char*>(workspace);
+  c->workspace = workspace;
+  c->workspace_bytes = workspace_bytes;
   c->status = reinterpret_cast<int*>(ws + l.status);
   c->counters = reinterpret_cast<int*>(ws + l.counters);
   c->splits = reinterpret_cast<PagedSplit*>(ws + l.splits);
@@ -492,17 +496,26 @@ cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void
   const long long us = wl != nullptr ? atoll(wl) : 0;
   c->wait_limit_ns = us > 0 ? (unsigned long long)us * 1000ull : 2000000000ull;
   if (cs_paged_tc_maps(c) != CS_OK) {
-    snprintf(t_paged_err, sizeof(t_paged_err), "cs_paged_create: %.200s", c->err);
+    snprintf(t_paged_err, sizeof(t_paged_err), "%s: %.200s", name, c->err);
     free(c);
     return CS_ERR_CUDA;
   }
-  const cudaError_t e = cudaMemsetAsync(ws, 0, l.parts, static_cast<cudaStream_t>(stream));
+  const cudaError_t e = clear ? cudaMemsetAsync(ws, 0, l.parts, static_cast<cudaStream_t>(stream)) : cudaSuccess;
   if (e != cudaSuccess) {
     free(c);
     return refuse(CS_ERR_CUDA, cudaGetErrorString(e));
   }
   *out = c;
   return CS_OK;
+}
+}  // namespace
+
+cs_status cs_paged_create(cs_paged_cache** out, const cs_paged_config* cfg, void* workspace, size_t workspace_bytes, void* stream) {
+  return create("cs_paged_create", out, cfg, workspace, workspace_bytes, true, stream);
+}
+
+cs_status cs_paged_create_beside(cs_paged_cache** out, const cs_paged_config* cfg, const cs_paged_cache* first) {
+  return create("cs_paged_create_beside", out, cfg, first != nullptr ? first->workspace : nullptr, first != nullptr ? first->workspace_bytes : 0, false, nullptr);
 }
 
 void cs_paged_destroy(cs_paged_cache* cache) { free(cache); }

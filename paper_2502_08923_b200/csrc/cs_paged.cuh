@@ -34,6 +34,8 @@ struct cs_paged_cache {
   cs_paged_config cfg;
   PagedView view;
   CUtensorMap tmK, tmV;        // [page][head][slot][dim], boxes of up to 64 dims x up to 128 slots
+  void* workspace;
+  size_t workspace_bytes;
   int* status;                 // device status word
   int* counters;               // pieces of an item that are done, by the CTA that holds its first tile; 0 between launches
   PagedSplit* splits;          // of the last launch on the tensor cores, by CTA [kPagedMaxCtas]
