@@ -106,7 +106,7 @@ k_paged_few(PagedAttnArgs a) {
   bool f_more = true;
   // page-table entries of this warp's slices of the next 32 tiles, one per lane: asked for a slice before the first is needed
   auto entries = [&]() {
-    const int k = (f.tile0 + f_tile + lane) * kPagedTile + warp * kSlice;
+    const long long k = (long long)(f.tile0 + f_tile + lane) * kPagedTile + warp * kSlice;      // (the last lanes' may lie behind 2^31)
     f_entry = k < f.hi && k + kSlice > f.lo ? __ldcg(a.blk.table + (long long)f.seq * a.blk.table_width + (k >> a.kv.page_shift)) : 0;
   };
   const long long lane_off = (lane / CPR * a.kv.slot_stride + lane % CPR * 8) * 2, hop = 32 / CPR * a.kv.slot_stride * 2;   // this lane's chunks of a slice, bytes

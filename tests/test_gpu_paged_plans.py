@@ -49,6 +49,34 @@ def test_long_contexts(D, lens, cached):
     run(Case(lens, cached, 2, 1, D, page=256, seed=len(lens)))
 
 
+@pytest.mark.parametrize("lens", [[1], [4], [100]])
+@pytest.mark.parametrize("append", [False, True])
+def test_positions_next_to_2_to_the_31(lens, append):
+    """The last positions that a call takes, behind a window: every page of the table is the same one."""
+    page, n, window = 1 << 20, lens[0], 300
+    last = 0x7fffff00
+    kp, vp = (torch.randn(1, 1, page, 32, device="cuda").to(BF) for _ in range(2))
+    table = torch.zeros(1, -(-last // page), dtype=torch.int32, device="cuda")
+    q, new = (torch.randn(n, h, 32, device="cuda").to(BF) for h in (4, 1))
+    blocks = (torch.zeros(1, dtype=torch.int32, device="cuda"), *(torch.tensor([x], dtype=torch.int32, device="cuda") for x in (n, last - n)), table)
+    cache = cs.PagedCache(kp, vp)
+    at = [(last - n + r) % page for r in range(n)]
+    if append:
+        cache.cs_paged_append(new, -new, *blocks)
+        assert torch.equal(kp[0, 0, at], new[:, 0]) and torch.equal(vp[0, 0, at], -new[:, 0])
+    out, lse = cache.cs_paged_attention(q, *blocks, window=window, with_lse=True)
+    assert cache.cs_paged_status() == cs.CS_OK
+    for r in range(n):
+        keys = torch.arange(last - n + r + 1 - window, last - n + r + 1, device="cuda") % page
+        k, v = kp[0, 0, keys].double(), vp[0, 0, keys].double()
+        x = q[r].double() @ k.T * 32 ** -0.5
+        w = torch.softmax(x, dim=1)
+        want, size = w @ v, w @ v.abs()
+        u = U[BF]
+        assert bool(((out[r].double() - want).abs() <= u * want.abs() * (1 + u) + (u + 1e-4) * size + 2.0 ** -24).all())
+        assert float((lse[r].double() - torch.logsumexp(x, dim=1)).abs().max()) <= 1e-4
+
+
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("lens,cached", [([200] + [1] * 150, [900] + [70] * 150), ([1] * 60 + [700], [40] * 60 + [100])])
 def test_a_chunk_beside_single_tokens(D, lens, cached):
