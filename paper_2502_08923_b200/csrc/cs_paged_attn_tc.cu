@@ -117,23 +117,6 @@ __device__ __forceinline__ void set_flag(uint32_t addr, uint32_t v) { asm volati
 __device__ __forceinline__ void or_flag(uint32_t addr, uint32_t v) { asm volatile("red.shared.or.b32 [%0], %1;" ::"r"(addr), "r"(v) : "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pack2(float lo, float hi) {
-  f32x2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-  return r;
-}
-__device__ __forceinline__ void unpack2(f32x2 r, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(r)); }
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
-  f32x2 d;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-  return d;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
-  f32x2 d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 __device__ __forceinline__ void store32b(void* dst, const uint32_t* v) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
@@ -186,37 +169,34 @@ __device__ __forceinline__ uint32_t finite_only(uint32_t w) {
 template <typename T>
 __device__ __noinline__ void add_odd(const PagedAttnArgs& a, const TcPiece& p, int n_tiles, int lo, int hi, int c0, void* dst, bool part) {
   const int last = min(hi, (p.tile0 + n_tiles) * kPagedTile);
-#pragma unroll 1
-  for (int c = 0; c < 32; c += 32) {
-    float sum[32] = {};
-    for (int key = max(lo, p.tile0 * kPagedTile); key < last; ++key) {
-      if (key >= p.all_lo && key < p.all_hi) {
-        key = p.all_hi - 1;
-        continue;
-      }
-      const int page = __ldcg(a.blk.table + (long long)p.seq * a.blk.table_width + (key >> a.kv.page_shift));
-      if ((unsigned)page >= (unsigned)a.kv.n_pages) continue;
-      const uint4* src = reinterpret_cast<const uint4*>(a.kv.v + (page * a.kv.page_stride + p.head * a.kv.head_stride + (long long)(key & (a.kv.page_size - 1)) * a.kv.slot_stride + c0 + c) * 2);
+  float sum[32] = {};
+  for (int key = max(lo, p.tile0 * kPagedTile); key < last; ++key) {
+    if (key >= p.all_lo && key < p.all_hi) {
+      key = p.all_hi - 1;
+      continue;
+    }
+    const int page = __ldcg(a.blk.table + (long long)p.seq * a.blk.table_width + (key >> a.kv.page_shift));
+    if ((unsigned)page >= (unsigned)a.kv.n_pages) continue;
+    const uint4* src = reinterpret_cast<const uint4*>(a.kv.v + (page * a.kv.page_stride + p.head * a.kv.head_stride + (long long)(key & (a.kv.page_size - 1)) * a.kv.slot_stride + c0) * 2);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint4 v = __ldcg(src + j);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    for (int j = 0; j < 4; ++j) {
+      const uint4 v = __ldcg(src + j);
+      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float2 x = PagedType<T>::unpack(w[i] ^ finite_only<T>(w[i]));
-          sum[8 * j + 2 * i] += x.x;
-          sum[8 * j + 2 * i + 1] += x.y;
-        }
+      for (int i = 0; i < 4; ++i) {
+        const float2 x = PagedType<T>::unpack(w[i] ^ finite_only<T>(w[i]));
+        sum[8 * j + 2 * i] += x.x;
+        sum[8 * j + 2 * i + 1] += x.y;
       }
     }
+  }
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-      if (sum[i] == 0.f) continue;
-      if (part) reinterpret_cast<float*>(dst)[c + i] += sum[i];
-      else {
-        unsigned short* o = reinterpret_cast<unsigned short*>(dst) + c + i;
-        *o = (unsigned short)PagedType<T>::pack(PagedType<T>::unpack(*o).x + sum[i], 0.f);
-      }
+  for (int i = 0; i < 32; ++i) {
+    if (sum[i] == 0.f) continue;
+    if (part) reinterpret_cast<float*>(dst)[i] += sum[i];
+    else {
+      unsigned short* o = reinterpret_cast<unsigned short*>(dst) + i;
+      *o = (unsigned short)PagedType<T>::pack(PagedType<T>::unpack(*o).x + sum[i], 0.f);
     }
   }
 }
