@@ -63,7 +63,8 @@ template <int DH> constexpr int kSoftmaxRegs = DH == 128 ? 224 : 216;
 constexpr int kCtl = 512;
 // Descriptors of pieces.  A slot that is still at a piece's results holds the others up four pieces on at the latest: the other slot waits for it at the next piece whose tiles the slots take in turn, but the
 // scores of the piece after that may be made (of one tile each, they need neither slot), which frees the queries and makes two more known.
-constexpr int kPieces = 8, kPieceBytes = 72;
+constexpr int kPieces = 8;
+constexpr int kPieceBytes = 72;
 template <int DH> constexpr int kTcSmem = 1024 + (kStages<DH> + 2) * kTileBytes<DH> + kCtl + 2 * kM * 8 + kPieces * kPieceBytes + (int)sizeof(PagedPlan);
 
 // Operand descriptors as in cs_tcgen.cuh, for rows of 128 or (heads of 32) 64 bytes: eight of them a group, and the swizzle as wide
