@@ -461,7 +461,9 @@ cs_status cs_lm_head_static(const void* X, const void* W, int rows, int vocab, i
  * dropped by not counting them.  Page-table entries behind the last position in use may be anything.
  *
  * Types: CS_BF16 and CS_F16 caches; everything is computed in 32 bits and rounded (to nearest even) once, when it is
- * stored.  Softmax weights enter their product with V in 16 bits (two terms of them in the kernel for few rows). */
+ * stored.  Queries are rounded to the cache's type before the attention, and softmax weights enter their product with V in 16 bits: as one term in
+ * the kernel for tall blocks, as two in the one for few rows (up to 16 query rows per KV head on the average of a call's sequences), so the last
+ * bits of a row depend on the blocks that it shares a call with.  The contiguous cache's path (cs_verify_step) carries both in two terms. */
 typedef enum { CS_BF16 = 0, CS_F16 = 1, CS_F32 = 2 } cs_dtype;
 
 typedef struct cs_paged_cache cs_paged_cache; /* opaque; host memory owned by the library */
@@ -532,7 +534,7 @@ int cs_paged_head_dim(const cs_paged_cache* cache); /* 0 for NULL */
 const char* cs_paged_last_error(const cs_paged_cache* cache);
 
 /* Waits for `stream`, then returns and clears what the device found wrong: CS_ERR_CAPACITY (a block that does not fit its
- * row of the page table, or positions behind the rotation table), CS_ERR_ARG (a negative length, rows outside the tensors,
+ * row of the page table, or positions behind the rotation table: appended rows of these are dropped, values and queries with them), CS_ERR_ARG (a negative length, rows outside the tensors,
  * a page that does not exist among those a block needs), CS_ERR_TIMEOUT.  Sequences that fail a check of lengths are left out: none of
  * their rows is written.  Where single pages do not exist, appended rows that belong there are dropped and
  * attention takes their keys and values for zeros. */
@@ -555,7 +557,7 @@ cs_status cs_paged_append(cs_paged_cache* cache, const cs_blocks* blocks, const 
  * scores are all -inf, gets zeros and lse -inf.  Keys and values outside the range that a row of its block attends to are
  * never looked at, whatever they hold; non-finite values at positions that a row does not attend to do not reach it.
  * n_heads a multiple of n_kv_heads, at most 128 per KV head.  scale > 0; window >= 0.  Async.
- * Results are reproducible from run to run.  Errors: CS_ERR_ARG, CS_ERR_SHAPE, CS_ERR_CUDA. */
+ * (Such values cost time: the kernel for tall blocks goes through the items in question twice.)  Results are reproducible from run to run.  Errors: CS_ERR_ARG, CS_ERR_SHAPE, CS_ERR_CUDA. */
 cs_status cs_paged_attention(cs_paged_cache* cache, const cs_blocks* blocks, const void* q, int64_t q_row_stride,
                              int64_t q_head_stride, int n_heads, cs_mask mask, int window, float scale, void* out,
                              float* lse, void* stream);

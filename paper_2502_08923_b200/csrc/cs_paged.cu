@@ -7,7 +7,7 @@
 // reduction over its lanes), and nothing is exchanged.  Warps take a row each, or 2, 4 or 8 share one where there are few; three units of 32 / (D / 16) heads are in flight, in
 // a ring of shared memory for each warp (in registers instead, four of them, 16 warps fit on an SM and not 20, and the setup is there four times: 34 us for the 29 below).
 //
-// Bound by HBM where there are many rows: 8,192 of the 8B shape 29.3 us (172 MB, 5.9 TB/s of the 6.5 that a copy reaches), an append of 6k rows 29.7 us (150 MB, 5.0).  With an
+// Bound by HBM where there are many rows: 8,192 of the 8B shape 29.3 us (172 MB, 5.9 TB/s of the 6.5 that a copy reaches), an append of 6k rows 30.0 us (150 MB, 5.0).  With an
 // element's partner in another lane, fetched by shuffles, and the factors worked out for each head 61 us.  Few rows: launch and a chain of loads (whose block is the row's, which
 // page and, at the same time, its rotation): 2.4 - 4.3 us.
 #include "cs_paged.cuh"
@@ -586,8 +586,9 @@ cs_status cs_paged_attention(cs_paged_cache* c, const cs_blocks* blocks, const v
   a.parts = c->parts; a.parts_ml = c->parts_ml; a.counters = c->counters; a.splits = c->splits; a.status = c->status;
   a.wait_ns = c->wait_limit_ns;
   a.drop = -1;
-  // 16 query rows per KV head are a tile of the kernel for few rows (on tensor cores / by it, us: 11 rows of the 8B shape over 1,024 keys 15.0 / 13.0, over 4,096 16.2 / 18.3, over
-  // 16,384 26.4 / 40.4; 16 x 5 over 1,024 28.8 / 36.2); queries that repeat one row have no operand map
+  // 16 query rows per KV head are a tile of the kernel for few rows, and the average is what the host knows: where blocks differ much, some are in the other kernel's hands, more slowly, and a row's weights
+  // are rounded as the kernel of its call does it.  (On tensor cores / by it, us: 11 rows of the 8B shape over 1,024 keys 15.0 / 13.0, over 4,096 16.0 / 18.3, over 16,384 26.4 / 40.4; 16 x 5 over 1,024
+  // 28.8 / 36.2.  By the first it would be the better one for short contexts with 44 rows too; how long they are stands on the device.)  Queries that repeat one row have no operand map
   const bool few = (long long)blocks->rows * a.group <= 16ll * blocks->n_seqs || (blocks->rows > 1 && q_row_stride <= 0) || (n_heads > 1 && q_head_stride <= 0);
   if (!few) {
     a.drop = c->drop;

@@ -1,5 +1,5 @@
 // Attention of few query rows per KV head over a paged KV cache: single tokens and short verification blocks
-// (Sec. 3.2; App. B.2), on mma.sync.  cs_paged_attention's dispatch is here as well.
+// (Sec. 3.2; App. B.2), on mma.sync.  (Which calls come here: cs_paged_attention in cs_paged.cu.)
 //
 // out = softmax(scale Q K^T) V by one pass over the keys with a running maximum m and sum l per row:
 //     m' = max(m, max_j s_j),  l' = l 2^(m - m') + sum_j 2^(s_j - m'),  O' = O 2^(m - m') + sum_j 2^(s_j - m') V_j   (base-2 scores).
@@ -18,8 +18,8 @@
 // values that are not finite, since 0 x inf is not 0: with any, the second product is done by plain arithmetic over the keys each row sees.
 //
 // Bound by HBM (K and V once) where the cache is long, by a chain of latencies (plan 1.5 us, piece 0.5, page entries and first slices 1.4, results 1.3, adding pieces up 4) where it is
-// short.  8B shape, bf16 or fp16: one token over 30,720 keys 29 us (126 MB, 19.2 at the copy rate; the keys themselves come in 18), 64 over 500 - 4,097 keys 72 us (404 MB, 62); the small model's 11
-// rows over 512 keys 7.9 us.  What made it: queries fetched with their piece instead of behind all keys in flight (3 us a piece), shared items settled after the run and added up from shared
+// short.  8B shape, bf16 or fp16: one token over 30,720 keys 29 us (126 MB, 19.2 at the copy rate; the keys themselves come in 18), 64 over 500 - 4,097 keys 72 us (404 MB, 62; 78 among calls on other caches); the small model's 11
+// rows over 512 keys 8.0 us.  What made it: queries fetched with their piece instead of behind all keys in flight (3 us a piece), shared items settled after the run and added up from shared
 // memory (10 -> 4 us), two places of the line for changing items.  ex2 and the products take a third of the issue slots at most.
 #include <type_traits>
 

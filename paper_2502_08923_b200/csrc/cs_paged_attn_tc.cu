@@ -27,11 +27,11 @@
 // Every wait is bounded: on expiry the CTA flags CS_DEV_TIMEOUT, stops issuing, walks through its barriers, drains what is in flight, frees its TMEM and returns.  Items that it had not
 // finished, shared ones among them whatever their other CTAs have done, stay unwritten.
 //
-// What bounds it.  Long chunks: 3,350 clocks for a pair of 128 x 128 tiles with heads of 128, of which the products take 2,048 at their peak rate; a slot's chain is scores into registers
-// 190, maxima 300, weights 1,200 (ex2, 16 a clock, is 1,024 of it), into tensor memory 200, product 512, next scores 512, hand-overs 400.  A 2,048-row chunk behind 30,720
-// keys of the 8B shape: 0.94 ms in short runs (1.13 PFLOP/s), 1.08 ms at the power cap (1.49 GHz, 990 W).  Heads of 64: 3,700 clocks a pair, all of it the softmax warps' way through their instructions (two warps a scheduler, one
-// instruction in three clocks, no unit above 35 %): 8 x 21 rows over 16,384 keys 65 us, 63.5 without the exponentials, 65 with half of the products, 64 with all pages in L2.  11 rows over 4,096 keys 16 us, a chain of latencies (plan and piece 1.5, page entries,
-// first tiles 3, one step 1.8, results 1.4, sums of pieces 5).
+// What bounds it.  Long chunks: 2,950 clocks for a pair of 128 x 128 tiles with heads of 128 (1,184 rows, what 4,096 to 16,384 keys differ by), of which the products take 2,048 at their peak rate.  A slot's chain, measured with some
+// registers spilled and 3,350 a pair: scores into registers 190, maxima 300, weights 1,200 (ex2, 16 a clock, is 1,024 of it), into tensor memory 200, product 512, next scores 512, hand-overs 400.  A 2,048-row chunk
+// behind 30,720 keys of the 8B shape: 0.91 ms in short runs (1.17 PFLOP/s), 1.03 - 1.06 ms at the power cap (1.49 GHz, 990 W).  Heads of 64: 2,700 clocks a pair, all of it the softmax warps' way through their instructions (two
+// warps a scheduler, one instruction in three clocks, no unit above 35 %): 8 x 21 rows over 16,384 keys 64 us; measured at 65: 63.5 without the exponentials, 65 with half of the products, 64 with all pages in L2.  11 rows over
+// 4,096 keys 16 us, a chain of latencies (plan and piece 1.5, page entries, first tiles 3, one step 1.8, results 1.4, sums of pieces 5).
 // Tried and not kept: maxima left out, with reference points that follow the sums (3,350 -> 3,400 clocks: they hide behind ex2); a quarter of the exponentials by a polynomial in
 // packed arithmetic (-2 % of the clocks, +1 % of the time at the power cap); products with the first 64 keys only when all weights are there (no slower by themselves); sixteen softmax
 // warps, two to a row with half of the keys each (104 registers; heads of 128 166 -> 180 us for 1,184 rows over 8,192 keys, heads of 64 138 -> 145: a barrier a tile for the common reference
@@ -998,7 +998,7 @@ cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& args, cudaS
   const int tokens = kM / a.group;                 // rows of the block in a slot, with all heads of the group
   a.item_rows = 2 * tokens * a.group;
   a.by_item_rows = PagedDivisor::by(a.item_rows);
-  a.item_cost = 2;                                 // (one: the three windowed chunks 111 us instead of 109)
+  a.item_cost = 2;                                 // (one: 2 us more for the three windowed chunks)
   a.keep = 5;                                      // (a step takes 0.9 us, adding pieces up 5)
   const int box_rows = tokens < a.blk.rows ? tokens : a.blk.rows, dh = c->cfg.head_dim;
   CUtensorMap tmQ;
