@@ -282,13 +282,14 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     return i + min(i + ahead, tiles);
   };
 
-  // The end of a pass, where all roles meet once, whatever has become of their waits: is there a second one?
+  // The end of a pass, where all roles meet once, whatever has become of their waits: is there a second one?  Only if no role has given up: one that has leaves here, and must not be
+  // waited for again.  (Nobody adds to f_odd between here and a second pass.)
   auto again = [&](bool second) -> bool {
-    uint32_t odd;
+    uint32_t fine;
     fence_before();
-    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %1, 0;\nbar.red.or.pred q, 0, p;\nselp.u32 %0, 1, 0, q;\n}" : "=r"(odd) : "r"(flag(f_odd)) : "memory");
+    asm volatile("{\n.reg .pred p, q;\nsetp.eq.b32 p, %1, 0;\nbar.red.and.pred q, 0, p;\nselp.u32 %0, 1, 0, q;\n}" : "=r"(fine) : "r"(flag(f_abort)) : "memory");
     fence_after();
-    return !second && odd != 0;
+    return !second && fine != 0 && flag(f_odd) != 0;
   };
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs<DH>));

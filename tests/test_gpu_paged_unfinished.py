@@ -55,3 +55,29 @@ def test_in_the_middle_of_a_run(D, tile, lens, cached, Hkv, monkeypatch):
     assert bool(left.any())
     if lens == [200] and tile < 3:                        # items of 71 tiles and more, no CTA gets as far as the end of one
         assert bool(left.all())
+
+
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("tile", [1, 3, 6])
+def test_with_a_second_pass_to_come(D, tile, monkeypatch):
+    """CTAs that give up after results that are not finite, which would have them go through those items again: they do not, and nobody waits."""
+    monkeypatch.setenv("CS_WAIT_LIMIT_US", "2000")
+    lens = [20] * 200                                     # items of one to three tiles: some are done before the tile that does not come
+    case = Case(lens, [(29 * b) % 300 for b in range(200)], 32, 8, D, seed=tile)
+    for b in range(0, 200, 3):
+        case.v[b][case.cached[b] + 10, :, 1] = float("nan")
+        case.put(b)
+    cache = cs.PagedCache(case.kp, case.vp)
+    good = cache.cs_paged_attention(case.q, *case.blocks(), with_lse=True)
+    assert cache.cs_paged_status() == cs.CS_OK
+    out, lse = torch.full_like(case.q, 7.0), torch.full(case.q.shape[:2], 7.0, device="cuda")
+    cache.cs_paged_debug_drop_tile(tile)
+    cache.cs_paged_attention(case.q, *case.blocks(), out=out, lse=lse)
+    assert cache.cs_paged_status() == cs.CS_ERR_TIMEOUT and cache.cs_paged_status() == cs.CS_OK
+    # rows of sequences without such values are as they should be, or as they were
+    clean = torch.tensor([r for b in range(200) if b % 3 for r in range(case.starts[b], case.starts[b] + 20)], device="cuda")
+    left = (out == 7.0).all(dim=-1) & (lse == 7.0)
+    assert bool(left.any()) and bool((left | ((out == good[0]).all(dim=-1) & (lse == good[1])))[clean].all())
+    again = cache.cs_paged_attention(case.q, *case.blocks(), with_lse=True)
+    assert cache.cs_paged_status() == cs.CS_OK
+    assert torch.equal(again[0].view(torch.int16), good[0].view(torch.int16)) and torch.equal(again[1], good[1])

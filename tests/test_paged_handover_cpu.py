@@ -146,3 +146,14 @@ def test_descriptors_outlive_the_slot_that_lags(apart):
                 assert not run.run() and run.passed[2 + slot] == at
                 furthest = max(furthest, run.published)
     assert furthest == 4 and furthest < places, (furthest, places)
+
+
+def test_a_second_pass_is_agreed_on():
+    """Where a pass ends all roles meet.  One whose wait has run out leaves there, so the others may go on to a second pass, and to its end, only if the
+    meeting itself has found that none has: a flag looked at before or after it may be another one for every role."""
+    body = _kernel("cs_paged_attn_tc.cu", "k_paged_tc")
+    again = re.search(r"auto again = \[&\]\(bool second\) -> bool \{(.*?)\n  \};", body, flags=re.S).group(1)
+    asked = re.search(r"setp\.eq\.b32 p, %1, 0;\\n(bar\.red\.and\.pred) q, 0, p;.*?: \"=r\"\((\w+)\) : \"r\"\(flag\(f_abort\)\)", again, flags=re.S)
+    assert asked and re.search(rf"return !second && {asked.group(2)} != 0 &&", again)
+    # every way out of a role's loop comes by exactly one meeting: the one at a pass's end, or the one behind the loop
+    assert body.count("if (!met) again(true);") == 2 and body.count("met = true;") == 4 and len(re.findall(r"\bagain\(", body)) == 6
