@@ -567,6 +567,67 @@ cs_status cs_paged_attention(cs_paged_cache* cache, const cs_blocks* blocks, con
  * products in flight end, the rows it had not finished stay as they were (with those of other CTAs that share an item with it), cs_paged_status reports CS_ERR_TIMEOUT.  Calls of few rows have no such waits.  tile < 0 clears it. */
 cs_status cs_paged_debug_drop_tile(cs_paged_cache* cache, int tile);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators around a paged KV cache held in 4 bits: 4.5 bits a value instead of 16, for servers whose contexts fill the memory or whose decoding waits for it (the paper has no
+ * counterpart; blocks, masks and page tables are those of the paged cache above).
+ *
+ * A row (one position, one KV head) is cut into groups of 32 neighbouring elements.  With a = max |x| of a group, s = a / 7 rounded to five significant bits (nearest, halves to even; at most 2^123)
+ * and n = x / s rounded to the nearest whole number (halves to even), |n| <= 7, the group is held as s in bf16 and numbers n + 8 of 4 bits, and stands for s n.  No element is off by more than s / 2 (but for
+ * scales below 2^-126 or at the limit, beyond which values saturate); every value held is exactly a bf16 number.  A group with an element that is not finite has the scale NaN and reads as NaN throughout, as does any scale that is not finite.  Zeros stay zeros.
+ *
+ * Pools, for K and for V: numbers, of page `p`, KV head `h`, slot `s` from byte p * page_stride + (h * page_size + s) * head_dim / 2 on, and bf16 scales from element
+ * p * scale_page_stride + (h * page_size + s) * head_dim / 32 on.  Eight elements are a 32-bit word; its elements 2i and 2i + 1 are at bits 4i and 16 + 4i.  16-byte aligned, strides multiples of 16
+ * bytes.  Numbers 0 (-8) may be there as well as 1 to 15.  Scales of more than five significant bits are read with a rounding.
+ *
+ * Blocks of more than some 96 query rows per KV head (rows of the block x heads of the group, on the average of a call's sequences) are worked out from copies in 16 bits, made by the call in the workspace, where
+ * the positions that the page table has room for (n_seqs x table_width x page_size) are not more than tall_positions; without that room they take the way of short blocks, which is several
+ * times slower for long chunks.  Copies for fp16 queries saturate at 65504. */
+typedef struct cs_quant_cache cs_quant_cache; /* opaque; host memory owned by the library */
+
+typedef struct {
+  void *k, *v;                                    /* numbers                                                */
+  void *k_scale, *v_scale;                        /* scales                                                 */
+  int64_t page_stride, scale_page_stride;         /* bytes; elements                                        */
+  int32_t n_pages, page_size;                     /* page_size a power of two from 16 on                    */
+  int32_t n_kv_heads, head_dim;                   /* head_dim 32, 64 or 128                                 */
+  int64_t tall_positions;                         /* room for copies: 4 * head_dim * n_kv_heads bytes each  */
+} cs_quant_config;
+
+/* Bytes of device workspace cs_quant_create needs (0 on a bad configuration).  Host-only arithmetic; needs no GPU. */
+size_t cs_quant_workspace_bytes(const cs_quant_config* cfg);
+
+/* As cs_paged_create and cs_paged_create_beside: `workspace` is 256-byte aligned, of at least cs_quant_workspace_bytes(cfg) bytes; its counters are cleared on `stream` (async); work of one
+ * workspace must stay on one stream at a time.  Caches that share a workspace need the same heads and tall_positions, and share what cs_quant_status says.
+ * Errors: CS_ERR_ARG, CS_ERR_SHAPE, CS_ERR_CAPACITY, CS_ERR_CUDA; the text is cs_quant_last_error(NULL). */
+cs_status cs_quant_create(cs_quant_cache** out, const cs_quant_config* cfg, void* workspace, size_t workspace_bytes,
+                          void* stream);
+cs_status cs_quant_create_beside(cs_quant_cache** out, const cs_quant_config* cfg, const cs_quant_cache* first);
+void cs_quant_destroy(cs_quant_cache* cache);
+int cs_quant_head_dim(const cs_quant_cache* cache); /* 0 for NULL */
+const char* cs_quant_last_error(const cs_quant_cache* cache);
+
+/* As cs_paged_status. */
+cs_status cs_quant_status(cs_quant_cache* cache, void* stream);
+
+/* As cs_paged_append, quantising: keys are normed with their gain and rotated, then quantised in their pages (the level is that of the exact result: what is normed or rotated is
+ * worked out in 64 bits), values are quantised; with `q` the block's queries are normed and rotated into q->y.  `in`: type of q, k and v; `out`: CS_BF16 or CS_F16, type of q->y and of both gains;
+ * `in` is `out` or CS_F32.  k->y, v->y and v->gain are not used.  Async.  Errors: CS_ERR_ARG, CS_ERR_SHAPE, CS_ERR_CUDA. */
+cs_status cs_quant_append(cs_quant_cache* cache, const cs_blocks* blocks, const cs_heads* k, const cs_heads* v,
+                          const cs_heads* q, cs_dtype in, cs_dtype out, const float* rope, int n_positions, int rot_dim,
+                          float eps, void* stream);
+
+/* Reads back what the cache stands for at the blocks' positions: row start[b] + r of k->y and v->y, in type `out`, gets position kv_len[b] + r of sequence b, as cs_quant_append takes them.  (A whole
+ * sequence: kv_len 0 and its length.)  Rows of no block stay as they are; positions whose page does not exist read as zeros.  CS_F16 saturates at 65504.  k->x, v->x and the gains are not used.
+ * Async.  Errors: CS_ERR_ARG, CS_ERR_SHAPE, CS_ERR_CUDA. */
+cs_status cs_quant_read(cs_quant_cache* cache, const cs_blocks* blocks, const cs_heads* k, const cs_heads* v, cs_dtype out,
+                        void* stream);
+
+/* As cs_paged_attention, over the values that the cache stands for.  `dtype`: type of q and out, CS_BF16 or CS_F16.  Weights enter the product with V as two 16-bit terms, in calls of tall blocks with
+ * copies as one.  Async.  Errors: CS_ERR_ARG, CS_ERR_SHAPE, CS_ERR_CUDA. */
+cs_status cs_quant_attention(cs_quant_cache* cache, const cs_blocks* blocks, const void* q, int64_t q_row_stride,
+                             int64_t q_head_stride, int n_heads, cs_dtype dtype, cs_mask mask, int window, float scale,
+                             void* out, float* lse, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -58,6 +58,11 @@ class CsPagedConfig(C.Structure):
                [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim", "dtype")]
 
 
+class CsQuantConfig(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "k_scale", "v_scale")] + [(n, C.c_int64) for n in ("page_stride", "scale_page_stride")] + \
+               [(n, C.c_int32) for n in ("n_pages", "page_size", "n_kv_heads", "head_dim")] + [("tall_positions", C.c_int64)]
+
+
 class CsBlocks(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("start", "len", "kv_len", "page_table")] + \
                [(n, C.c_int32) for n in ("n_seqs", "table_width", "rows")]
@@ -76,7 +81,9 @@ EXPORTS = ("cs_workspace_bytes", "cs_create", "cs_destroy", "cs_last_error", "cs
            "cs_loop_launches_per_step", "cs_lm_head", "cs_lm_head_static", "cs_gram_index_bytes",
            "cs_gram_index_reset", "cs_gram_index_update", "cs_find_match_indexed", "cs_gram_index_status",
            "cs_rope_table", "cs_qk_norm_rope", "cs_paged_workspace_bytes", "cs_paged_create", "cs_paged_create_beside", "cs_paged_destroy", "cs_paged_last_error",
-           "cs_paged_status", "cs_paged_append", "cs_paged_attention", "cs_paged_head_dim", "cs_paged_debug_drop_tile")
+           "cs_paged_status", "cs_paged_append", "cs_paged_attention", "cs_paged_head_dim", "cs_paged_debug_drop_tile",
+           "cs_quant_workspace_bytes", "cs_quant_create", "cs_quant_create_beside", "cs_quant_destroy", "cs_quant_head_dim", "cs_quant_last_error", "cs_quant_status",
+           "cs_quant_append", "cs_quant_read", "cs_quant_attention")
 
 _lib = None
 _search = None      # cs_find_match in native code, for plain arguments
@@ -190,6 +197,26 @@ def load(build_if_missing: bool = True) -> C.CDLL:
     lib.cs_paged_append.argtypes = [vp, blocks, heads, heads, heads, i, vp, i, i, f, vp]
     lib.cs_paged_attention.restype = i
     lib.cs_paged_attention.argtypes = [vp, blocks, vp, ll, ll, i, i, i, f, vp, vp, vp]
+    lib.cs_quant_workspace_bytes.restype = C.c_size_t
+    lib.cs_quant_workspace_bytes.argtypes = [C.POINTER(CsQuantConfig)]
+    lib.cs_quant_create.restype = i
+    lib.cs_quant_create.argtypes = [C.POINTER(C.c_void_p), C.POINTER(CsQuantConfig), vp, C.c_size_t, vp]
+    lib.cs_quant_create_beside.restype = i
+    lib.cs_quant_create_beside.argtypes = [C.POINTER(C.c_void_p), C.POINTER(CsQuantConfig), vp]
+    lib.cs_quant_destroy.restype = None
+    lib.cs_quant_destroy.argtypes = [vp]
+    lib.cs_quant_head_dim.restype = i
+    lib.cs_quant_head_dim.argtypes = [vp]
+    lib.cs_quant_last_error.restype = C.c_char_p
+    lib.cs_quant_last_error.argtypes = [vp]
+    lib.cs_quant_status.restype = i
+    lib.cs_quant_status.argtypes = [vp, vp]
+    lib.cs_quant_append.restype = i
+    lib.cs_quant_append.argtypes = [vp, blocks, heads, heads, heads, i, i, vp, i, i, f, vp]
+    lib.cs_quant_read.restype = i
+    lib.cs_quant_read.argtypes = [vp, blocks, heads, heads, i, vp]
+    lib.cs_quant_attention.restype = i
+    lib.cs_quant_attention.argtypes = [vp, blocks, vp, ll, ll, i, i, i, i, f, vp, vp, vp]
     _search = _native_search()
     _lib = lib
     return lib
@@ -667,6 +694,13 @@ def cs_qk_norm_rope(q, k, pos, rope, q_gain=None, k_gain=None, eps=1e-5, dtype=N
     return out
 
 
+def _blocks(start, length, kv_len, table, rows):
+    B = start.shape[0]
+    if length.shape != (B,) or kv_len.shape != (B,) or start.dim() != 1 or table.dim() != 2 or table.shape[0] != B:
+        raise ValueError("block_start, block_len and kv_len must be [B], page_table [B][pages]")
+    return CsBlocks(_i32(start, "block_start"), _i32(length, "block_len"), _i32(kv_len, "kv_len"), _i32(table, "page_table"), B, table.shape[1], rows)
+
+
 class PagedCache:
     """One layer's paged KV cache: k_pages and v_pages are the caller's pools [n_pages][Hkv][page_size][D] (bf16 or fp16; any
     order of the strides, the same in both, heads contiguous), kept alive here.  Owns the workspace and the handle; caches of several layers whose work is on one stream
@@ -727,12 +761,6 @@ class PagedCache:
             msg = self.lib.cs_paged_last_error(self.handle)
             raise CsError(rc, where, msg.decode() if msg else "")
 
-    def _blocks(self, start, length, kv_len, table, rows):
-        B = start.shape[0]
-        if length.shape != (B,) or kv_len.shape != (B,) or start.dim() != 1 or table.dim() != 2 or table.shape[0] != B:
-            raise ValueError("block_start, block_len and kv_len must be [B], page_table [B][pages]")
-        return CsBlocks(_i32(start, "block_start"), _i32(length, "block_len"), _i32(kv_len, "kv_len"), _i32(table, "page_table"), B, table.shape[1], rows)
-
     def cs_paged_append(self, k, v, block_start, block_len, kv_len, page_table, rope=None, k_gain=None, q=None, q_gain=None, eps=1e-5, q_out=None):
         """Appends the blocks' keys (normed where there is a gain, rotated) and values [rows][Hkv][D] to their pages; with `q`
         [rows][H][D] norms and rotates the block's queries in the same launch and returns them in the cache's type."""
@@ -749,7 +777,7 @@ class PagedCache:
         if q is not None and q_out is None:
             q_out = torch.empty(q.shape, dtype=self.dtype, device=q.device)
         hk, hv, hq = _heads(k, None, k_gain, self.dtype, "k"), _heads(v, None, None, self.dtype, "v"), _heads(q, q_out, q_gain, self.dtype, "q")
-        blocks = self._blocks(block_start, block_len, kv_len, page_table, k.shape[0])
+        blocks = _blocks(block_start, block_len, kv_len, page_table, k.shape[0])
         table, n, rot = _table(rope)
         with torch.cuda.device(self.device):
             rc = self.lib.cs_paged_append(self.handle, blocks, hk, hv, hq, _DTYPE[k.dtype], table, n, rot, eps, _stream())
@@ -782,7 +810,7 @@ class PagedCache:
             lse = torch.empty(T, H, dtype=torch.float32, device=q.device)
         elif lse is not None and (lse.shape != (T, H) or lse.dtype is not torch.float32 or not lse.is_cuda or not lse.is_contiguous()):
             raise ValueError("lse must be a contiguous fp32 CUDA tensor [rows][heads]")
-        blocks = self._blocks(block_start, block_len, kv_len, page_table, T)
+        blocks = _blocks(block_start, block_len, kv_len, page_table, T)
         with torch.cuda.device(self.device):
             rc = self.lib.cs_paged_attention(self.handle, blocks, ptr, row, head, H, mask, window, self.scale if scale is None else scale, out.data_ptr(),
                                              None if lse is None else lse.data_ptr(), _stream())
@@ -796,3 +824,162 @@ class PagedCache:
 
     def cs_paged_debug_drop_tile(self, tile):
         self._check(self.lib.cs_paged_debug_drop_tile(self.handle, tile), "cs_paged_debug_drop_tile")
+
+
+# ------------------------------------------------------------------ operators around a paged KV cache held in 4 bits
+class QuantCache:
+    """One layer's paged KV cache in 4 bits: k_data and v_data are the caller's pools [n_pages][Hkv][page_size][D / 2] uint8, k_scale and v_scale [n_pages][Hkv][page_size][D / 32] bf16
+    (the format stands in the C header), kept alive here.  Pages may lie apart (any stride between them, the same for K and V), everything within a page is contiguous.  `QuantCache.empty` makes pools as well.
+
+    `tall_positions`: room in the workspace for copies in 16 bits of the positions that a call of tall blocks (prompts' chunks) attends to, 4 * D * Hkv bytes each; what counts is the room of the call's page
+    table, n_seqs x width x page_size.  Caches of several layers whose work is on one stream may share a workspace (`workspace`: another QuantCache of the same heads and tall_positions, which are taken from it), and then
+    what cs_quant_status says.  As with PagedCache, the calls of one workspace must be on one stream at a time.
+
+    Blocks of rows are given as to PagedCache."""
+
+    def __init__(self, k_data, v_data, k_scale, v_scale, tall_positions=0, workspace=None):
+        for name, x, dtype in (("k_data", k_data, torch.uint8), ("v_data", v_data, torch.uint8), ("k_scale", k_scale, torch.bfloat16), ("v_scale", v_scale, torch.bfloat16)):
+            if not x.is_cuda or x.dim() != 4 or x.dtype != dtype:
+                raise ValueError(f"{name} must be a CUDA tensor of four dimensions and type {dtype}")
+            if x.device != k_data.device or (x.shape[0] > 0 and not x[0].is_contiguous()):
+                raise ValueError("all pools must be on one device, each page contiguous")
+        n, h, s, half = k_data.shape
+        if v_data.shape != k_data.shape or k_scale.shape != (n, h, s, half // 16) or v_scale.shape != k_scale.shape or half % 16 != 0:
+            raise ValueError("pools must be [n_pages][heads][page_size][D / 2], scales [n_pages][heads][page_size][D / 32]")
+        if n > 1 and (v_data.stride(0) != k_data.stride(0) or v_scale.stride(0) != k_scale.stride(0)):
+            raise ValueError("K and V must have the same strides")
+        self.lib = load()
+        self.k_data, self.v_data, self.k_scale, self.v_scale = k_data, v_data, k_scale, v_scale
+        self.head_dim, self.n_kv_heads, self.device, self.scale = 2 * half, h, k_data.device, (2 * half) ** -0.5 if half else 0.0
+        self.tall_positions = tall_positions if workspace is None else workspace.tall_positions
+        # (a stride that no second page uses may be anything)
+        strides = (k_data.stride(0), k_scale.stride(0)) if n > 1 else (h * s * half, h * s * (half // 16))
+        self.c_cfg = CsQuantConfig(k_data.data_ptr(), v_data.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), *strides, n, s, h, 2 * half, self.tall_positions)
+        with torch.cuda.device(self.device):
+            self.handle, call = C.c_void_p(), "cs_quant_create"
+            if workspace is None:
+                nbytes = self.lib.cs_quant_workspace_bytes(C.byref(self.c_cfg))
+                self.workspace = torch.empty(max(nbytes, 1), dtype=torch.uint8, device=self.device)
+                rc = self.lib.cs_quant_create(C.byref(self.handle), C.byref(self.c_cfg), self.workspace.data_ptr(), self.workspace.numel(), _stream())
+            else:
+                self.workspace, call = workspace.workspace, "cs_quant_create_beside"
+                if self.workspace.device != self.device:
+                    raise ValueError("the workspace is another device's")
+                rc = self.lib.cs_quant_create_beside(C.byref(self.handle), C.byref(self.c_cfg), workspace.handle)
+        if rc != CS_OK:
+            msg = self.lib.cs_quant_last_error(None)
+            raise CsError(rc, call, msg.decode() if msg else "")
+        self._id = (self.handle.value, self.device.index)
+
+    @classmethod
+    def empty(cls, n_pages, n_kv_heads, page_size, head_dim, tall_positions=0, workspace=None, device="cuda"):
+        """A cache with pools of its own, of zeros."""
+        data = torch.full((2, n_pages, n_kv_heads, page_size, head_dim // 2), 0x88, dtype=torch.uint8, device=device)
+        scale = torch.zeros(2, n_pages, n_kv_heads, page_size, head_dim // 32, dtype=torch.bfloat16, device=device)
+        return cls(data[0], data[1], scale[0], scale[1], tall_positions, workspace)
+
+    def close(self):
+        if getattr(self, "handle", None):
+            self.lib.cs_quant_destroy(self.handle)
+            self.handle, self._id = None, (0, -1)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _check(self, rc, where):
+        if rc != CS_OK:
+            msg = self.lib.cs_quant_last_error(self.handle)
+            raise CsError(rc, where, msg.decode() if msg else "")
+
+    def cs_quant_append(self, k, v, block_start, block_len, kv_len, page_table, rope=None, k_gain=None, q=None, q_gain=None, eps=1e-5, dtype=None, q_out=None):
+        """Quantises the blocks' keys (normed where there is a gain, rotated) and values [rows][Hkv][D] into their pages; with `q` [rows][H][D] norms and rotates the block's queries in the same
+        launch and returns them in `dtype` (bf16 or fp16, the gains' type too; default: the rows' type, bf16 for fp32 rows)."""
+        dtype = dtype or (torch.bfloat16 if k.dtype is torch.float32 else k.dtype)
+        if q_out is None and _native is not None:
+            got = _native.quant_append(*self._id, k, v, block_start, block_len, kv_len, page_table, rope, k_gain, q, q_gain, eps, _DTYPE.get(dtype, -1))
+            if got.__class__ is tuple:
+                return got[0]
+            if got is not None:
+                self._check(got, "cs_quant_append")
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("dtype must be bf16 or fp16")
+        d = self.head_dim
+        if k.dtype != v.dtype or k.shape != v.shape or k.dim() != 3 or k.shape[2] != d or (q is not None and (q.dtype != k.dtype or q.dim() != 3 or q.shape[0] != k.shape[0] or q.shape[2] != d)):
+            raise ValueError("q, k and v must have the same rows and type and the cache's head size")
+        _on(self.device, k=k, v=v, block_start=block_start, block_len=block_len, kv_len=kv_len, page_table=page_table, rope=rope, k_gain=k_gain, q=q, q_gain=q_gain, q_out=q_out)
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=dtype, device=q.device)
+        hk, hv, hq = _heads(k, None, k_gain, dtype, "k"), _heads(v, None, None, dtype, "v"), _heads(q, q_out, q_gain, dtype, "q")
+        blocks = _blocks(block_start, block_len, kv_len, page_table, k.shape[0])
+        table, n, rot = _table(rope)
+        with torch.cuda.device(self.device):
+            rc = self.lib.cs_quant_append(self.handle, blocks, hk, hv, hq, _DTYPE[k.dtype], _DTYPE[dtype], table, n, rot, eps, _stream())
+        self._check(rc, "cs_quant_append")
+        return q_out
+
+    def cs_quant_read(self, block_start, block_len, kv_len, page_table, rows=None, dtype=torch.bfloat16, out=None):
+        """What the cache stands for at the blocks' positions, as cs_quant_append takes them: (keys, values) [rows][Hkv][D] in `dtype` (bf16, fp16 or fp32).  `out` may supply those tensors (their type
+        and rows count then), of which rows of no block stay as they were; without it such rows hold anything."""
+        if out is None:
+            if rows is None:
+                raise ValueError("rows (or out) must say how many rows there are")
+            if _native is not None:
+                got = _native.quant_read(*self._id, self.n_kv_heads, self.head_dim, block_start, block_len, kv_len, page_table, rows, _DTYPE.get(dtype, -1))
+                if got.__class__ is tuple:
+                    return got
+                if got is not None:
+                    self._check(got, "cs_quant_read")
+            if dtype not in _DTYPE:
+                raise ValueError("bf16, fp16 and fp32 are known")
+            out = tuple(torch.empty(rows, self.n_kv_heads, self.head_dim, dtype=dtype, device=self.device) for _ in range(2))
+        k, v = out
+        if k.dim() != 3 or k.shape != v.shape or k.dtype != v.dtype or k.shape[1:] != (self.n_kv_heads, self.head_dim):
+            raise ValueError("out must be two tensors [rows][heads][head_dim] of one type")
+        _on(self.device, block_start=block_start, block_len=block_len, kv_len=kv_len, page_table=page_table, k=k, v=v)
+        hk, hv = CsHeads(), CsHeads()
+        for h, x, name in ((hk, k, "keys"), (hv, v, "values")):
+            h.y, h.y_row_stride, h.y_head_stride = _rows(x, name)
+            h.n_heads = self.n_kv_heads
+        blocks = _blocks(block_start, block_len, kv_len, page_table, k.shape[0])
+        with torch.cuda.device(self.device):
+            rc = self.lib.cs_quant_read(self.handle, blocks, hk, hv, _DTYPE[k.dtype], _stream())
+        self._check(rc, "cs_quant_read")
+        return out
+
+    def cs_quant_attention(self, q, block_start, block_len, kv_len, page_table, mask=MASK_CAUSAL, window=0, scale=None, out=None, with_lse=False, lse=None):
+        """As PagedCache.cs_paged_attention, over the values that the cache stands for; q and out are bf16 or fp16."""
+        if out is None and lse is None and _native is not None:
+            got = _native.quant_attention(*self._id, q, block_start, block_len, kv_len, page_table, mask, window, self.scale if scale is None else scale, with_lse)
+            if got.__class__ is tuple:
+                return got if with_lse else got[0]
+            if got is not None:
+                self._check(got, "cs_quant_attention")
+        if q.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError("q must be bf16 or fp16")
+        _on(self.device, q=q, block_start=block_start, block_len=block_len, kv_len=kv_len, page_table=page_table, out=out, lse=lse)
+        ptr, row, head = _rows(q, "q")
+        T, H, D = q.shape
+        if D != self.head_dim:
+            raise ValueError("q must have the cache's head size")
+        if out is None:
+            out = torch.empty(T, H, D, dtype=q.dtype, device=q.device)
+        elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+            raise ValueError("out must be contiguous, of q's shape and type")
+        if lse is None and with_lse:
+            lse = torch.empty(T, H, dtype=torch.float32, device=q.device)
+        elif lse is not None and (lse.shape != (T, H) or lse.dtype is not torch.float32 or not lse.is_contiguous()):
+            raise ValueError("lse must be a contiguous fp32 CUDA tensor [rows][heads]")
+        blocks = _blocks(block_start, block_len, kv_len, page_table, T)
+        with torch.cuda.device(self.device):
+            rc = self.lib.cs_quant_attention(self.handle, blocks, ptr, row, head, H, _DTYPE[q.dtype], mask, window, self.scale if scale is None else scale, out.data_ptr(),
+                                             None if lse is None else lse.data_ptr(), _stream())
+        self._check(rc, "cs_quant_attention")
+        return out if lse is None else (out, lse)
+
+    def cs_quant_status(self):
+        """Waits for the stream; what the device found wrong since the last call (CS_OK: nothing)."""
+        with torch.cuda.device(self.device):
+            return self.lib.cs_quant_status(self.handle, _stream())

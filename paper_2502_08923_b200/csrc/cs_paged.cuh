@@ -135,16 +135,19 @@ __device__ __forceinline__ long long paged_block_tiles(const PagedAttnArgs& a, i
   return sum;
 }
 
-struct PagedPlan {                              // in shared memory
-  long long before[kPagedMaxSeqs + 1];          // places of the sequences before this one
-  long long per_head[kPagedMaxSeqs];            // places of one of its KV heads
-  int start[kPagedMaxSeqs], len[kPagedMaxSeqs], kv[kPagedMaxSeqs];
+template <int kSeqs>
+struct PagedPlanOf {                            // in shared memory; of up to kSeqs sequences
+  long long before[kSeqs + 1];                  // places of the sequences before this one
+  long long per_head[kSeqs];                    // places of one of its KV heads
+  int start[kSeqs], len[kSeqs], kv[kSeqs];
   long long warp_sum[32];
-  int tall[kPagedMaxSeqs], n_tall;              // sequences whose row groups a warp adds up
+  int tall[kSeqs], n_tall;                      // sequences whose row groups a warp adds up
 };
+typedef PagedPlanOf<kPagedMaxSeqs> PagedPlan;
 
 // one sequence's block, left out (length 0) if something is wrong with it
-__device__ __forceinline__ void paged_load_block(const PagedAttnArgs& a, PagedPlan& p, int b, bool report, int& len, int& kv) {
+template <int kSeqs>
+__device__ __forceinline__ void paged_load_block(const PagedAttnArgs& a, PagedPlanOf<kSeqs>& p, int b, bool report, int& len, int& kv) {
   const int start = __ldcg(a.blk.start + b);
   len = __ldcg(a.blk.len + b);
   kv = __ldcg(a.blk.kv_len + b);
@@ -158,7 +161,8 @@ __device__ __forceinline__ void paged_load_block(const PagedAttnArgs& a, PagedPl
 
 // By all threads of a CTA (a multiple of 32, 128 at least).  Up to 32 sequences every warp works the plan out for itself - all write the same - and
 // nothing is waited for; else it ends with a barrier.
-__device__ __forceinline__ void paged_plan(const PagedAttnArgs& a, PagedPlan& p) {
+template <int kSeqs>
+__device__ __forceinline__ void paged_plan(const PagedAttnArgs& a, PagedPlanOf<kSeqs>& p) {
   const int tid = threadIdx.x, nt = blockDim.x, warp = tid >> 5, lane = tid & 31, B = a.blk.n_seqs;
   if (B <= 32) {
     int len = 0, kv = 0, n = 0;
@@ -241,7 +245,8 @@ struct PagedPiece {
 };
 
 // Piece that begins at place `at` of the line, by a whole warp (all lanes get it); `end`: where the CTA's run ends.  It may be empty: n_tiles 0.
-__device__ __forceinline__ PagedPiece paged_piece(const PagedAttnArgs& a, const PagedPlan& p, long long at, long long end, int lane) {
+template <int kSeqs>
+__device__ __forceinline__ PagedPiece paged_piece(const PagedAttnArgs& a, const PagedPlanOf<kSeqs>& p, long long at, long long end, int lane) {
   PagedPiece o;
   // the last sequence that begins at or before it (32 at a time)
   const int B = a.blk.n_seqs;
@@ -287,7 +292,8 @@ __device__ __forceinline__ PagedPiece paged_piece(const PagedAttnArgs& a, const 
   return o;
 }
 // The piece after one, if the CTA's run goes on behind it.
-__device__ __forceinline__ bool paged_next(const PagedAttnArgs& a, const PagedPlan& plan, PagedPiece& p, long long end) {
+template <int kSeqs>
+__device__ __forceinline__ bool paged_next(const PagedAttnArgs& a, const PagedPlanOf<kSeqs>& plan, PagedPiece& p, long long end) {
   const long long at = p.item_at + p.item_tiles + a.item_cost;
   if (at + a.item_cost >= end) return false;
   if (p.rg + 1 < paged_row_groups(a, p.len)) ++p.rg;
@@ -318,7 +324,8 @@ __device__ __forceinline__ int paged_last_cta(const PagedAttnArgs& a, const Page
 // The first piece of a CTA's run, by a whole warp, and where the run ends; empty (n_tiles 0) if there is nothing to do.  Where CTAs have little to do, items of up to `keep` tiles are left
 // to the CTA that has the last place of them: reading a few more tiles takes less time than adding pieces up.  (The small model's 11 rows over 512 keys, five
 // tiles a head, cut / whole: 8.7 / 7.9 us.)
-__device__ __forceinline__ PagedPiece paged_run(const PagedAttnArgs& a, const PagedPlan& plan, long long total, int n_cta, int cta, int lane, long long& end) {
+template <int kSeqs>
+__device__ __forceinline__ PagedPiece paged_run(const PagedAttnArgs& a, const PagedPlanOf<kSeqs>& plan, long long total, int n_cta, int cta, int lane, long long& end) {
   const long long begin = paged_div(total * cta, n_cta);
   end = paged_div(total * (cta + 1), n_cta);
   PagedPiece p = paged_piece(a, plan, begin, end, lane);

@@ -239,10 +239,112 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// ------------------------------------------------------------------ and around the cache held in 4 bits
+cs_quant_cache* quant_of(PyObject* handle, PyObject* device, int64_t head_dim) {
+  long d;
+  if (!PyLong_CheckExact(handle) || !small_int(device, d) || d != c10::cuda::current_device()) return nullptr;
+  cs_quant_cache* const cache = static_cast<cs_quant_cache*>(PyLong_AsVoidPtr(handle));
+  return cache != nullptr && cs_quant_head_dim(cache) == (int)head_dim ? cache : nullptr;
+}
+
+// quant_append(handle, device, k, v, block_start, block_len, kv_len, page_table, rope, k_gain, q, q_gain, eps, dtype code) -> (q,)
+PyObject* quant_append(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  const at::Tensor *q, *k, *v, *rope, *qg, *kg;
+  long code;
+  if (n_args != 14 || c10::impl::TorchDispatchModeTLS::any_modes_set() || !tensor_of(args[2], k) || !tensor_of(args[3], v) || !optional_of(args[8], rope) || !optional_of(args[9], kg) ||
+      !optional_of(args[10], q) || !optional_of(args[11], qg) || !PyFloat_CheckExact(args[12]) || !small_int(args[13], code) || (code != CS_BF16 && code != CS_F16))
+    Py_RETURN_NONE;
+  cs_heads hq = {}, hk = {}, hv = {};
+  cs_blocks blocks;
+  const float* table;
+  int n, rot;
+  const at::ScalarType type = type_of((int)code);
+  if (!rows_of(*k, hk) || !rows_of(*v, hv) || k->scalar_type() != v->scalar_type() || k->sizes() != v->sizes() || !gain_of(kg, k->size(2), type, hk) || !table_of(rope, table, n, rot) ||
+      !blocks_of(args + 4, k->size(0), blocks) ||
+      (q != nullptr && (!rows_of(*q, hq) || q->scalar_type() != k->scalar_type() || q->size(0) != k->size(0) || q->size(2) != k->size(2) || !gain_of(qg, k->size(2), type, hq))))
+    Py_RETURN_NONE;
+  cs_quant_cache* const cache = quant_of(args[0], args[1], k->size(2));
+  if (cache == nullptr) Py_RETURN_NONE;
+  const at::Tensor yq = q != nullptr ? output_for(*q, type, hq) : at::Tensor();
+  void* const stream = c10::cuda::getCurrentCUDAStream().stream();
+  const float eps = (float)PyFloat_AS_DOUBLE(args[12]);
+  const int in = code_of(k->scalar_type());
+  cs_status s;
+  Py_BEGIN_ALLOW_THREADS
+  s = cs_quant_append(cache, &blocks, &hk, &hv, &hq, (cs_dtype)in, (cs_dtype)code, table, n, rot, eps, stream);
+  Py_END_ALLOW_THREADS
+  if (s != CS_OK) return PyLong_FromLong(s);
+  PyObject* out = PyTuple_New(1);
+  if (out == nullptr) return nullptr;
+  PyTuple_SET_ITEM(out, 0, yq.defined() ? THPVariable_Wrap(yq) : Py_NewRef(Py_None));
+  return out;
+  END_HANDLE_TH_ERRORS
+}
+
+// quant_read(handle, device, KV heads, head_dim, block_start, block_len, kv_len, page_table, rows, dtype code) -> (keys, values)
+PyObject* quant_read(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  long heads, dim, rows, code;
+  cs_blocks blocks;
+  if (n_args != 10 || c10::impl::TorchDispatchModeTLS::any_modes_set() || !small_int(args[2], heads) || !small_int(args[3], dim) || !small_int(args[8], rows) || !small_int(args[9], code) ||
+      rows < 1 || heads < 1 || code < 0 || code > 2 || !blocks_of(args + 4, rows, blocks))
+    Py_RETURN_NONE;
+  cs_quant_cache* const cache = quant_of(args[0], args[1], dim);
+  if (cache == nullptr) Py_RETURN_NONE;
+  const at::Device device = THPVariable_Unpack(args[4]).device();
+  const at::Tensor k = at::detail::empty_cuda({rows, heads, dim}, type_of((int)code), device, std::nullopt), v = at::detail::empty_cuda({rows, heads, dim}, type_of((int)code), device, std::nullopt);
+  cs_heads hk = {}, hv = {};
+  hk.y = k.mutable_data_ptr(); hv.y = v.mutable_data_ptr();
+  hk.y_row_stride = hv.y_row_stride = heads * dim;
+  hk.y_head_stride = hv.y_head_stride = dim;
+  hk.n_heads = hv.n_heads = (int32_t)heads;
+  void* const stream = c10::cuda::getCurrentCUDAStream().stream();
+  cs_status s;
+  Py_BEGIN_ALLOW_THREADS
+  s = cs_quant_read(cache, &blocks, &hk, &hv, (cs_dtype)code, stream);
+  Py_END_ALLOW_THREADS
+  if (s != CS_OK) return PyLong_FromLong(s);
+  return pair_of(k, v);
+  END_HANDLE_TH_ERRORS
+}
+
+// quant_attention(handle, device, q, block_start, block_len, kv_len, page_table, mask, window, scale, with_lse) -> (out, lse or None)
+PyObject* quant_attention(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  const at::Tensor* q;
+  long mask, window;
+  if (n_args != 11 || c10::impl::TorchDispatchModeTLS::any_modes_set() || !tensor_of(args[2], q) || !small_int(args[7], mask) || !small_int(args[8], window) || !PyFloat_CheckExact(args[9]) ||
+      !PyBool_Check(args[10]))
+    Py_RETURN_NONE;
+  cs_heads hq = {};
+  cs_blocks blocks;
+  if (!rows_of(*q, hq) || q->scalar_type() == at::kFloat || !blocks_of(args + 3, q->size(0), blocks)) Py_RETURN_NONE;
+  cs_quant_cache* const cache = quant_of(args[0], args[1], q->size(2));
+  if (cache == nullptr) Py_RETURN_NONE;
+  const bool with_lse = args[10] == Py_True;
+  const at::Tensor out = output_for(*q, q->scalar_type(), hq);
+  const at::Tensor lse = with_lse ? at::detail::empty_cuda({q->size(0), q->size(1)}, at::kFloat, q->device(), std::nullopt) : at::Tensor();
+  void* const stream = c10::cuda::getCurrentCUDAStream().stream();
+  float* const lse_p = with_lse ? static_cast<float*>(lse.mutable_data_ptr()) : nullptr;
+  const float scale = (float)PyFloat_AS_DOUBLE(args[9]);
+  const int type = code_of(q->scalar_type());
+  cs_status s;
+  Py_BEGIN_ALLOW_THREADS
+  s = cs_quant_attention(cache, &blocks, hq.x, hq.row_stride, hq.head_stride, hq.n_heads, (cs_dtype)type, (cs_mask)mask, (int)window, scale, hq.y, lse_p, stream);
+  Py_END_ALLOW_THREADS
+  if (s != CS_OK) return PyLong_FromLong(s);
+  return pair_of(out, lse);
+  END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {{"find_match", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(find_match)), METH_FASTCALL, nullptr},
                          {"qk_norm_rope", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(qk_norm_rope)), METH_FASTCALL, nullptr},
                          {"paged_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(paged_append)), METH_FASTCALL, nullptr},
                          {"paged_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(paged_attention)), METH_FASTCALL, nullptr},
+                         {"quant_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(quant_append)), METH_FASTCALL, nullptr},
+                         {"quant_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(quant_read)), METH_FASTCALL, nullptr},
+                         {"quant_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(quant_attention)), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

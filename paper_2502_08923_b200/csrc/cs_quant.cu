@@ -1,0 +1,711 @@
+// Rows quantised into a paged cache of 4 bits, and read back; the host side of that cache.  (The format: cs_quant.cuh.)
+//
+// Append: keys are normed and rotated as in cs_paged.cu, u = x rsqrt(mean(x^2) + eps) gain, y_i = u_i c_i - u_{i+h} s_i, y_{i+h} = u_{i+h} c_i + u_i s_i, then quantised; values are
+// quantised; queries are normed and rotated.  A lane holds eight elements of a head's first half and their eight partners, which are a word each; a group's maximum is that of four words,
+// by way of shared memory.  Keys that are normed or rotated are worked out in 64 bits up to their level: which of fifteen levels an element goes to is then decided by its value, not by
+// the order of some sums (in 32 bits one element in some three million ends up a whole step from where another order puts it).  Elements that come as they are need no more than 32 bits: a correctly rounded quotient
+// of numbers of 24 and 5 bits is a whole number and a half only where it is one.
+#include <type_traits>
+
+#include "cs_quant.cuh"
+
+namespace {
+
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+
+struct QuantAppendArgs {
+  const char *q, *k, *v;             // sources; no queries: n_q = 0
+  char* yq;
+  long long q_row, q_head, k_row, k_head, v_row, v_head, yq_row, yq_head;   // elements
+  const char *q_gain, *k_gain;
+  int n_q, n_kv, n_rows;
+  int warps_per_row;                 // 1, 2 or 4
+  const float* rope;
+  int n_positions, rot_dim;
+  float eps;
+  QuantView kv;
+  BlocksView blk;
+  int* status;
+};
+
+template <typename T> __device__ __forceinline__ void load8(const char* p, float (&f)[8]) {
+  const uint4 x = __ldg(reinterpret_cast<const uint4*>(p));
+  if constexpr (sizeof(T) == 4) {
+    const uint4 y = __ldg(reinterpret_cast<const uint4*>(p) + 1);
+    f[0] = __uint_as_float(x.x); f[1] = __uint_as_float(x.y); f[2] = __uint_as_float(x.z); f[3] = __uint_as_float(x.w);
+    f[4] = __uint_as_float(y.x); f[5] = __uint_as_float(y.y); f[6] = __uint_as_float(y.z); f[7] = __uint_as_float(y.w);
+  } else {
+    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 y = PagedType<T>::unpack(w[i]);
+      f[2 * i] = y.x; f[2 * i + 1] = y.y;
+    }
+  }
+}
+template <typename T> __device__ __forceinline__ void store8(char* p, const float (&f)[8]) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(PagedType<T>::pack(f[0], f[1]), PagedType<T>::pack(f[2], f[3]), PagedType<T>::pack(f[4], f[5]), PagedType<T>::pack(f[6], f[7]));
+}
+
+// The scale of a group whose largest element is `most`, which may be NaN: five significant bits, halves to even, and multiples of 2^-133; at most 2^123, so that 24 of it are finite
+__device__ __forceinline__ float scale_of(float most) {
+  uint32_t b = __float_as_uint(__fdiv_rn(most, 7.f));
+  if ((b & 0x7f800000u) == 0x7f800000u) return __uint_as_float(0x7fc00000u);
+  b += 0x3ffffu + (b >> 19 & 1u);
+  const float s = fminf(__uint_as_float(b & 0xfff80000u), 1.0633823966279327e37f);
+  return __bfloat162float(__float2bfloat16_rn(s));
+}
+__device__ __forceinline__ float scale_of(double most) {
+  const double x = most / 7.0;
+  if (!(x <= 1.0633823966279327e37)) return x != x ? __uint_as_float(0x7fc00000u) : 1.0633823966279327e37f;
+  long long b = __double_as_longlong(x);
+  b += 0x7fffffffffffll + (b >> 48 & 1);
+  return __bfloat162float(__float2bfloat16_rn((float)__longlong_as_double(b >> 48 << 48)));
+}
+__device__ __forceinline__ uint32_t field_of(int i, int n) { return (uint32_t)(min(max(n, -7), 7) + 8) << (4 * (i / 2 + 4 * (i & 1))); }
+// eight elements of a group as a word
+__device__ __forceinline__ uint32_t word_of(const float (&y)[8], float s) {
+  uint32_t w = 0;
+  const bool some = s > 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w |= field_of(i, some ? __float2int_rn(__fdiv_rn(y[i], s)) : 0);
+  return w;
+}
+// In 64 bits: the quotient, by the product with the reciprocal, is rounded to a multiple of 2^-44 first (the sum with 384 does that), which makes a whole number and a half of one that is a rounding beside it, and
+// then to a whole number (the sum with 1.5 2^52).
+__device__ __forceinline__ uint32_t word_of(const double (&y)[8], float s) {
+  uint32_t w = 0;
+  const double inv = s > 0.f ? 1.0 / (double)s : 0.0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w |= field_of(i, __double2loint(fma(y[i], inv, 384.0) + (6755399441055744.0 - 384.0)));
+  return w;
+}
+// the largest of some, NaN if one is not finite  (fmax leaves NaN out, and 0 x inf is NaN)
+template <int N, typename R> __device__ __forceinline__ R most_of(const R* y) {
+  R m = fabs(y[0]), z = y[0] * R(0);
+#pragma unroll
+  for (int i = 1; i < N; ++i) {
+    m = fmax(m, fabs(y[i]));
+    z += y[i] * R(0);
+  }
+  return m + z;
+}
+
+template <typename S, typename D, int DH>
+__global__ void __launch_bounds__(kThreads)
+k_quant_append(const __grid_constant__ QuantAppendArgs a) {
+  CS_PDL_PROLOGUE();
+  constexpr int kLanes = DH / 16, kPer = 32 / kLanes, kWords = DH / 8;      // lanes of a head, heads of a unit, words of a head
+  __shared__ int s_seq[kWarps], s_pos[kWarps];
+  __shared__ double s_most[kWarps][64];          // [head][word]
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = lane % kLanes, sub = lane / kLanes;
+  const int n_here = kWarps / a.warps_per_row;
+  const long long row0 = (long long)blockIdx.x * n_here, row = row0 + warp / a.warps_per_row;
+  // the blocks these rows belong to
+  if (threadIdx.x < kWarps) s_seq[threadIdx.x] = -1;
+  __syncthreads();
+  for (int b = threadIdx.x; b < a.blk.n_seqs; b += kThreads) {
+    const int start = __ldcg(a.blk.start + b), len = __ldcg(a.blk.len + b), kv = __ldcg(a.blk.kv_len + b);
+    const int flag = paged_block_flag(a.blk, a.kv.page_size, true, start, len, kv);
+    if (flag != 0) {
+      if (blockIdx.x == 0) atomicOr(a.status, flag);
+    } else {
+      for (int i = 0; i < n_here; ++i)
+        if (row0 + i >= start && row0 + i - start < len) { s_seq[i] = b; s_pos[i] = kv + (int)(row0 + i - start); }
+    }
+  }
+  __syncthreads();
+  const int b = s_seq[warp / a.warps_per_row];
+  if (b < 0 || row >= a.n_rows) return;
+  const int pos = s_pos[warp / a.warps_per_row];
+  if (a.rot_dim > 0 && pos >= a.n_positions) {
+    if (lane == 0) atomicOr(a.status, CS_DEV_CAPACITY);
+    return;
+  }
+  const int page = __ldcg(a.blk.table + (long long)b * a.blk.table_width + (pos >> a.kv.page_shift)), slot = pos & (a.kv.page_size - 1);
+  const bool kept = (unsigned)page < (unsigned)a.kv.n_pages;
+  if (!kept && lane == 0) atomicOr(a.status, CS_DEV_BADARG);
+
+  // this lane's words: partners of the rotation, or two neighbours behind what is rotated
+  const int half = a.rot_dim >> 4;
+  const bool rotated = pair < half;
+  const int c0 = rotated ? pair : 2 * pair, c1 = rotated ? pair + half : c0 + 1;
+  float cs[8], sn[8];
+  if (rotated) {
+    load8<float>(reinterpret_cast<const char*>(a.rope + (long long)pos * a.rot_dim + c0 * 8), cs);
+    load8<float>(reinterpret_cast<const char*>(a.rope + (long long)pos * a.rot_dim + (c0 + half) * 8), sn);
+  }
+  const int uq = (a.n_q + kPer - 1) / kPer, uk = uq + (a.n_kv + kPer - 1) / kPer, units = uk + (a.n_kv + kPer - 1) / kPer;
+  for (int u = warp % a.warps_per_row; u < units; u += a.warps_per_row) {
+    const int kind = u < uq ? 0 : u < uk ? 1 : 2;
+    const int h = (u - (kind == 0 ? 0 : kind == 1 ? uq : uk)) * kPer + sub;
+    const bool live = h < (kind == 0 ? a.n_q : a.n_kv);
+    float x0[8] = {}, x1[8] = {};
+    if (live) {
+      const char* src = kind == 0 ? a.q + (row * a.q_row + h * a.q_head) * (long long)sizeof(S) : kind == 1 ? a.k + (row * a.k_row + h * a.k_head) * (long long)sizeof(S) : a.v + (row * a.v_row + h * a.v_head) * (long long)sizeof(S);
+      load8<S>(src + c0 * 8 * (int)sizeof(S), x0);
+      load8<S>(src + c1 * 8 * (int)sizeof(S), x1);
+    }
+    const char* gain = kind == 0 ? a.q_gain : kind == 1 ? a.k_gain : nullptr;
+    float g0[8], g1[8];
+    if (gain != nullptr) {
+      load8<D>(gain + c0 * 8 * (int)sizeof(D), g0);
+      load8<D>(gain + c1 * 8 * (int)sizeof(D), g1);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g0[i] = g1[i] = 1.f;
+    }
+    if (kind == 0) {
+      float r = 1.f;
+      if (gain != nullptr) {
+        float sq = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sq = fmaf(x0[i], x0[i], fmaf(x1[i], x1[i], sq));
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+        r = rsqrtf(sq * (1.f / DH) + a.eps);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float u0 = x0[i] * r * g0[i], u1 = x1[i] * r * g1[i];
+        x0[i] = rotated ? u0 * cs[i] - u1 * sn[i] : u0;
+        x1[i] = rotated ? u1 * cs[i] + u0 * sn[i] : u1;
+      }
+      if (live) {
+        char* dst = a.yq + (row * a.yq_row + h * a.yq_head) * (long long)sizeof(D);
+        store8<D>(dst + c0 * 8 * (int)sizeof(D), x0);
+        store8<D>(dst + c1 * 8 * (int)sizeof(D), x1);
+      }
+      continue;
+    }
+    uint32_t w0, w1;
+    float s0, s1;
+    if (kind == 1 && (gain != nullptr || a.rot_dim > 0)) {
+      double y0[8], y1[8], r = 1.0;
+      if (gain != nullptr) {
+        double sq = 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sq = fma((double)x0[i], (double)x0[i], fma((double)x1[i], (double)x1[i], sq));
+#pragma unroll
+        for (int o = 1; o < kLanes; o <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
+        r = rsqrt(sq * (1.0 / DH) + (double)a.eps);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const double u0 = (double)x0[i] * (double)g0[i], u1 = (double)x1[i] * (double)g1[i];
+        y0[i] = r * (rotated ? u0 * (double)cs[i] - u1 * (double)sn[i] : u0);
+        y1[i] = r * (rotated ? u1 * (double)cs[i] + u0 * (double)sn[i] : u1);
+      }
+      double* most = &s_most[warp][sub * kWords];
+      most[c0] = most_of<8>(y0);
+      most[c1] = most_of<8>(y1);
+      __syncwarp();
+      s0 = scale_of(most_of<4>(most + (c0 & ~3)));
+      s1 = scale_of(most_of<4>(most + (c1 & ~3)));
+      __syncwarp();
+      w0 = word_of(y0, s0);
+      w1 = word_of(y1, s1);
+    } else {
+      float* most = reinterpret_cast<float*>(&s_most[warp][0]) + sub * kWords;
+      most[c0] = most_of<8>(x0);
+      most[c1] = most_of<8>(x1);
+      __syncwarp();
+      s0 = scale_of(most_of<4>(most + (c0 & ~3)));
+      s1 = scale_of(most_of<4>(most + (c1 & ~3)));
+      __syncwarp();
+      w0 = word_of(x0, s0);
+      w1 = word_of(x1, s1);
+    }
+    if (live && kept) {
+      const long long in_page = (long long)h * a.kv.page_size + slot;
+      uint32_t* data = (kind == 1 ? a.kv.k : a.kv.v) + page * a.kv.data_page + in_page * kWords;
+      unsigned short* scale = (kind == 1 ? a.kv.ks : a.kv.vs) + page * a.kv.scale_page + in_page * (DH / kQuantGroup);
+      data[c0] = w0;
+      data[c1] = w1;
+      if ((c0 & 3) == 0) scale[c0 >> 2] = __bfloat16_as_ushort(__float2bfloat16_rn(s0));
+      if ((c1 & 3) == 0) scale[c1 >> 2] = __bfloat16_as_ushort(__float2bfloat16_rn(s1));
+    }
+  }
+}
+
+// ------------------------------------------------------------------ reading back
+// One word, a lane: eight elements of 16 bits are 16 bytes side by side with its neighbours'.  A warp has eight of them in flight.
+struct QuantReadArgs {
+  QuantView kv;
+  BlocksView blk;
+  char *k, *v;                       // destinations of rows, or of copies
+  long long k_row, k_head, v_row, v_head;      // elements; copies: page, head (of both)
+  int mask, window;                  // copies: which keys the blocks attend to
+  int copy_pages, copy_shift;        // pages of a sequence's copies, their size
+  int* copy_len;                     // lengths of blocks that nothing is wrong with
+  int* status;
+};
+
+// a word's eight values in type T (0 fp32, bf16, fp16), 16-byte stores.  (fp16 ends at 65504: what lies beyond it becomes that.)
+template <typename T> __device__ __forceinline__ void put8(char* dst, uint32_t word, unsigned scale) {
+  uint32_t r[4];
+  quant_expand(word, QuantScale::of(scale * 0x10001u), r);
+  if constexpr (sizeof(T) == 4) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 y = PagedType<__nv_bfloat16>::unpack(r[i]);
+      f[2 * i] = y.x; f[2 * i + 1] = y.y;
+    }
+    reinterpret_cast<float4*>(dst)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4*>(dst)[1] = make_float4(f[4], f[5], f[6], f[7]);
+  } else {
+    if constexpr (std::is_same<T, __half>::value) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float2 y = PagedType<__nv_bfloat16>::unpack(r[i]);
+        const float lo = fabsf(y.x) > 65504.f ? copysignf(65504.f, y.x) : y.x, hi = fabsf(y.y) > 65504.f ? copysignf(65504.f, y.y) : y.y;      // (NaN stays)
+        r[i] = PagedType<__half>::pack(lo, hi);
+      }
+    }
+    *reinterpret_cast<uint4*>(dst) = make_uint4(r[0], r[1], r[2], r[3]);
+  }
+}
+
+// the words of one row of K and V, by a warp
+template <typename T, int DH>
+__device__ __forceinline__ void read_row(const QuantView& kv, int page, int slot, bool exists, char* k, long long k_head, char* v, long long v_head, int lane) {
+  constexpr int kWords = DH / 8, kAhead = 4;
+  const int n = kv.n_kv_heads * kWords;
+  const long long head_words = (long long)kv.page_size * kWords, head_scales = (long long)kv.page_size * (DH / kQuantGroup);
+  for (int i0 = lane; i0 < n; i0 += 32 * kAhead) {
+    uint32_t w[2][kAhead];
+    unsigned s[2][kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = i0 + 32 * j, h = i / kWords, c = i % kWords;
+      w[0][j] = w[1][j] = 0x88888888u;
+      s[0][j] = s[1][j] = 0;
+      if (i < n && exists) {
+        const long long d = page * kv.data_page + h * head_words + slot * kWords + c, g = page * kv.scale_page + h * head_scales + slot * (DH / kQuantGroup) + c / 4;
+        w[0][j] = __ldcs(kv.k + d); s[0][j] = __ldcs(kv.ks + g);
+        w[1][j] = __ldcs(kv.v + d); s[1][j] = __ldcs(kv.vs + g);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      const int i = i0 + 32 * j, h = i / kWords, c = i % kWords;
+      if (i < n) {
+        put8<T>(k + (h * k_head + c * 8) * (long long)sizeof(T), w[0][j], s[0][j]);
+        put8<T>(v + (h * v_head + c * 8) * (long long)sizeof(T), w[1][j], s[1][j]);
+      }
+    }
+  }
+}
+
+constexpr int kReadWarps = 8;
+
+template <typename T, int DH>
+__global__ void __launch_bounds__(kReadWarps * 32)
+k_quant_read(const __grid_constant__ QuantReadArgs a) {
+  CS_PDL_PROLOGUE();
+  __shared__ int s_seq[kReadWarps], s_pos[kReadWarps];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const long long row0 = (long long)blockIdx.x * kReadWarps, row = row0 + warp;
+  if (threadIdx.x < kReadWarps) s_seq[threadIdx.x] = -1;
+  __syncthreads();
+  for (int b = threadIdx.x; b < a.blk.n_seqs; b += kReadWarps * 32) {
+    const int start = __ldcg(a.blk.start + b), len = __ldcg(a.blk.len + b), kv = __ldcg(a.blk.kv_len + b);
+    const int flag = paged_block_flag(a.blk, a.kv.page_size, true, start, len, kv);
+    if (flag != 0) {
+      if (blockIdx.x == 0) atomicOr(a.status, flag);
+    } else {
+      for (int i = 0; i < kReadWarps; ++i)
+        if (row0 + i >= start && row0 + i - start < len) { s_seq[i] = b; s_pos[i] = kv + (int)(row0 + i - start); }
+    }
+  }
+  __syncthreads();
+  const int b = s_seq[warp];
+  if (b < 0 || row >= a.blk.rows) return;
+  const int pos = s_pos[warp], page = __ldcg(a.blk.table + (long long)b * a.blk.table_width + (pos >> a.kv.page_shift));
+  const bool exists = (unsigned)page < (unsigned)a.kv.n_pages;
+  if (!exists && lane == 0) atomicOr(a.status, CS_DEV_BADARG);
+  read_row<T, DH>(a.kv, page, pos & (a.kv.page_size - 1), exists, a.k + row * a.k_row * (long long)sizeof(T), a.k_head, a.v + row * a.v_row * (long long)sizeof(T), a.v_head, lane);
+}
+
+// Copies in 16 bits of the positions that blocks attend to, for the attention of tall blocks: sequence b's in the pages from b copy_pages on.
+template <typename T, int DH>
+__global__ void __launch_bounds__(kReadWarps * 32)
+k_quant_copy(const __grid_constant__ QuantReadArgs a) {
+  CS_PDL_PROLOGUE();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (blockIdx.x == 0)
+    for (int b = threadIdx.x; b < a.blk.n_seqs; b += kReadWarps * 32) {
+      const int len = __ldcg(a.blk.len + b), flag = paged_block_flag(a.blk, a.kv.page_size, a.mask != CS_MASK_PREFIX, __ldcg(a.blk.start + b), len, __ldcg(a.blk.kv_len + b));
+      if (flag != 0) atomicOr(a.status, flag);
+      a.copy_len[b] = flag != 0 ? 0 : len;
+    }
+  // eight positions a CTA at a time, which no page splits
+  const int chunks = (a.copy_pages << a.copy_shift) / kReadWarps;
+  for (long long i = blockIdx.x; i < (long long)a.blk.n_seqs * chunks; i += gridDim.x) {
+    const int b = (int)(i / chunks), pos0 = (int)(i - (long long)b * chunks) * kReadWarps;
+    const int len = __ldcg(a.blk.len + b), kv = __ldcg(a.blk.kv_len + b);
+    if (len <= 0 || paged_block_flag(a.blk, a.kv.page_size, a.mask != CS_MASK_PREFIX, __ldcg(a.blk.start + b), len, kv) != 0) continue;
+    int lo, hi;
+    paged_range(a.mask, a.window, len, kv, 0, len - 1, lo, hi);
+    const int pos = pos0 + warp;
+    if (pos < lo || pos >= hi) continue;
+    const int page = __ldcg(a.blk.table + (long long)b * a.blk.table_width + (pos >> a.kv.page_shift));
+    const bool exists = (unsigned)page < (unsigned)a.kv.n_pages;
+    if (!exists && lane == 0) atomicOr(a.status, CS_DEV_BADARG);
+    const long long at = (((long long)b * a.copy_pages + (pos >> a.copy_shift)) * a.k_row + (long long)(pos & ((1 << a.copy_shift) - 1)) * DH) * (long long)sizeof(T);
+    read_row<T, DH>(a.kv, page, pos & (a.kv.page_size - 1), exists, a.k + at, a.k_head, a.v + at, a.k_head, lane);
+  }
+}
+
+__global__ void k_quant_iota(int* p, int n) {
+  CS_PDL_PROLOGUE();
+  for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) p[i] = i;
+}
+
+thread_local char t_quant_err[256] = "";
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+int bytes_of(int dtype) { return dtype == CS_F32 ? 4 : 2; }
+
+cs_status fail(cs_quant_cache* c, cs_status s, const char* text) {
+  snprintf(c->err, sizeof(c->err), "%s", text);
+  return s;
+}
+// source rows (of type `in`) and, where out >= 0, destination rows
+cs_status check_rows(const cs_heads* h, int in, int out) {
+  if (h->n_heads < 0) return CS_ERR_ARG;
+  if (h->n_heads == 0) return CS_OK;
+  if (in >= 0 && (h->x == nullptr || !aligned16(h->x) || h->row_stride % (16 / bytes_of(in)) != 0 || h->head_stride % (16 / bytes_of(in)) != 0 || !aligned16(h->gain))) return CS_ERR_ARG;
+  if (out >= 0 && (h->y == nullptr || !aligned16(h->y) || h->y_row_stride % (16 / bytes_of(out)) != 0 || h->y_head_stride % (16 / bytes_of(out)) != 0)) return CS_ERR_ARG;
+  return CS_OK;
+}
+cs_status check_blocks(const cs_blocks* b) {
+  if (b->n_seqs < 0 || b->rows < 0 || b->table_width < 0) return CS_ERR_ARG;
+  if (b->n_seqs == 0 || b->rows == 0) return CS_OK;
+  return b->start == nullptr || b->len == nullptr || b->kv_len == nullptr || (b->page_table == nullptr && b->table_width > 0) ? CS_ERR_ARG : CS_OK;
+}
+BlocksView view_of(const cs_blocks* b) { return BlocksView{b->start, b->len, b->kv_len, b->page_table, b->n_seqs, b->table_width, b->rows}; }
+
+// why a configuration is refused (CS_OK: it is not)
+cs_status check_config(const cs_quant_config* c, const char** why) {
+  *why = "";
+  if (c == nullptr) { *why = "NULL argument"; return CS_ERR_ARG; }
+  if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) { *why = "head_dim must be 32, 64 or 128"; return CS_ERR_SHAPE; }
+  if (c->page_size < 16 || (c->page_size & (c->page_size - 1)) != 0) { *why = "page_size must be a power of two from 16 on"; return CS_ERR_SHAPE; }
+  if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 0x0fffffff) { *why = "no pages or no heads"; return CS_ERR_ARG; }
+  const int64_t row = (int64_t)c->n_kv_heads * c->page_size;
+  if (c->page_stride % 16 != 0 || c->scale_page_stride % 8 != 0 || (c->n_pages > 1 && (c->page_stride < row * (c->head_dim / 2) || c->scale_page_stride < row * (c->head_dim / kQuantGroup)))) {
+    *why = "pages must not overlap, their strides must be multiples of 16 bytes";
+    return CS_ERR_ARG;
+  }
+  if (c->tall_positions < 0 || c->tall_positions > (1ll << 30)) { *why = "tall_positions must be between 0 and 2^30"; return CS_ERR_ARG; }
+  return CS_OK;
+}
+
+struct QuantLayout {
+  size_t status, counters, parts, parts_ml, table, len, k, v, paged, total;
+  size_t paged_bytes;
+  long long positions;         // room for copies
+};
+// a cache of 16 bits over the copies, with pages of 128 >> i slots
+cs_paged_config copies_config(const cs_quant_config& c, long long positions, char* k, char* v, int i, int dtype) {
+  cs_paged_config p = {};
+  p.page_size = kQuantCopyPage >> i;
+  p.k = k; p.v = v;
+  p.slot_stride = c.head_dim; p.head_stride = (int64_t)p.page_size * c.head_dim; p.page_stride = p.head_stride * c.n_kv_heads;
+  p.n_pages = (int32_t)(positions >> (7 - i)); p.n_kv_heads = c.n_kv_heads; p.head_dim = c.head_dim; p.dtype = dtype;
+  return p;
+}
+QuantLayout layout_of(const cs_quant_config& c) {
+  QuantLayout l = {};
+  size_t at = 0;
+  auto put = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) & ~(size_t)255; return o; };
+  l.status = put(256);
+  l.counters = put(kQuantMaxCtas * sizeof(int));
+  l.parts = put((size_t)kQuantMaxCtas * 2 * kQuantMaxRows * c.head_dim * 4);
+  l.parts_ml = put((size_t)kQuantMaxCtas * 2 * kQuantMaxRows * 8);
+  l.positions = (c.tall_positions + 15) & ~15ll;
+  if (l.positions > 0) {
+    const cs_paged_config p = copies_config(c, l.positions, nullptr, nullptr, 3, CS_BF16);
+    const size_t pool = (size_t)l.positions * c.n_kv_heads * c.head_dim * 2;
+    l.paged_bytes = cs_paged_workspace_bytes(&p);
+    l.table = put((size_t)l.positions / 16 * 4);
+    l.len = put((size_t)l.positions / 16 * 4);
+    l.k = put(pool);
+    l.v = put(pool);
+    l.paged = put(l.paged_bytes);
+  }
+  l.total = at;
+  return l;
+}
+
+// `first`: the cache whose workspace it is already (nullptr: nobody's)
+cs_status create(const char* name, cs_quant_cache** out, const cs_quant_config* cfg, void* workspace, size_t workspace_bytes, const cs_quant_cache* first, void* stream) {
+  auto refuse = [&](cs_status s, const char* text) {
+    snprintf(t_quant_err, sizeof(t_quant_err), "%s: %s", name, text);
+    return s;
+  };
+  t_quant_err[0] = 0;
+  const char* why;
+  if (out == nullptr) return refuse(CS_ERR_ARG, "NULL argument");
+  *out = nullptr;
+  const cs_status s = check_config(cfg, &why);
+  if (s != CS_OK) return refuse(s, why);
+  if (cfg->k == nullptr || cfg->v == nullptr || cfg->k_scale == nullptr || cfg->v_scale == nullptr || workspace == nullptr) return refuse(CS_ERR_ARG, "NULL pointer");
+  if (!aligned16(cfg->k) || !aligned16(cfg->v) || !aligned16(cfg->k_scale) || !aligned16(cfg->v_scale)) return refuse(CS_ERR_ARG, "the pools must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return refuse(CS_ERR_ARG, "the workspace must be 256-byte aligned");
+  const QuantLayout l = layout_of(*cfg);
+  if (workspace_bytes < l.total) return refuse(CS_ERR_CAPACITY, "the workspace is too small");
+  if (first != nullptr && (first->cfg.head_dim != cfg->head_dim || first->cfg.n_kv_heads != cfg->n_kv_heads || first->cfg.tall_positions != cfg->tall_positions))
+    return refuse(CS_ERR_SHAPE, "caches that share a workspace need the same heads and tall_positions");
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return refuse(CS_ERR_CUDA, "no device");
+  cs_quant_cache* c = static_cast<cs_quant_cache*>(calloc(1, sizeof(cs_quant_cache)));
+  if (c == nullptr) return refuse(CS_ERR_CAPACITY, "out of host memory");
+  c->cfg = *cfg;
+  c->num_sms = 2 * sms < kQuantMaxCtas ? sms : kQuantMaxCtas / 2;
+  int shift = 0;
+  while ((1 << shift) < cfg->page_size) ++shift;
+  c->view = QuantView{static_cast<uint32_t*>(cfg->k), static_cast<uint32_t*>(cfg->v), static_cast<unsigned short*>(cfg->k_scale), static_cast<unsigned short*>(cfg->v_scale),
+                      cfg->page_stride / 4, cfg->scale_page_stride, cfg->n_pages, cfg->page_size, shift, cfg->n_kv_heads};
+  char* ws = static_cast<char*>(workspace);
+  c->workspace = workspace;
+  c->workspace_bytes = workspace_bytes;
+  c->status = reinterpret_cast<int*>(ws + l.status);
+  c->counters = reinterpret_cast<int*>(ws + l.counters);
+  c->parts = reinterpret_cast<float*>(ws + l.parts);
+  c->parts_ml = reinterpret_cast<float*>(ws + l.parts_ml);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  if (first == nullptr) {
+    const cudaError_t e = cudaMemsetAsync(ws, 0, l.parts, st);
+    if (e != cudaSuccess) {
+      free(c);
+      return refuse(CS_ERR_CUDA, cudaGetErrorString(e));
+    }
+  }
+  if (l.positions > 0) {
+    c->tall_positions = l.positions;
+    c->tall_k = ws + l.k;
+    c->tall_v = ws + l.v;
+    c->tall_table = reinterpret_cast<int*>(ws + l.table);
+    c->tall_len = reinterpret_cast<int*>(ws + l.len);
+    // (the smallest pages first: there is one at least)
+    const cs_paged_cache* beside = first != nullptr ? first->tall[0][3] : nullptr;
+    cs_status r = CS_OK;
+    for (int i = 3; i >= 0; --i)
+      for (int type = 0; type < 2 && r == CS_OK; ++type) {
+        const cs_paged_config p = copies_config(*cfg, l.positions, c->tall_k, c->tall_v, i, type == 0 ? CS_BF16 : CS_F16);
+        if (p.n_pages < 1) continue;
+        r = beside != nullptr ? cs_paged_create_beside(&c->tall[type][i], &p, beside) : cs_paged_create(&c->tall[type][i], &p, ws + l.paged, l.paged_bytes, stream);
+        if (beside == nullptr) beside = c->tall[type][i];
+      }
+    const int n = (int)(l.positions / 16);
+    if (r == CS_OK && first == nullptr && cs_launch_pdl(k_quant_iota, dim3((unsigned)(n < 1 << 18 ? (n + 1023) / 1024 : 256)), dim3(256), 0, st, c->tall_table, n) != cudaSuccess) r = CS_ERR_CUDA;
+    if (r != CS_OK) {
+      refuse(r, cs_paged_last_error(nullptr)[0] != 0 ? cs_paged_last_error(nullptr) : "launch failed");
+      cs_quant_destroy(c);
+      return r;
+    }
+  }
+  *out = c;
+  return CS_OK;
+}
+
+template <typename S, typename D>
+cudaError_t launch_append(QuantAppendArgs a, int head_dim, cudaStream_t st) {
+  const int per = 512 / head_dim, units = cs_ceil_div(a.n_q, per) + 2 * cs_ceil_div(a.n_kv, per);
+  a.warps_per_row = kWarps;
+  while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)a.n_rows * a.warps_per_row > 148 * 16)) a.warps_per_row /= 2;
+  const dim3 grid((unsigned)(((long long)a.n_rows * a.warps_per_row + kWarps - 1) / kWarps)), block(kThreads);
+  switch (head_dim) {
+    case 32: return cs_launch_pdl(k_quant_append<S, D, 32>, grid, block, 0, st, a);
+    case 64: return cs_launch_pdl(k_quant_append<S, D, 64>, grid, block, 0, st, a);
+    default: return cs_launch_pdl(k_quant_append<S, D, 128>, grid, block, 0, st, a);
+  }
+}
+template <typename T>
+cudaError_t launch_read(const QuantReadArgs& a, int head_dim, cudaStream_t st) {
+  const dim3 grid((unsigned)(((long long)a.blk.rows + kReadWarps - 1) / kReadWarps)), block(kReadWarps * 32);
+  switch (head_dim) {
+    case 32: return cs_launch_pdl(k_quant_read<T, 32>, grid, block, 0, st, a);
+    case 64: return cs_launch_pdl(k_quant_read<T, 64>, grid, block, 0, st, a);
+    default: return cs_launch_pdl(k_quant_read<T, 128>, grid, block, 0, st, a);
+  }
+}
+template <typename T>
+cudaError_t launch_copy(const QuantReadArgs& a, int head_dim, int sms, cudaStream_t st) {
+  const long long chunks = (long long)a.blk.n_seqs * ((a.copy_pages << a.copy_shift) / kReadWarps);
+  const dim3 grid((unsigned)(chunks < 8 * sms ? (chunks > 0 ? chunks : 1) : 8 * sms)), block(kReadWarps * 32);
+  switch (head_dim) {
+    case 32: return cs_launch_pdl(k_quant_copy<T, 32>, grid, block, 0, st, a);
+    case 64: return cs_launch_pdl(k_quant_copy<T, 64>, grid, block, 0, st, a);
+    default: return cs_launch_pdl(k_quant_copy<T, 128>, grid, block, 0, st, a);
+  }
+}
+
+}  // namespace
+
+size_t cs_quant_workspace_bytes(const cs_quant_config* cfg) {
+  const char* why;
+  return check_config(cfg, &why) == CS_OK ? layout_of(*cfg).total : 0;
+}
+
+cs_status cs_quant_create(cs_quant_cache** out, const cs_quant_config* cfg, void* workspace, size_t workspace_bytes, void* stream) {
+  return create("cs_quant_create", out, cfg, workspace, workspace_bytes, nullptr, stream);
+}
+
+cs_status cs_quant_create_beside(cs_quant_cache** out, const cs_quant_config* cfg, const cs_quant_cache* first) {
+  if (first == nullptr) {
+    snprintf(t_quant_err, sizeof(t_quant_err), "cs_quant_create_beside: NULL argument");
+    if (out != nullptr) *out = nullptr;
+    return CS_ERR_ARG;
+  }
+  return create("cs_quant_create_beside", out, cfg, first->workspace, first->workspace_bytes, first, nullptr);
+}
+
+void cs_quant_destroy(cs_quant_cache* c) {
+  if (c == nullptr) return;
+  for (int type = 0; type < 2; ++type)
+    for (int i = 0; i < 4; ++i) cs_paged_destroy(c->tall[type][i]);
+  free(c);
+}
+
+int cs_quant_head_dim(const cs_quant_cache* c) { return c != nullptr ? c->cfg.head_dim : 0; }
+
+const char* cs_quant_last_error(const cs_quant_cache* c) { return c != nullptr ? c->err : t_quant_err; }
+
+cs_status cs_quant_status(cs_quant_cache* c, void* stream) {
+  if (c == nullptr) return CS_ERR_ARG;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  int bits = 0;
+  CS_CUDA_OK(c, cudaMemcpyAsync(&bits, c->status, sizeof(int), cudaMemcpyDeviceToHost, st));
+  CS_CUDA_OK(c, cudaStreamSynchronize(st));
+  cs_status tall = CS_OK;
+  if (c->tall[0][3] != nullptr && (tall = cs_paged_status(c->tall[0][3], stream)) != CS_OK) fail(c, tall, cs_paged_last_error(c->tall[0][3]));
+  if (bits == 0 || tall == CS_ERR_TIMEOUT || tall == CS_ERR_CUDA) {
+    if (bits != 0) CS_CUDA_OK(c, cudaMemsetAsync(c->status, 0, sizeof(int), st));
+    return tall;
+  }
+  CS_CUDA_OK(c, cudaMemsetAsync(c->status, 0, sizeof(int), st));
+  CS_CUDA_OK(c, cudaStreamSynchronize(st));
+  if (bits & CS_DEV_CAPACITY) return fail(c, CS_ERR_CAPACITY, "a block does not fit its row of the page table, or the rotation table is too short");
+  return fail(c, CS_ERR_ARG, "a length is negative, rows lie outside the tensors, or a page does not exist");
+}
+
+cs_status cs_quant_append(cs_quant_cache* c, const cs_blocks* blocks, const cs_heads* k, const cs_heads* v, const cs_heads* q, cs_dtype in, cs_dtype out, const float* rope, int n_positions,
+                          int rot_dim, float eps, void* stream) {
+  if (c == nullptr) return CS_ERR_ARG;
+  if (blocks == nullptr || k == nullptr || v == nullptr) return fail(c, CS_ERR_ARG, "NULL argument");
+  if ((out != CS_BF16 && out != CS_F16) || (in != out && in != CS_F32)) return fail(c, CS_ERR_ARG, "queries and gains are CS_BF16 or CS_F16, rows of the same type or CS_F32");
+  cs_status s = check_blocks(blocks);
+  if (s != CS_OK) return fail(c, s, "bad blocks");
+  if (blocks->n_seqs == 0 || blocks->rows == 0) return CS_OK;
+  if (rot_dim < 0 || !(eps >= 0.f) || (rot_dim > 0 && (rope == nullptr || n_positions < 1 || !aligned16(rope)))) return fail(c, CS_ERR_ARG, "bad rotation table or eps");
+  if (rot_dim % 16 != 0 || rot_dim > c->cfg.head_dim) return fail(c, CS_ERR_SHAPE, "rot_dim must be a multiple of 16, at most head_dim");
+  if (k->n_heads != c->cfg.n_kv_heads || v->n_heads != c->cfg.n_kv_heads) return fail(c, CS_ERR_SHAPE, "keys and values need the cache's heads");
+  if ((q != nullptr && (s = check_rows(q, in, out)) != CS_OK) || (s = check_rows(k, in, -1)) != CS_OK || (s = check_rows(v, in, -1)) != CS_OK)
+    return fail(c, s, "rows need 16-byte aligned bases and strides of multiples of 16 bytes");
+  if ((q != nullptr ? q->n_heads : 0) > 0x0fffffff) return fail(c, CS_ERR_SHAPE, "too many heads");
+  QuantAppendArgs a = {};
+  if (q != nullptr && q->n_heads > 0) {
+    a.q = static_cast<const char*>(q->x); a.q_row = q->row_stride; a.q_head = q->head_stride;
+    a.yq = static_cast<char*>(q->y); a.yq_row = q->y_row_stride; a.yq_head = q->y_head_stride;
+    a.q_gain = static_cast<const char*>(q->gain); a.n_q = q->n_heads;
+  }
+  a.k = static_cast<const char*>(k->x); a.k_row = k->row_stride; a.k_head = k->head_stride;
+  a.k_gain = static_cast<const char*>(k->gain); a.n_kv = k->n_heads;
+  a.v = static_cast<const char*>(v->x); a.v_row = v->row_stride; a.v_head = v->head_stride;
+  a.n_rows = blocks->rows;
+  a.rope = rope; a.n_positions = n_positions; a.rot_dim = rot_dim; a.eps = eps;
+  a.kv = c->view; a.blk = view_of(blocks); a.status = c->status;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int dh = c->cfg.head_dim;
+  if (out == CS_BF16) CS_CUDA_OK(c, in == CS_F32 ? (launch_append<float, __nv_bfloat16>(a, dh, st)) : (launch_append<__nv_bfloat16, __nv_bfloat16>(a, dh, st)));
+  else CS_CUDA_OK(c, in == CS_F32 ? (launch_append<float, __half>(a, dh, st)) : (launch_append<__half, __half>(a, dh, st)));
+  return CS_OK;
+}
+
+cs_status cs_quant_read(cs_quant_cache* c, const cs_blocks* blocks, const cs_heads* k, const cs_heads* v, cs_dtype out, void* stream) {
+  if (c == nullptr) return CS_ERR_ARG;
+  if (blocks == nullptr || k == nullptr || v == nullptr) return fail(c, CS_ERR_ARG, "NULL argument");
+  if (out < CS_BF16 || out > CS_F32) return fail(c, CS_ERR_ARG, "rows are CS_BF16, CS_F16 or CS_F32");
+  cs_status s = check_blocks(blocks);
+  if (s != CS_OK) return fail(c, s, "bad blocks");
+  if (blocks->n_seqs == 0 || blocks->rows == 0) return CS_OK;
+  if (k->n_heads != c->cfg.n_kv_heads || v->n_heads != c->cfg.n_kv_heads) return fail(c, CS_ERR_SHAPE, "keys and values need the cache's heads");
+  if ((s = check_rows(k, -1, out)) != CS_OK || (s = check_rows(v, -1, out)) != CS_OK) return fail(c, s, "rows need 16-byte aligned bases and strides of multiples of 16 bytes");
+  QuantReadArgs a = {};
+  a.kv = c->view; a.blk = view_of(blocks); a.status = c->status;
+  a.k = static_cast<char*>(k->y); a.k_row = k->y_row_stride; a.k_head = k->y_head_stride;
+  a.v = static_cast<char*>(v->y); a.v_row = v->y_row_stride; a.v_head = v->y_head_stride;
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int dh = c->cfg.head_dim;
+  CS_CUDA_OK(c, out == CS_F32 ? launch_read<float>(a, dh, st) : out == CS_BF16 ? launch_read<__nv_bfloat16>(a, dh, st) : launch_read<__half>(a, dh, st));
+  return CS_OK;
+}
+
+cs_status cs_quant_attention(cs_quant_cache* c, const cs_blocks* blocks, const void* q, int64_t q_row_stride, int64_t q_head_stride, int n_heads, cs_dtype dtype, cs_mask mask, int window,
+                             float scale, void* out, float* lse, void* stream) {
+  if (c == nullptr) return CS_ERR_ARG;
+  if (blocks == nullptr) return fail(c, CS_ERR_ARG, "NULL argument");
+  const cs_status s = check_blocks(blocks);
+  if (s != CS_OK) return fail(c, s, "bad blocks");
+  if (dtype != CS_BF16 && dtype != CS_F16) return fail(c, CS_ERR_ARG, "queries are CS_BF16 or CS_F16");
+  if (mask < CS_MASK_CAUSAL || mask > CS_MASK_FULL || window < 0 || !(scale > 0.f) || !(scale <= 2.0e38f)) return fail(c, CS_ERR_ARG, "bad mask, window or scale");
+  if (n_heads < 1 || n_heads % c->cfg.n_kv_heads != 0 || n_heads / c->cfg.n_kv_heads > 128) return fail(c, CS_ERR_SHAPE, "n_heads must be a multiple of the cache's heads, at most 128 per KV head");
+  if ((long long)blocks->rows * n_heads > 0x7fffff00ll) return fail(c, CS_ERR_SHAPE, "too many rows");
+  if (blocks->n_seqs == 0 || blocks->rows == 0) return CS_OK;
+  if (q == nullptr || out == nullptr) return fail(c, CS_ERR_ARG, "NULL pointer");
+  if (!aligned16(q) || !aligned16(out) || q_row_stride % 8 != 0 || q_head_stride % 8 != 0) return fail(c, CS_ERR_ARG, "q and out need 16-byte aligned bases, q strides of multiples of 8 elements");
+  if ((reinterpret_cast<uintptr_t>(lse) & 3) != 0) return fail(c, CS_ERR_ARG, "lse must be aligned to its type");
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const int group = n_heads / c->cfg.n_kv_heads;
+  const long long per_seq = ((long long)blocks->rows * group + blocks->n_seqs - 1) / blocks->n_seqs;      // query rows of a KV head, on the average
+  // Copies in pages as large as fit: a tile of 128 keys is fetched page by page
+  const long long room = (long long)blocks->table_width * c->cfg.page_size;
+  int size = 0;
+  long long copy_pages = 0;
+  for (; size < 4; ++size) {
+    copy_pages = (room + (kQuantCopyPage >> size) - 1) >> (7 - size);
+    if ((copy_pages << (7 - size)) <= c->tall_positions / blocks->n_seqs) break;
+  }
+  if (per_seq > 96 && size < 4 && copy_pages > 0) {
+    QuantReadArgs r = {};
+    r.kv = c->view; r.blk = view_of(blocks); r.status = c->status;
+    r.k = c->tall_k; r.v = c->tall_v;
+    r.k_head = (long long)(kQuantCopyPage >> size) * c->cfg.head_dim; r.k_row = r.k_head * c->cfg.n_kv_heads;
+    r.mask = mask; r.window = window; r.copy_pages = (int)copy_pages; r.copy_shift = 7 - size; r.copy_len = c->tall_len;
+    CS_CUDA_OK(c, dtype == CS_BF16 ? launch_copy<__nv_bfloat16>(r, c->cfg.head_dim, c->num_sms, st) : launch_copy<__half>(r, c->cfg.head_dim, c->num_sms, st));
+    cs_blocks b = *blocks;
+    b.len = c->tall_len;
+    b.page_table = c->tall_table;
+    b.table_width = (int)copy_pages;
+    cs_paged_cache* paged = c->tall[dtype == CS_BF16 ? 0 : 1][size];
+    const cs_status t = cs_paged_attention(paged, &b, q, q_row_stride, q_head_stride, n_heads, mask, window, scale, out, lse, stream);
+    return t == CS_OK ? t : fail(c, t, cs_paged_last_error(paged));
+  }
+  QuantAttnArgs a = {};
+  a.kv = c->view;
+  a.half = dtype == CS_F16;
+  PagedAttnArgs& p = a.p;
+  p.kv.n_pages = c->view.n_pages; p.kv.page_size = c->view.page_size; p.kv.page_shift = c->view.page_shift; p.kv.n_kv_heads = c->view.n_kv_heads;
+  p.blk = view_of(blocks);
+  p.q = static_cast<const char*>(q); p.q_row = q_row_stride; p.q_head = q_head_stride;
+  p.out = static_cast<char*>(out); p.lse = lse;
+  p.n_heads = n_heads; p.group = group;
+  p.by_group = PagedDivisor::by(group);
+  p.mask = mask; p.window = window;
+  p.scale = scale; p.scale_log2e = (float)(1.4426950408889634 * (double)scale);
+  p.parts = c->parts; p.parts_ml = c->parts_ml; p.counters = c->counters; p.status = c->status;
+  p.drop = -1;
+  for (int b = 0; b < blocks->n_seqs; b += kQuantMaxSeqs) {      // (a launch's plan holds so many)
+    QuantAttnArgs part = a;
+    part.p.blk.n_seqs = blocks->n_seqs - b < kQuantMaxSeqs ? blocks->n_seqs - b : kQuantMaxSeqs;
+    part.p.blk.start += b; part.p.blk.len += b; part.p.blk.kv_len += b;
+    part.p.blk.table += (long long)b * blocks->table_width;
+    const cs_status r = cs_launch_quant_few(c, part, st);
+    if (r != CS_OK) return r;
+  }
+  return CS_OK;
+}

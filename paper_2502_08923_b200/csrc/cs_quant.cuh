@@ -1,0 +1,99 @@
+// Shared by the operators around the paged cache held in 4 bits: the handle, the format, what kernels get of a cache.
+//
+// A row (one position, one KV head) is cut into groups of 32 neighbouring elements.  With a = max |x| of a group,
+//     s = a / 7 rounded to five significant bits,   n = x / s rounded to a whole number, |n| <= 7;
+// the group is held as s (bf16) and 4-bit numbers n + 8, and stands for s n.  Five bits and three make eight, so every value that the cache stands for is exactly a bf16 number: keys and
+// values go into the tensor cores as they are held, without a further rounding, whatever the queries' type, and reading back in bf16 is exact.  Rounding the scale (by 1/32 at most) makes
+// x / s at most 7.22, so the largest element still is off by less than half a step, as all others.  A group with an element that is not finite has the scale NaN, and all of it reads as NaN.
+//
+// Eight elements make a word: 2i and 2i + 1 are its fields i and i + 4, field f begins at bit 4f, so that a mask takes neighbouring elements out as the two halves of a register.
+// Pools: [page][KV head][slot] rows of words, and of scales; 4.5 bits an element.
+#pragma once
+
+#include "cs_paged.cuh"
+
+static constexpr int kQuantGroup = 32;
+static constexpr int kQuantMaxCtas = 320;      // CTAs of an attention launch at most (two on an SM)
+static constexpr int kQuantMaxRows = 32;       // query rows of one work item at most
+static constexpr int kQuantMaxSeqs = 256;      // sequences of one attention launch; more are further launches
+static constexpr int kQuantCopyPage = 128;     // slots of a page of the copies that tall blocks are worked out from; 64, 32 or 16 where sequences in whole pages would not fit
+
+struct QuantView {
+  uint32_t *k, *v;                   // words of eight elements
+  unsigned short *ks, *vs;           // scales, bf16
+  long long data_page, scale_page;   // from page to page, in words and in scales
+  int n_pages, page_size, page_shift, n_kv_heads;
+};
+
+struct cs_quant_cache {
+  cs_quant_config cfg;
+  QuantView view;
+  void* workspace;
+  size_t workspace_bytes;
+  int* status;                 // device status word
+  int* counters;               // pieces of an item that are done, by the CTA that holds its first tile; 0 between launches
+  float* parts;                // un-normalised pieces [kQuantMaxCtas][2][kQuantMaxRows][head_dim]
+  float* parts_ml;             // their (reference point, sum)
+  int num_sms;
+  unsigned attr_set;           // shared-memory opt-ins made, a bit per kernel instance
+  // copies in 16 bits of the positions that a call of tall blocks attends to
+  long long tall_positions;    // room, a multiple of 16; 0: none
+  char *tall_k, *tall_v;       // [page][KV head][slot][head_dim]
+  int *tall_table, *tall_len;  // 0, 1, 2, ...; lengths of the blocks that nothing is wrong with
+  cs_paged_cache* tall[2][4];  // by the queries' type (CS_BF16, CS_F16) and the size of a page (128 >> i)
+  char err[256];
+};
+
+// what an attention launch of few rows is about: what cs_paged.cuh deals work out by (pools left out), and the cache
+struct QuantAttnArgs {
+  PagedAttnArgs p;
+  QuantView kv;
+  int half;                    // queries and results are fp16 (else bf16)
+};
+
+cs_status cs_launch_quant_few(cs_quant_cache* c, const QuantAttnArgs& a, cudaStream_t st);
+
+#ifdef __CUDACC__
+namespace {
+
+__device__ __forceinline__ uint32_t bf2_mul(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t bf2_sub(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t bf2_fma(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+// (a & b) | c in one instruction
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+
+// The scales of a register's two halves, and what the conversion makes of them once.
+struct QuantScale {
+  uint32_t s, s8, c;           // s, s / 8, -24 s: all exact in bf16
+  __device__ __forceinline__ static QuantScale of(uint32_t pair) { return QuantScale{pair, bf2_mul(pair, 0x3e003e00u), bf2_mul(pair, 0xc1c0c1c0u)}; }
+};
+// Two 16-bit halves of four fields u = n + 8 each -> field i of both, times their scales: exact.  A field at bits 3 - 6 under the exponent of 128 reads 128 + 8 u, and one product and sum make s (u - 8) of it;
+// the one at bits 0 - 3 reads 128 + u, where -136 s would need ten bits, and takes a difference and a product instead of a shift.
+__device__ __forceinline__ void quant_expand(uint32_t w, const QuantScale& q, uint32_t (&r)[4]) {
+  r[0] = bf2_mul(bf2_sub(and_or(w, 0x000f000fu, 0x43004300u), 0x43084308u), q.s);
+  r[1] = bf2_fma(and_or(w >> 1, 0x00780078u, 0x43004300u), q.s8, q.c);
+  r[2] = bf2_fma(and_or(w >> 5, 0x00780078u, 0x43004300u), q.s8, q.c);
+  r[3] = bf2_fma(and_or(w >> 9, 0x00780078u, 0x43004300u), q.s8, q.c);
+}
+
+// is a scale not finite?
+__device__ __forceinline__ bool quant_odd(unsigned scale) { return (scale & 0x7f80u) == 0x7f80u; }
+
+}  // namespace
+#endif
