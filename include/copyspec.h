@@ -573,7 +573,7 @@ cs_status cs_paged_debug_drop_tile(cs_paged_cache* cache, int tile);
  *
  * A row (one position, one KV head) is cut into groups of 32 neighbouring elements.  With a = max |x| of a group, s = a / 7 rounded to five significant bits (nearest, halves to even; at most 2^123)
  * and n = x / s rounded to the nearest whole number (halves to even), |n| <= 7, the group is held as s in bf16 and numbers n + 8 of 4 bits, and stands for s n.  No element is off by more than s / 2 (but for
- * scales below 2^-126 or at the limit, beyond which values saturate); every value held is exactly a bf16 number.  A group with an element that is not finite has the scale NaN and reads as NaN throughout, as does any scale that is not finite.  Zeros stay zeros.
+ * scales below 2^-126 or at the limit, beyond which values saturate); every value held is exactly a bf16 number.  A group with an element that is not finite has the scale NaN and reads as NaN throughout.  Zeros stay zeros.
  *
  * Pools, for K and for V: numbers, of page `p`, KV head `h`, slot `s` from byte p * page_stride + (h * page_size + s) * head_dim / 2 on, and bf16 scales from element
  * p * scale_page_stride + (h * page_size + s) * head_dim / 32 on.  Eight elements are a 32-bit word; its elements 2i and 2i + 1 are at bits 4i and 16 + 4i.  16-byte aligned, strides multiples of 16

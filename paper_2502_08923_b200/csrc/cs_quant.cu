@@ -394,17 +394,19 @@ cs_status check_config(const cs_quant_config* c, const char** why) {
   if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) { *why = "head_dim must be 32, 64 or 128"; return CS_ERR_SHAPE; }
   if (c->page_size < 16 || (c->page_size & (c->page_size - 1)) != 0) { *why = "page_size must be a power of two from 16 on"; return CS_ERR_SHAPE; }
   if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 0x0fffffff) { *why = "no pages or no heads"; return CS_ERR_ARG; }
-  const int64_t row = (int64_t)c->n_kv_heads * c->page_size;
+  const int64_t row = (int64_t)c->n_kv_heads * c->page_size;         // rows of a page
   if (c->page_stride % 16 != 0 || c->scale_page_stride % 8 != 0 || (c->n_pages > 1 && (c->page_stride < row * (c->head_dim / 2) || c->scale_page_stride < row * (c->head_dim / kQuantGroup)))) {
     *why = "pages must not overlap, their strides must be multiples of 16 bytes";
     return CS_ERR_ARG;
   }
+  // (rows of a page times 64 bytes, and strides in 16 bytes, in 32 bits)
+  if (row > (1 << 26) || c->page_stride > (1ll << 35) || c->scale_page_stride > (1ll << 34)) { *why = "pages of more than 2^26 rows, or farther apart than 2^35 bytes"; return CS_ERR_SHAPE; }
   if (c->tall_positions < 0 || c->tall_positions > (1ll << 30)) { *why = "tall_positions must be between 0 and 2^30"; return CS_ERR_ARG; }
   return CS_OK;
 }
 
 struct QuantLayout {
-  size_t status, counters, parts, parts_ml, table, len, k, v, paged, total;
+  size_t status, splits, parts, parts_ml, table, len, k, v, paged, total;
   size_t paged_bytes;
   long long positions;         // room for copies
 };
@@ -422,9 +424,9 @@ QuantLayout layout_of(const cs_quant_config& c) {
   size_t at = 0;
   auto put = [&](size_t bytes) { const size_t o = at; at += (bytes + 255) & ~(size_t)255; return o; };
   l.status = put(256);
-  l.counters = put(kQuantMaxCtas * sizeof(int));
-  l.parts = put((size_t)kQuantMaxCtas * 2 * kQuantMaxRows * c.head_dim * 4);
-  l.parts_ml = put((size_t)kQuantMaxCtas * 2 * kQuantMaxRows * 8);
+  l.splits = put(kQuantMaxSms * kQuantCtasPerSm * sizeof(PagedSplit));
+  l.parts = put((size_t)kQuantMaxSms * kQuantRowsPerSm * 2 * c.head_dim * 4);
+  l.parts_ml = put((size_t)kQuantMaxSms * kQuantRowsPerSm * 2 * 8);
   l.positions = (c.tall_positions + 15) & ~15ll;
   if (l.positions > 0) {
     const cs_paged_config p = copies_config(c, l.positions, nullptr, nullptr, 3, CS_BF16);
@@ -464,21 +466,21 @@ cs_status create(const char* name, cs_quant_cache** out, const cs_quant_config* 
   cs_quant_cache* c = static_cast<cs_quant_cache*>(calloc(1, sizeof(cs_quant_cache)));
   if (c == nullptr) return refuse(CS_ERR_CAPACITY, "out of host memory");
   c->cfg = *cfg;
-  c->num_sms = 2 * sms < kQuantMaxCtas ? sms : kQuantMaxCtas / 2;
+  c->num_sms = sms < kQuantMaxSms ? sms : kQuantMaxSms;
   int shift = 0;
   while ((1 << shift) < cfg->page_size) ++shift;
   c->view = QuantView{static_cast<uint32_t*>(cfg->k), static_cast<uint32_t*>(cfg->v), static_cast<unsigned short*>(cfg->k_scale), static_cast<unsigned short*>(cfg->v_scale),
-                      cfg->page_stride / 4, cfg->scale_page_stride, cfg->n_pages, cfg->page_size, shift, cfg->n_kv_heads};
+                      cfg->page_stride / 4, cfg->scale_page_stride, (uint32_t)(cfg->page_stride / 16), (uint32_t)(cfg->scale_page_stride / 8), cfg->n_pages, cfg->page_size, shift, cfg->n_kv_heads};
   char* ws = static_cast<char*>(workspace);
   c->workspace = workspace;
   c->workspace_bytes = workspace_bytes;
   c->status = reinterpret_cast<int*>(ws + l.status);
-  c->counters = reinterpret_cast<int*>(ws + l.counters);
+  c->splits = reinterpret_cast<PagedSplit*>(ws + l.splits);
   c->parts = reinterpret_cast<float*>(ws + l.parts);
   c->parts_ml = reinterpret_cast<float*>(ws + l.parts_ml);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (first == nullptr) {
-    const cudaError_t e = cudaMemsetAsync(ws, 0, l.parts, st);
+    const cudaError_t e = cudaMemsetAsync(ws, 0, l.splits, st);
     if (e != cudaSuccess) {
       free(c);
       return refuse(CS_ERR_CUDA, cudaGetErrorString(e));
@@ -697,7 +699,7 @@ cs_status cs_quant_attention(cs_quant_cache* c, const cs_blocks* blocks, const v
   p.by_group = PagedDivisor::by(group);
   p.mask = mask; p.window = window;
   p.scale = scale; p.scale_log2e = (float)(1.4426950408889634 * (double)scale);
-  p.parts = c->parts; p.parts_ml = c->parts_ml; p.counters = c->counters; p.status = c->status;
+  p.parts = c->parts; p.parts_ml = c->parts_ml; p.splits = c->splits; p.status = c->status;
   p.drop = -1;
   for (int b = 0; b < blocks->n_seqs; b += kQuantMaxSeqs) {      // (a launch's plan holds so many)
     QuantAttnArgs part = a;

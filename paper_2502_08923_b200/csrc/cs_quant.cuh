@@ -13,15 +13,18 @@
 #include "cs_paged.cuh"
 
 static constexpr int kQuantGroup = 32;
-static constexpr int kQuantMaxCtas = 320;      // CTAs of an attention launch at most (two on an SM)
+static constexpr int kQuantMaxSms = 160;
+static constexpr int kQuantCtasPerSm = 4;      // of an attention launch, at most
 static constexpr int kQuantMaxRows = 32;       // query rows of one work item at most
-static constexpr int kQuantMaxSeqs = 256;      // sequences of one attention launch; more are further launches
+static constexpr int kQuantRowsPerSm = 64;     // query rows of the items that CTAs of an SM have at hand, at most
+static constexpr int kQuantMaxSeqs = 128;      // sequences of one attention launch; more are further launches
 static constexpr int kQuantCopyPage = 128;     // slots of a page of the copies that tall blocks are worked out from; 64, 32 or 16 where sequences in whole pages would not fit
 
 struct QuantView {
   uint32_t *k, *v;                   // words of eight elements
   unsigned short *ks, *vs;           // scales, bf16
   long long data_page, scale_page;   // from page to page, in words and in scales
+  uint32_t data_units, scale_units;  // the same in 16 bytes
   int n_pages, page_size, page_shift, n_kv_heads;
 };
 
@@ -31,8 +34,8 @@ struct cs_quant_cache {
   void* workspace;
   size_t workspace_bytes;
   int* status;                 // device status word
-  int* counters;               // pieces of an item that are done, by the CTA that holds its first tile; 0 between launches
-  float* parts;                // un-normalised pieces [kQuantMaxCtas][2][kQuantMaxRows][head_dim]
+  PagedSplit* splits;          // of the last launch of few rows, by CTA
+  float* parts;                // un-normalised pieces [CTA][2][query rows of an item][head_dim]
   float* parts_ml;             // their (reference point, sum)
   int num_sms;
   unsigned attr_set;           // shared-memory opt-ins made, a bit per kernel instance
@@ -64,6 +67,11 @@ __device__ __forceinline__ uint32_t bf2_mul(uint32_t a, uint32_t b) {
 __device__ __forceinline__ uint32_t bf2_sub(uint32_t a, uint32_t b) {
   uint32_t d;
   asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t h2_sub(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
 __device__ __forceinline__ uint32_t bf2_fma(uint32_t a, uint32_t b, uint32_t c) {
