@@ -43,6 +43,22 @@ template <typename T> __device__ __forceinline__ void load8(const char* p, float
     }
   }
 }
+// the same from shared memory
+template <typename T> __device__ __forceinline__ void lds8(const char* p, float (&f)[8]) {
+  const uint4 x = *reinterpret_cast<const uint4*>(p);
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  if constexpr (sizeof(T) == 4) {
+    const uint4 y = *(reinterpret_cast<const uint4*>(p) + 1);
+    f[0] = __uint_as_float(x.x); f[1] = __uint_as_float(x.y); f[2] = __uint_as_float(x.z); f[3] = __uint_as_float(x.w);
+    f[4] = __uint_as_float(y.x); f[5] = __uint_as_float(y.y); f[6] = __uint_as_float(y.z); f[7] = __uint_as_float(y.w);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 y = PagedType<T>::unpack(w[i]);
+      f[2 * i] = y.x; f[2 * i + 1] = y.y;
+    }
+  }
+}
 template <typename T> __device__ __forceinline__ void store8(char* p, const float (&f)[8]) {
   *reinterpret_cast<uint4*>(p) = make_uint4(PagedType<T>::pack(f[0], f[1]), PagedType<T>::pack(f[2], f[3]), PagedType<T>::pack(f[4], f[5]), PagedType<T>::pack(f[6], f[7]));
 }
@@ -63,13 +79,19 @@ __device__ __forceinline__ float scale_of(double most) {
   return __bfloat162float(__float2bfloat16_rn((float)__longlong_as_double(b >> 48 << 48)));
 }
 __device__ __forceinline__ uint32_t field_of(int i, int n) { return (uint32_t)(min(max(n, -7), 7) + 8) << (4 * (i / 2 + 4 * (i & 1))); }
-// eight elements of a group as a word
+// Eight elements of a group as a word.  The product with the reciprocal ends up beside the quotient, and so perhaps on the wrong side of a border; what is left of the element, exact in 32 bits, says so.
 __device__ __forceinline__ uint32_t word_of(const float (&y)[8], float s) {
   uint32_t w = 0;
-  const bool some = s > 0.f;
+  const float inv = s >= 1.17549435e-38f ? __fdiv_rn(1.f, s) : 0.f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w |= field_of(i, some ? __float2int_rn(__fdiv_rn(y[i], s)) : 0);
-  return w;
+  for (int i = 0; i < 8; ++i) {
+    // (the sum with 1.5 2^23 rounds to a whole number, halves to even)
+    const float q = fminf(fmaxf(y[i] * inv, -8.f), 8.f) + 12582912.f;
+    const float n = q - 12582912.f, rest = fmaf(-n, s, y[i]), beyond = fmaf(2.f, fabsf(rest), -s);
+    const int m = (int)__float_as_uint(q) - 0x4b400000;
+    w |= field_of(i, beyond > 0.f || (beyond == 0.f && (m & 1)) ? (rest > 0.f ? m + 1 : m - 1) : m);
+  }
+  return s > 0.f ? w : 0x88888888u;
 }
 // In 64 bits: the quotient, by the product with the reciprocal, is rounded to a multiple of 2^-44 first (the sum with 384 does that), which makes a whole number and a half of one that is a rounding beside it, and
 // then to a whole number (the sum with 1.5 2^52).
@@ -78,7 +100,7 @@ __device__ __forceinline__ uint32_t word_of(const double (&y)[8], float s) {
   const double inv = s > 0.f ? 1.0 / (double)s : 0.0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) w |= field_of(i, __double2loint(fma(y[i], inv, 384.0) + (6755399441055744.0 - 384.0)));
-  return w;
+  return s > 0.f ? w : 0x88888888u;
 }
 // the largest of some, NaN if one is not finite  (fmax leaves NaN out, and 0 x inf is NaN)
 template <int N, typename R> __device__ __forceinline__ R most_of(const R* y) {
@@ -91,16 +113,46 @@ template <int N, typename R> __device__ __forceinline__ R most_of(const R* y) {
   return m + z;
 }
 
+__device__ __forceinline__ void fetch16(uint32_t dst, const char* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// A unit is 512 elements: up to kPer neighbouring heads of the queries, the keys or the values of a row.  Units lie in a ring of shared memory for each warp, as in memory; three are in flight.
 template <typename S, typename D, int DH>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 3)
 k_quant_append(const __grid_constant__ QuantAppendArgs a) {
   CS_PDL_PROLOGUE();
   constexpr int kLanes = DH / 16, kPer = 32 / kLanes, kWords = DH / 8;      // lanes of a head, heads of a unit, words of a head
+  constexpr int kSize = (int)sizeof(S), kUnit = 512 * kSize, kPieces = kUnit / 512, kHeadPieces = DH * kSize / 16, kSlots = 4;      // bytes of a unit; 16-byte pieces of a lane, of a head
+  __shared__ __align__(16) uint8_t s_ring[kWarps][kSlots][kUnit];
   __shared__ int s_seq[kWarps], s_pos[kWarps];
   __shared__ double s_most[kWarps][64];          // [head][word]
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, pair = lane % kLanes, sub = lane / kLanes;
   const int n_here = kWarps / a.warps_per_row;
   const long long row0 = (long long)blockIdx.x * n_here, row = row0 + warp / a.warps_per_row;
+  const int uq = (a.n_q + kPer - 1) / kPer, uk = uq + (a.n_kv + kPer - 1) / kPer, units = row < a.n_rows ? uk + (a.n_kv + kPer - 1) / kPer : 0;
+  const int step = a.warps_per_row, u0 = warp % step;
+  const uint32_t ring = (uint32_t)__cvta_generic_to_shared(&s_ring[warp][0][0]);
+  int fu = u0;
+  uint32_t f_at = 0;
+  auto fetch = [&]() {
+    if (fu < units) {
+      const int kind = fu < uq ? 0 : fu < uk ? 1 : 2, h0 = (fu - (kind == 0 ? 0 : kind == 1 ? uq : uk)) * kPer, n = kind == 0 ? a.n_q : a.n_kv;
+      const long long head = kind == 0 ? a.q_head : kind == 1 ? a.k_head : a.v_head;
+      const char* src = kind == 0 ? a.q + row * a.q_row * kSize : kind == 1 ? a.k + row * a.k_row * kSize : a.v + row * a.v_row * kSize;
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i) {
+        const int e = i * 32 + lane, h = h0 + e / kHeadPieces, c = e % kHeadPieces;
+        if (h < n) fetch16(ring + f_at + e * 16, src + h * head * kSize + c * 16);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    fu += step;
+    f_at = f_at == (kSlots - 1) * kUnit ? 0 : f_at + kUnit;
+  };
+#pragma unroll
+  for (int i = 0; i < kSlots - 1; ++i) fetch();  // (whose row it is, and where it goes, takes three loads in a row: these are under way meanwhile)
+
   // the blocks these rows belong to
   if (threadIdx.x < kWarps) s_seq[threadIdx.x] = -1;
   __syncthreads();
@@ -115,16 +167,14 @@ k_quant_append(const __grid_constant__ QuantAppendArgs a) {
     }
   }
   __syncthreads();
-  const int b = s_seq[warp / a.warps_per_row];
-  if (b < 0 || row >= a.n_rows) return;
-  const int pos = s_pos[warp / a.warps_per_row];
-  if (a.rot_dim > 0 && pos >= a.n_positions) {
-    if (lane == 0) atomicOr(a.status, CS_DEV_CAPACITY);
+  const int b = s_seq[warp / a.warps_per_row], pos = s_pos[warp / a.warps_per_row];
+  const bool lost = b >= 0 && a.rot_dim > 0 && pos >= a.n_positions;
+  if (lost && lane == 0) atomicOr(a.status, CS_DEV_CAPACITY);
+  if (b < 0 || lost) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
     return;
   }
   const int page = __ldcg(a.blk.table + (long long)b * a.blk.table_width + (pos >> a.kv.page_shift)), slot = pos & (a.kv.page_size - 1);
-  const bool kept = (unsigned)page < (unsigned)a.kv.n_pages;
-  if (!kept && lane == 0) atomicOr(a.status, CS_DEV_BADARG);
 
   // this lane's words: partners of the rotation, or two neighbours behind what is rotated
   const int half = a.rot_dim >> 4;
@@ -135,26 +185,25 @@ k_quant_append(const __grid_constant__ QuantAppendArgs a) {
     load8<float>(reinterpret_cast<const char*>(a.rope + (long long)pos * a.rot_dim + c0 * 8), cs);
     load8<float>(reinterpret_cast<const char*>(a.rope + (long long)pos * a.rot_dim + (c0 + half) * 8), sn);
   }
-  const int uq = (a.n_q + kPer - 1) / kPer, uk = uq + (a.n_kv + kPer - 1) / kPer, units = uk + (a.n_kv + kPer - 1) / kPer;
-  for (int u = warp % a.warps_per_row; u < units; u += a.warps_per_row) {
+  const bool kept = (unsigned)page < (unsigned)a.kv.n_pages;
+  if (!kept && lane == 0) atomicOr(a.status, CS_DEV_BADARG);
+  uint32_t at = 0;
+  for (int u = u0; u < units; u += step) {
     const int kind = u < uq ? 0 : u < uk ? 1 : 2;
     const int h = (u - (kind == 0 ? 0 : kind == 1 ? uq : uk)) * kPer + sub;
     const bool live = h < (kind == 0 ? a.n_q : a.n_kv);
-    float x0[8] = {}, x1[8] = {};
-    if (live) {
-      const char* src = kind == 0 ? a.q + (row * a.q_row + h * a.q_head) * (long long)sizeof(S) : kind == 1 ? a.k + (row * a.k_row + h * a.k_head) * (long long)sizeof(S) : a.v + (row * a.v_row + h * a.v_head) * (long long)sizeof(S);
-      load8<S>(src + c0 * 8 * (int)sizeof(S), x0);
-      load8<S>(src + c1 * 8 * (int)sizeof(S), x1);
+    asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 2) : "memory");
+    __syncwarp();
+    float x0[8], x1[8];
+    {
+      const char* mine = reinterpret_cast<const char*>(&s_ring[warp][0][0]) + at + sub * DH * kSize;
+      lds8<S>(mine + c0 * 8 * kSize, x0);
+      lds8<S>(mine + c1 * 8 * kSize, x1);
     }
+    __syncwarp();
+    fetch();                                     // (into the place of the unit before: all lanes have read it)
+    at = at == (kSlots - 1) * kUnit ? 0 : at + kUnit;
     const char* gain = kind == 0 ? a.q_gain : kind == 1 ? a.k_gain : nullptr;
-    float g0[8], g1[8];
-    if (gain != nullptr) {
-      load8<D>(gain + c0 * 8 * (int)sizeof(D), g0);
-      load8<D>(gain + c1 * 8 * (int)sizeof(D), g1);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) g0[i] = g1[i] = 1.f;
-    }
     if (kind == 0) {
       float r = 1.f;
       if (gain != nullptr) {
@@ -164,12 +213,21 @@ k_quant_append(const __grid_constant__ QuantAppendArgs a) {
 #pragma unroll
         for (int o = 1; o < kLanes; o <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
         r = rsqrtf(sq * (1.f / DH) + a.eps);
-      }
+        float g[8];
+        load8<D>(gain + c0 * 8 * (int)sizeof(D), g);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float u0 = x0[i] * r * g0[i], u1 = x1[i] * r * g1[i];
-        x0[i] = rotated ? u0 * cs[i] - u1 * sn[i] : u0;
-        x1[i] = rotated ? u1 * cs[i] + u0 * sn[i] : u1;
+        for (int i = 0; i < 8; ++i) x0[i] *= r * g[i];
+        load8<D>(gain + c1 * 8 * (int)sizeof(D), g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x1[i] *= r * g[i];
+      }
+      if (rotated) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float y = x0[i] * cs[i] - x1[i] * sn[i];
+          x1[i] = x1[i] * cs[i] + x0[i] * sn[i];
+          x0[i] = y;
+        }
       }
       if (live) {
         char* dst = a.yq + (row * a.yq_row + h * a.yq_head) * (long long)sizeof(D);
@@ -178,23 +236,38 @@ k_quant_append(const __grid_constant__ QuantAppendArgs a) {
       }
       continue;
     }
+    if (!live) {                                 // (what lies in the ring there is another unit's)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x0[i] = x1[i] = 0.f;
+    }
     uint32_t w0, w1;
     float s0, s1;
     if (kind == 1 && (gain != nullptr || a.rot_dim > 0)) {
       double y0[8], y1[8], r = 1.0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) { y0[i] = (double)x0[i]; y1[i] = (double)x1[i]; }
       if (gain != nullptr) {
         double sq = 0.0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sq = fma((double)x0[i], (double)x0[i], fma((double)x1[i], (double)x1[i], sq));
+        for (int i = 0; i < 8; ++i) sq = fma(y0[i], y0[i], fma(y1[i], y1[i], sq));
 #pragma unroll
         for (int o = 1; o < kLanes; o <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
         r = rsqrt(sq * (1.0 / DH) + (double)a.eps);
-      }
+        float g[8];
+        load8<D>(gain + c0 * 8 * (int)sizeof(D), g);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const double u0 = (double)x0[i] * (double)g0[i], u1 = (double)x1[i] * (double)g1[i];
-        y0[i] = r * (rotated ? u0 * (double)cs[i] - u1 * (double)sn[i] : u0);
-        y1[i] = r * (rotated ? u1 * (double)cs[i] + u0 * (double)sn[i] : u1);
+        for (int i = 0; i < 8; ++i) y0[i] *= r * (double)g[i];
+        load8<D>(gain + c1 * 8 * (int)sizeof(D), g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y1[i] *= r * (double)g[i];
+      }
+      if (rotated) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const double c = (double)cs[i], s = (double)sn[i], y = y0[i] * c - y1[i] * s;
+          y1[i] = y1[i] * c + y0[i] * s;
+          y0[i] = y;
+        }
       }
       double* most = &s_most[warp][sub * kWords];
       most[c0] = most_of<8>(y0);
@@ -230,13 +303,16 @@ k_quant_append(const __grid_constant__ QuantAppendArgs a) {
 
 // ------------------------------------------------------------------ reading back
 // One word, a lane: eight elements of 16 bits are 16 bytes side by side with its neighbours'.  A warp has eight of them in flight.
+constexpr int kReadRows = 8;
 struct QuantReadArgs {
   QuantView kv;
   BlocksView blk;
   char *k, *v;                       // destinations of rows, or of copies
   long long k_row, k_head, v_row, v_head;      // elements; copies: page, head (of both)
   int mask, window;                  // copies: which keys the blocks attend to
+  int rows_per_warp;                 // up to kReadRows
   int copy_pages, copy_shift;        // pages of a sequence's copies, their size
+  int shares;                        // warps that share the heads of sixteen positions
   int* copy_len;                     // lengths of blocks that nothing is wrong with
   int* status;
 };
@@ -283,8 +359,8 @@ __device__ __forceinline__ void read_row(const QuantView& kv, int page, int slot
       s[0][j] = s[1][j] = 0;
       if (i < n && exists) {
         const long long d = page * kv.data_page + h * head_words + slot * kWords + c, g = page * kv.scale_page + h * head_scales + slot * (DH / kQuantGroup) + c / 4;
-        w[0][j] = __ldcs(kv.k + d); s[0][j] = __ldcs(kv.ks + g);
-        w[1][j] = __ldcs(kv.v + d); s[1][j] = __ldcs(kv.vs + g);
+        w[0][j] = __ldg(kv.k + d); s[0][j] = __ldg(kv.ks + g);
+        w[1][j] = __ldg(kv.v + d); s[1][j] = __ldg(kv.vs + g);
       }
     }
 #pragma unroll
@@ -300,14 +376,15 @@ __device__ __forceinline__ void read_row(const QuantView& kv, int page, int slot
 
 constexpr int kReadWarps = 8;
 
+// A warp has rows_per_warp neighbouring rows: what finding a row takes (whose block, which page, one load after the other) is under way for all of them at once.
 template <typename T, int DH>
 __global__ void __launch_bounds__(kReadWarps * 32)
 k_quant_read(const __grid_constant__ QuantReadArgs a) {
   CS_PDL_PROLOGUE();
-  __shared__ int s_seq[kReadWarps], s_pos[kReadWarps];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long row0 = (long long)blockIdx.x * kReadWarps, row = row0 + warp;
-  if (threadIdx.x < kReadWarps) s_seq[threadIdx.x] = -1;
+  __shared__ int s_seq[kReadWarps * kReadRows], s_pos[kReadWarps * kReadRows];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, here = kReadWarps * a.rows_per_warp;
+  const long long row0 = (long long)blockIdx.x * here;
+  if (threadIdx.x < here) s_seq[threadIdx.x] = -1;
   __syncthreads();
   for (int b = threadIdx.x; b < a.blk.n_seqs; b += kReadWarps * 32) {
     const int start = __ldcg(a.blk.start + b), len = __ldcg(a.blk.len + b), kv = __ldcg(a.blk.kv_len + b);
@@ -315,24 +392,36 @@ k_quant_read(const __grid_constant__ QuantReadArgs a) {
     if (flag != 0) {
       if (blockIdx.x == 0) atomicOr(a.status, flag);
     } else {
-      for (int i = 0; i < kReadWarps; ++i)
-        if (row0 + i >= start && row0 + i - start < len) { s_seq[i] = b; s_pos[i] = kv + (int)(row0 + i - start); }
+      // (rows of this CTA that are the block's)
+      const int from = (int)max(0ll, start - row0), to = (int)min((long long)here, (long long)start + len - row0);
+      for (int i = from; i < to; ++i) { s_seq[i] = b; s_pos[i] = kv + (int)(row0 + i - start); }
     }
   }
   __syncthreads();
-  const int b = s_seq[warp];
-  if (b < 0 || row >= a.blk.rows) return;
-  const int pos = s_pos[warp], page = __ldcg(a.blk.table + (long long)b * a.blk.table_width + (pos >> a.kv.page_shift));
-  const bool exists = (unsigned)page < (unsigned)a.kv.n_pages;
-  if (!exists && lane == 0) atomicOr(a.status, CS_DEV_BADARG);
-  read_row<T, DH>(a.kv, page, pos & (a.kv.page_size - 1), exists, a.k + row * a.k_row * (long long)sizeof(T), a.k_head, a.v + row * a.v_row * (long long)sizeof(T), a.v_head, lane);
+  int b = -1, pos = 0, page = -1;
+  if (lane < a.rows_per_warp) {
+    b = s_seq[warp * a.rows_per_warp + lane];
+    pos = s_pos[warp * a.rows_per_warp + lane];
+    if (b >= 0) {
+      page = __ldcg(a.blk.table + (long long)b * a.blk.table_width + (pos >> a.kv.page_shift));
+      if ((unsigned)page >= (unsigned)a.kv.n_pages) atomicOr(a.status, CS_DEV_BADARG);
+    }
+  }
+  for (int i = 0; i < a.rows_per_warp; ++i) {
+    if (__shfl_sync(0xffffffffu, b, i) < 0) continue;
+    const int at = __shfl_sync(0xffffffffu, page, i), p = __shfl_sync(0xffffffffu, pos, i);
+    const long long row = row0 + warp * a.rows_per_warp + i;
+    read_row<T, DH>(a.kv, at, p & (a.kv.page_size - 1), (unsigned)at < (unsigned)a.kv.n_pages, a.k + row * a.k_row * (long long)sizeof(T), a.k_head, a.v + row * a.v_row * (long long)sizeof(T), a.v_head, lane);
+  }
 }
 
-// Copies in 16 bits of the positions that blocks attend to, for the attention of tall blocks: sequence b's in the pages from b copy_pages on.
+// Copies in 16 bits of the positions that blocks attend to, for the attention of tall blocks: sequence b's in the pages from b copy_pages on.  Sixteen positions of a head are one run of words, of scales and of copied
+// elements; a warp has several heads of them, so that finding them (lengths, page) is paid once.
 template <typename T, int DH>
 __global__ void __launch_bounds__(kReadWarps * 32)
 k_quant_copy(const __grid_constant__ QuantReadArgs a) {
   CS_PDL_PROLOGUE();
+  constexpr int kWords = 16 * DH / 8, kEach = kWords / 32;               // words of a run, of a lane
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (blockIdx.x == 0)
     for (int b = threadIdx.x; b < a.blk.n_seqs; b += kReadWarps * 32) {
@@ -340,21 +429,42 @@ k_quant_copy(const __grid_constant__ QuantReadArgs a) {
       if (flag != 0) atomicOr(a.status, flag);
       a.copy_len[b] = flag != 0 ? 0 : len;
     }
-  // eight positions a CTA at a time, which no page splits
-  const int chunks = (a.copy_pages << a.copy_shift) / kReadWarps;
-  for (long long i = blockIdx.x; i < (long long)a.blk.n_seqs * chunks; i += gridDim.x) {
-    const int b = (int)(i / chunks), pos0 = (int)(i - (long long)b * chunks) * kReadWarps;
-    const int len = __ldcg(a.blk.len + b), kv = __ldcg(a.blk.kv_len + b);
-    if (len <= 0 || paged_block_flag(a.blk, a.kv.page_size, a.mask != CS_MASK_PREFIX, __ldcg(a.blk.start + b), len, kv) != 0) continue;
+  const int runs = (a.copy_pages << a.copy_shift) / 16, H = a.kv.n_kv_heads;
+  // tasks: (sequence, sixteen positions, share of the heads)
+  const long long n = (long long)a.blk.n_seqs * runs * a.shares;
+  for (long long i = (long long)blockIdx.x * kReadWarps + warp; i < n; i += (long long)gridDim.x * kReadWarps) {
+    const int share = (int)(i % a.shares), b = (int)(i / a.shares / runs), pos = (int)(i / a.shares - (long long)b * runs) * 16;
+    const int start = __ldcg(a.blk.start + b), len = __ldcg(a.blk.len + b), kv = __ldcg(a.blk.kv_len + b);
+    if (len <= 0 || paged_block_flag(a.blk, a.kv.page_size, a.mask != CS_MASK_PREFIX, start, len, kv) != 0) continue;
     int lo, hi;
     paged_range(a.mask, a.window, len, kv, 0, len - 1, lo, hi);
-    const int pos = pos0 + warp;
-    if (pos < lo || pos >= hi) continue;
+    if (pos + 16 <= lo || pos >= hi) continue;
     const int page = __ldcg(a.blk.table + (long long)b * a.blk.table_width + (pos >> a.kv.page_shift));
     const bool exists = (unsigned)page < (unsigned)a.kv.n_pages;
     if (!exists && lane == 0) atomicOr(a.status, CS_DEV_BADARG);
-    const long long at = (((long long)b * a.copy_pages + (pos >> a.copy_shift)) * a.k_row + (long long)(pos & ((1 << a.copy_shift) - 1)) * DH) * (long long)sizeof(T);
-    read_row<T, DH>(a.kv, page, pos & (a.kv.page_size - 1), exists, a.k + at, a.k_head, a.v + at, a.k_head, lane);
+    const int slot = pos & (a.kv.page_size - 1);
+    const long long at = ((long long)b * a.copy_pages + (pos >> a.copy_shift)) * a.k_row + (long long)(pos & ((1 << a.copy_shift) - 1)) * DH;
+    for (int h = share; h < H; h += a.shares) {
+      const long long row = (long long)h * a.kv.page_size + slot;
+      uint32_t w[2][kEach];
+      unsigned s[2][kEach];
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        w[0][j] = w[1][j] = 0x88888888u;
+        s[0][j] = s[1][j] = 0;
+        if (exists) {
+          const long long d = page * a.kv.data_page + row * (DH / 8) + j * 32 + lane, g = page * a.kv.scale_page + row * (DH / kQuantGroup) + (j * 32 + lane) / 4;
+          w[0][j] = __ldg(a.kv.k + d); s[0][j] = __ldg(a.kv.ks + g);
+          w[1][j] = __ldg(a.kv.v + d); s[1][j] = __ldg(a.kv.vs + g);
+        }
+      }
+      const long long to = (at + h * a.k_head) * (long long)sizeof(T);
+#pragma unroll
+      for (int j = 0; j < kEach; ++j) {
+        put8<T>(a.k + to + (j * 32 + lane) * 8 * (int)sizeof(T), w[0][j], s[0][j]);
+        put8<T>(a.v + to + (j * 32 + lane) * 8 * (int)sizeof(T), w[1][j], s[1][j]);
+      }
+    }
   }
 }
 
@@ -518,7 +628,7 @@ template <typename S, typename D>
 cudaError_t launch_append(QuantAppendArgs a, int head_dim, cudaStream_t st) {
   const int per = 512 / head_dim, units = cs_ceil_div(a.n_q, per) + 2 * cs_ceil_div(a.n_kv, per);
   a.warps_per_row = kWarps;
-  while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)a.n_rows * a.warps_per_row > 148 * 16)) a.warps_per_row /= 2;
+  while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)a.n_rows * a.warps_per_row > 148 * 12)) a.warps_per_row /= 2;
   const dim3 grid((unsigned)(((long long)a.n_rows * a.warps_per_row + kWarps - 1) / kWarps)), block(kThreads);
   switch (head_dim) {
     case 32: return cs_launch_pdl(k_quant_append<S, D, 32>, grid, block, 0, st, a);
@@ -527,8 +637,12 @@ cudaError_t launch_append(QuantAppendArgs a, int head_dim, cudaStream_t st) {
   }
 }
 template <typename T>
-cudaError_t launch_read(const QuantReadArgs& a, int head_dim, cudaStream_t st) {
-  const dim3 grid((unsigned)(((long long)a.blk.rows + kReadWarps - 1) / kReadWarps)), block(kReadWarps * 32);
+cudaError_t launch_read(QuantReadArgs a, int head_dim, int sms, cudaStream_t st) {
+  // (as many rows a warp as leave every SM its warps)
+  a.rows_per_warp = kReadRows;
+  while (a.rows_per_warp > 1 && (long long)a.blk.rows < (long long)sms * 32 * a.rows_per_warp) a.rows_per_warp /= 2;
+  const int here = kReadWarps * a.rows_per_warp;
+  const dim3 grid((unsigned)(((long long)a.blk.rows + here - 1) / here)), block(kReadWarps * 32);
   switch (head_dim) {
     case 32: return cs_launch_pdl(k_quant_read<T, 32>, grid, block, 0, st, a);
     case 64: return cs_launch_pdl(k_quant_read<T, 64>, grid, block, 0, st, a);
@@ -536,9 +650,12 @@ cudaError_t launch_read(const QuantReadArgs& a, int head_dim, cudaStream_t st) {
   }
 }
 template <typename T>
-cudaError_t launch_copy(const QuantReadArgs& a, int head_dim, int sms, cudaStream_t st) {
-  const long long chunks = (long long)a.blk.n_seqs * ((a.copy_pages << a.copy_shift) / kReadWarps);
-  const dim3 grid((unsigned)(chunks < 8 * sms ? (chunks > 0 ? chunks : 1) : 8 * sms)), block(kReadWarps * 32);
+cudaError_t launch_copy(QuantReadArgs a, int head_dim, int sms, cudaStream_t st) {
+  const long long runs = (long long)a.blk.n_seqs * ((a.copy_pages << a.copy_shift) / 16);
+  a.shares = 1;
+  while (2 * a.shares <= a.kv.n_kv_heads && runs * a.shares < 64ll * sms) a.shares *= 2;
+  const long long ctas = (runs * a.shares + kReadWarps - 1) / kReadWarps;
+  const dim3 grid((unsigned)(ctas < 8 * sms ? (ctas > 0 ? ctas : 1) : 8 * sms)), block(kReadWarps * 32);
   switch (head_dim) {
     case 32: return cs_launch_pdl(k_quant_copy<T, 32>, grid, block, 0, st, a);
     case 64: return cs_launch_pdl(k_quant_copy<T, 64>, grid, block, 0, st, a);
@@ -643,7 +760,7 @@ cs_status cs_quant_read(cs_quant_cache* c, const cs_blocks* blocks, const cs_hea
   a.v = static_cast<char*>(v->y); a.v_row = v->y_row_stride; a.v_head = v->y_head_stride;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int dh = c->cfg.head_dim;
-  CS_CUDA_OK(c, out == CS_F32 ? launch_read<float>(a, dh, st) : out == CS_BF16 ? launch_read<__nv_bfloat16>(a, dh, st) : launch_read<__half>(a, dh, st));
+  CS_CUDA_OK(c, out == CS_F32 ? launch_read<float>(a, dh, c->num_sms, st) : out == CS_BF16 ? launch_read<__nv_bfloat16>(a, dh, c->num_sms, st) : launch_read<__half>(a, dh, c->num_sms, st));
   return CS_OK;
 }
 
@@ -655,6 +772,7 @@ cs_status cs_quant_attention(cs_quant_cache* c, const cs_blocks* blocks, const v
   if (s != CS_OK) return fail(c, s, "bad blocks");
   if (dtype != CS_BF16 && dtype != CS_F16) return fail(c, CS_ERR_ARG, "queries are CS_BF16 or CS_F16");
   if (mask < CS_MASK_CAUSAL || mask > CS_MASK_FULL || window < 0 || !(scale > 0.f) || !(scale <= 2.0e38f)) return fail(c, CS_ERR_ARG, "bad mask, window or scale");
+  if ((long long)blocks->table_width * c->cfg.page_size > (1ll << 30)) return fail(c, CS_ERR_SHAPE, "a sequence has room for 2^30 positions at most");
   if (n_heads < 1 || n_heads % c->cfg.n_kv_heads != 0 || n_heads / c->cfg.n_kv_heads > 128) return fail(c, CS_ERR_SHAPE, "n_heads must be a multiple of the cache's heads, at most 128 per KV head");
   if ((long long)blocks->rows * n_heads > 0x7fffff00ll) return fail(c, CS_ERR_SHAPE, "too many rows");
   if (blocks->n_seqs == 0 || blocks->rows == 0) return CS_OK;
@@ -672,7 +790,7 @@ cs_status cs_quant_attention(cs_quant_cache* c, const cs_blocks* blocks, const v
     copy_pages = (room + (kQuantCopyPage >> size) - 1) >> (7 - size);
     if ((copy_pages << (7 - size)) <= c->tall_positions / blocks->n_seqs) break;
   }
-  if (per_seq > 96 && size < 4 && copy_pages > 0) {
+  if (per_seq > 64 && size < 4 && copy_pages > 0) {
     QuantReadArgs r = {};
     r.kv = c->view; r.blk = view_of(blocks); r.status = c->status;
     r.k = c->tall_k; r.v = c->tall_v;

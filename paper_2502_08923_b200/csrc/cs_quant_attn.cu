@@ -41,9 +41,9 @@ template <int DH, int NT> struct Few {
   static constexpr int kExchange = kWarps * kCols * kLd * 4;
   static constexpr int kQRow = DH * 2 + (DH == 32 ? 0 : 64); // bytes of a query row (the rest keeps rows out of each other's banks)
   static constexpr int kQ = kCols * kQRow;
-  static constexpr int kMl = kWarps * kCols * 8;
+  static constexpr int kMl = (kWarps + 1) * kCols * 8;
   static constexpr int kPiece = (sizeof(PagedPiece) + 15) / 16 * 16;
-  static constexpr int kSmem = kRing + kExchange + kQ + kMl + kWarps * kPieces * kPiece + (int)sizeof(Plan) + 128;
+  static constexpr int kSmem = kRing + kExchange + kQ + kMl + kWarps * kPieces * kPiece + (int)sizeof(Plan) + 16 + 128;
 };
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool on) {
@@ -133,29 +133,35 @@ k_quant_few(const __grid_constant__ QuantAttnArgs qa) {
   float* s_x = reinterpret_cast<float*>(ring + F::kRing);                        // [warp][row][kLd]
   uint8_t* s_q = reinterpret_cast<uint8_t*>(s_x) + F::kExchange;                 // [row][DH]
   float2* s_ml = reinterpret_cast<float2*>(s_q + F::kQ);                         // [warp][row]
+  float2* s_row = s_ml + kWarps * kCols;                                         // [row]
   uint8_t* s_piece = reinterpret_cast<uint8_t*>(s_ml) + F::kMl;                  // [warp][piece]
   Plan& plan = *reinterpret_cast<Plan*>(s_piece + kWarps * F::kPieces * F::kPiece);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
 
-  paged_plan(a, plan);
+  // (One warp where one can do it: sixteen of an SM's at the same thing take twice as long.)
+  if (a.blk.n_seqs > 32 || warp == 0) paged_plan(a, plan);
+  if (a.blk.n_seqs <= 32) __syncthreads();
   const long long total = plan.before[a.blk.n_seqs];
   const int n_cta = (int)min((long long)gridDim.x, total), cta = blockIdx.x;
   if (cta >= n_cta) {
     if (tid == 0) a.splits[cta].last = kPagedNone;
     return;
   }
-  long long run1;
+  long long& s_end = *reinterpret_cast<long long*>(&plan + 1);                    // where the run ends
   // Pieces are described in shared memory, for each warp by itself, and read where they are used: kept in registers they would spill.  (Piece number k in place k % kPieces.)
   uint8_t* my_pieces = s_piece + warp * F::kPieces * F::kPiece;
   auto piece = [&](int k) -> PagedPiece& { return *reinterpret_cast<PagedPiece*>(my_pieces + (k & (F::kPieces - 1)) * F::kPiece); };
-  {
-    const PagedPiece first = paged_run(a, plan, total, n_cta, cta, lane, run1);
-    if (first.n_tiles == 0) {
-      if (tid == 0) a.splits[cta].last = kPagedNone;
-      return;
-    }
-    piece(0) = first;
-    __syncwarp();
+  if (warp == 0) {
+    long long end;
+    const PagedPiece first = paged_run(a, plan, total, n_cta, cta, lane, end);
+    if (lane == 0) s_end = end;
+    for (int w = 0; w < kWarps; ++w) *reinterpret_cast<PagedPiece*>(s_piece + w * F::kPieces * F::kPiece) = first;
+  }
+  __syncthreads();
+  const long long run1 = s_end;
+  if (piece(0).n_tiles == 0) {
+    if (tid == 0) a.splits[cta].last = kPagedNone;
+    return;
   }
   int n_known = 1, n_pieces = 0x7fffffff;        // pieces described; pieces of the run, once that is known
   // is there a piece k?  (k is at most n_known)
@@ -475,6 +481,7 @@ k_quant_few(const __grid_constant__ QuantAttnArgs qa) {
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
+          if (8 * nt + 2 * t + e >= rows) continue;
           float4* dst = reinterpret_cast<float4*>(s_x + (warp * kCols + 8 * nt + 2 * t + e) * F::kLd + kMine * g);
 #pragma unroll
           for (int i = 0; i < kMine / 4; ++i) {
@@ -483,36 +490,50 @@ k_quant_few(const __grid_constant__ QuantAttnArgs qa) {
           }
         }
       __syncthreads();
-#pragma unroll 1
-      for (int n = warp; n < rows; n += kWarps) {
-        if (2 * lane >= F::kPass) break;
-        float2 ml[kWarps], y[kWarps];
-        float M = -INFINITY, L = 0.f, x0 = 0.f, x1 = 0.f;
+      if (w == 0) {
+        // a row's common reference point and sum, and what each warp's share of it counts
+        if (tid < rows) {
+          float2 ml[kWarps];
+          float M = -INFINITY, L = 0.f;
+#pragma unroll
+          for (int v = 0; v < kWarps; ++v) {
+            ml[v] = s_ml[v * kCols + tid];
+            M = fmaxf(M, ml[v].x);
+          }
+#pragma unroll
+          for (int v = 0; v < kWarps; ++v) {
+            const float k = ml[v].x == -INFINITY ? 0.f : paged_ex2(ml[v].x - M);
+            L += ml[v].x == -INFINITY && ml[v].y == 0.f ? 0.f : k * ml[v].y;      // (without a maximum, but a sum: NaN)
+            s_ml[v * kCols + tid] = make_float2(k, ml[v].y);
+          }
+          s_row[tid] = make_float2(M, L);
+        }
+        __syncthreads();
+      }
+      constexpr int kQuads = F::kPass / 4;       // four columns of a row a thread
+#pragma unroll 2
+      for (int i = tid; i < rows * kQuads; i += kThreads) {
+        const int n = i / kQuads, c = i % kQuads;
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int v = 0; v < kWarps; ++v) {
-          ml[v] = s_ml[v * kCols + n];
-          y[v] = *reinterpret_cast<const float2*>(s_x + (v * kCols + n) * F::kLd + 2 * lane);
-          M = fmaxf(M, ml[v].x);
+          const float2 k = s_ml[v * kCols + n];
+          const float4 y = *reinterpret_cast<const float4*>(s_x + (v * kCols + n) * F::kLd + 4 * c);
+          if (k.x == 0.f && k.y == 0.f) continue;                  // (it saw nothing)
+          acc[0] = fmaf(k.x, y.x, acc[0]); acc[1] = fmaf(k.x, y.y, acc[1]); acc[2] = fmaf(k.x, y.z, acc[2]); acc[3] = fmaf(k.x, y.w, acc[3]);
         }
-#pragma unroll
-        for (int v = 0; v < kWarps; ++v) {
-          if (ml[v].x == -INFINITY && ml[v].y == 0.f) continue;      // (it saw nothing)
-          const float k = ml[v].x == -INFINITY ? 0.f : paged_ex2(ml[v].x - M);
-          L = fmaf(k, ml[v].y, L);
-          x0 = fmaf(k, y[v].x, x0);
-          x1 = fmaf(k, y[v].y, x1);
-        }
-        const int d = 2 * lane / kMine * (kMine * kPasses) + kMine * w + 2 * lane % kMine;
+        const float2 row = s_row[n];
+        const int d = 4 * c / kMine * (kMine * kPasses) + kMine * w + 4 * c % kMine;
         if (p.whole) {
-          const float inv = L == 0.f ? 0.f : 1.f / L;
+          const float inv = row.y == 0.f ? 0.f : 1.f / row.y;
           const int mrow = p.rg * kCols + n, r = a.by_group.of(mrow);
           const long long at = (long long)(p.start + r) * a.n_heads + p.head * G + (mrow - r * G);
-          *reinterpret_cast<uint32_t*>(a.out + (at * DH + d) * 2) = PagedType<T>::pack(x0 * inv, x1 * inv);
-          if (a.lse != nullptr && lane == 0 && w == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+          *reinterpret_cast<uint2*>(a.out + (at * DH + d) * 2) = make_uint2(PagedType<T>::pack(acc[0] * inv, acc[1] * inv), PagedType<T>::pack(acc[2] * inv, acc[3] * inv));
+          if (a.lse != nullptr && c == 0 && w == 0) a.lse[at] = row.y == 0.f ? -INFINITY : (row.x + log2f(row.y)) * 0.6931471805599453f;
         } else {
           const long long at = ((long long)cta * 2 + (p.opens ? 1 : 0)) * kCols + n;
-          *reinterpret_cast<float2*>(a.parts + at * DH + d) = make_float2(x0, x1);
-          if (lane == 0 && w == 0) *(reinterpret_cast<float2*>(a.parts_ml) + at) = make_float2(M, L);
+          *reinterpret_cast<float4*>(a.parts + at * DH + d) = make_float4(acc[0], acc[1], acc[2], acc[3]);
+          if (c == 0 && w == 0) *(reinterpret_cast<float2*>(a.parts_ml) + at) = row;
         }
       }
       __syncthreads();                           // (the exchange rows are free again)
@@ -529,22 +550,23 @@ k_quant_few(const __grid_constant__ QuantAttnArgs qa) {
   asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-// Items that several CTAs share: a row's pieces added up, in the order of the keys.  Two rows a block, four warps each, a quarter of the pieces a warp.  (Added up by the last CTA to arrive, inside the kernel, ten
-// pieces of 22 rows took 14 us and 74 of four rows 11: all of them come through one SM.)
-constexpr int kMergeRows = 2, kMergeWarps = 4;
+// Items that several CTAs share: a row's pieces added up, in the order of the keys.  A block looks at sixteen of those CTAs and has one row of all items that begin in them, a warp each, or its warps an eighth of the pieces of one that has many.  (Added
+// up by the last CTA to arrive, inside the kernel, ten pieces of 22 rows took 14 us and 74 of four rows 11: all of them come through one SM.)
+constexpr int kMergeWarps = 8, kMergeCtas = 16;
 template <typename T, int DH>
-__global__ void __launch_bounds__(kMergeRows * kMergeWarps * 32)
-k_quant_merge(const __grid_constant__ PagedAttnArgs a, int cols) {
+__global__ void __launch_bounds__(kMergeWarps * 32)
+k_quant_merge(const __grid_constant__ PagedAttnArgs a, int cols, int n_ctas) {
   CS_PDL_PROLOGUE();
   constexpr int kV = DH / 32, kBatch = 8;         // columns of a lane; pieces in flight
-  __shared__ float2 s_ml[kMergeRows][kMergeWarps];
-  __shared__ float s_o[kMergeRows][kMergeWarps][DH];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, which = warp / kMergeWarps, share = warp % kMergeWarps, c0 = blockIdx.x, row = blockIdx.y * kMergeRows + which;
-  const PagedSplit* src = a.splits + c0;
-  PagedSplit d;
-  d.last = __ldcg(&src->last); d.rows = __ldcg(&src->rows); d.first_row = __ldcg(&src->first_row); d.head = __ldcg(&src->head); d.start = __ldcg(&src->start);
-  if (d.last < 0 || (int)blockIdx.y * kMergeRows >= d.rows) return;
-  float M = -INFINITY, L = 0.f, acc[kV] = {};
+  __shared__ float2 s_ml[kMergeWarps];
+  __shared__ __align__(16) float s_o[kMergeWarps][DH];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.y, first = blockIdx.x * kMergeCtas;
+  float M, L, acc[kV];
+  auto none = [&]() {
+    M = -INFINITY; L = 0.f;
+#pragma unroll
+    for (int e = 0; e < kV; ++e) acc[e] = 0.f;
+  };
   auto add = [&](float2 ml, const float (&v)[kV]) {
     if (ml.x == -INFINITY && ml.y == 0.f) return;                  // (it saw nothing)
     const float top = fmaxf(M, ml.x), keep = M == -INFINITY ? (L == 0.f ? 0.f : L) : paged_ex2(M - top), k = ml.x == -INFINITY ? 0.f : paged_ex2(ml.x - top);   // (a sum without a maximum is NaN)
@@ -553,44 +575,77 @@ k_quant_merge(const __grid_constant__ PagedAttnArgs a, int cols) {
 #pragma unroll
     for (int e = 0; e < kV; ++e) acc[e] = fmaf(k, v[e], acc[e] * keep);
   };
-  if (row < d.rows)
-    for (int cb = c0 + share; cb <= d.last; cb += kBatch * kMergeWarps) {
+  auto load = [&](const float* p, float (&v)[kV]) {
+    if constexpr (kV == 4) {
+      const float4 x = __ldcg(reinterpret_cast<const float4*>(p));
+      v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w;
+    } else if constexpr (kV == 2) {
+      const float2 x = __ldcg(reinterpret_cast<const float2*>(p));
+      v[0] = x.x; v[1] = x.y;
+    } else {
+      v[0] = __ldcg(p);
+    }
+  };
+  int last = kPagedNone, n_rows = 0;
+  if (lane < kMergeCtas && first + lane < n_ctas) { last = __ldcg(&a.splits[first + lane].last); n_rows = __ldcg(&a.splits[first + lane].rows); }
+  // every so-manieth piece of an item
+  auto gather = [&](int c0, int c1, int from, int step) {
+    none();
+    for (int cb = c0 + from; cb <= c1; cb += kBatch * step) {
       float2 ml[kBatch];
       float v[kBatch][kV];
 #pragma unroll
       for (int i = 0; i < kBatch; ++i) {
-        const int c = cb + i * kMergeWarps;
-        if (c > d.last) continue;
+        const int c = cb + i * step;
+        if (c > c1) continue;
         const long long at = ((long long)c * 2 + (c == c0 ? 1 : 0)) * cols + row;
         ml[i] = __ldcg(reinterpret_cast<const float2*>(a.parts_ml) + at);
-#pragma unroll
-        for (int e = 0; e < kV; ++e) v[i][e] = __ldcg(a.parts + at * DH + e * 32 + lane);
+        load(a.parts + at * DH + lane * kV, v[i]);
       }
 #pragma unroll
       for (int i = 0; i < kBatch; ++i)
-        if (cb + i * kMergeWarps <= d.last) add(ml[i], v[i]);
+        if (cb + i * step <= c1) add(ml[i], v[i]);
     }
-  if (lane == 0) s_ml[which][share] = make_float2(M, L);
-#pragma unroll
-  for (int e = 0; e < kV; ++e) s_o[which][share][e * 32 + lane] = acc[e];
-  __syncthreads();
-  if (share != 0 || row >= d.rows) return;
-  M = -INFINITY; L = 0.f;
-#pragma unroll
-  for (int e = 0; e < kV; ++e) acc[e] = 0.f;
-#pragma unroll 1
-  for (int i = 0; i < kMergeWarps; ++i) {
-    float v[kV];
-#pragma unroll
-    for (int e = 0; e < kV; ++e) v[e] = s_o[which][i][e * 32 + lane];
-    add(s_ml[which][i], v);
+  };
+  auto write = [&](int c0) {
+    const PagedSplit* d = a.splits + c0;
+    const float inv = L == 0.f ? 0.f : 1.f / L;
+    const int m = __ldcg(&d->first_row) + row, r = a.by_group.of(m);
+    const long long at = (long long)(__ldcg(&d->start) + r) * a.n_heads + __ldcg(&d->head) * a.group + (m - r * a.group);
+    char* dst = a.out + (at * DH + lane * kV) * 2;
+    if constexpr (kV == 4) *reinterpret_cast<uint2*>(dst) = make_uint2(PagedType<T>::pack(acc[0] * inv, acc[1] * inv), PagedType<T>::pack(acc[2] * inv, acc[3] * inv));
+    else if constexpr (kV == 2) *reinterpret_cast<uint32_t*>(dst) = PagedType<T>::pack(acc[0] * inv, acc[1] * inv);
+    else *reinterpret_cast<unsigned short*>(dst) = (unsigned short)PagedType<T>::pack(acc[0] * inv, 0.f);
+    if (a.lse != nullptr && lane == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+  };
+  const bool some = last >= 0 && row < n_rows, many = last - (first + lane) >= kBatch;
+  int nth = 0;
+  for (unsigned todo = __ballot_sync(0xffffffffu, some && !many); todo != 0; todo &= todo - 1) {
+    const int c0 = first + __ffs(todo) - 1, c1 = __shfl_sync(0xffffffffu, last, c0 - first);
+    if (nth++ % kMergeWarps != warp) continue;
+    gather(c0, c1, 0, 1);
+    write(c0);
   }
-  const float inv = L == 0.f ? 0.f : 1.f / L;
-  const int m = d.first_row + row, r = a.by_group.of(m);
-  const long long at = (long long)(d.start + r) * a.n_heads + d.head * a.group + (m - r * a.group);
+  for (unsigned todo = __ballot_sync(0xffffffffu, some && many); todo != 0; todo &= todo - 1) {
+    const int c0 = first + __ffs(todo) - 1, c1 = __shfl_sync(0xffffffffu, last, c0 - first);
+    gather(c0, c1, warp, kMergeWarps);
+    s_ml[warp] = make_float2(M, L);
 #pragma unroll
-  for (int e = 0; e < kV; ++e) *reinterpret_cast<unsigned short*>(a.out + (at * DH + e * 32 + lane) * 2) = (unsigned short)PagedType<T>::pack(acc[e] * inv, 0.f);
-  if (a.lse != nullptr && lane == 0) a.lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    for (int e = 0; e < kV; ++e) s_o[warp][lane * kV + e] = acc[e];
+    __syncthreads();
+    if (warp == 0) {
+      none();
+#pragma unroll 1
+      for (int i = 0; i < kMergeWarps; ++i) {
+        float v[kV];
+#pragma unroll
+        for (int e = 0; e < kV; ++e) v[e] = s_o[i][lane * kV + e];
+        add(s_ml[i], v);
+      }
+      write(c0);
+    }
+    __syncthreads();
+  }
 }
 
 template <typename T, int DH, int NT>
@@ -601,9 +656,13 @@ cs_status launch_few(cs_quant_cache* c, const QuantAttnArgs& a, unsigned bit, cu
     CS_CUDA_OK(c, cudaFuncSetAttribute(k_quant_few<T, DH, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kSmem));
     c->attr_set |= bit;
   }
-  const int ctas = getenv("CSQ") ? min(atoi(getenv("CSQ")), c->num_sms * F::kCtas) : c->num_sms * F::kCtas;
+  // (no more CTAs than the page table's room has places for)
+  const BlocksView& b = a.p.blk;
+  const long long groups = ((long long)b.rows * a.p.group + F::kCols - 1) / F::kCols + b.n_seqs, tiles = (long long)b.table_width * a.p.kv.page_size / kPagedTile + 2 + a.p.item_cost;
+  int ctas = c->num_sms * F::kCtas;
+  if (groups < ctas && tiles < ctas && a.p.kv.n_kv_heads < ctas && groups * tiles * a.p.kv.n_kv_heads < ctas) ctas = (int)(groups * tiles * a.p.kv.n_kv_heads);
   CS_CUDA_OK(c, cs_launch_pdl(k_quant_few<T, DH, NT>, dim3(ctas), dim3(kThreads), F::kSmem, st, a));
-  CS_CUDA_OK(c, cs_launch_pdl(k_quant_merge<T, DH>, dim3(ctas, F::kCols / kMergeRows), dim3(kMergeRows * kMergeWarps * 32), 0, st, a.p, F::kCols));
+  CS_CUDA_OK(c, cs_launch_pdl(k_quant_merge<T, DH>, dim3((ctas + kMergeCtas - 1) / kMergeCtas, F::kCols), dim3(kMergeWarps * 32), 0, st, a.p, F::kCols, ctas));
   return CS_OK;
 }
 template <typename T, int DH>
@@ -634,6 +693,6 @@ cs_status cs_launch_quant_few(cs_quant_cache* c, const QuantAttnArgs& args, cuda
   a.p.item_rows = 8 * tiles;
   a.p.by_item_rows = PagedDivisor::by(a.p.item_rows);
   a.p.item_cost = 2;
-  a.p.keep = getenv("CSK") ? atoi(getenv("CSK")) : 4;
+  a.p.keep = 4;
   return a.half ? launch_few_type<__half>(c, a, tiles, 1u << 12, st) : launch_few_type<__nv_bfloat16>(c, a, tiles, 1u, st);
 }
