@@ -63,54 +63,87 @@ template <typename T> __device__ __forceinline__ void store8(char* p, const floa
   *reinterpret_cast<uint4*>(p) = make_uint4(PagedType<T>::pack(f[0], f[1]), PagedType<T>::pack(f[2], f[3]), PagedType<T>::pack(f[4], f[5]), PagedType<T>::pack(f[6], f[7]));
 }
 
-// The scale of a group whose largest element is `most`, which may be NaN: five significant bits, halves to even, and multiples of 2^-133; at most 2^123, so that 24 of it are finite
+// Quotients are products with a reciprocal in two terms, 1 / d = hi + lo up to 2^-48: what that gives in 32 bits is a whole number and a half, or halfway between two scales, only where the quotient is.  (A quotient
+// of a number of 24 bits by one of five is farther from those than half a unit in the last place, unless it is one of them.)
+struct Reciprocal {
+  float hi, lo;
+  __device__ __forceinline__ static Reciprocal of(float d) {
+    Reciprocal r;
+    r.hi = __fdiv_rn(1.f, d);
+    r.lo = fmaf(-d, r.hi, 1.f) * r.hi;
+    return r;
+  }
+  __device__ __forceinline__ float times(float x) const { return fmaf(x, hi, x * lo); }
+};
+constexpr float kMostScale = 1.0633823966279327e37f;         // 2^123: 24 times it is finite
+// The scale of a group whose largest element is `most`, which may be inf or NaN: five significant bits, halves to even, and multiples of 2^-133; at most 2^123
 __device__ __forceinline__ float scale_of(float most) {
-  uint32_t b = __float_as_uint(__fdiv_rn(most, 7.f));
+  const Reciprocal seventh{0.14285714924335479736328125f, -6.386212e-9f};      // 1 / 7: rounded, and what that leaves out
+  uint32_t b = __float_as_uint(seventh.times(most));
   if ((b & 0x7f800000u) == 0x7f800000u) return __uint_as_float(0x7fc00000u);
   b += 0x3ffffu + (b >> 19 & 1u);
-  const float s = fminf(__uint_as_float(b & 0xfff80000u), 1.0633823966279327e37f);
+  const float s = fminf(__uint_as_float(b & 0xfff80000u), kMostScale);
   return __bfloat162float(__float2bfloat16_rn(s));
 }
 __device__ __forceinline__ float scale_of(double most) {
   const double x = most / 7.0;
-  if (!(x <= 1.0633823966279327e37)) return x != x ? __uint_as_float(0x7fc00000u) : 1.0633823966279327e37f;
+  if (!(x <= (double)kMostScale)) return x <= 1e300 ? kMostScale : __uint_as_float(0x7fc00000u);
   long long b = __double_as_longlong(x);
   b += 0x7fffffffffffll + (b >> 48 & 1);
   return __bfloat162float(__float2bfloat16_rn((float)__longlong_as_double(b >> 48 << 48)));
 }
-__device__ __forceinline__ uint32_t field_of(int i, int n) { return (uint32_t)(min(max(n, -7), 7) + 8) << (4 * (i / 2 + 4 * (i & 1))); }
-// Eight elements of a group as a word.  The product with the reciprocal ends up beside the quotient, and so perhaps on the wrong side of a border; what is left of the element, exact in 32 bits, says so.
+constexpr uint32_t kZeros = 0x88888888u;
+__device__ __forceinline__ constexpr int field_at(int i) { return 4 * (i / 2 + 4 * (i & 1)); }
+// Eight elements of a group as a word.  The sum with 1.5 2^23 + 8 rounds to a whole number, halves to even, and leaves n + 8 in its last bits; what stands above them is taken out of the word at the end.
 __device__ __forceinline__ uint32_t word_of(const float (&y)[8], float s) {
-  uint32_t w = 0;
-  const float inv = s >= 1.17549435e-38f ? __fdiv_rn(1.f, s) : 0.f;
+  if (!(s >= 1.17549435e-38f && s < kMostScale)) {           // (nothing to divide by, or elements that have to be held back)
+    uint32_t w = 0;
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+      float x = y[0];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    // (the sum with 1.5 2^23 rounds to a whole number, halves to even)
-    const float q = fminf(fmaxf(y[i] * inv, -8.f), 8.f) + 12582912.f;
-    const float n = q - 12582912.f, rest = fmaf(-n, s, y[i]), beyond = fmaf(2.f, fabsf(rest), -s);
-    const int m = (int)__float_as_uint(q) - 0x4b400000;
-    w |= field_of(i, beyond > 0.f || (beyond == 0.f && (m & 1)) ? (rest > 0.f ? m + 1 : m - 1) : m);
+      for (int k = 1; k < 8; ++k) x = i == k ? y[k] : x;
+      w |= (uint32_t)((s > 0.f ? min(max(__float2int_rn(__fdiv_rn(x, s)), -7), 7) : 0) + 8) << field_at(i);
+    }
+    return w;
   }
-  return s > 0.f ? w : 0x88888888u;
+  const Reciprocal r = Reciprocal::of(s);
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w += (__float_as_uint(r.times(y[i]) + 12582920.f) - 0x4b400000u) << field_at(i);
+  return w;
 }
 // In 64 bits: the quotient, by the product with the reciprocal, is rounded to a multiple of 2^-44 first (the sum with 384 does that), which makes a whole number and a half of one that is a rounding beside it, and
-// then to a whole number (the sum with 1.5 2^52).
+// then to a whole number (the sum with 1.5 2^52 + 8).
 __device__ __forceinline__ uint32_t word_of(const double (&y)[8], float s) {
+  if (!(s > 0.f)) return kZeros;
   uint32_t w = 0;
-  const double inv = s > 0.f ? 1.0 / (double)s : 0.0;
+  const double inv = 1.0 / (double)s;
+  const bool held_back = s >= kMostScale || s < 1.17549435e-38f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w |= field_of(i, __double2loint(fma(y[i], inv, 384.0) + (6755399441055744.0 - 384.0)));
-  return s > 0.f ? w : 0x88888888u;
+  for (int i = 0; i < 8; ++i) {
+    int u = __double2loint(fma(y[i], inv, 384.0) + (6755399441055752.0 - 384.0));
+    if (held_back) u = min(max(u, 1), 15);
+    w += (uint32_t)u << field_at(i);
+  }
+  return w;
 }
-// the largest of some, NaN if one is not finite  (fmax leaves NaN out, and 0 x inf is NaN)
-template <int N, typename R> __device__ __forceinline__ R most_of(const R* y) {
-  R m = fabs(y[0]), z = y[0] * R(0);
+// the largest of some, inf or NaN if one is not finite
+template <int N> __device__ __forceinline__ float most_of(const float* y) {
+  float m = fabsf(y[0]);
+#pragma unroll
+  for (int i = 1; i < N; ++i) asm("max.NaN.f32 %0, %0, %1;" : "+f"(m) : "f"(fabsf(y[i])));
+  return m;
+}
+template <int N> __device__ __forceinline__ double most_of(const double* y) {
+  double m = fabs(y[0]), z = y[0] * 0.0;
 #pragma unroll
   for (int i = 1; i < N; ++i) {
-    m = fmax(m, fabs(y[i]));
-    z += y[i] * R(0);
+    const double x = fabs(y[i]);
+    m = x > m ? x : m;
+    z = fma(x, 0.0, z);
   }
-  return m + z;
+  return m + z;                                  // (0 x inf is NaN)
 }
 
 __device__ __forceinline__ void fetch16(uint32_t dst, const char* src) {
@@ -187,66 +220,106 @@ k_quant_append(const __grid_constant__ QuantAppendArgs a) {
   }
   const bool kept = (unsigned)page < (unsigned)a.kv.n_pages;
   if (!kept && lane == 0) atomicOr(a.status, CS_DEV_BADARG);
+  // The next unit's two words of this lane, once they are there; the one behind those in flight is asked for.
   uint32_t at = 0;
-  for (int u = u0; u < units; u += step) {
-    const int kind = u < uq ? 0 : u < uk ? 1 : 2;
-    const int h = (u - (kind == 0 ? 0 : kind == 1 ? uq : uk)) * kPer + sub;
-    const bool live = h < (kind == 0 ? a.n_q : a.n_kv);
+  auto take = [&](float (&x0)[8], float (&x1)[8]) {
     asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 2) : "memory");
     __syncwarp();
-    float x0[8], x1[8];
-    {
-      const char* mine = reinterpret_cast<const char*>(&s_ring[warp][0][0]) + at + sub * DH * kSize;
-      lds8<S>(mine + c0 * 8 * kSize, x0);
-      lds8<S>(mine + c1 * 8 * kSize, x1);
-    }
+    const char* mine = reinterpret_cast<const char*>(&s_ring[warp][0][0]) + at + sub * DH * kSize;
+    lds8<S>(mine + c0 * 8 * kSize, x0);
+    lds8<S>(mine + c1 * 8 * kSize, x1);
     __syncwarp();
     fetch();                                     // (into the place of the unit before: all lanes have read it)
     at = at == (kSlots - 1) * kUnit ? 0 : at + kUnit;
-    const char* gain = kind == 0 ? a.q_gain : kind == 1 ? a.k_gain : nullptr;
-    if (kind == 0) {
-      float r = 1.f;
-      if (gain != nullptr) {
-        float sq = 0.f;
+  };
+  auto gains = [&](const char* gain, int word, float (&g)[8]) {
+    if (gain != nullptr) load8<D>(gain + word * 8 * (int)sizeof(D), g);
+    else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sq = fmaf(x0[i], x0[i], fmaf(x1[i], x1[i], sq));
+      for (int i = 0; i < 8; ++i) g[i] = 1.f;
+    }
+  };
+  int u = u0;
+  // ---- queries: y0 = r (x0 C0 - x1 S0), y1 = r (x1 C1 + x0 S1), C = gain cos, S = gain sin worked out once
+  if (u < uq) {
+    f32x2 C0[4], C1[4], S0[4], S1[4];
+    {
+      float g0[8], g1[8];
+      gains(a.q_gain, c0, g0);
+      gains(a.q_gain, c1, g1);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x2 a0 = pack2(g0[2 * i], g0[2 * i + 1]), a1 = pack2(g1[2 * i], g1[2 * i + 1]);
+        const f32x2 c = rotated ? pack2(cs[2 * i], cs[2 * i + 1]) : pack2(1.f, 1.f), s = rotated ? pack2(sn[2 * i], sn[2 * i + 1]) : pack2(0.f, 0.f);
+        C0[i] = mul2(a0, c); C1[i] = mul2(a1, c);
+        S1[i] = mul2(a0, s); S0[i] = mul2(a1, mul2(s, pack2(-1.f, -1.f)));
+      }
+    }
+    const bool norm = a.q_gain != nullptr;
+    char* dst = a.yq + (row * a.yq_row + (u * kPer + sub) * a.yq_head) * (long long)sizeof(D);
+    const long long dst_step = step * kPer * a.yq_head * (long long)sizeof(D);
+    for (; u < uq; u += step, dst += dst_step) {
+      float x0[8], x1[8];
+      take(x0, x1);
+      f32x2 p0[4], p1[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { p0[i] = pack2(x0[2 * i], x0[2 * i + 1]); p1[i] = pack2(x1[2 * i], x1[2 * i + 1]); }
+      if (norm) {
+        f32x2 s2 = mul2(p0[0], p0[0]);
+#pragma unroll
+        for (int i = 1; i < 4; ++i) s2 = fma2(p0[i], p0[i], s2);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s2 = fma2(p1[i], p1[i], s2);
+        float lo, hi;
+        unpack2(s2, lo, hi);
+        float sq = lo + hi;
 #pragma unroll
         for (int o = 1; o < kLanes; o <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
-        r = rsqrtf(sq * (1.f / DH) + a.eps);
-        float g[8];
-        load8<D>(gain + c0 * 8 * (int)sizeof(D), g);
+        const float r = rsqrtf(sq * (1.f / DH) + a.eps);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x0[i] *= r * g[i];
-        load8<D>(gain + c1 * 8 * (int)sizeof(D), g);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x1[i] *= r * g[i];
+        for (int i = 0; i < 4; ++i) { p0[i] = mul2(p0[i], pack2(r, r)); p1[i] = mul2(p1[i], pack2(r, r)); }
       }
-      if (rotated) {
+      // (what is not rotated has no partner: its product with a sine of 0 would make NaN of an inf)
+      if (a.rot_dim > 0) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float y = x0[i] * cs[i] - x1[i] * sn[i];
-          x1[i] = x1[i] * cs[i] + x0[i] * sn[i];
-          x0[i] = y;
+        for (int i = 0; i < 4; ++i) {
+          const f32x2 t0 = mul2(p0[i], C0[i]), t1 = mul2(p1[i], C1[i]);
+          const f32x2 y0 = rotated ? fma2(p1[i], S0[i], t0) : t0, y1 = rotated ? fma2(p0[i], S1[i], t1) : t1;
+          unpack2(y0, x0[2 * i], x0[2 * i + 1]);
+          unpack2(y1, x1[2 * i], x1[2 * i + 1]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          unpack2(mul2(p0[i], C0[i]), x0[2 * i], x0[2 * i + 1]);
+          unpack2(mul2(p1[i], C1[i]), x1[2 * i], x1[2 * i + 1]);
         }
       }
-      if (live) {
-        char* dst = a.yq + (row * a.yq_row + h * a.yq_head) * (long long)sizeof(D);
+      if (u * kPer + sub < a.n_q) {
         store8<D>(dst + c0 * 8 * (int)sizeof(D), x0);
         store8<D>(dst + c1 * 8 * (int)sizeof(D), x1);
       }
-      continue;
     }
+  }
+  // ---- keys, values
+  const bool plain_keys = a.k_gain == nullptr && a.rot_dim == 0;
+  for (; u < units; u += step) {
+    const bool keys = u < uk;
+    const int h = (u - (keys ? uq : uk)) * kPer + sub;
+    const bool live = h < a.n_kv;
+    float x0[8], x1[8];
+    take(x0, x1);
     if (!live) {                                 // (what lies in the ring there is another unit's)
 #pragma unroll
       for (int i = 0; i < 8; ++i) x0[i] = x1[i] = 0.f;
     }
     uint32_t w0, w1;
     float s0, s1;
-    if (kind == 1 && (gain != nullptr || a.rot_dim > 0)) {
+    if (keys && !plain_keys) {
       double y0[8], y1[8], r = 1.0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) { y0[i] = (double)x0[i]; y1[i] = (double)x1[i]; }
-      if (gain != nullptr) {
+      if (a.k_gain != nullptr) {
         double sq = 0.0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) sq = fma(y0[i], y0[i], fma(y1[i], y1[i], sq));
@@ -254,18 +327,18 @@ k_quant_append(const __grid_constant__ QuantAppendArgs a) {
         for (int o = 1; o < kLanes; o <<= 1) sq += __shfl_xor_sync(0xffffffffu, sq, o);
         r = rsqrt(sq * (1.0 / DH) + (double)a.eps);
         float g[8];
-        load8<D>(gain + c0 * 8 * (int)sizeof(D), g);
+        gains(a.k_gain, c0, g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) y0[i] *= r * (double)g[i];
-        load8<D>(gain + c1 * 8 * (int)sizeof(D), g);
+        gains(a.k_gain, c1, g);
 #pragma unroll
         for (int i = 0; i < 8; ++i) y1[i] *= r * (double)g[i];
       }
       if (rotated) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          const double c = (double)cs[i], s = (double)sn[i], y = y0[i] * c - y1[i] * s;
-          y1[i] = y1[i] * c + y0[i] * s;
+          const double c = (double)cs[i], s = (double)sn[i], y = fma(y0[i], c, -(y1[i] * s));
+          y1[i] = fma(y1[i], c, y0[i] * s);
           y0[i] = y;
         }
       }
@@ -291,14 +364,15 @@ k_quant_append(const __grid_constant__ QuantAppendArgs a) {
     }
     if (live && kept) {
       const long long in_page = (long long)h * a.kv.page_size + slot;
-      uint32_t* data = (kind == 1 ? a.kv.k : a.kv.v) + page * a.kv.data_page + in_page * kWords;
-      unsigned short* scale = (kind == 1 ? a.kv.ks : a.kv.vs) + page * a.kv.scale_page + in_page * (DH / kQuantGroup);
+      uint32_t* data = (keys ? a.kv.k : a.kv.v) + page * a.kv.data_page + in_page * kWords;
+      unsigned short* scale = (keys ? a.kv.ks : a.kv.vs) + page * a.kv.scale_page + in_page * (DH / kQuantGroup);
       data[c0] = w0;
       data[c1] = w1;
       if ((c0 & 3) == 0) scale[c0 >> 2] = __bfloat16_as_ushort(__float2bfloat16_rn(s0));
       if ((c1 & 3) == 0) scale[c1 >> 2] = __bfloat16_as_ushort(__float2bfloat16_rn(s1));
     }
   }
+  asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 // ------------------------------------------------------------------ reading back
