@@ -152,7 +152,7 @@ __device__ __forceinline__ void fetch16(uint32_t dst, const char* src) {
 
 // A unit is 512 elements: up to kPer neighbouring heads of the queries, the keys or the values of a row.  Units lie in a ring of shared memory for each warp, as in memory; three are in flight.
 template <typename S, typename D, int DH>
-__global__ void __launch_bounds__(kThreads, 3)
+__global__ void __launch_bounds__(kThreads, 4)
 k_quant_append(const __grid_constant__ QuantAppendArgs a) {
   CS_PDL_PROLOGUE();
   constexpr int kLanes = DH / 16, kPer = 32 / kLanes, kWords = DH / 8;      // lanes of a head, heads of a unit, words of a head
@@ -702,7 +702,7 @@ template <typename S, typename D>
 cudaError_t launch_append(QuantAppendArgs a, int head_dim, cudaStream_t st) {
   const int per = 512 / head_dim, units = cs_ceil_div(a.n_q, per) + 2 * cs_ceil_div(a.n_kv, per);
   a.warps_per_row = kWarps;
-  while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)a.n_rows * a.warps_per_row > 148 * 12)) a.warps_per_row /= 2;
+  while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)a.n_rows * a.warps_per_row > 148 * 16)) a.warps_per_row /= 2;
   const dim3 grid((unsigned)(((long long)a.n_rows * a.warps_per_row + kWarps - 1) / kWarps)), block(kThreads);
   switch (head_dim) {
     case 32: return cs_launch_pdl(k_quant_append<S, D, 32>, grid, block, 0, st, a);
