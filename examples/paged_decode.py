@@ -1,7 +1,7 @@
 """Copy-and-verify decoding of a batch of sequences over a paged KV cache (Sec. 3.1, 3.2; App. B.3), with the library's operators
 and torch for what lies between them.
 
-    python examples/paged_decode.py [--batch 4] [--prompt 300] [--new 64] [--k 10] [--qk-norm]
+    python examples/paged_decode.py [--batch 4] [--prompt 300] [--new 64] [--k 10] [--qk-norm] [--bits 4]
 
 Every step looks the last tokens of each history up (cs_find_match), runs the blocks [last token, copied draft] of all
 sequences side by side - blocks of different heights, no padding - and keeps the longest agreeing prefix and one token more.  Rows of rejected tokens stay in
@@ -10,7 +10,7 @@ their pages behind kv_len and are overwritten by the next block.  Prompts go thr
     cs_paged_append      the block's keys and values into the pages, normed and rotated, and its queries with them
     cs_paged_attention   the block's rows over the pages
 
-(or, with fused=False, cs_qk_norm_rope for queries and keys and an append of what it returns: the same bits).
+(or, with fused=False, cs_qk_norm_rope for queries and keys and an append of what it returns: the same bits).  With bits=4 the pages hold 4.5 bits a value (cs_quant_append, cs_quant_attention).
 """
 from __future__ import annotations
 
@@ -28,14 +28,19 @@ from paper_2502_08923_b200 import binding as cs, inputs  # noqa: E402
 class PagedModel:
     """A pre-norm decoder (RMSNorm, rotation, grouped heads, SwiGLU) whose keys and values live in pages, handed out as sequences grow."""
 
-    def __init__(self, cfg, weights, batch, max_tokens, page_size=16, qk_norm=False, fused=True, seed=0):
-        self.cfg, self.w, self.fused = cfg, weights, fused
+    def __init__(self, cfg, weights, batch, max_tokens, page_size=16, qk_norm=False, fused=True, seed=0, bits=16):
+        self.cfg, self.w, self.fused, self.bits = cfg, weights, fused, bits
         self.wide = -(-max_tokens // page_size)
         n_pages = batch * self.wide
-        pools = torch.zeros(cfg.n_layers, 2, n_pages, cfg.n_kv_heads, page_size, cfg.head_dim, dtype=torch.bfloat16, device="cuda")
         self.caches = []
+        if bits == 16:
+            pools = torch.zeros(cfg.n_layers, 2, n_pages, cfg.n_kv_heads, page_size, cfg.head_dim, dtype=torch.bfloat16, device="cuda")
         for l in range(cfg.n_layers):      # one workspace for all layers: their work is on one stream
-            self.caches.append(cs.PagedCache(pools[l, 0], pools[l, 1], workspace=self.caches[0] if self.caches else None))
+            first = self.caches[0] if self.caches else None
+            if bits == 16:
+                self.caches.append(cs.PagedCache(pools[l, 0], pools[l, 1], workspace=first))
+            else:      # (room for copies of all that a batch's prompts attend to)
+                self.caches.append(cs.QuantCache.empty(n_pages, cfg.n_kv_heads, page_size, cfg.head_dim, tall_positions=n_pages * page_size, workspace=first))
         # a server hands pages out as it gets them back: in any order
         self.free = np.random.default_rng(seed).permutation(n_pages).tolist()
         self.page_size = page_size
@@ -68,14 +73,16 @@ class PagedModel:
             qkv = self._norm(x, w["attn_norm"]) @ w["wqkv"].T
             q, k, v = (t.unflatten(1, (-1, c.head_dim)) for t in qkv.split([c.q_dim, c.kv_dim, c.kv_dim], dim=1))
             cache, blocks = self.caches[l], (start, length, self.kv_len, self.table)
-            if self.fused:
+            if self.bits == 4:
+                q = cache.cs_quant_append(k, v, *blocks, self.rope, self.k_gain, q, self.q_gain, eps=c.rms_eps, dtype=torch.bfloat16)
+            elif self.fused:
                 q = cache.cs_paged_append(k, v, *blocks, self.rope, self.k_gain, q, self.q_gain, eps=c.rms_eps)
             else:
                 # rows of a block sit at kv_len + r; rows of none (there are none here) could have any position
                 pos = (self.kv_len - start).repeat_interleave(length.long()) + torch.arange(len(tokens), device="cuda", dtype=torch.int32)
                 q, k = cs.cs_qk_norm_rope(q, k, pos, self.rope, self.q_gain, self.k_gain, eps=c.rms_eps, dtype=torch.bfloat16)
                 cache.cs_paged_append(k, v.to(torch.bfloat16), *blocks)
-            a = cache.cs_paged_attention(q, *blocks)
+            a = cache.cs_quant_attention(q, *blocks) if self.bits == 4 else cache.cs_paged_attention(q, *blocks)
             x = x + a.flatten(1).float() @ w["wo"].T
             gate, up = (self._norm(x, w["ffn_norm"]) @ w["w_gate_up"].T).chunk(2, dim=1)
             x = x + (torch.nn.functional.silu(gate) * up) @ w["w_down"].T
@@ -153,7 +160,7 @@ def generate(model, prompts, max_new, gamma=3, k=10, policy=cs.LATEST):
         model.kv_len += torch.from_numpy(keep).cuda()
         hist_dev.copy_(torch.from_numpy(hist))
     for c in model.caches[:1]:
-        if c.cs_paged_status() != cs.CS_OK:
+        if (c.cs_quant_status() if model.bits == 4 else c.cs_paged_status()) != cs.CS_OK:
             raise RuntimeError("the paged cache reports an error")
     return out, stats
 
@@ -177,13 +184,14 @@ def main():
     ap.add_argument("--new", type=int, default=64)
     ap.add_argument("--k", type=int, default=10)
     ap.add_argument("--qk-norm", action="store_true")
+    ap.add_argument("--bits", type=int, default=16, choices=(16, 4))
     a = ap.parse_args()
     cfg = inputs.TINY
     w = inputs.weights_to(inputs.make_weights(cfg, seed=0), "cuda")
     prompts = prompts_with_repeats(cfg, a.batch, a.prompt, seed=1)
     results = {}
     for k in (0, a.k):
-        model = PagedModel(cfg, w, a.batch, a.prompt + a.new + a.k + 1, qk_norm=a.qk_norm)
+        model = PagedModel(cfg, w, a.batch, a.prompt + a.new + a.k + 1, qk_norm=a.qk_norm, bits=a.bits)
         results[k], stats = generate(model, prompts, a.new, k=k)
         model.close()
         print(f"k = {k}: {stats['emitted']} tokens in {stats['steps']} blocks, {stats['accepted']} copied tokens accepted in {stats['attempts']} attempts")

@@ -480,8 +480,8 @@ k_quant_read(const __grid_constant__ QuantReadArgs a) {
         dst[j] = e < n ? a.k + (row * a.k_row + h * a.k_head + c * kQuantGroup) * (long long)sizeof(T) : a.v + (row * a.v_row + h * a.v_head + c * kQuantGroup) * (long long)sizeof(T);
         if ((unsigned)rp < (unsigned)a.kv.n_pages) {
           const uint32_t in_page = ((uint32_t)h * a.kv.page_size + slot) * kGroups + c;
-          w[j] = __ldg(reinterpret_cast<const uint4*>(e < n ? a.kv.k : a.kv.v) + ((unsigned long long)rp * a.kv.data_units + in_page));
-          s[j] = __ldg((e < n ? a.kv.ks : a.kv.vs) + ((unsigned long long)rp * a.kv.scale_page + in_page));
+          w[j] = __ldcg(reinterpret_cast<const uint4*>(e < n ? a.kv.k : a.kv.v) + ((unsigned long long)rp * a.kv.data_units + in_page));
+          s[j] = __ldcg((e < n ? a.kv.ks : a.kv.vs) + ((unsigned long long)rp * a.kv.scale_page + in_page));
         }
       }
     }
@@ -531,8 +531,8 @@ k_quant_copy(const __grid_constant__ QuantReadArgs a) {
         s[0][j] = s[1][j] = 0;
         if (exists && j * 32 + lane < kRun) {
           const unsigned long long d = (unsigned long long)page * a.kv.data_units + in_page + j * 32 + lane, g = (unsigned long long)page * a.kv.scale_page + in_page + j * 32 + lane;
-          w[0][j] = __ldg(reinterpret_cast<const uint4*>(a.kv.k) + d); s[0][j] = __ldg(a.kv.ks + g);
-          w[1][j] = __ldg(reinterpret_cast<const uint4*>(a.kv.v) + d); s[1][j] = __ldg(a.kv.vs + g);
+          w[0][j] = __ldcg(reinterpret_cast<const uint4*>(a.kv.k) + d); s[0][j] = __ldcg(a.kv.ks + g);
+          w[1][j] = __ldcg(reinterpret_cast<const uint4*>(a.kv.v) + d); s[1][j] = __ldcg(a.kv.vs + g);
         }
       }
 #pragma unroll

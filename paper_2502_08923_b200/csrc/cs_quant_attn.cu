@@ -189,7 +189,7 @@ k_quant_few(const __grid_constant__ QuantAttnArgs qa) {
     for (int i = 0; i < kQWords; ++i) {
       const int e = tid + i * kThreads, row = e / (DH / 8), c = e % (DH / 8), m = x.rg * kCols + row, r = a.by_group.of(m);
       q_next[i] = make_uint4(0u, 0u, 0u, 0u);
-      if (row < kCols && m < x.len * G) q_next[i] = __ldg(reinterpret_cast<const uint4*>(a.q + ((x.start + r) * a.q_row + (x.head * G + m - r * G) * a.q_head + c * 8) * 2));
+      if (row < kCols && m < x.len * G) q_next[i] = __ldcg(reinterpret_cast<const uint4*>(a.q + ((x.start + r) * a.q_row + (x.head * G + m - r * G) * a.q_head + c * 8) * 2));
     }
   };
   auto keep = [&]() {
