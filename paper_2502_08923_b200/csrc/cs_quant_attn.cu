@@ -302,6 +302,17 @@ k_quant_few(const __grid_constant__ QuantAttnArgs qa) {
         const bool mixed = key0 < all_lo || key0 + kSlice > all_hi;      // some row does not see all of it
         // ---- S^T = K Q^T
         float s[2][NT][4];
+        uint32_t ksc[2][2][kGroups > 1 ? kGroups / 2 : 1];      // scales of the keys of rows g, g + 8, two groups a register
+        each<2>([&](auto mt) {
+          each<2>([&](auto b) {
+            constexpr int kAt = (16 * mt + 8 * b) * F::kScaleBytes;
+            if constexpr (DH == 128) {
+              const uint2 x = lds64<kAt>(a_ks + stage);
+              ksc[mt][b][0] = x.x; ksc[mt][b][kGroups / 2 - 1] = x.y;
+            } else if constexpr (DH == 64) ksc[mt][b][0] = lds32<kAt>(a_ks + stage);
+            else ksc[mt][b][0] = lds16<kAt>(a_ks + stage);
+          });
+        });
         each<kGroups>([&](auto w) {
           uint4 q[NT];
           each<NT>([&](auto nt) { q[nt] = lds128<nt * 8 * F::kQRow + w * 64>(a_q); });
@@ -311,7 +322,7 @@ k_quant_few(const __grid_constant__ QuantAttnArgs qa) {
             float sc[2];
             each<2>([&](auto b) {
               expand_numbers<T>(lds32<(16 * mt + 8 * b) * F::kKeyBytes>(kd), x[b]);
-              sc[b] = __uint_as_float(lds16<(16 * mt + 8 * b) * F::kScaleBytes + w * 2>(a_ks + stage) << 16);
+              sc[b] = __uint_as_float(w & 1 ? ksc[mt][b][w / 2] & 0xffff0000u : ksc[mt][b][w / 2] << 16);
             });
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -550,17 +561,17 @@ k_quant_few(const __grid_constant__ QuantAttnArgs qa) {
   asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
-// Items that several CTAs share: a row's pieces added up, in the order of the keys.  A block looks at sixteen of those CTAs and has one row of all items that begin in them, a warp each, or its warps an eighth of the pieces of one that has many.  (Added
+// Items that several CTAs share: a row's pieces added up, in the order of the keys.  A block looks at some of those CTAs and has one row of all items that begin in them, a warp each, or its warps an eighth of the pieces of one that has many.  (Added
 // up by the last CTA to arrive, inside the kernel, ten pieces of 22 rows took 14 us and 74 of four rows 11: all of them come through one SM.)
-constexpr int kMergeWarps = 8, kMergeCtas = 16;
+constexpr int kMergeWarps = 8;
 template <typename T, int DH>
 __global__ void __launch_bounds__(kMergeWarps * 32)
-k_quant_merge(const __grid_constant__ PagedAttnArgs a, int cols, int n_ctas) {
+k_quant_merge(const __grid_constant__ PagedAttnArgs a, int cols, int n_ctas, int per_block) {
   CS_PDL_PROLOGUE();
   constexpr int kV = DH / 32, kBatch = 8;         // columns of a lane; pieces in flight
   __shared__ float2 s_ml[kMergeWarps];
   __shared__ __align__(16) float s_o[kMergeWarps][DH];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.y, first = blockIdx.x * kMergeCtas;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = blockIdx.y, first = blockIdx.x * per_block;
   float M, L, acc[kV];
   auto none = [&]() {
     M = -INFINITY; L = 0.f;
@@ -587,7 +598,7 @@ k_quant_merge(const __grid_constant__ PagedAttnArgs a, int cols, int n_ctas) {
     }
   };
   int last = kPagedNone, n_rows = 0;
-  if (lane < kMergeCtas && first + lane < n_ctas) { last = __ldcg(&a.splits[first + lane].last); n_rows = __ldcg(&a.splits[first + lane].rows); }
+  if (lane < per_block && first + lane < n_ctas) { last = __ldcg(&a.splits[first + lane].last); n_rows = __ldcg(&a.splits[first + lane].rows); }
   // every so-manieth piece of an item
   auto gather = [&](int c0, int c1, int from, int step) {
     none();
@@ -662,7 +673,9 @@ cs_status launch_few(cs_quant_cache* c, const QuantAttnArgs& a, unsigned bit, cu
   int ctas = c->num_sms * F::kCtas;
   if (groups < ctas && tiles < ctas && a.p.kv.n_kv_heads < ctas && groups * tiles * a.p.kv.n_kv_heads < ctas) ctas = (int)(groups * tiles * a.p.kv.n_kv_heads);
   CS_CUDA_OK(c, cs_launch_pdl(k_quant_few<T, DH, NT>, dim3(ctas), dim3(kThreads), F::kSmem, st, a));
-  CS_CUDA_OK(c, cs_launch_pdl(k_quant_merge<T, DH>, dim3((ctas + kMergeCtas - 1) / kMergeCtas, F::kCols), dim3(kMergeWarps * 32), 0, st, a.p, F::kCols, ctas));
+  // (eight or sixteen CTAs' items a block, us: 64 ragged tokens of the 8B shape 41.6 / 42.8, 11 rows over 4,096 keys 18.2 / 17.7)
+  const int per_block = NT == 1 ? 8 : 16;
+  CS_CUDA_OK(c, cs_launch_pdl(k_quant_merge<T, DH>, dim3((ctas + per_block - 1) / per_block, F::kCols), dim3(kMergeWarps * 32), 0, st, a.p, F::kCols, ctas, per_block));
   return CS_OK;
 }
 template <typename T, int DH>
@@ -692,7 +705,8 @@ cs_status cs_launch_quant_few(cs_quant_cache* c, const QuantAttnArgs& args, cuda
   const int tiles = (int)(((rows + items - 1) / items + 7) / 8);
   a.p.item_rows = 8 * tiles;
   a.p.by_item_rows = PagedDivisor::by(a.p.item_rows);
-  a.p.item_cost = 2;
+  // (what changing items takes, in tiles.  One / two, us: 64 ragged tokens of the 8B shape 42.8 / 43.7, 32 x 4 rows over 2,000 keys 31.1 / 30.2)
+  a.p.item_cost = tiles == 1 ? 1 : 2;
   a.p.keep = 4;
   return a.half ? launch_few_type<__half>(c, a, tiles, 1u << 12, st) : launch_few_type<__nv_bfloat16>(c, a, tiles, 1u, st);
 }
