@@ -831,8 +831,8 @@ class QuantCache:
     """One layer's paged KV cache in 4 bits: k_data and v_data are the caller's pools [n_pages][Hkv][page_size][D / 2] uint8, k_scale and v_scale [n_pages][Hkv][page_size][D / 32] bf16
     (the format stands in the C header), kept alive here.  Pages may lie apart (any stride between them, the same for K and V), everything within a page is contiguous.  `QuantCache.empty` makes pools as well.
 
-    `tall_positions`: room in the workspace for copies in 16 bits of the positions that a call of tall blocks (prompts' chunks) attends to, 4 * D * Hkv bytes each; what counts is the room of the call's page
-    table, n_seqs x width x page_size.  Caches of several layers whose work is on one stream may share a workspace (`workspace`: another QuantCache of the same heads and tall_positions, which are taken from it), and then
+    `tall_positions`: room in the workspace for copies in 16 bits of the positions that a call of prompts' chunks (more than 2,560 query rows per KV head) attends to, 4 * D * Hkv bytes each; what counts is the room of the call's page
+    table, n_seqs x width x page_size.  Without it such calls take up to a tenth longer.  Caches of several layers whose work is on one stream may share a workspace (`workspace`: another QuantCache of the same heads and tall_positions, which are taken from it), and then
     what cs_quant_status says.  As with PagedCache, the calls of one workspace must be on one stream at a time.
 
     Blocks of rows are given as to PagedCache."""

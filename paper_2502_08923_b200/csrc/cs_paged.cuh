@@ -81,10 +81,14 @@ struct PagedAttnArgs {
   PagedSplit* splits;
   unsigned long long wait_ns;
   int drop;
+  // a cache of 4 bits: kv.k and kv.v are its numbers, kv.page_stride bytes; scales, from page to page in elements
+  const unsigned short *ks, *vs;
+  long long scale_page;
 };
 
 cs_status cs_launch_paged_few(cs_paged_cache* c, const PagedAttnArgs& a, cudaStream_t st);
 cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& a, cudaStream_t st);
+cs_status cs_launch_quant_tc(cs_paged_cache* c, const PagedAttnArgs& a, cudaStream_t st);   // over a cache of 4 bits; `c`: type, workspace
 cs_status cs_paged_tc_maps(cs_paged_cache* c);   // the pools' operand maps
 
 #ifdef __CUDACC__

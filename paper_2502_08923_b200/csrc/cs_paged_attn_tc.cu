@@ -1,4 +1,4 @@
-// Attention of tall blocks over a paged KV cache on the 5th-generation tensor cores (Sec. 3.2; App. B.2).
+// Attention of tall blocks over a paged KV cache, in 16 bits or in 4, on the 5th-generation tensor cores (Sec. 3.2; App. B.2).
 //
 // The mathematics is that of cs_paged_attn.cu.  Query rows (row of the block x head of the group) are the M = 128 of both products, so that TMEM
 // lane = query row and one thread has a whole row of scores:
@@ -38,12 +38,13 @@
 // point, and no phase shorter for it); slots that keep out of each other's exponentials (141 -> 154); exponentials in blocks of 16 (138 -> 142).
 #include <type_traits>
 
-#include "cs_paged.cuh"
+#include "cs_quant.cuh"
 #include "cs_tcgen.cuh"
 
 namespace {
 
-constexpr int kThreads = 384, kMmaWarp = 8, kKWarp = 9, kQWarp = 11;   // (10: V)
+constexpr int kMmaWarp = 8, kKWarp = 9, kQWarp = 11, kExpandWarp = 12;   // (10: V; 12, 13: out of four bits, K; 14, 15: V)
+template <bool kQuant> constexpr int kThreads = kQuant ? 512 : 384;
 constexpr int kM = 128;                                            // query rows of a slot
 // Tensor memory: scores of slot s at 128 s, output from 256 on.  With heads of 128 that is all there is, and weights lie over the scores they come from; with smaller heads
 // they have 64 columns of their own, and a slot's next scores are made while the softmax is at work on the last ones, which it has in registers.
@@ -54,18 +55,24 @@ constexpr uint32_t kOCol = 256;
 template <int DH> constexpr uint32_t kPCol = kApart<DH> ? 384 : 0;
 template <int DH> constexpr uint32_t kPStep = kApart<DH> ? 64 : 128;
 template <int DH> constexpr int kTileBytes = kPagedTile * DH * 2;  // of K, of V, and of a slot's queries
-template <int DH> constexpr int kStages = DH == 128 ? 4 : 8;
+template <int DH, bool kQuant> constexpr int kStages = DH == 128 ? (kQuant ? 3 : 4) : 8;
+// In a cache of 4 bits: tiles as they lie there, numbers, then scales; so many for keys and for values (four with heads of 64: no faster)
+constexpr int kPackedTiles = 2;
+template <int DH> constexpr int kPackedData = kPagedTile * DH / 2;
+template <int DH> constexpr int kPacked = kPackedData<DH> + kPagedTile * DH / 16;
 template <int DH> constexpr int kRowBytes = DH == 32 ? 64 : 128;    // of a row in shared memory, swizzled over so many bytes; heads of 128 are two halves one behind the other
 // Registers of the warpgroups: two of the softmax and one of the others share the 384 x 168 that the block is launched with.  (What the softmax spills it fetches again for every tile: heads of 128 with 72 / 216, 68 bytes spilled,
 // windowed chunks 110 us, with 56 / 224 and none 102; heads of 64 the other way round, 32 bytes and 64 us against 88 and 69.)
-template <int DH> constexpr int kOtherRegs = DH == 128 ? 56 : 72;
-template <int DH> constexpr int kSoftmaxRegs = DH == 128 ? 224 : 216;
+// Over 4 bits there is a warpgroup more, and 512 x 128 registers: 2,048 rows over 30,720 keys 931 us with 56 for both of the others and 200, 968 with 48 and 208, 1,046 with 40 and 216, 959 with 56, 40 and 208, 915 with these.
+template <int DH, bool kQuant> constexpr int kOtherRegs = kQuant ? 56 : DH == 128 ? 56 : 72;
+constexpr int kExpandRegs = 48;
+template <int DH, bool kQuant> constexpr int kSoftmaxRegs = kQuant ? 200 : DH == 128 ? 224 : 216;
 constexpr int kCtl = 512;
 // Descriptors of pieces.  A slot that is still at a piece's results holds the others up four pieces on at the latest: the other slot waits for it at the next piece whose tiles the slots take in turn, but the
 // scores of the piece after that may be made (of one tile each, they need neither slot), which frees the queries and makes two more known.
 constexpr int kPieces = 8;
 constexpr int kPieceBytes = 72;
-template <int DH> constexpr int kTcSmem = 1024 + (kStages<DH> + 2) * kTileBytes<DH> + kCtl + 2 * kM * 8 + kPieces * kPieceBytes + (int)sizeof(PagedPlan);
+template <int DH, bool kQuant> constexpr int kTcSmem = 1024 + (kStages<DH, kQuant> + 2) * kTileBytes<DH> + kCtl + 2 * kM * 8 + kPieces * kPieceBytes + (kQuant ? 2 * kPackedTiles * kPacked<DH> : 0) + (int)sizeof(PagedPlan);
 
 // Operand descriptors as in cs_tcgen.cuh, for rows of 128 or (heads of 32) 64 bytes: eight of them a group, and the swizzle as wide
 template <int kRow> __device__ __forceinline__ uint64_t desc_rows(uint32_t saddr, uint32_t lbo) {
@@ -74,6 +81,9 @@ template <int kRow> __device__ __forceinline__ uint64_t desc_rows(uint32_t saddr
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1, int c2, int c3) {
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                ::"r"(dst), "l"(tm), "r"(bar), "r"(c0), "r"(c1), "r"(c2), "r"(c3) : "memory");
+}
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 __device__ __forceinline__ void umma_ta(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
   asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
@@ -167,7 +177,7 @@ __device__ __forceinline__ uint32_t finite_only(uint32_t w) {
 }
 
 // In a second pass: 32 columns of a row, as stored (`part`: fp32, else T), get the values that are not finite at keys the row sees and others of its item do not.  (Any positive weight makes the same of them.)
-template <typename T>
+template <typename T, int DH, bool kQuant>
 __device__ __noinline__ void add_odd(const PagedAttnArgs& a, const TcPiece& p, int n_tiles, int lo, int hi, int c0, void* dst, bool part) {
   const int last = min(hi, (p.tile0 + n_tiles) * kPagedTile);
   float sum[32] = {};
@@ -178,6 +188,14 @@ __device__ __noinline__ void add_odd(const PagedAttnArgs& a, const TcPiece& p, i
     }
     const int page = __ldcg(a.blk.table + (long long)p.seq * a.blk.table_width + (key >> a.kv.page_shift));
     if ((unsigned)page >= (unsigned)a.kv.n_pages) continue;
+    if constexpr (kQuant) {                      // (32 columns are a group: all of it, or nothing)
+      const unsigned short s = __ldcg(a.vs + (page * a.scale_page + ((long long)p.head * a.kv.page_size + (key & (a.kv.page_size - 1))) * (DH / kQuantGroup) + c0 / kQuantGroup));
+      if (quant_odd(s)) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sum[i] = __int_as_float(0x7fc00000);
+      }
+      continue;
+    }
     const uint4* src = reinterpret_cast<const uint4*>(a.kv.v + (page * a.kv.page_stride + p.head * a.kv.head_stride + (long long)(key & (a.kv.page_size - 1)) * a.kv.slot_stride + c0) * 2);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -202,10 +220,44 @@ __device__ __noinline__ void add_odd(const PagedAttnArgs& a, const TcPiece& p, i
   }
 }
 
-template <typename T, int DH>
-__global__ void __launch_bounds__(kThreads, 1)
+// Sixteen-bit values of a group's four words, each as the 16-byte chunk of eight elements that it is in a row of 16 bits.  fp16 ends at 65504: what lies beyond it becomes that.
+template <typename T>
+__device__ __forceinline__ void expand_group(const uint4& words, unsigned scale, uint4 (&out)[4]) {
+  const uint32_t w[4] = {words.x, words.y, words.z, words.w};
+  if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+    const QuantScale s = QuantScale::of(scale * 0x10001u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t r[4];
+      quant_expand(w[i], s, r);
+      out[i] = make_uint4(r[0], r[1], r[2], r[3]);
+    }
+  } else {
+    const float s = __uint_as_float(scale << 16);
+    const __half2 h = __float2half2_rn(s);
+    const uint32_t hs = *reinterpret_cast<const uint32_t*>(&h);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t r[4];
+      expand_numbers<__half>(w[i], r);
+      out[i] = make_uint4(h2_mul(r[0], hs), h2_mul(r[1], hs), h2_mul(r[2], hs), h2_mul(r[3], hs));
+    }
+    if (fabsf(s) > 8192.f) {                     // (eight of it are beyond 65504)
+      auto far = [&](int i, int k) { return fminf(fmaxf((float)((int)(w[i] >> (4 * k) & 15) - 8) * s, -65504.f), 65504.f); };
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        out[i] = make_uint4(PagedType<__half>::pack(far(i, 0), far(i, 4)), PagedType<__half>::pack(far(i, 1), far(i, 5)), PagedType<__half>::pack(far(i, 2), far(i, 6)), PagedType<__half>::pack(far(i, 3), far(i, 7)));
+    }
+  }
+}
+
+// kQuant: over a cache of 4 bits (cs_quant.cuh).  The warps that fetch keys and values have tiles copied as they lie there, and two warps more for either write them out in 16 bits, half of the rows each, where the other kind has
+// TMA put them; all else is the same.  8 x 21 rows of heads of 64 over 16,384 keys (us): 133 with keys and values written out by the warp that fetches them, 94 with warps of their own, 76 with a page's copies by a lane each (one after
+// the other they took 150 clocks apiece); the softmax alone takes 64.  84 rows of heads of 128 over 30,720 keys 39 (by the kernel for few rows 85).
+template <typename T, int DH, bool kQuant>
+__global__ void __launch_bounds__(kThreads<kQuant>, 1)
 k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ PagedAttnArgs a, int q_box_bytes) {
-  constexpr int kTB = kTileBytes<DH>, kNS = kStages<DH>, kRow = kRowBytes<DH>, kHalves = DH == 128 ? 2 : 1, kHalf = kPagedTile * 128;
+  constexpr int kTB = kTileBytes<DH>, kNS = kStages<DH, kQuant>, kRow = kRowBytes<DH>, kHalves = DH == 128 ? 2 : 1, kHalf = kPagedTile * 128;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* ring = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));   // [stage][64 dims][128 keys][128 B]
   uint8_t* sq = ring + kNS * kTB;                                       // [slot][64 dims][128 rows][128 B]
@@ -214,7 +266,10 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   float2* s_ml = reinterpret_cast<float2*>(reinterpret_cast<uint8_t*>(bars) + kCtl);      // [slot][128 rows]
   TcPiece* s_piece = reinterpret_cast<TcPiece*>(s_ml + 2 * kM);
   static_assert(sizeof(TcPiece) <= kPieceBytes, "");
-  PagedPlan& plan = *reinterpret_cast<PagedPlan*>(reinterpret_cast<uint8_t*>(s_piece) + kPieces * kPieceBytes);
+  uint8_t* packed = reinterpret_cast<uint8_t*>(s_piece) + kPieces * kPieceBytes;        // [keys, values][kPackedTiles]
+  PagedPlan& plan = *reinterpret_cast<PagedPlan*>(packed + (kQuant ? 2 * kPackedTiles * kPacked<DH> : 0));
+  const uint32_t b_packed = smem_u32(bars) + kCtl - 16 * 2 * kPackedTiles, b_unpacked = b_packed + 8 * 2 * kPackedTiles;    // [keys, values][kPackedTiles]
+  static_assert(8 * (2 * kNS + 25) <= kCtl - 16 * 2 * kPackedTiles && (kPieces * kPieceBytes) % 16 == 0 && kPacked<DH> % 16 == 0, "");
   const uint32_t b_full = smem_u32(bars), b_empty = b_full + 8 * kNS, b_s = b_empty + 8 * kNS, b_p = b_s + 16, b_p2 = b_p + 16, b_o = b_p2 + 16, b_taken = b_o + 16, b_qfull = b_taken + 16, b_qfree = b_qfull + 8,
                  b_drain = b_qfree + 8, b_piece = b_drain + 8, b_ml = b_piece + 8 * kPieces, b_read = b_ml + 8;
   // flags, by 32-bit addresses: a wait has run out; an item has been announced; results that are not finite, a bit a piece (the last one for all from there on)
@@ -227,14 +282,17 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
   // (nothing of this depends on the kernel before, so it is done while that one ends)
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (tid == 0) {
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmK) : "memory");
-    asm volatile("prefetch.tensormap [%0];" ::"l"(&tmV) : "memory");
+    if constexpr (!kQuant) {
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&tmK) : "memory");
+      asm volatile("prefetch.tensormap [%0];" ::"l"(&tmV) : "memory");
+    }
     asm volatile("prefetch.tensormap [%0];" ::"l"(&tmQ) : "memory");
-    for (int s = 0; s < kNS; ++s) { mbar_init(b_full + 8 * s, 1); mbar_init(b_empty + 8 * s, 1); }
+    for (int s = 0; s < kNS; ++s) { mbar_init(b_full + 8 * s, kQuant ? 2 : 1); mbar_init(b_empty + 8 * s, 1); }
     for (int s = 0; s < 2; ++s) { mbar_init(b_s + 8 * s, 1); mbar_init(b_p + 8 * s, 4); mbar_init(b_p2 + 8 * s, 4); mbar_init(b_o + 8 * s, 1); mbar_init(b_taken + 8 * s, 4); }
     mbar_init(b_qfull, 1); mbar_init(b_qfree, 1); mbar_init(b_drain, 1);
     for (int s = 0; s < kPieces; ++s) mbar_init(b_piece + 8 * s, 1);
     mbar_init(b_ml, 8); mbar_init(b_read, 8);
+    if constexpr (kQuant) for (int s = 0; s < 2 * kPackedTiles; ++s) { mbar_init(b_packed + 8 * s, 1); mbar_init(b_unpacked + 8 * s, 2); }
     set_flag(f_abort, 0);
     set_flag(f_shares, 0);
     set_flag(f_odd, 0);
@@ -292,7 +350,8 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
     return !second && fine != 0 && flag(f_odd) != 0;
   };
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs<DH>));
+    if (kQuant && warp >= kExpandWarp) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kExpandRegs));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs<DH, kQuant>));
     uint32_t base = 0, piece = 0;                 // ring entries before this piece; pieces
     bool ok = true, met = false;
     if (warp == kMmaWarp) {
@@ -437,10 +496,11 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
       }
     } else {
       // ------------------------------------------------------------------ K tiles, V tiles
-      const bool is_k = warp == kKWarp;
+      const bool is_k = kQuant ? warp == kKWarp || (warp & ~1) == kExpandWarp : warp == kKWarp;
       const CUtensorMap* tm = is_k ? &tmK : &tmV;
       const int rows = min(a.kv.page_size, kPagedTile), per_tile = kPagedTile / rows, shift = a.kv.page_shift;
       uint32_t asked = 0;                          // entries this warp has started copies for, + 1
+      uint32_t packed_no = 0;                      // kQuant: tiles asked for, or written out
       int tile_no = 0;
       for (;; ++piece) {
         if (!known(piece)) break;
@@ -456,12 +516,12 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
         const int inc = both ? 2 : 1;
         int entry = 0, first = -64;                // this lane's page-table entry, and of which page the first lane has one
         const int* table = a.blk.table + (long long)seq * a.blk.table_width;
-        for (int s = 0; s < n && ok; s += inc) {
-          const uint32_t e = base + (is_k ? k_entry(both, s) : v_entry(both, s, n)), st = e % kNS;
-          const int key0 = (tile0 + (both ? s >> 1 : s)) * kPagedTile, page0 = key0 >> shift;
-          // pages of the tile that hold keys of the item
+        // pages of a step's tile that hold keys of the item: [j0, j1) from page0 on
+        auto pages_of = [&](int s, int& key0, int& page0, int& j0, int& j1) {
+          key0 = (tile0 + (both ? s >> 1 : s)) * kPagedTile;
+          page0 = key0 >> shift;
           const int pa = max(key0, lo), pz = min(key0 + kPagedTile, hi);
-          int j0 = 0, j1 = 0;
+          j0 = j1 = 0;
           if (pz > pa) { j0 = (pa >> shift) - page0; j1 = ((pz - 1) >> shift) - page0 + 1; }
           if (page0 < first || page0 + per_tile > first + 32) {
             first = page0;
@@ -469,39 +529,117 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
             entry = -1;
             if (((long long)(page + 1) << shift) > lo && ((long long)page << shift) < hi) entry = __ldcg(table + page);
           }
-          ok = wait_warp(b_empty + 8 * st, ((e / kNS) & 1) ^ 1);
-          if (!ok) break;
-          if (is_k && tile_no++ == a.drop) continue;             // (test hook: these keys never arrive)
-          if (elect_one()) mbar_expect_tx(b_full + 8 * st, (uint32_t)((j1 - j0) * rows * kRow * kHalves));
-          __syncwarp();
-          for (int j = j0; j < j1; ++j) {
-            int page = (int)__shfl_sync(0xffffffffu, entry, page0 + j - first);
-            if ((unsigned)page >= (unsigned)a.kv.n_pages) {      // (a page behind the last one reads as zeros)
-              page = a.kv.n_pages;
-              if (lane == 0) atomicOr(a.status, CS_DEV_BADARG);
+        };
+        if constexpr (kQuant) {
+          constexpr uint32_t kTiles = kPackedTiles;
+          const uint32_t first_buffer = is_k ? 0 : kTiles;
+          if (warp < kExpandWarp) {
+            // tiles as they lie in the cache (scales of pages that do not exist: zeros)
+            for (int s = 0; s < n && ok; s += inc, ++packed_no) {
+              int key0, page0, j0, j1;
+              pages_of(s, key0, page0, j0, j1);
+              const uint32_t buffer = first_buffer + packed_no % kTiles, bar = b_packed + 8 * buffer;
+              ok = wait_warp(b_unpacked + 8 * buffer, ((packed_no / kTiles) & 1) ^ 1);
+              if (!ok) break;
+              // (a page's numbers by one lane, its scales by another: one after the other by the same lane, 8 x 21 rows of heads of 64 over 16,384 keys in pages of 32 takes 94 us)
+              const int j = lane & 7;
+              const int page = (int)__shfl_sync(0xffffffffu, entry, page0 + j - first);
+              const bool here = lane < 16 && j >= j0 && j < j1, there = (unsigned)page < (unsigned)a.kv.n_pages;
+              uint8_t* numbers = packed + buffer * kPacked<DH> + j * rows * (DH / 2);
+              uint8_t* scales = packed + buffer * kPacked<DH> + kPackedData<DH> + j * rows * (DH / 16);
+              if (here && !there) {
+                if (lane < 8) for (int x = 0; x < rows * DH / 64; ++x) reinterpret_cast<uint32_t*>(scales)[x] = 0u;
+                atomicOr(a.status, CS_DEV_BADARG);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (copies follow in the same place later)
+              }
+              __syncwarp();
+              const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xffffffffu, here && there && lane < 8)) * (uint32_t)(rows * (DH / 2 + DH / 16));
+              if (lane == 0) mbar_expect_tx(bar, bytes);
+              __syncwarp();
+              if (here && there) {
+                const long long row = (long long)head * a.kv.page_size + ((key0 + j * rows) & (a.kv.page_size - 1));
+                if (lane < 8) bulk_load(smem_u32(numbers), (is_k ? a.kv.k : a.kv.v) + page * a.kv.page_stride + row * (DH / 2), rows * (DH / 2), bar);
+                else bulk_load(smem_u32(scales), (is_k ? a.ks : a.vs) + page * a.scale_page + row * (DH / kQuantGroup), rows * (DH / 16), bar);
+              }
+              __syncwarp();
             }
-            const int slot = (key0 + j * rows) & (a.kv.page_size - 1);
-            if (elect_one()) {
-              const uint32_t dst = smem_u32(ring) + st * kTB + j * rows * kRow;
+          } else {
+            // half of a tile's rows, out of four bits
+            for (int s = 0; s < n && ok; s += inc, ++packed_no) {
+              const uint32_t e = base + (is_k ? k_entry(both, s) : v_entry(both, s, n)), st = e % kNS, buffer = first_buffer + packed_no % kTiles;
+              ok = wait_warp(b_packed + 8 * buffer, (packed_no / kTiles) & 1);
+              if (!ok) break;
+              ok = wait_warp(b_empty + 8 * st, ((e / kNS) & 1) ^ 1);
+              if (!ok) break;
+              // Groups of a row go two to a lane's neighbour, rows on: eight lanes write all eight places of 16 bytes that 128 bytes of banks have
+              constexpr int kPerRow = DH >= 64 ? 2 : 1, kRowsAtOnce = 32 / kPerRow;
+              const uint8_t* src = packed + buffer * kPacked<DH>;
+              uint8_t* out = ring + st * kTB;
+              const int c = lane % kPerRow, r0 = (warp & 1) * (kPagedTile / 2) + lane / kPerRow;
+#pragma unroll 2
+              for (int i = 0; i < kPagedTile / 2 / kRowsAtOnce * kHalves; ++i) {
+                const int h = i % kHalves, r = r0 + i / kHalves * kRowsAtOnce, group = h * 2 + c;
+                uint4 v[4];
+                expand_group<T>(*reinterpret_cast<const uint4*>(src + r * (DH / 2) + group * 16), *reinterpret_cast<const unsigned short*>(src + kPackedData<DH> + (r * (DH / kQuantGroup) + group) * 2), v);
 #pragma unroll
-              for (int h = 0; h < kHalves; ++h) tma_load_4d(dst + h * kHalf, tm, b_full + 8 * st, 64 * h, slot, head, page);
+                for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(out + h * kHalf + r * kRow + (DH >= 64 ? (c * 4 + k) ^ (r & 7) : k ^ (r >> 1 & 3)) * 16) = v[k];
+              }
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+              __syncwarp();
+              if (lane == 0) mbar_arrive(b_unpacked + 8 * buffer);
+              if (is_k && tile_no++ == a.drop) continue;           // (test hook: these keys never arrive)
+              if (lane == 0) mbar_arrive(b_full + 8 * st);
             }
           }
-          asked = e + 1;
+        } else {
+          for (int s = 0; s < n && ok; s += inc) {
+            const uint32_t e = base + (is_k ? k_entry(both, s) : v_entry(both, s, n)), st = e % kNS;
+            int key0, page0, j0, j1;
+            pages_of(s, key0, page0, j0, j1);
+            ok = wait_warp(b_empty + 8 * st, ((e / kNS) & 1) ^ 1);
+            if (!ok) break;
+            if (is_k && tile_no++ == a.drop) continue;             // (test hook: these keys never arrive)
+            if (elect_one()) mbar_expect_tx(b_full + 8 * st, (uint32_t)((j1 - j0) * rows * kRow * kHalves));
+            __syncwarp();
+            for (int j = j0; j < j1; ++j) {
+              int page = (int)__shfl_sync(0xffffffffu, entry, page0 + j - first);
+              if ((unsigned)page >= (unsigned)a.kv.n_pages) {      // (a page behind the last one reads as zeros)
+                page = a.kv.n_pages;
+                if (lane == 0) atomicOr(a.status, CS_DEV_BADARG);
+              }
+              const int slot = (key0 + j * rows) & (a.kv.page_size - 1);
+              if (elect_one()) {
+                const uint32_t dst = smem_u32(ring) + st * kTB + j * rows * kRow;
+#pragma unroll
+                for (int h = 0; h < kHalves; ++h) tma_load_4d(dst + h * kHalf, tm, b_full + 8 * st, 64 * h, slot, head, page);
+              }
+            }
+            asked = e + 1;
+          }
         }
         base += both ? n : 2 * n;
         if (!ok) break;
       }
-      if (flag(f_abort))                                // copies that nobody will consume must land before the shared memory goes away
+      if (flag(f_abort)) {                              // copies that nobody will consume must land before the shared memory goes away
+        if constexpr (kQuant) {
+          if (warp < kExpandWarp) {
+            constexpr uint32_t kTiles = kPackedTiles;
+            for (uint32_t e = packed_no > kTiles ? packed_no - kTiles : 0; e < packed_no; ++e) {
+              const unsigned long long t0 = globaltimer_ns();
+              while (!mbar_try_wait(b_packed + 8 * ((is_k ? 0 : kTiles) + e % kTiles), (e / kTiles) & 1) && globaltimer_ns() - t0 < a.wait_ns) {}
+            }
+          }
+        }
         for (uint32_t e = asked > kNS ? asked - kNS : 0; e < asked; ++e) {
           // (entries of the other warp's are waited for as well; one that was never started runs into the limit)
           const unsigned long long t0 = globaltimer_ns();
           while (!mbar_try_wait(b_full + 8 * (e % kNS), (e / kNS) & 1) && globaltimer_ns() - t0 < a.wait_ns) {}
         }
+      }
     }
     if (!met) again(true);
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs<DH>));
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs<DH, kQuant>));
     // -------------------------------------------------------------------- softmax and results: one thread per query row
     const int slot = warp >> 2, row = tid & 127, G = a.group;
     const bool out_32 = (reinterpret_cast<uintptr_t>(a.out) & 31) == 0;      // (rows are multiples of 32 bytes)
@@ -731,7 +869,7 @@ k_paged_tc(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUte
             if (p.again) {
               int lo, hi;
               range(lo, hi);
-              add_odd<T>(a, p, both ? n >> 1 : n, lo, hi, c0, dst, !whole);
+              add_odd<T, DH, kQuant>(a, p, both ? n >> 1 : n, lo, hi, c0, dst, !whole);
             }
           }
           __syncwarp();
@@ -968,13 +1106,14 @@ cs_status encode(cs_paged_cache* c, CUtensorMap* tm, const void* base, int rank,
   return CS_ERR_CUDA;
 }
 
-template <typename T, int DH>
+template <typename T, int DH, bool kQuant>
 cs_status launch_tc(cs_paged_cache* c, const PagedAttnArgs& a, const CUtensorMap& tmQ, int q_box_bytes, unsigned bit, cudaStream_t st) {
+  static_assert(kTcSmem<DH, kQuant> <= 227 * 1024, "");
   if (!(c->attr_set & bit)) {
-    CS_CUDA_OK(c, cudaFuncSetAttribute(k_paged_tc<T, DH>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem<DH>));
+    CS_CUDA_OK(c, cudaFuncSetAttribute(k_paged_tc<T, DH, kQuant>, cudaFuncAttributeMaxDynamicSharedMemorySize, kTcSmem<DH, kQuant>));
     c->attr_set |= bit;
   }
-  CS_CUDA_OK(c, cs_launch_pdl(k_paged_tc<T, DH>, dim3(c->num_sms), dim3(kThreads), kTcSmem<DH>, st, c->tmK, c->tmV, tmQ, a, q_box_bytes));
+  CS_CUDA_OK(c, cs_launch_pdl(k_paged_tc<T, DH, kQuant>, dim3(c->num_sms), dim3(kThreads<kQuant>), kTcSmem<DH, kQuant>, st, c->tmK, c->tmV, tmQ, a, q_box_bytes));
   CS_CUDA_OK(c, cs_launch_pdl(k_paged_merge<T, DH>, dim3(c->num_sms * kMergeCtas), dim3(kMergeWarps * 32), 0, st, a, c->num_sms));
   return CS_OK;
 }
@@ -994,7 +1133,9 @@ cs_status cs_paged_tc_maps(cs_paged_cache* c) {
   return s != CS_OK ? s : encode(c, &c->tmV, f.v, 4, dims, strides, box, promote);
 }
 
-cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& args, cudaStream_t st) {
+namespace {
+template <bool kQuant>
+cs_status launch_any(cs_paged_cache* c, const PagedAttnArgs& args, cudaStream_t st) {
   PagedAttnArgs a = args;
   const int tokens = kM / a.group;                 // rows of the block in a slot, with all heads of the group
   a.item_rows = 2 * tokens * a.group;
@@ -1011,7 +1152,12 @@ cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& args, cudaS
   if (s != CS_OK) return s;
   const int bytes = (dh == 32 ? 64 : 128) * a.group * box_rows;
   const bool bf = c->cfg.dtype == CS_BF16;
-  if (dh == 32) return bf ? launch_tc<__nv_bfloat16, 32>(c, a, tmQ, bytes, 1024, st) : launch_tc<__half, 32>(c, a, tmQ, bytes, 2048, st);
-  if (dh == 64) return bf ? launch_tc<__nv_bfloat16, 64>(c, a, tmQ, bytes, 64, st) : launch_tc<__half, 64>(c, a, tmQ, bytes, 128, st);
-  return bf ? launch_tc<__nv_bfloat16, 128>(c, a, tmQ, bytes, 256, st) : launch_tc<__half, 128>(c, a, tmQ, bytes, 512, st);
+  constexpr unsigned kFirst = kQuant ? 4096 : 64;  // (bits of the instances)
+  if (dh == 32) return bf ? launch_tc<__nv_bfloat16, 32, kQuant>(c, a, tmQ, bytes, kFirst * 16, st) : launch_tc<__half, 32, kQuant>(c, a, tmQ, bytes, kFirst * 32, st);
+  if (dh == 64) return bf ? launch_tc<__nv_bfloat16, 64, kQuant>(c, a, tmQ, bytes, kFirst, st) : launch_tc<__half, 64, kQuant>(c, a, tmQ, bytes, kFirst * 2, st);
+  return bf ? launch_tc<__nv_bfloat16, 128, kQuant>(c, a, tmQ, bytes, kFirst * 4, st) : launch_tc<__half, 128, kQuant>(c, a, tmQ, bytes, kFirst * 8, st);
 }
+}  // namespace
+
+cs_status cs_launch_paged_tc(cs_paged_cache* c, const PagedAttnArgs& a, cudaStream_t st) { return launch_any<false>(c, a, st); }
+cs_status cs_launch_quant_tc(cs_paged_cache* c, const PagedAttnArgs& a, cudaStream_t st) { return launch_any<true>(c, a, st); }

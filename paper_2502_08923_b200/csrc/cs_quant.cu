@@ -5,6 +5,7 @@
 // by way of shared memory.  Keys that are normed or rotated are worked out in 64 bits up to their level: which of fifteen levels an element goes to is then decided by its value, not by
 // the order of some sums (in 32 bits one element in some three million ends up a whole step from where another order puts it).  Elements that come as they are need no more than 32 bits: a correctly rounded quotient
 // of numbers of 24 and 5 bits is a whole number and a half only where it is one.
+#include <algorithm>
 #include <type_traits>
 
 #include "cs_quant.cuh"
@@ -151,6 +152,9 @@ __device__ __forceinline__ void fetch16(uint32_t dst, const char* src) {
 }
 
 // A unit is 512 elements: up to kPer neighbouring heads of the queries, the keys or the values of a row.  Units lie in a ring of shared memory for each warp, as in memory; three are in flight.
+// What bounds it: instructions.  Four chunks of up to 2,048 rows (32 query heads, 8 of keys, norms and rotation) with their positions read back: 50 us, 44 of them here; 26 M instructions, the schedulers issue in 61 of 100 clocks; 7 us are the
+// keys' 64-bit arithmetic, in what an SM has units for.  (87 us with rows fetched as they are needed, 66 with the ring, 54 with factors and quotients worked out once, 50 with four blocks of four warps an SM; five of them: no faster, nor
+// several rows a warp.)  A token each of 64 sequences and one verification block: 4 us, a chain of loads (whose row, which page) and one row's arithmetic.
 template <typename S, typename D, int DH>
 __global__ void __launch_bounds__(kThreads, 4)
 k_quant_append(const __grid_constant__ QuantAppendArgs a) {
@@ -429,6 +433,8 @@ __device__ __forceinline__ bool whole_sectors(const void* p, long long row, long
 constexpr int kReadWarps = 8;
 
 // A warp has rows_per_warp neighbouring rows: what finding a row takes (whose block, which page, one load after the other) is under way for all of them at once, and so are two rows' groups.
+// Traffic bounds it, what is written above all: a lane has a whole group (16 bytes of numbers, one scale) and stores whole sectors.  Two sequences of 16,384 positions of eight heads of 128: 31.9 us, 5.4 TB/s of the
+// 172 MB that are read and written; 36.6 with eight elements a lane, 16 bytes a store.  Three short blocks: 3.1 us, what finding a row takes.
 template <typename T, int DH>
 __global__ void __launch_bounds__(kReadWarps * 32)
 k_quant_read(const __grid_constant__ QuantReadArgs a) {
@@ -492,7 +498,7 @@ k_quant_read(const __grid_constant__ QuantReadArgs a) {
 }
 
 // Copies in 16 bits of the positions that blocks attend to, for the attention of tall blocks: sequence b's in the pages from b copy_pages on.  Sixteen positions of a head are one run of words, of scales and of copied
-// elements; a warp has several heads of them, so that finding them (lengths, page) is paid once.
+// elements; a warp has several heads of them, so that finding them (lengths, page) is paid once.  8 x 16,405 positions of eight heads of 64: 62 us, 5.5 TB/s.
 template <typename T, int DH>
 __global__ void __launch_bounds__(kReadWarps * 32)
 k_quant_copy(const __grid_constant__ QuantReadArgs a) {
@@ -549,6 +555,12 @@ __global__ void k_quant_iota(int* p, int n) {
   CS_PDL_PROLOGUE();
   for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) p[i] = i;
 }
+
+// Query rows per KV head (on the average of a call's sequences) that the kernel for few rows always has, up to 32: a pass over the keys; the tensor cores always have, more than 128; that are worked out
+// from copies there, where they fit, more than 2,560.  In between it is the work that decides, rows x positions x KV heads x sequences: the tensor cores' kernel has more to set up (32 query heads in groups of four, us here
+// and there; 84 rows over 512 keys 16.7 and 20.9, over 4,096 27.9 and 21.3; 44 rows over 4,096 keys 17.9 and 18.6, over 30,720 48 and 37; 24 rows 30 and 36; 8 sequences over 16,384 keys, 24 rows 54 and 73, 44 rows 97 and 74,
+// 84 rows 168 and 76).  Expanded by the kernel and from copies: 84 rows over 8 x 16,384 keys 76 and 129, 2,400 rows over 30,720 keys 307 and 308, 8,192 rows 936 and 896; windows of 1,000 keys, 2,400 rows 61 and 63, 4,500 rows 124 and 113.
+constexpr long long kFewRows = 32, kTallRows = 128, kTallWork = 3 << 19, kCopyRows = 2560;
 
 thread_local char t_quant_err[256] = "";
 
@@ -614,17 +626,16 @@ QuantLayout layout_of(const cs_quant_config& c) {
   l.splits = put(kQuantMaxSms * kQuantCtasPerSm * sizeof(PagedSplit));
   l.parts = put((size_t)kQuantMaxSms * kQuantRowsPerSm * 2 * c.head_dim * 4);
   l.parts_ml = put((size_t)kQuantMaxSms * kQuantRowsPerSm * 2 * 8);
-  l.positions = (c.tall_positions + 15) & ~15ll;
-  if (l.positions > 0) {
-    const cs_paged_config p = copies_config(c, l.positions, nullptr, nullptr, 3, CS_BF16);
-    const size_t pool = (size_t)l.positions * c.n_kv_heads * c.head_dim * 2;
-    l.paged_bytes = cs_paged_workspace_bytes(&p);
-    l.table = put((size_t)l.positions / 16 * 4);
-    l.len = put((size_t)l.positions / 16 * 4);
-    l.k = put(pool);
-    l.v = put(pool);
-    l.paged = put(l.paged_bytes);
-  }
+  // (a page of copies at least: the caches over them are also what tall blocks have their sums in)
+  l.positions = c.tall_positions > 0 ? (c.tall_positions + 15) & ~15ll : 16;
+  const cs_paged_config p = copies_config(c, l.positions, nullptr, nullptr, 3, CS_BF16);
+  const size_t pool = (size_t)l.positions * c.n_kv_heads * c.head_dim * 2;
+  l.paged_bytes = cs_paged_workspace_bytes(&p);
+  l.table = put((size_t)l.positions / 16 * 4);
+  l.len = put((size_t)l.positions / 16 * 4);
+  l.k = put(pool);
+  l.v = put(pool);
+  l.paged = put(l.paged_bytes);
   l.total = at;
   return l;
 }
@@ -673,29 +684,27 @@ cs_status create(const char* name, cs_quant_cache** out, const cs_quant_config* 
       return refuse(CS_ERR_CUDA, cudaGetErrorString(e));
     }
   }
-  if (l.positions > 0) {
-    c->tall_positions = l.positions;
-    c->tall_k = ws + l.k;
-    c->tall_v = ws + l.v;
-    c->tall_table = reinterpret_cast<int*>(ws + l.table);
-    c->tall_len = reinterpret_cast<int*>(ws + l.len);
-    // (the smallest pages first: there is one at least)
-    const cs_paged_cache* beside = first != nullptr ? first->tall[0][3] : nullptr;
-    cs_status r = CS_OK;
-    for (int i = 3; i >= 0; --i)
-      for (int type = 0; type < 2 && r == CS_OK; ++type) {
-        const cs_paged_config p = copies_config(*cfg, l.positions, c->tall_k, c->tall_v, i, type == 0 ? CS_BF16 : CS_F16);
-        if (p.n_pages < 1) continue;
-        r = beside != nullptr ? cs_paged_create_beside(&c->tall[type][i], &p, beside) : cs_paged_create(&c->tall[type][i], &p, ws + l.paged, l.paged_bytes, stream);
-        if (beside == nullptr) beside = c->tall[type][i];
-      }
-    const int n = (int)(l.positions / 16);
-    if (r == CS_OK && first == nullptr && cs_launch_pdl(k_quant_iota, dim3((unsigned)(n < 1 << 18 ? (n + 1023) / 1024 : 256)), dim3(256), 0, st, c->tall_table, n) != cudaSuccess) r = CS_ERR_CUDA;
-    if (r != CS_OK) {
-      refuse(r, cs_paged_last_error(nullptr)[0] != 0 ? cs_paged_last_error(nullptr) : "launch failed");
-      cs_quant_destroy(c);
-      return r;
+  c->tall_positions = cfg->tall_positions > 0 ? l.positions : 0;
+  c->tall_k = ws + l.k;
+  c->tall_v = ws + l.v;
+  c->tall_table = reinterpret_cast<int*>(ws + l.table);
+  c->tall_len = reinterpret_cast<int*>(ws + l.len);
+  // (the smallest pages first: there is one at least)
+  const cs_paged_cache* beside = first != nullptr ? first->tall[0][3] : nullptr;
+  cs_status r = CS_OK;
+  for (int i = 3; i >= 0; --i)
+    for (int type = 0; type < 2 && r == CS_OK; ++type) {
+      const cs_paged_config p = copies_config(*cfg, l.positions, c->tall_k, c->tall_v, i, type == 0 ? CS_BF16 : CS_F16);
+      if (p.n_pages < 1) continue;
+      r = beside != nullptr ? cs_paged_create_beside(&c->tall[type][i], &p, beside) : cs_paged_create(&c->tall[type][i], &p, ws + l.paged, l.paged_bytes, stream);
+      if (beside == nullptr) beside = c->tall[type][i];
     }
+  const int n = (int)(l.positions / 16);
+  if (r == CS_OK && first == nullptr && cs_launch_pdl(k_quant_iota, dim3((unsigned)(n < 1 << 18 ? (n + 1023) / 1024 : 256)), dim3(256), 0, st, c->tall_table, n) != cudaSuccess) r = CS_ERR_CUDA;
+  if (r != CS_OK) {
+    refuse(r, cs_paged_last_error(nullptr)[0] != 0 ? cs_paged_last_error(nullptr) : "launch failed");
+    cs_quant_destroy(c);
+    return r;
   }
   *out = c;
   return CS_OK;
@@ -777,14 +786,15 @@ cs_status cs_quant_status(cs_quant_cache* c, void* stream) {
   int bits = 0;
   CS_CUDA_OK(c, cudaMemcpyAsync(&bits, c->status, sizeof(int), cudaMemcpyDeviceToHost, st));
   CS_CUDA_OK(c, cudaStreamSynchronize(st));
-  cs_status tall = CS_OK;
-  if (c->tall[0][3] != nullptr && (tall = cs_paged_status(c->tall[0][3], stream)) != CS_OK) fail(c, tall, cs_paged_last_error(c->tall[0][3]));
+  const cs_status tall = cs_paged_status(c->tall[0][3], stream);
+  if (tall != CS_OK) fail(c, tall, cs_paged_last_error(c->tall[0][3]));
   if (bits == 0 || tall == CS_ERR_TIMEOUT || tall == CS_ERR_CUDA) {
     if (bits != 0) CS_CUDA_OK(c, cudaMemsetAsync(c->status, 0, sizeof(int), st));
     return tall;
   }
   CS_CUDA_OK(c, cudaMemsetAsync(c->status, 0, sizeof(int), st));
   CS_CUDA_OK(c, cudaStreamSynchronize(st));
+  if (bits & CS_DEV_TIMEOUT) return fail(c, CS_ERR_TIMEOUT, "a bounded wait ran out");
   if (bits & CS_DEV_CAPACITY) return fail(c, CS_ERR_CAPACITY, "a block does not fit its row of the page table, or the rotation table is too short");
   return fail(c, CS_ERR_ARG, "a length is negative, rows lie outside the tensors, or a page does not exist");
 }
@@ -859,15 +869,18 @@ cs_status cs_quant_attention(cs_quant_cache* c, const cs_blocks* blocks, const v
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int group = n_heads / c->cfg.n_kv_heads;
   const long long per_seq = ((long long)blocks->rows * group + blocks->n_seqs - 1) / blocks->n_seqs;      // query rows of a KV head, on the average
-  // Copies in pages as large as fit: a tile of 128 keys is fetched page by page
   const long long room = (long long)blocks->table_width * c->cfg.page_size;
+  const long long seen = window > 0 ? std::min(room, (long long)window + blocks->rows / blocks->n_seqs) : room;      // positions of a sequence, at most about
+  // (queries that repeat one row have no operand map)
+  const bool tall = per_seq > kFewRows && (per_seq > kTallRows || per_seq * blocks->n_seqs * c->cfg.n_kv_heads * seen > kTallWork) && (blocks->rows == 1 || q_row_stride > 0) && (n_heads == 1 || q_head_stride > 0);
+  // Copies in pages as large as fit: a tile of 128 keys is fetched page by page
   int size = 0;
   long long copy_pages = 0;
   for (; size < 4; ++size) {
     copy_pages = (room + (kQuantCopyPage >> size) - 1) >> (7 - size);
     if ((copy_pages << (7 - size)) <= c->tall_positions / blocks->n_seqs) break;
   }
-  if (per_seq > 64 && size < 4 && copy_pages > 0) {
+  if (tall && per_seq > kCopyRows && size < 4 && copy_pages > 0) {
     QuantReadArgs r = {};
     r.kv = c->view; r.blk = view_of(blocks); r.status = c->status;
     r.k = c->tall_k; r.v = c->tall_v;
@@ -878,13 +891,14 @@ cs_status cs_quant_attention(cs_quant_cache* c, const cs_blocks* blocks, const v
     b.len = c->tall_len;
     b.page_table = c->tall_table;
     b.table_width = (int)copy_pages;
-    cs_paged_cache* paged = c->tall[dtype == CS_BF16 ? 0 : 1][size];
-    const cs_status t = cs_paged_attention(paged, &b, q, q_row_stride, q_head_stride, n_heads, mask, window, scale, out, lse, stream);
-    return t == CS_OK ? t : fail(c, t, cs_paged_last_error(paged));
+    cs_paged_cache* const copies = c->tall[dtype == CS_BF16 ? 0 : 1][size];
+    const cs_status t = cs_paged_attention(copies, &b, q, q_row_stride, q_head_stride, n_heads, mask, window, scale, out, lse, stream);
+    return t == CS_OK ? t : fail(c, t, cs_paged_last_error(copies));
   }
   QuantAttnArgs a = {};
   a.kv = c->view;
   a.half = dtype == CS_F16;
+  cs_paged_cache* const paged = c->tall[a.half][3];
   PagedAttnArgs& p = a.p;
   p.kv.n_pages = c->view.n_pages; p.kv.page_size = c->view.page_size; p.kv.page_shift = c->view.page_shift; p.kv.n_kv_heads = c->view.n_kv_heads;
   p.blk = view_of(blocks);
@@ -894,15 +908,24 @@ cs_status cs_quant_attention(cs_quant_cache* c, const cs_blocks* blocks, const v
   p.by_group = PagedDivisor::by(group);
   p.mask = mask; p.window = window;
   p.scale = scale; p.scale_log2e = (float)(1.4426950408889634 * (double)scale);
-  p.parts = c->parts; p.parts_ml = c->parts_ml; p.splits = c->splits; p.status = c->status;
+  p.status = c->status;
+  p.wait_ns = paged->wait_limit_ns;
   p.drop = -1;
-  for (int b = 0; b < blocks->n_seqs; b += kQuantMaxSeqs) {      // (a launch's plan holds so many)
+  if (tall) {
+    p.kv.k = reinterpret_cast<char*>(c->view.k); p.kv.v = reinterpret_cast<char*>(c->view.v); p.kv.page_stride = c->view.data_page * 4;
+    p.ks = c->view.ks; p.vs = c->view.vs; p.scale_page = c->view.scale_page;
+    p.parts = paged->parts; p.parts_ml = paged->parts_ml; p.splits = paged->splits;
+  } else {
+    p.parts = c->parts; p.parts_ml = c->parts_ml; p.splits = c->splits;
+  }
+  const int most = tall ? kPagedMaxSeqs : kQuantMaxSeqs;
+  for (int b = 0; b < blocks->n_seqs; b += most) {      // (a launch's plan holds so many)
     QuantAttnArgs part = a;
-    part.p.blk.n_seqs = blocks->n_seqs - b < kQuantMaxSeqs ? blocks->n_seqs - b : kQuantMaxSeqs;
+    part.p.blk.n_seqs = blocks->n_seqs - b < most ? blocks->n_seqs - b : most;
     part.p.blk.start += b; part.p.blk.len += b; part.p.blk.kv_len += b;
     part.p.blk.table += (long long)b * blocks->table_width;
-    const cs_status r = cs_launch_quant_few(c, part, st);
-    if (r != CS_OK) return r;
+    const cs_status r = tall ? cs_launch_quant_tc(paged, part.p, st) : cs_launch_quant_few(c, part, st);
+    if (r != CS_OK) return tall ? fail(c, r, cs_paged_last_error(paged)) : r;
   }
   return CS_OK;
 }

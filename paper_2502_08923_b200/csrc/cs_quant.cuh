@@ -10,6 +10,8 @@
 // Pools: [page][KV head][slot] rows of words, and of scales; 4.5 bits an element.
 #pragma once
 
+#include <type_traits>
+
 #include "cs_paged.cuh"
 
 static constexpr int kQuantGroup = 32;
@@ -18,7 +20,7 @@ static constexpr int kQuantCtasPerSm = 4;      // of an attention launch, at mos
 static constexpr int kQuantMaxRows = 32;       // query rows of one work item at most
 static constexpr int kQuantRowsPerSm = 64;     // query rows of the items that CTAs of an SM have at hand, at most
 static constexpr int kQuantMaxSeqs = 128;      // sequences of one attention launch; more are further launches
-static constexpr int kQuantCopyPage = 128;     // slots of a page of the copies that tall blocks are worked out from; 64, 32 or 16 where sequences in whole pages would not fit
+static constexpr int kQuantCopyPage = 128;     // slots of a page of the copies that prompts' chunks are worked out from; 64, 32 or 16 where sequences in whole pages would not fit
 
 struct QuantView {
   uint32_t *k, *v;                   // words of eight elements
@@ -39,11 +41,11 @@ struct cs_quant_cache {
   float* parts_ml;             // their (reference point, sum)
   int num_sms;
   unsigned attr_set;           // shared-memory opt-ins made, a bit per kernel instance
-  // copies in 16 bits of the positions that a call of tall blocks attends to
-  long long tall_positions;    // room, a multiple of 16; 0: none
+  // copies in 16 bits of the positions that a call of prompts' chunks attends to
+  long long tall_positions;    // room asked for, a multiple of 16; 0: none
   char *tall_k, *tall_v;       // [page][KV head][slot][head_dim]
   int *tall_table, *tall_len;  // 0, 1, 2, ...; lengths of the blocks that nothing is wrong with
-  cs_paged_cache* tall[2][4];  // by the queries' type (CS_BF16, CS_F16) and the size of a page (128 >> i)
+  cs_paged_cache* tall[2][4];  // over the copies, by the queries' type (CS_BF16, CS_F16) and the size of a page (128 >> i); tall blocks without copies have their sums in the last one's workspace
   char err[256];
 };
 
@@ -67,6 +69,11 @@ __device__ __forceinline__ uint32_t bf2_mul(uint32_t a, uint32_t b) {
 __device__ __forceinline__ uint32_t bf2_sub(uint32_t a, uint32_t b) {
   uint32_t d;
   asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+__device__ __forceinline__ uint32_t h2_mul(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
 __device__ __forceinline__ uint32_t h2_sub(uint32_t a, uint32_t b) {
@@ -98,6 +105,22 @@ __device__ __forceinline__ void quant_expand(uint32_t w, const QuantScale& q, ui
   r[1] = bf2_fma(and_or(w >> 1, 0x00780078u, 0x43004300u), q.s8, q.c);
   r[2] = bf2_fma(and_or(w >> 5, 0x00780078u, 0x43004300u), q.s8, q.c);
   r[3] = bf2_fma(and_or(w >> 9, 0x00780078u, 0x43004300u), q.s8, q.c);
+}
+
+// Eight fields u = n + 8 of a word -> whole numbers n in type T: field i and i + 4 as the halves of register i.  (bf16 has room for a field at bits 0 - 3 under the exponent of 128, fp16 at bits 0 - 3 under that of 1024 and at
+// 4 - 7 under that of 64.)
+template <typename T>
+__device__ __forceinline__ void expand_numbers(uint32_t w, uint32_t (&r)[4]) {
+  if constexpr (std::is_same<T, __half>::value) {
+    const uint32_t v = w >> 8;
+    r[0] = h2_sub(and_or(w, 0x000f000fu, 0x64006400u), 0x64086408u);
+    r[1] = h2_sub(and_or(w, 0x00f000f0u, 0x54005400u), 0x54805480u);
+    r[2] = h2_sub(and_or(v, 0x000f000fu, 0x64006400u), 0x64086408u);
+    r[3] = h2_sub(and_or(v, 0x00f000f0u, 0x54005400u), 0x54805480u);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = bf2_sub(and_or(w >> (4 * i), 0x000f000fu, 0x43004300u), 0x43084308u);
+  }
 }
 
 // is a scale not finite?

@@ -1,4 +1,4 @@
-// Attention of few query rows per KV head over a paged cache held in 4 bits: single tokens, verification blocks, and taller blocks where there is no room for copies (Sec. 3.2; App. B.2),
+// Attention of few query rows per KV head over a paged cache held in 4 bits: single tokens, verification blocks, and what is too short for the tensor cores' kernel to pay (Sec. 3.2; App. B.2),
 // on mma.sync.  (Which calls come here: cs_quant_attention in cs_quant.cu.)
 //
 // out = softmax(scale Q K^T) V by one pass over the keys with a running reference point m and sum l per row, as in cs_paged_attn.cu.  What differs comes from the cache: a value costs 4.5 bits of
@@ -15,6 +15,13 @@
 // Every warp has its own ring of slices, fetched by cp.async, its own reference points, sums and output; the warps' results meet in shared memory where the item ends, and items that
 // CTAs share are added up, in the order of the keys, by a launch behind (k_quant_merge).
 // The reference point moves only past 2^8, by a vote; where no score is above, no maximum is worked out.
+//
+// What bounds it.  Contexts of many sequences: instructions.  A slice costs a warp some 800 of them (one row tile; of 285 us for 983,040 keys of eight heads of 128 the expansion of K takes 40, that of V 36, weights' second terms 22, the
+// copies 19), the schedulers issue in 67 of 100 clocks, the ALU is busy in 57, the tensor cores in 24 - 32: 3.9 TB/s where contexts differ in length.  64 ragged tokens of the 8B shape (32 query heads, 8 of keys, up to 4,097) 41 us: first data
+// after 6, SMs done after 31 to 38, the pieces' sums 4.6.  A token over 30,720 keys 21 us, the length of the chain: plan and page entries 3, first data 3, slices 7, the warps' results 1.5, the pieces' sums 4.  11 rows over 512 keys of the smallest
+// shape 8 us, 3 of them for fetching instructions.
+// Tried and not kept: units of a warp with claims by a counter (44 -> 60 us: warps out of step miss the instruction cache), CTAs of eight warps, sixteen keys at a time for more than eight rows (5 - 11 % slower), more CTAs an SM for heads of 64
+// (spills).
 //
 // Masked keys: scores become -inf.  Slices that lie outside of [lo, hi) of the item's rows are not fetched.  In slices that some rows see and others do not, V scales that are not
 // finite become 0 and the rows that see such a key are given NaN (0 x NaN is not 0).
@@ -105,22 +112,6 @@ __device__ __forceinline__ uint32_t at_chunk(uint32_t j, uint32_t c) {
   else if constexpr (DH == 64) return (j * 2 + c) ^ (j >> 2 & 1);
   else return j;
 }
-// Eight fields u = n + 8 of a word -> whole numbers n in type T: field i and i + 4 as the halves of register i.  (bf16 has room for a field at bits 0 - 3 under the exponent of 128, fp16 at bits 0 - 3 under that of 1024 and at
-// 4 - 7 under that of 64.)
-template <typename T>
-__device__ __forceinline__ void expand_numbers(uint32_t w, uint32_t (&r)[4]) {
-  if constexpr (std::is_same<T, __half>::value) {
-    const uint32_t v = w >> 8;
-    r[0] = h2_sub(and_or(w, 0x000f000fu, 0x64006400u), 0x64086408u);
-    r[1] = h2_sub(and_or(w, 0x00f000f0u, 0x54005400u), 0x54805480u);
-    r[2] = h2_sub(and_or(v, 0x000f000fu, 0x64006400u), 0x64086408u);
-    r[3] = h2_sub(and_or(v, 0x00f000f0u, 0x54005400u), 0x54805480u);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r[i] = bf2_sub(and_or(w >> (4 * i), 0x000f000fu, 0x43004300u), 0x43084308u);
-  }
-}
-
 template <typename T, int DH, int NT>
 __global__ void __launch_bounds__(kThreads, Few<DH, NT>::kCtas)
 k_quant_few(const __grid_constant__ QuantAttnArgs qa) {

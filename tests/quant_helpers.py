@@ -142,8 +142,16 @@ class QuantCase:
         return out, lse, size
 
 
+def is_tall(case, window=0):
+    """Worked out on the 5th-generation tensor cores, with one 16-bit term of every weight (queries that repeat one row are not)."""
+    B = len(case.lens)
+    rows, room = -(-case.q.shape[0] * (case.H // case.Hkv) // B), case.table.shape[1] * case.page
+    seen = min(room, window + case.q.shape[0] // B) if window else room
+    return rows > 32 and (rows > 128 or rows * B * case.Hkv * seen > 3 << 19) and case.q.stride(0) > 0 and case.q.stride(1) > 0
+
+
 def check_attention(case, got, lse, want, want_lse, size, tall=False):
-    """Rounding when stored (u of the type); weights as two bf16 terms, 16 bits of them, or with copies as one term (u of the type); scores in 32 bits: a score of D products is off by at most about
+    """Rounding when stored (u of the type); weights as two bf16 terms, 16 bits of them, or in tall blocks as one term (u of the type); scores in 32 bits: a score of D products is off by at most about
     D 2^-24 times the sum of their sizes, which for these inputs is below 1e-4, and so are a weight and the log of the sum.  Values are exact."""
     u = U[case.dtype]
     live = case.live()

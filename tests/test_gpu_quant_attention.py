@@ -5,15 +5,15 @@ import pytest
 import torch
 
 from paper_2502_08923_b200 import binding as cs
-from quant_helpers import QuantCase, check_attention, i32
+from quant_helpers import QuantCase, check_attention, i32, is_tall
 
 pytestmark = pytest.mark.gpu
 
 
-def run(case, mask=cs.MASK_CAUSAL, window=0, scale=None, tall=False):
+def run(case, mask=cs.MASK_CAUSAL, window=0, scale=None):
     got, lse = case.cache.cs_quant_attention(case.q, *case.blocks(), mask=mask, window=window, scale=scale, with_lse=True)
     assert case.cache.cs_quant_status() == cs.CS_OK
-    check_attention(case, got, lse, *case.attention(mask, window, scale), tall=tall)
+    check_attention(case, got, lse, *case.attention(mask, window, scale), tall=is_tall(case, window))
     return got, lse
 
 
@@ -36,7 +36,8 @@ def test_masks(mask, window, D, lens, cached):
 
 
 # tall blocks, with copies and without
-@pytest.mark.parametrize("lens,cached,H,Hkv,D,page", [([200], [0], 8, 2, 128, 16), ([130, 64], [700, 129], 32, 8, 64, 32), ([257], [1000], 4, 4, 32, 64), ([500, 1, 90], [3, 2000, 130], 8, 2, 128, 128)])
+@pytest.mark.parametrize("lens,cached,H,Hkv,D,page", [([200], [0], 8, 2, 128, 16), ([130, 64], [700, 129], 32, 8, 64, 32), ([257], [1000], 4, 4, 32, 64), ([500, 1, 90], [3, 2000, 130], 8, 2, 128, 128),
+                                                    ([30, 25], [700, 129], 128, 1, 64, 32), ([700], [100], 4, 1, 128, 16), ([110, 1, 140], [0, 2000, 130], 64, 2, 32, 128)])      # (prompts' chunks by their rows per KV head)
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("room", [True, False])
 def test_tall_blocks(lens, cached, H, Hkv, D, page, dtype, room):
@@ -44,7 +45,55 @@ def test_tall_blocks(lens, cached, H, Hkv, D, page, dtype, room):
     need = len(lens) * wide * page
     for mask, window in ((cs.MASK_CAUSAL, 0), (cs.MASK_PREFIX, 0), (cs.MASK_CAUSAL, 100), (cs.MASK_FULL, 64)):
         case = QuantCase(lens, cached, H, Hkv, D, dtype, page=page, seed=3, tall=need if room else need - 16, gaps=3)
-        run(case, mask, window, tall=room)
+        assert is_tall(case)
+        run(case, mask, window)
+
+
+@pytest.mark.parametrize("D,page", [(128, 16), (64, 32), (32, 16), (128, 256)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_blocks_of_one_row_group(D, page, dtype):
+    """Expanded by the kernel: slots that take tiles in turn and slots with rows of their own; long contexts, ends inside pages and tiles."""
+    for lens, cached in (([20], [5000]), ([21, 17, 33], [130, 0, 1777]), ([64], [300]), ([17] * 9, [100 * i for i in range(9)]), ([1, 60], [4000, 10])):
+        for mask, window in ((cs.MASK_CAUSAL, 0), (cs.MASK_FULL, 0), (cs.MASK_PREFIX, 0), (cs.MASK_CAUSAL, 200)):
+            case = QuantCase(lens, cached, 32, 4, D, dtype, page=page, seed=5, gaps=1)
+            assert is_tall(case)
+            run(case, mask, window)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_between_few_and_tall(D):
+    """Rows per KV head from 33 to 128: by the work, which goes by the room of the page table and by the window."""
+    ways = set()
+    for rows in (8, 9, 32):
+        for cached in (100, 5000, 17000):
+            for window in (0, 600):
+                case = QuantCase([rows], [cached], 16, 4, D, torch.bfloat16, page=64, seed=rows)
+                run(case, window=window)
+                ways.add((rows * 4 > 32, is_tall(case, window)))
+    assert ways == {(False, False), (True, False), (True, True)}
+
+
+def test_repeated_queries():
+    """Queries that repeat one row have no operand map: tall blocks of them take the way of short ones."""
+    case = QuantCase([100, 60], [200, 30], 8, 2, 64, torch.bfloat16, seed=4)
+    case.q = case.q[:1].expand(case.rows, 8, 64)
+    assert not is_tall(case)
+    run(case)
+    case.q = case.q[:1, :1].expand(case.rows, 8, 64)
+    run(case)
+
+
+def test_scales_beyond_fp16():
+    """fp16 queries over values beyond 65504, which the tensor cores take for that in tall blocks."""
+    case = QuantCase([30, 40], [100, 20], 8, 2, 64, torch.float16, seed=4, tall=0)
+    for b in range(2):
+        case.v[b] = torch.randn(case.v[b].shape, device="cuda") * 40000.0
+        case.k[b] = case.k[b].float()
+        case.put(b)
+        case.v[b] = case.v[b].clamp(-65504, 65504)
+    got, lse = case.cache.cs_quant_attention(case.q, *case.blocks(), with_lse=True)
+    assert is_tall(case) and case.cache.cs_quant_status() == cs.CS_OK
+    check_attention(case, got, lse, *case.attention(), tall=True)
 
 
 def test_scales_and_strides():
@@ -73,11 +122,11 @@ def test_sharp_and_flat_scores():
 
 
 @pytest.mark.parametrize("D", [32, 64, 128])
-@pytest.mark.parametrize("tall", [False, True])
-def test_what_is_not_finite(D, tall):
+@pytest.mark.parametrize("tall,room", [(False, 0), (True, 0), (True, 1 << 14)])
+def test_what_is_not_finite(D, tall, room):
     """Keys and values that are NaN at positions that some rows see and others do not."""
     lens, cached = ([150, 140], [300, 40]) if tall else ([6, 3], [300, 40])
-    case = QuantCase(lens, cached, 8, 2, D, torch.bfloat16, seed=5, tall=1 << 14 if tall else 0)
+    case = QuantCase(lens, cached, 64 if room else 8, 2, D, torch.bfloat16, seed=5, tall=room)
     for name, rows, scales, at in (("v", case.v, case.vs, [(0, cached[0] + 2, 1, 0), (0, 7, 0, D // 32 - 1), (1, cached[1] + 1, 1, 0)]), ("k", case.k, case.ks, [(0, cached[0] + 4, 0, 0)])):
         for b, pos, head, group in at:
             scales[case.table[b, pos // case.page].long(), head, pos % case.page, group] = math.nan
@@ -96,14 +145,15 @@ def test_many_sequences():
     run(QuantCase(lens, cached, 4, 2, 32, torch.bfloat16, seed=6))
 
 
-def test_pages_far_apart():
+@pytest.mark.parametrize("rows", [2, 140])
+def test_pages_far_apart(rows):
     """Element offsets beyond 2^31: the sequence's pages are the last ones of a pool of 4.6 GB."""
     page, D, Hkv = 128, 128, 8
-    case = QuantCase([2], [700], 8, Hkv, D, torch.bfloat16, page=page, seed=8, first_page=72000, n_pages=72010)
+    case = QuantCase([rows], [700], 8, Hkv, D, torch.bfloat16, page=page, seed=8, first_page=72000, n_pages=72010)
     run(case)
-    q, k, v = torch.randn(3, 2, Hkv, D, device="cuda").to(torch.bfloat16).unbind(0)
+    q, k, v = torch.randn(3, rows, Hkv, D, device="cuda").to(torch.bfloat16).unbind(0)
     case.cache.cs_quant_append(k, v, *case.blocks())
-    assert torch.equal(*(x.double() for x in (case.cache.cs_quant_read(*case.blocks(), rows=2)[0], __import__("quant_helpers").held(*__import__("quant_helpers").quantise(k)))))
+    assert torch.equal(*(x.double() for x in (case.cache.cs_quant_read(*case.blocks(), rows=rows)[0], __import__("quant_helpers").held(*__import__("quant_helpers").quantise(k)))))
 
 
 def test_same_result_every_time():
@@ -115,12 +165,12 @@ def test_same_result_every_time():
 
 
 def test_wrong_blocks_and_pages():
-    for tall in (False, True):
+    for tall, room in ((False, 0), (True, 0), (True, 1 << 14)):
         lens = [3, 4] if not tall else [150, 140]
-        case = QuantCase(lens, [20, 300], 8, 2, 64, torch.bfloat16, seed=4, tall=1 << 14 if tall else 0)
+        case = QuantCase(lens, [20, 300], 64 if room else 8, 2, 64, torch.bfloat16, seed=4, tall=room)
         want, want_lse, size = case.attention()
-        out = torch.full((case.rows, 8, 64), 9.0, dtype=torch.bfloat16, device="cuda")
-        lse = torch.full((case.rows, 8), 9.0, device="cuda")
+        out = torch.full((case.rows, case.H, 64), 9.0, dtype=torch.bfloat16, device="cuda")
+        lse = torch.full((case.rows, case.H), 9.0, device="cuda")
         case.cache.cs_quant_attention(case.q, case.start, case.len, i32([5000, 300]), case.table, out=out, lse=lse)
         assert case.cache.cs_quant_status() == cs.CS_ERR_CAPACITY and case.cache.cs_quant_status() == cs.CS_OK
         n = lens[0]

@@ -7,7 +7,7 @@ import torch
 
 from paper_2502_08923_b200 import binding as cs, inputs
 from paged_helpers import i32, norm_rope
-from quant_helpers import QuantCase, check_attention, held, quantise
+from quant_helpers import QuantCase, check_attention, is_tall, held, quantise
 
 pytestmark = pytest.mark.gpu
 PATH = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_decode.py")
@@ -17,7 +17,7 @@ PATH = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
 def test_further_layers_on_one_workspace(lens):
     case = QuantCase(lens, [200, 90], 8, 2, 128, seed=1, tall=1 << 12)
     first, want = case.cache, case.attention()
-    tall = sum(lens) * 4 > 64 * len(lens)
+    tall = is_tall(case)
     pools = lambda: (case.data[0].clone(), case.data[1].clone(), case.scales[0].clone(), case.scales[1].clone())
     first.cs_quant_attention(case.q, case.start, i32([lens[0], -1]), case.kv_len, case.table)
     second = cs.QuantCache(*pools(), workspace=first)      # (made while the first is at work: nothing is cleared)
@@ -110,7 +110,7 @@ def test_other_than_the_current_stream():
         for lens in ([3, 1], [90, 40]):
             case = QuantCase(lens, [100, 33], 8, 2, 64, seed=3, tall=1 << 12)
             got = case.cache.cs_quant_attention(case.q, *case.blocks(), with_lse=True)
-            check_attention(case, *got, *case.attention(), tall=sum(lens) * 4 > 128)
+            check_attention(case, *got, *case.attention(), tall=is_tall(case))
             assert case.cache.cs_quant_status() == cs.CS_OK
 
 
