@@ -242,7 +242,8 @@ __device__ __forceinline__ void expand_group(const uint4& words, unsigned scale,
       expand_numbers<__half>(w[i], r);
       out[i] = make_uint4(h2_mul(r[0], hs), h2_mul(r[1], hs), h2_mul(r[2], hs), h2_mul(r[3], hs));
     }
-    if (fabsf(s) > 8192.f) {                     // (eight of it are beyond 65504)
+    // (eight of it are beyond 65504; five bits of it go below 2^-24: worked out in 32 bits, rounded once)
+    if (fabsf(s) > 8192.f || (fabsf(s) < 0x1p-20f && s != 0.f)) {
       auto far = [&](int i, int k) { return fminf(fmaxf((float)((int)(w[i] >> (4 * k) & 15) - 8) * s, -65504.f), 65504.f); };
 #pragma unroll
       for (int i = 0; i < 4; ++i)

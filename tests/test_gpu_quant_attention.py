@@ -73,6 +73,17 @@ def test_between_few_and_tall(D):
     assert ways == {(False, False), (True, False), (True, True)}
 
 
+@pytest.mark.parametrize("room", [0, 1 << 12])
+def test_no_rows_of_any_block(room):
+    """A call of tall blocks' size in which no sequence has a row: everything stays as it was."""
+    case = QuantCase([0, 0], [300, 0], 64, 2, 64, torch.bfloat16, seed=2, gaps=100, tall=room)
+    assert is_tall(case)
+    out, lse = torch.full_like(case.q, 9.0), torch.full((case.rows, 64), 9.0, device="cuda")
+    for _ in range(2):
+        case.cache.cs_quant_attention(case.q, *case.blocks(), out=out, lse=lse)
+    assert case.cache.cs_quant_status() == cs.CS_OK and bool((out == 9.0).all()) and bool((lse == 9.0).all())
+
+
 def test_repeated_queries():
     """Queries that repeat one row have no operand map: tall blocks of them take the way of short ones."""
     case = QuantCase([100, 60], [200, 30], 8, 2, 64, torch.bfloat16, seed=4)
@@ -83,17 +94,18 @@ def test_repeated_queries():
     run(case)
 
 
-def test_scales_beyond_fp16():
-    """fp16 queries over values beyond 65504, which the tensor cores take for that in tall blocks."""
-    case = QuantCase([30, 40], [100, 20], 8, 2, 64, torch.float16, seed=4, tall=0)
-    for b in range(2):
-        case.v[b] = torch.randn(case.v[b].shape, device="cuda") * 40000.0
-        case.k[b] = case.k[b].float()
-        case.put(b)
-        case.v[b] = case.v[b].clamp(-65504, 65504)
-    got, lse = case.cache.cs_quant_attention(case.q, *case.blocks(), with_lse=True)
-    assert is_tall(case) and case.cache.cs_quant_status() == cs.CS_OK
-    check_attention(case, got, lse, *case.attention(), tall=True)
+def test_values_beyond_fp16():
+    """fp16 queries over values beyond 65504, which the tensor cores take for that in tall blocks, and over some so small that fp16 rounds them: each by 2^-25 at most, and so do their averages (the result's own rounding is as much)."""
+    for size in (40000.0, 3e-6, 4e-8):
+        case = QuantCase([30, 40], [100, 20], 8, 2, 64, torch.float16, seed=4)
+        for b in range(2):
+            case.v[b] = torch.randn(case.v[b].shape, device="cuda") * size
+            case.k[b] = case.k[b].float()
+            case.put(b)
+            case.v[b] = case.v[b].clamp(-65504, 65504)
+        got, lse = case.cache.cs_quant_attention(case.q, *case.blocks(), with_lse=True)
+        assert is_tall(case) and case.cache.cs_quant_status() == cs.CS_OK
+        check_attention(case, got, lse, *case.attention(), tall=True)
 
 
 def test_scales_and_strides():
