@@ -559,7 +559,7 @@ __global__ void k_quant_iota(int* p, int n) {
 // Query rows per KV head (on the average of a call's sequences) that the kernel for few rows always has, up to 32: a pass over the keys; the tensor cores always have, more than 128; that are worked out
 // from copies there, where they fit, more than 2,560.  In between it is the work that decides, rows x positions x KV heads x sequences: the tensor cores' kernel has more to set up (32 query heads in groups of four, us here
 // and there; 84 rows over 512 keys 16.7 and 20.9, over 4,096 27.9 and 21.3; 44 rows over 4,096 keys 17.9 and 18.6, over 30,720 48 and 37; 24 rows 30 and 36; 8 sequences over 16,384 keys, 24 rows 54 and 73, 44 rows 97 and 74,
-// 84 rows 168 and 76).  Expanded by the kernel and from copies: 84 rows over 8 x 16,384 keys 76 and 129, 2,400 rows over 30,720 keys 307 and 308, 8,192 rows 936 and 896; windows of 1,000 keys, 2,400 rows 61 and 63, 4,500 rows 124 and 113.
+// 84 rows 168 and 76; 132 rows over 200 keys 17.5 and 18.0, of four sequences 19.3 and 18.6, of sixteen 48 and 19; 512 rows over 200 keys 21.7 and 22.8, heads of 64 15.1 and 19.2).  Expanded by the kernel and from copies: 84 rows over 8 x 16,384 keys 76 and 129, 2,400 rows over 30,720 keys 307 and 308, 8,192 rows 936 and 896; windows of 1,000 keys, 2,400 rows 61 and 63, 4,500 rows 124 and 113.
 constexpr long long kFewRows = 32, kTallRows = 128, kTallWork = 3 << 19, kCopyRows = 2560;
 
 thread_local char t_quant_err[256] = "";
