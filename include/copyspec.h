@@ -629,6 +629,9 @@ cs_status cs_quant_attention(cs_quant_cache* cache, const cs_blocks* blocks, con
                              int64_t q_head_stride, int n_heads, cs_dtype dtype, cs_mask mask, int window, float scale,
                              void* out, float* lse, void* stream);
 
+/* As cs_paged_debug_drop_tile, for the next cs_quant_attention of tall blocks. */
+cs_status cs_quant_debug_drop_tile(cs_quant_cache* cache, int tile);
+
 #ifdef __cplusplus
 }
 #endif

@@ -83,7 +83,7 @@ EXPORTS = ("cs_workspace_bytes", "cs_create", "cs_destroy", "cs_last_error", "cs
            "cs_rope_table", "cs_qk_norm_rope", "cs_paged_workspace_bytes", "cs_paged_create", "cs_paged_create_beside", "cs_paged_destroy", "cs_paged_last_error",
            "cs_paged_status", "cs_paged_append", "cs_paged_attention", "cs_paged_head_dim", "cs_paged_debug_drop_tile",
            "cs_quant_workspace_bytes", "cs_quant_create", "cs_quant_create_beside", "cs_quant_destroy", "cs_quant_head_dim", "cs_quant_last_error", "cs_quant_status",
-           "cs_quant_append", "cs_quant_read", "cs_quant_attention")
+           "cs_quant_append", "cs_quant_read", "cs_quant_attention", "cs_quant_debug_drop_tile")
 
 _lib = None
 _search = None      # cs_find_match in native code, for plain arguments
@@ -209,6 +209,8 @@ def load(build_if_missing: bool = True) -> C.CDLL:
     lib.cs_quant_head_dim.argtypes = [vp]
     lib.cs_quant_last_error.restype = C.c_char_p
     lib.cs_quant_last_error.argtypes = [vp]
+    lib.cs_quant_debug_drop_tile.restype = i
+    lib.cs_quant_debug_drop_tile.argtypes = [vp, i]
     lib.cs_quant_status.restype = i
     lib.cs_quant_status.argtypes = [vp, vp]
     lib.cs_quant_append.restype = i
@@ -983,3 +985,6 @@ class QuantCache:
         """Waits for the stream; what the device found wrong since the last call (CS_OK: nothing)."""
         with torch.cuda.device(self.device):
             return self.lib.cs_quant_status(self.handle, _stream())
+
+    def cs_quant_debug_drop_tile(self, tile):
+        self._check(self.lib.cs_quant_debug_drop_tile(self.handle, tile), "cs_quant_debug_drop_tile")

@@ -684,6 +684,7 @@ cs_status create(const char* name, cs_quant_cache** out, const cs_quant_config* 
       return refuse(CS_ERR_CUDA, cudaGetErrorString(e));
     }
   }
+  c->drop = -1;
   c->tall_positions = cfg->tall_positions > 0 ? l.positions : 0;
   c->tall_k = ws + l.k;
   c->tall_v = ws + l.v;
@@ -779,6 +780,12 @@ void cs_quant_destroy(cs_quant_cache* c) {
 int cs_quant_head_dim(const cs_quant_cache* c) { return c != nullptr ? c->cfg.head_dim : 0; }
 
 const char* cs_quant_last_error(const cs_quant_cache* c) { return c != nullptr ? c->err : t_quant_err; }
+
+cs_status cs_quant_debug_drop_tile(cs_quant_cache* c, int tile) {
+  if (c == nullptr) return CS_ERR_ARG;
+  c->drop = tile < 0 ? -1 : tile;
+  return CS_OK;
+}
 
 cs_status cs_quant_status(cs_quant_cache* c, void* stream) {
   if (c == nullptr) return CS_ERR_ARG;
@@ -892,6 +899,8 @@ cs_status cs_quant_attention(cs_quant_cache* c, const cs_blocks* blocks, const v
     b.page_table = c->tall_table;
     b.table_width = (int)copy_pages;
     cs_paged_cache* const copies = c->tall[dtype == CS_BF16 ? 0 : 1][size];
+    cs_paged_debug_drop_tile(copies, c->drop);
+    c->drop = -1;
     const cs_status t = cs_paged_attention(copies, &b, q, q_row_stride, q_head_stride, n_heads, mask, window, scale, out, lse, stream);
     return t == CS_OK ? t : fail(c, t, cs_paged_last_error(copies));
   }
@@ -912,6 +921,8 @@ cs_status cs_quant_attention(cs_quant_cache* c, const cs_blocks* blocks, const v
   p.wait_ns = paged->wait_limit_ns;
   p.drop = -1;
   if (tall) {
+    p.drop = c->drop;
+    c->drop = -1;
     p.kv.k = reinterpret_cast<char*>(c->view.k); p.kv.v = reinterpret_cast<char*>(c->view.v); p.kv.page_stride = c->view.data_page * 4;
     p.ks = c->view.ks; p.vs = c->view.vs; p.scale_page = c->view.scale_page;
     p.parts = paged->parts; p.parts_ml = paged->parts_ml; p.splits = paged->splits;

@@ -46,6 +46,7 @@ struct cs_quant_cache {
   char *tall_k, *tall_v;       // [page][KV head][slot][head_dim]
   int *tall_table, *tall_len;  // 0, 1, 2, ...; lengths of the blocks that nothing is wrong with
   cs_paged_cache* tall[2][4];  // over the copies, by the queries' type (CS_BF16, CS_F16) and the size of a page (128 >> i); tall blocks without copies have their sums in the last one's workspace
+  int drop;                    // test hook: K tile that the next call of tall blocks leaves out; -1: none
   char err[256];
 };
 

@@ -59,7 +59,7 @@ def test_calls_without_a_handle():
     assert lib.cs_quant_append(None, None, None, None, None, 0, 0, None, 0, 0, 1e-5, None) == cs.CS_ERR_ARG
     assert lib.cs_quant_read(None, None, None, None, 0, None) == cs.CS_ERR_ARG
     assert lib.cs_quant_attention(None, None, None, 0, 0, 1, 0, 0, 0, 1.0, None, None, None) == cs.CS_ERR_ARG
-    assert lib.cs_quant_head_dim(None) == 0
+    assert lib.cs_quant_head_dim(None) == 0 and lib.cs_quant_debug_drop_tile(None, 0) == cs.CS_ERR_ARG
     lib.cs_quant_destroy(None)
 
 
