@@ -577,7 +577,7 @@ cs_status cs_paged_debug_drop_tile(cs_paged_cache* cache, int tile);
  *
  * Pools, for K and for V: numbers, of page `p`, KV head `h`, slot `s` from byte p * page_stride + (h * page_size + s) * head_dim / 2 on, and bf16 scales from element
  * p * scale_page_stride + (h * page_size + s) * head_dim / 32 on.  Eight elements are a 32-bit word; its elements 2i and 2i + 1 are at bits 4i and 16 + 4i.  16-byte aligned, strides multiples of 16
- * bytes.  Numbers 0 (-8) may be there as well as 1 to 15.  Scales of more than five significant bits are read with a rounding.
+ * bytes.  Numbers 0 (-8) may be there as well as 1 to 15.  Scales of more than five significant bits are read with a rounding; of those beyond 2^123 nothing is said but that they do not reach rows that do not attend to them.
  *
  * Tall blocks are worked out on the 5th-generation tensor cores, from values in 16 bits in shared memory (for fp16 queries that is fp16: beyond 65504 they saturate, below 2^-14 they are rounded to steps of 2^-24), others by a kernel for few
  * rows.  Tall are those of more than 128 query rows per KV head (rows of the block x heads of the group, on the average of a call's sequences), and of more than 32 where that times positions (n_seqs x table_width x

@@ -124,8 +124,8 @@ __device__ __forceinline__ void expand_numbers(uint32_t w, uint32_t (&r)[4]) {
   }
 }
 
-// is a scale not finite?
-__device__ __forceinline__ bool quant_odd(unsigned scale) { return (scale & 0x7f80u) == 0x7f80u; }
+// is a scale not finite, or so far beyond the format's 2^123 that what it is expanded with (24 s) is not?
+__device__ __forceinline__ bool quant_odd(unsigned scale) { return (scale & 0x7fffu) > 0x7d2au; }
 
 }  // namespace
 #endif

@@ -23,8 +23,8 @@
 // Tried and not kept: units of a warp with claims by a counter (44 -> 60 us: warps out of step miss the instruction cache), CTAs of eight warps, sixteen keys at a time for more than eight rows (5 - 11 % slower), more CTAs an SM for heads of 64
 // (spills).
 //
-// Masked keys: scores become -inf.  Slices that lie outside of [lo, hi) of the item's rows are not fetched.  In slices that some rows see and others do not, V scales that are not
-// finite become 0 and the rows that see such a key are given NaN (0 x NaN is not 0).
+// Masked keys: scores become -inf.  Slices that lie outside of [lo, hi) of the item's rows are not fetched; of one that lies partly outside, V scales out there become 0 whatever they are (nobody may have written those
+// slots, and 0 x inf is not 0).  In slices that some rows see and others do not, so do V scales that values cannot be worked out with, and the rows that see such a key are given NaN.
 #include <type_traits>
 #include <utility>
 
@@ -327,6 +327,16 @@ k_quant_few(const __grid_constant__ QuantAttnArgs qa) {
         });
         // ---- masks  (key of row g + 8 b of S^T: as loaded)
         if (mixed) {
+          // (in shared memory, a key a lane: compared where scales are taken out, 64 ragged tokens took 42.0 us)
+          if (key0 < p.lo || key0 + kSlice > p.hi) {
+            if (key0 + lane < p.lo || key0 + lane >= p.hi) {
+              const uint32_t at = my_ring + stage + 2 * F::kData + F::kScales + lane * F::kScaleBytes;
+              if constexpr (DH == 128) asm volatile("st.shared.v2.u32 [%0], {%1, %1};" ::"r"(at), "r"(0) : "memory");
+              else if constexpr (DH == 64) asm volatile("st.shared.u32 [%0], %1;" ::"r"(at), "r"(0) : "memory");
+              else asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"((unsigned short)0) : "memory");
+            }
+            __syncwarp();
+          }
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
