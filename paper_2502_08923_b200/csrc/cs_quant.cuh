@@ -96,16 +96,17 @@ __device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t b, uint32_t c) {
 
 // The scales of a register's two halves, and what the conversion makes of them once.
 struct QuantScale {
-  uint32_t s, s8, c;           // s, s / 8, -24 s: all exact in bf16
-  __device__ __forceinline__ static QuantScale of(uint32_t pair) { return QuantScale{pair, bf2_mul(pair, 0x3e003e00u), bf2_mul(pair, 0xc1c0c1c0u)}; }
+  uint32_t s, c;               // s, -24 s: both exact in bf16, where it ends as well (a multiple of 2^-133 stays one)
+  __device__ __forceinline__ static QuantScale of(uint32_t pair) { return QuantScale{pair, bf2_mul(pair, 0xc1c0c1c0u)}; }
 };
-// Two 16-bit halves of four fields u = n + 8 each -> field i of both, times their scales: exact.  A field at bits 3 - 6 under the exponent of 128 reads 128 + 8 u, and one product and sum make s (u - 8) of it;
-// the one at bits 0 - 3 reads 128 + u, where -136 s would need ten bits, and takes a difference and a product instead of a shift.
+// Two 16-bit halves of four fields u = n + 8 each -> field i of both, times their scales: exact.  A field at bits 3 - 6 under the exponent of 16 reads 16 + u, and one product and sum make s (u - 8) of it.
+// (Without a shift, at bits 0 - 3 under the exponent of 128, the first field takes a difference and a product, and two more constants: as many instructions, and registers that heads of 128 have not got.  64 ragged tokens
+// 42.4 us, so 41.4.)
 __device__ __forceinline__ void quant_expand(uint32_t w, const QuantScale& q, uint32_t (&r)[4]) {
-  r[0] = bf2_mul(bf2_sub(and_or(w, 0x000f000fu, 0x43004300u), 0x43084308u), q.s);
-  r[1] = bf2_fma(and_or(w >> 1, 0x00780078u, 0x43004300u), q.s8, q.c);
-  r[2] = bf2_fma(and_or(w >> 5, 0x00780078u, 0x43004300u), q.s8, q.c);
-  r[3] = bf2_fma(and_or(w >> 9, 0x00780078u, 0x43004300u), q.s8, q.c);
+  r[0] = bf2_fma(and_or(w << 3, 0x00780078u, 0x41804180u), q.s, q.c);
+  r[1] = bf2_fma(and_or(w >> 1, 0x00780078u, 0x41804180u), q.s, q.c);
+  r[2] = bf2_fma(and_or(w >> 5, 0x00780078u, 0x41804180u), q.s, q.c);
+  r[3] = bf2_fma(and_or(w >> 9, 0x00780078u, 0x41804180u), q.s, q.c);
 }
 
 // Eight fields u = n + 8 of a word -> whole numbers n in type T: field i and i + 4 as the halves of register i.  (bf16 has room for a field at bits 0 - 3 under the exponent of 128, fp16 at bits 0 - 3 under that of 1024 and at
