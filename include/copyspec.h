@@ -571,8 +571,8 @@ cs_status cs_paged_debug_drop_tile(cs_paged_cache* cache, int tile);
  * Operators around a paged KV cache held in 4 bits: 4.5 bits a value instead of 16, for servers whose contexts fill the memory or whose decoding waits for it (the paper has no
  * counterpart; blocks, masks and page tables are those of the paged cache above).
  *
- * A row (one position, one KV head) is cut into groups of 32 neighbouring elements.  With a = max |x| of a group, s = a / 7 rounded to five significant bits (nearest, halves to even; at most 2^123)
- * and n = x / s rounded to the nearest whole number (halves to even), |n| <= 7, the group is held as s in bf16 and numbers n + 8 of 4 bits, and stands for s n.  No element is off by more than s / 2 (but for
+ * A row (one position, one KV head) is cut into groups of 32 neighbouring elements.  With a = max |x| of a group, s = a / 7 rounded to five significant bits (nearest, halves to even; at most 2^123, below 2^-126 to
+ * the nearest multiple of 2^-133, where bf16 ends) and n = x / s rounded to the nearest whole number (halves to even), |n| <= 7, the group is held as s in bf16 and numbers n + 8 of 4 bits, and stands for s n.  No element is off by more than s / 2 (but for
  * scales below 2^-126 or at the limit, beyond which values saturate); every value held is exactly a bf16 number.  A group with an element that is not finite has the scale NaN and reads as NaN throughout.  Zeros stay zeros.
  *
  * Pools, for K and for V: numbers, of page `p`, KV head `h`, slot `s` from byte p * page_stride + (h * page_size + s) * head_dim / 2 on, and bf16 scales from element

@@ -77,21 +77,21 @@ struct Reciprocal {
   __device__ __forceinline__ float times(float x) const { return fmaf(x, hi, x * lo); }
 };
 constexpr float kMostScale = 1.0633823966279327e37f;         // 2^123: 24 times it is finite
-// The scale of a group whose largest element is `most`, which may be inf or NaN: five significant bits, halves to even, and multiples of 2^-133; at most 2^123
-__device__ __forceinline__ float scale_of(float most) {
-  const Reciprocal seventh{0.14285714924335479736328125f, -6.386212e-9f};      // 1 / 7: rounded, and what that leaves out
-  uint32_t b = __float_as_uint(seventh.times(most));
-  if ((b & 0x7f800000u) == 0x7f800000u) return __uint_as_float(0x7fc00000u);
-  b += 0x3ffffu + (b >> 19 & 1u);
-  const float s = fminf(__uint_as_float(b & 0xfff80000u), kMostScale);
-  return __bfloat162float(__float2bfloat16_rn(s));
-}
+// The scale of a group whose largest element is `most`, which may be inf or NaN: five significant bits, halves to even, below 2^-126 the nearest multiple of 2^-133; at most 2^123
 __device__ __forceinline__ float scale_of(double most) {
   const double x = most / 7.0;
   if (!(x <= (double)kMostScale)) return x <= 1e300 ? kMostScale : __uint_as_float(0x7fc00000u);
   long long b = __double_as_longlong(x);
   b += 0x7fffffffffffll + (b >> 48 & 1);
   return __bfloat162float(__float2bfloat16_rn((float)__longlong_as_double(b >> 48 << 48)));
+}
+__device__ __forceinline__ float scale_of(float most) {
+  const Reciprocal seventh{0.14285714924335479736328125f, -6.386212e-9f};      // 1 / 7: rounded, and what that leaves out
+  const bool small = most < 0x1p-60f;            // (the quotient's second term, and near 2^-126 the quotient, would have fewer bits there)
+  uint32_t b = __float_as_uint(seventh.times(most * (small ? 0x1p64f : 1.f)));
+  if ((b & 0x7f800000u) == 0x7f800000u) return __uint_as_float(0x7fc00000u);
+  b += 0x3ffffu + (b >> 19 & 1u);
+  return __bfloat162float(__float2bfloat16_rn(fminf(__uint_as_float(b & 0xfff80000u), kMostScale) * (small ? 0x1p-64f : 1.f)));
 }
 constexpr uint32_t kZeros = 0x88888888u;
 __device__ __forceinline__ constexpr int field_at(int i) { return 4 * (i / 2 + 4 * (i & 1)); }
