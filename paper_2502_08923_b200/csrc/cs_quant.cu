@@ -935,7 +935,7 @@ cs_status cs_quant_attention(cs_quant_cache* c, const cs_blocks* blocks, const v
     part.p.blk.n_seqs = blocks->n_seqs - b < most ? blocks->n_seqs - b : most;
     part.p.blk.start += b; part.p.blk.len += b; part.p.blk.kv_len += b;
     part.p.blk.table += (long long)b * blocks->table_width;
-    const cs_status r = tall ? cs_launch_quant_tc(paged, part.p, st) : cs_launch_quant_few(c, part, st);
+    const cs_status r = tall ? cs_launch_quant_tc(paged, part.p, st) : cs_launch_quant_few(c, part, per_seq, st);
     if (r != CS_OK) return tall ? fail(c, r, cs_paged_last_error(paged)) : r;
   }
   return CS_OK;

@@ -57,7 +57,7 @@ struct QuantAttnArgs {
   int half;                    // queries and results are fp16 (else bf16)
 };
 
-cs_status cs_launch_quant_few(cs_quant_cache* c, const QuantAttnArgs& a, cudaStream_t st);
+cs_status cs_launch_quant_few(cs_quant_cache* c, const QuantAttnArgs& a, long long rows, cudaStream_t st);   // `rows`: query rows of a KV head, on the average of the call's sequences
 
 #ifdef __CUDACC__
 namespace {

@@ -699,10 +699,10 @@ cs_status launch_few_type(cs_quant_cache* c, const QuantAttnArgs& a, int tiles, 
 
 }  // namespace
 
-cs_status cs_launch_quant_few(cs_quant_cache* c, const QuantAttnArgs& args, cudaStream_t st) {
+cs_status cs_launch_quant_few(cs_quant_cache* c, const QuantAttnArgs& args, long long rows, cudaStream_t st) {
   QuantAttnArgs a = args;
-  // Items of as few query rows as leave no fewer items: a KV head's rows (on the average of the sequences, which is what the host knows) in equal shares of up to 32
-  const long long rows = ((long long)a.p.blk.rows * a.p.group + a.p.blk.n_seqs - 1) / a.p.blk.n_seqs, items = (rows + kQuantMaxRows - 1) / kQuantMaxRows;
+  // Items of as few query rows as leave no fewer items: a KV head's rows (on the average of the call's sequences, which is what the host knows; a launch may have part of them, but has all rows at hand) in equal shares of up to 32
+  const long long items = (rows + kQuantMaxRows - 1) / kQuantMaxRows;
   const int tiles = (int)(((rows + items - 1) / items + 7) / 8);
   a.p.item_rows = 8 * tiles;
   a.p.by_item_rows = PagedDivisor::by(a.p.item_rows);
