@@ -712,10 +712,10 @@ cs_status create(const char* name, cs_quant_cache** out, const cs_quant_config* 
 }
 
 template <typename S, typename D>
-cudaError_t launch_append(QuantAppendArgs a, int head_dim, cudaStream_t st) {
+cudaError_t launch_append(QuantAppendArgs a, int head_dim, int sms, cudaStream_t st) {
   const int per = 512 / head_dim, units = cs_ceil_div(a.n_q, per) + 2 * cs_ceil_div(a.n_kv, per);
   a.warps_per_row = kWarps;
-  while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)a.n_rows * a.warps_per_row > 148 * 16)) a.warps_per_row /= 2;
+  while (a.warps_per_row > 1 && (a.warps_per_row >= 2 * units || (long long)a.n_rows * a.warps_per_row > 16 * sms)) a.warps_per_row /= 2;
   const dim3 grid((unsigned)(((long long)a.n_rows * a.warps_per_row + kWarps - 1) / kWarps)), block(kThreads);
   switch (head_dim) {
     case 32: return cs_launch_pdl(k_quant_append<S, D, 32>, grid, block, 0, st, a);
@@ -834,8 +834,8 @@ cs_status cs_quant_append(cs_quant_cache* c, const cs_blocks* blocks, const cs_h
   a.kv = c->view; a.blk = view_of(blocks); a.status = c->status;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const int dh = c->cfg.head_dim;
-  if (out == CS_BF16) CS_CUDA_OK(c, in == CS_F32 ? (launch_append<float, __nv_bfloat16>(a, dh, st)) : (launch_append<__nv_bfloat16, __nv_bfloat16>(a, dh, st)));
-  else CS_CUDA_OK(c, in == CS_F32 ? (launch_append<float, __half>(a, dh, st)) : (launch_append<__half, __half>(a, dh, st)));
+  if (out == CS_BF16) CS_CUDA_OK(c, in == CS_F32 ? (launch_append<float, __nv_bfloat16>(a, dh, c->num_sms, st)) : (launch_append<__nv_bfloat16, __nv_bfloat16>(a, dh, c->num_sms, st)));
+  else CS_CUDA_OK(c, in == CS_F32 ? (launch_append<float, __half>(a, dh, c->num_sms, st)) : (launch_append<__half, __half>(a, dh, c->num_sms, st)));
   return CS_OK;
 }
 
