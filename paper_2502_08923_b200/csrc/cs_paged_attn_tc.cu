@@ -142,7 +142,9 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// Weights 2^(score scale - m) of 32 keys, rounded to T, to tensor memory, and their sum.  (The 16-a-clock unit behind ex2 is busy for half of the loop's
+// Weights 2^(score scale - m) of 32 keys, rounded to T, to tensor memory, and their sum, of the weights as they were.  One term of 16 bits is a choice: a second one would make half as many products again (2,048 rows over
+// 30,720 keys 757 -> 1,135 us at the rate that the power cap leaves a library's product) and as much more to pack, for errors of 2.2e-3 (bf16) and 2.8e-4 (fp16) against 64 bits, of which 1.7e-3 and 2.1e-4 are the result's own
+// rounding.  (The 16-a-clock unit behind ex2 is busy for half of the loop's
 // time.  A polynomial in packed arithmetic for a quarter to three eighths of them was no faster in short runs and 2 - 4 % slower at the power cap.)
 template <typename T>
 __device__ __forceinline__ void weights(const float* v, uint32_t taddr, f32x2 sc2, f32x2 nm2, f32x2& l2) {

@@ -152,7 +152,7 @@ __device__ __forceinline__ void fetch16(uint32_t dst, const char* src) {
 }
 
 // A unit is 512 elements: up to kPer neighbouring heads of the queries, the keys or the values of a row.  Units lie in a ring of shared memory for each warp, as in memory; three are in flight.
-// What bounds it: instructions.  Four chunks of up to 2,048 rows (32 query heads, 8 of keys, norms and rotation) with their positions read back: 50 us, 44 of them here; 26 M instructions, the schedulers issue in 61 of 100 clocks; 7 us are the
+// What bounds it: instructions.  Four chunks of up to 2,048 rows (32 query heads, 8 of keys, norms and rotation) with their positions read back: 50 us (from rows in 32 bits 56), 44 of them here; 26 M instructions, the schedulers issue in 62 of 100 clocks; 7 us are the
 // keys' 64-bit arithmetic, in what an SM has units for.  (87 us with rows fetched as they are needed, 66 with the ring, 54 with factors and quotients worked out once, 50 with four blocks of four warps an SM; five of them: no faster, nor
 // several rows a warp.)  A token each of 64 sequences and one verification block: 4 us, a chain of loads (whose row, which page) and one row's arithmetic.
 template <typename S, typename D, int DH>
@@ -434,7 +434,7 @@ constexpr int kReadWarps = 8;
 
 // A warp has rows_per_warp neighbouring rows: what finding a row takes (whose block, which page, one load after the other) is under way for all of them at once, and so are two rows' groups.
 // Traffic bounds it, what is written above all: a lane has a whole group (16 bytes of numbers, one scale) and stores whole sectors.  Two sequences of 16,384 positions of eight heads of 128: 31.9 us, 5.4 TB/s of the
-// 172 MB that are read and written; 36.6 with eight elements a lane, 16 bytes a store.  Three short blocks: 3.1 us, what finding a row takes.
+// 172 MB that are read and written, in 32 bits 68.7 us, 4.5 TB/s of 306; 36.6 with eight elements a lane, 16 bytes a store.  Three short blocks: 3.1 us, what finding a row takes.
 template <typename T, int DH>
 __global__ void __launch_bounds__(kReadWarps * 32)
 k_quant_read(const __grid_constant__ QuantReadArgs a) {

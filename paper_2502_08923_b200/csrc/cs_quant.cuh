@@ -2,8 +2,9 @@
 //
 // A row (one position, one KV head) is cut into groups of 32 neighbouring elements.  With a = max |x| of a group,
 //     s = a / 7 rounded to five significant bits,   n = x / s rounded to a whole number, |n| <= 7;
-// the group is held as s (bf16) and 4-bit numbers n + 8, and stands for s n.  Five bits and three make eight, so every value that the cache stands for is exactly a bf16 number: keys and
-// values go into the tensor cores as they are held, without a further rounding, whatever the queries' type, and reading back in bf16 is exact.  Rounding the scale (by 1/32 at most) makes
+// the group is held as s (bf16) and 4-bit numbers n + 8, and stands for s n.  Five bits and three make eight, so every value that the cache stands for is exactly a bf16 number: reading back in bf16 is
+// exact, and keys and values go into the tensor cores as they are held, without a further rounding, in the kernel for few rows whatever the queries' type, in tall blocks of bf16 queries.  (Tall blocks of fp16 queries have them
+// in fp16, which ends at 65504 and has steps of 2^-24 below 2^-14.)  Scales below 2^-126 are multiples of 2^-133, where bf16 ends.  Rounding the scale (by 1/32 at most) makes
 // x / s at most 7.22, so the largest element still is off by less than half a step, as all others.  A group with an element that is not finite has the scale NaN, and all of it reads as NaN.
 //
 // Eight elements make a word: 2i and 2i + 1 are its fields i and i + 4, field f begins at bit 4f, so that a mask takes neighbouring elements out as the two halves of a register.
@@ -19,7 +20,8 @@ static constexpr int kQuantMaxSms = 160;
 static constexpr int kQuantCtasPerSm = 4;      // of an attention launch, at most
 static constexpr int kQuantMaxRows = 32;       // query rows of one work item at most
 static constexpr int kQuantRowsPerSm = 64;     // query rows of the items that CTAs of an SM have at hand, at most
-static constexpr int kQuantMaxSeqs = 128;      // sequences of one attention launch; more are further launches
+static constexpr int kQuantMaxSeqs = 128;      // sequences of one attention launch; more are further launches.  (The plan of 512 takes 17 KB of shared memory a CTA, which four of them on an SM have not got.  Ragged tokens over up
+                                               // to 4,097 keys of the 8B shape: 128 of them 77 us, 256 in two pairs of launches 159.)
 static constexpr int kQuantCopyPage = 128;     // slots of a page of the copies that prompts' chunks are worked out from; 64, 32 or 16 where sequences in whole pages would not fit
 
 struct QuantView {
